@@ -309,6 +309,104 @@ int gs_weight_grad_workspace(int64_t n, int64_t a, int64_t b, uint64_t *bytes);
 int gs_weight_grad(const float *H, int64_t ldh, const float *G, int64_t ldg, int64_t n, int64_t a, int64_t b,
                    float *out, void *work, uint64_t work_bytes, gs_stream s);
 
+/* ---- low-bit forms of a layer's dense operands ----
+ *
+ * Two microscaled formats hold a row-major matrix as blocks of 32 consecutive
+ * columns of a row (the last block of a row may be short) with one scale byte
+ * E a block, which stands for 2^(E - 127); E = 255 marks a block that held a
+ * NaN or an infinity, all of whose values are NaN.  m is the largest magnitude
+ * of the block, k its fp32 exponent field, x an element of it.
+ *
+ *   saved activations, 8 bits:
+ *     GS_ACT_RELU  h = relu(x), E = max(k - 7, 1), code 0 where x <= 0, else
+ *                  rint(h 2^(127-E)) clamped to 1..255: a code is positive
+ *                  exactly where the gradient of the ReLU is 1
+ *     GS_ACT_NONE  h = x, E = max(k - 6, 1), code rint(x 2^(127-E)) clamped to
+ *                  -127..127, in two's complement
+ *     value = code 2^(E-127), at most one step from h; it has at most 8
+ *     significant bits, so bf16 holds it exactly
+ *   MXFP4 (OCP Microscaling: e2m1 elements, power-of-two scales):
+ *     E = max(k - 2, 0), element = the nearest of +-{0, 0.5, 1, 1.5, 2, 3, 4, 6}
+ *     to x 2^(127-E), ties to the even mantissa, clamped to +-6
+ *
+ * The arrays belong to the caller (gs_saved_layout, gs_mxfp4_layout give their
+ * row pitches) and are never written outside rows * pitch.  Columns are at most
+ * 2^24.  Dense operands are fp32 or bf16 with any leading dimension >= their
+ * width and any alignment of their elements.  Outputs must not overlap inputs
+ * except where a call says so.  All calls are deterministic, asynchronous on s
+ * and allocate nothing. */
+typedef enum { GS_F32 = 0, GS_BF16 = 1 } gs_dtype;
+typedef enum { GS_ACT_NONE = 0, GS_ACT_RELU = 1 } gs_act;
+
+typedef struct {
+    int64_t rows, cols;
+    int32_t act;     /* gs_act */
+    uint8_t *codes;  /* [dev] rows x code pitch, 16-byte aligned; code of (r, c) at r * pitch + c */
+    uint8_t *scales; /* [dev] rows x scale pitch; E of (r, c) at r * pitch + c / 32 */
+} gs_saved;
+
+/* Row pitches in bytes: cols rounded up to 32, and a byte per 32 of them. */
+int gs_saved_layout(int64_t cols, int64_t *code_pitch, int64_t *scale_pitch);
+
+/* Saves the activations of P [dev] (rows x cols of dtype) in 8 bits and, if H
+ * is not NULL, writes h in P's type to H [dev]. */
+int gs_save_activation(const void *P, int64_t ldp, int dtype, const gs_saved *out, void *H, int64_t ldh,
+                       gs_stream s);
+
+/* The values of saved activations, as fp32 or bf16 (both exact). */
+int gs_saved_dequantize(const gs_saved *A, void *out, int64_t ld, int dtype, gs_stream s);
+
+/* Gradient of the ReLU: dP = dH where A's code is positive, else 0 (also where
+ * dH is not finite).  dP may be dH itself with the same leading dimension.
+ * A->act must be GS_ACT_RELU. */
+int gs_relu_grad(const gs_saved *A, const void *dH, int64_t ldh, int dtype, void *dP, int64_t ldp, gs_stream s);
+
+/* Weight gradient from saved activations: out = value(A)^T . G, A.cols x b fp32
+ * row-major (leading dimension b), G [dev] rows x b with leading dimension ldg.
+ * The values of A are exact on the matrix cores and G is taken in three parts
+ * that add up to it, so products and sums are those of fp32.  A.cols and b at
+ * most 4096.  work [dev] holds at least the bytes that
+ * gs_saved_weight_grad_workspace reports. */
+int gs_saved_weight_grad_workspace(int64_t n, int64_t a, int64_t b, uint64_t *bytes);
+int gs_saved_weight_grad(const gs_saved *A, const void *G, int64_t ldg, int dtype, int64_t b, float *out,
+                         void *work, uint64_t work_bytes, gs_stream s);
+
+typedef struct {
+    int64_t rows, cols;
+    uint8_t *codes;  /* [dev] rows x code pitch, 16-byte aligned; (r, c) in the low (c even) or high
+                        half of byte r * pitch + c / 2: sign, two exponent bits, mantissa bit */
+    uint8_t *scales; /* [dev] rows x scale pitch, 4-byte aligned; E of (r, c) at r * pitch + c / 32 */
+} gs_mxfp4;
+
+/* Row pitches in bytes: cols / 2 and cols / 32 with cols rounded up to 64, above
+ * 64 to 128 (the products' steps); padding elements and scales are 0. */
+int gs_mxfp4_layout(int64_t cols, int64_t *code_pitch, int64_t *scale_pitch);
+
+/* Quantises X [dev] (rows x cols of dtype) along its rows (axis 1: out is rows x
+ * cols) or along its columns (axis 0: out is X^T, cols x rows, blocks of 32
+ * rows of X). */
+int gs_mxfp4_quantize(const void *X, int64_t ldx, int dtype, int64_t rows, int64_t cols, int axis,
+                      const gs_mxfp4 *out, gs_stream s);
+
+/* The values of an MXFP4 matrix, as fp32 or bf16 (both exact). */
+int gs_mxfp4_dequantize(const gs_mxfp4 *A, void *out, int64_t ld, int dtype, gs_stream s);
+
+/* C = A . B^T on the matrix cores: A m x k, B n x k in MXFP4, exact products,
+ * fp32 sums, C [dev] m x n of dtype with leading dimension ldc.  mask may be
+ * NULL, or m x n activations saved with GS_ACT_RELU: C is then 0 where their
+ * code is 0 (the gradient of the layer below, masked on the way out).  work
+ * [dev] holds at least the bytes that gs_mxfp4_matmul_workspace reports for
+ * a_dtype = -1 (it may be NULL if that is 0). */
+int gs_mxfp4_matmul(const gs_mxfp4 *A, const gs_mxfp4 *B, const gs_saved *mask, void *C, int64_t ldc, int dtype,
+                    void *work, uint64_t work_bytes, gs_stream s);
+
+/* The same with A dense (m x B->cols of a_dtype), quantised along its rows
+ * within the call. */
+int gs_mxfp4_matmul_dense(const void *A, int64_t lda, int a_dtype, int64_t m, const gs_mxfp4 *B,
+                          const gs_saved *mask, void *C, int64_t ldc, int dtype, void *work, uint64_t work_bytes,
+                          gs_stream s);
+int gs_mxfp4_matmul_workspace(int64_t m, int64_t n, int64_t k, int a_dtype, uint64_t *bytes);
+
 /* Thread-local description of the last error (never NULL). */
 const char *gs_last_error(void);
 

@@ -23,6 +23,8 @@ import torch
 __all__ = [
     "FORMATS", "FORMAT_NAMES", "GnnSpmmError", "Matrix", "SelectContext", "build_format",
     "extract_features", "lib", "library_path", "FEATURE_NAMES", "set_allocator",
+    "SavedActivation", "save_activation", "relu_grad", "saved_weight_grad",
+    "Mxfp4", "mxfp4_quantize", "mxfp4_matmul",
 ]
 
 _HERE = os.path.dirname(os.path.abspath(__file__))
@@ -71,6 +73,14 @@ class _SelStats(ctypes.Structure):
     _fields_ = [("t_features", ctypes.c_double), ("t_predict", ctypes.c_double),
                 ("t_convert", ctypes.c_double), ("chosen", _i32), ("feasible_mask", _i32),
                 ("scores", ctypes.c_double * len(FORMATS))]
+
+
+class _Saved(ctypes.Structure):
+    _fields_ = [("rows", _i64), ("cols", _i64), ("act", _i32), ("codes", _p), ("scales", _p)]
+
+
+class _Mxfp4(ctypes.Structure):
+    _fields_ = [("rows", _i64), ("cols", _i64), ("codes", _p), ("scales", _p)]
 
 
 _ALLOC_FN = ctypes.CFUNCTYPE(_p, ctypes.c_size_t, _p, _p)
@@ -134,6 +144,18 @@ def lib() -> ctypes.CDLL:
         "gs_ctx_stats": (c_int, [_p, P(_SelStats)]),
         "gs_weight_grad_workspace": (c_int, [_i64, _i64, _i64, P(_u64)]),
         "gs_weight_grad": (c_int, [_p, _i64, _p, _i64, _i64, _i64, _i64, _p, _p, _u64, _p]),
+        "gs_saved_layout": (c_int, [_i64, P(_i64), P(_i64)]),
+        "gs_save_activation": (c_int, [_p, _i64, c_int, P(_Saved), _p, _i64, _p]),
+        "gs_saved_dequantize": (c_int, [P(_Saved), _p, _i64, c_int, _p]),
+        "gs_relu_grad": (c_int, [P(_Saved), _p, _i64, c_int, _p, _i64, _p]),
+        "gs_saved_weight_grad_workspace": (c_int, [_i64, _i64, _i64, P(_u64)]),
+        "gs_saved_weight_grad": (c_int, [P(_Saved), _p, _i64, c_int, _i64, _p, _p, _u64, _p]),
+        "gs_mxfp4_layout": (c_int, [_i64, P(_i64), P(_i64)]),
+        "gs_mxfp4_quantize": (c_int, [_p, _i64, c_int, _i64, _i64, c_int, P(_Mxfp4), _p]),
+        "gs_mxfp4_dequantize": (c_int, [P(_Mxfp4), _p, _i64, c_int, _p]),
+        "gs_mxfp4_matmul": (c_int, [P(_Mxfp4), P(_Mxfp4), P(_Saved), _p, _i64, c_int, _p, _u64, _p]),
+        "gs_mxfp4_matmul_dense": (c_int, [_p, _i64, c_int, _i64, P(_Mxfp4), P(_Saved), _p, _i64, c_int, _p, _u64, _p]),
+        "gs_mxfp4_matmul_workspace": (c_int, [_i64, _i64, _i64, c_int, P(_u64)]),
         "gs_last_error": (ctypes.c_char_p, []),
         "gs_abi_version": (c_int, []),
     }
@@ -390,6 +412,226 @@ def weight_grad(H: torch.Tensor, G: torch.Tensor, stream=None) -> torch.Tensor:
     _check(lib().gs_weight_grad(H.data_ptr(), H.stride(0), G.data_ptr(), G.stride(0), n, a, b, out.data_ptr(),
                                 work.data_ptr(), need.value, _stream()))
     return out
+
+
+# ------------------------------------------------- low-bit forms of dense operands
+
+ACTIVATIONS = {"none": 0, "relu": 1}
+_DTYPES = {torch.float32: 0, torch.bfloat16: 1}
+
+
+def _dense(X: torch.Tensor, name: str, device=None) -> tuple:
+    """(tensor, leading dimension, dtype code) of a 2-D fp32 or bf16 operand on the current device."""
+    if (not isinstance(X, torch.Tensor) or not X.is_cuda or X.dtype not in _DTYPES or X.layout != torch.strided
+            or X.dim() != 2):
+        raise ValueError(f"{name} must be a 2-D CUDA float32 or bfloat16 tensor")
+    if X.device.index != torch._C._cuda_getDevice() or (device is not None and X.device != device):
+        raise ValueError(f"{name} is not on the current device")
+    if X.is_neg():
+        X = X.resolve_neg()
+    rows, cols = X.shape
+    if cols > 1 and rows > 0 and X.stride(1) != 1:
+        raise ValueError(f"{name} must have unit column stride")
+    ld = X.stride(0) if rows > 1 else cols
+    if rows > 1 and ld < cols:
+        raise ValueError(f"{name} must have a row stride of at least its width")
+    return X, max(ld, cols), _DTYPES[X.dtype]
+
+
+def _dtype_code(dtype) -> int:
+    if dtype not in _DTYPES:
+        raise ValueError("dtype must be torch.float32 or torch.bfloat16")
+    return _DTYPES[dtype]
+
+
+def _on(stream, call, *inputs):
+    """call() with `stream` as the current stream, so that what it allocates belongs to
+    it; memory of the inputs is not given out again before it has read them."""
+    if stream is None or _stream(stream) == _stream():
+        return call()
+    if not isinstance(stream, torch.cuda.Stream):
+        raw = _stream(stream)
+        stream = torch.cuda.ExternalStream(raw) if raw else torch.cuda.default_stream()
+    with torch.cuda.stream(stream):
+        out = call()
+    for t in inputs:
+        if isinstance(t, (SavedActivation, Mxfp4)):
+            t.codes.record_stream(stream)
+            t.scales.record_stream(stream)
+        elif t is not None:
+            t.record_stream(stream)
+    return out
+
+
+def _out(out, shape, dtype, device):
+    """`out`, or a new tensor, and its leading dimension."""
+    if out is None:
+        out = torch.empty(shape, dtype=dtype, device=device)
+        return out, shape[1]
+    if out.shape != torch.Size(shape) or out.dtype != dtype or out.is_neg():
+        raise ValueError("out has the wrong shape or dtype")
+    return out, _dense(out, "out", device)[1]
+
+
+def _arrays(rows, code_pitch, scale_pitch, device):
+    """Uninitialised code and scale arrays, from one allocation (both start 256-byte aligned)."""
+    nc = rows * code_pitch
+    at = -(-nc // 256) * 256
+    buf = torch.empty(at + rows * scale_pitch, dtype=torch.uint8, device=device)
+    return buf[:nc].view(rows, code_pitch), buf[at:].view(rows, scale_pitch)
+
+
+class SavedActivation:
+    """Activations kept in 8 bits (gs_saved): codes, one power-of-two step per 32 columns of a row."""
+
+    def __init__(self, codes: torch.Tensor, scales: torch.Tensor, shape, act: str):
+        self.codes, self.scales, self.act = codes, scales, act
+        self.shape = (int(shape[0]), int(shape[1]))
+        self.device = codes.device
+        self._c = _Saved(self.shape[0], self.shape[1], ACTIVATIONS[act], codes.data_ptr(), scales.data_ptr())
+        self._ref = ctypes.byref(self._c)
+
+    @property
+    def device_bytes(self) -> int:
+        return self.codes.numel() + self.scales.numel()
+
+    def dequantize(self, dtype=torch.float32, stream=None) -> torch.Tensor:
+        """The values the codes stand for, exact in either type (gs_saved_dequantize)."""
+        code = _dtype_code(dtype)
+
+        def call():
+            out = torch.empty(self.shape, dtype=dtype, device=self.device)
+            _check(lib().gs_saved_dequantize(self._ref, out.data_ptr(), self.shape[1], code, _stream()))
+            return out
+        return _on(stream, call, self)
+
+
+def save_activation(P: torch.Tensor, act: str = "relu", stream=None) -> tuple:
+    """(H, saved): H = relu(P) (act "relu") or P itself (act "none"), and H in 8 bits
+    for the backward pass (gs_save_activation)."""
+    if act not in ACTIVATIONS:
+        raise ValueError("act must be 'relu' or 'none'")
+    P, ld, code = _dense(P, "P")
+    n, a = P.shape
+
+    def call():
+        saved = SavedActivation(*_arrays(n, -(-a // 32) * 32, -(-a // 32), P.device), (n, a), act)
+        H = torch.empty((n, a), dtype=P.dtype, device=P.device) if act == "relu" else None
+        _check(lib().gs_save_activation(P.data_ptr(), ld, code, saved._ref, None if H is None else H.data_ptr(), a,
+                                        _stream()))
+        return (P if H is None else H), saved
+    return _on(stream, call, P)
+
+
+def relu_grad(saved: SavedActivation, dH: torch.Tensor, out: torch.Tensor | None = None, stream=None) -> torch.Tensor:
+    """dH where the saved ReLU was active, else 0 (gs_relu_grad); out may be dH."""
+    dH, ld, code = _dense(dH, "dH", saved.device)
+    if tuple(dH.shape) != saved.shape:
+        raise ValueError("dH and the saved activations have different shapes")
+
+    def call():
+        dP, ldp = _out(out, saved.shape, dH.dtype, dH.device)
+        _check(lib().gs_relu_grad(saved._ref, dH.data_ptr(), ld, code, dP.data_ptr(), ldp, _stream()))
+        return dP
+    return _on(stream, call, saved, dH, out)
+
+
+def saved_weight_grad(saved: SavedActivation, G: torch.Tensor, stream=None) -> torch.Tensor:
+    """H^T G in fp32 from saved activations H (n x a) and G (n x b) (gs_saved_weight_grad)."""
+    G, ld, code = _dense(G, "G", saved.device)
+    (n, a), b = saved.shape, G.shape[1]
+    if G.shape[0] != n:
+        raise ValueError("G and the saved activations must have the same number of rows")
+
+    def call():
+        need = _u64()
+        _check(lib().gs_saved_weight_grad_workspace(n, a, b, ctypes.byref(need)))
+        out = torch.empty((a, b), dtype=torch.float32, device=G.device)
+        work = torch.empty(need.value, dtype=torch.uint8, device=G.device) if need.value else None
+        _check(lib().gs_saved_weight_grad(saved._ref, G.data_ptr(), ld, code, b, out.data_ptr(),
+                                          None if work is None else work.data_ptr(), need.value, _stream()))
+        return out
+    return _on(stream, call, saved, G)
+
+
+class Mxfp4:
+    """A matrix in MXFP4 (gs_mxfp4): e2m1 codes, one power-of-two scale per 32 columns of a row."""
+
+    def __init__(self, codes: torch.Tensor, scales: torch.Tensor, shape):
+        self.codes, self.scales = codes, scales
+        self.shape = (int(shape[0]), int(shape[1]))
+        self.device = codes.device
+        self._c = _Mxfp4(self.shape[0], self.shape[1], codes.data_ptr(), scales.data_ptr())
+        self._ref = ctypes.byref(self._c)
+
+    @property
+    def device_bytes(self) -> int:
+        return self.codes.numel() + self.scales.numel()
+
+    def dequantize(self, dtype=torch.float32, stream=None) -> torch.Tensor:
+        """The values the codes stand for, exact in either type (gs_mxfp4_dequantize)."""
+        code = _dtype_code(dtype)
+
+        def call():
+            out = torch.empty(self.shape, dtype=dtype, device=self.device)
+            _check(lib().gs_mxfp4_dequantize(self._ref, out.data_ptr(), self.shape[1], code, _stream()))
+            return out
+        return _on(stream, call, self)
+
+
+def mxfp4_quantize(X: torch.Tensor, axis: int = 1, stream=None) -> Mxfp4:
+    """X in MXFP4, with blocks of 32 along its rows (axis 1), or X^T with blocks along
+    X's columns (axis 0): the operands of mxfp4_matmul for X W are X and W with axis 0
+    (gs_mxfp4_quantize)."""
+    if axis not in (0, 1):
+        raise ValueError("axis must be 0 or 1")
+    X, ld, code = _dense(X, "X")
+    rows, cols = X.shape
+    shape = (rows, cols) if axis == 1 else (cols, rows)
+
+    def call():
+        step = 64 if shape[1] <= 64 else 128
+        padded = -(-shape[1] // step) * step
+        q = Mxfp4(*_arrays(shape[0], padded // 2, padded // 32, X.device), shape)
+        _check(lib().gs_mxfp4_quantize(X.data_ptr(), ld, code, rows, cols, axis, q._ref, _stream()))
+        return q
+    return _on(stream, call, X)
+
+
+def mxfp4_matmul(A, B: Mxfp4, mask: SavedActivation | None = None, dtype=torch.float32,
+                 out: torch.Tensor | None = None, stream=None) -> torch.Tensor:
+    """A B^T for A (m x k: an Mxfp4, or a dense tensor that is quantised along its rows
+    within the call) and B (n x k, an Mxfp4), as fp32 or bf16 (gs_mxfp4_matmul).  mask:
+    activations saved by a ReLU (m x n); the product is 0 where they are."""
+    code = _dtype_code(dtype)
+    if not isinstance(B, Mxfp4):
+        raise ValueError("B must be an Mxfp4")
+    quantised = isinstance(A, Mxfp4)
+    if quantised:
+        if A.device != B.device:
+            raise ValueError("A and B must be on the same device")
+        a_code = -1
+    else:
+        A, lda, a_code = _dense(A, "A", B.device)
+    (m, k), n = A.shape, B.shape[0]
+    if k != B.shape[1]:
+        raise ValueError(f"A has {k} columns, B has {B.shape[1]}")
+    if mask is not None and (mask.shape != (m, n) or mask.device != B.device):
+        raise ValueError("the mask's shape or device is not the product's")
+
+    def call():
+        C, ldc = _out(out, (m, n), dtype, B.device)
+        need = _u64()
+        _check(lib().gs_mxfp4_matmul_workspace(m, n, k, a_code, ctypes.byref(need)))
+        work = torch.empty(need.value, dtype=torch.uint8, device=B.device) if need.value else None
+        tail = (B._ref, None if mask is None else mask._ref, C.data_ptr(), ldc, code,
+                None if work is None else work.data_ptr(), need.value, _stream())
+        if quantised:
+            _check(lib().gs_mxfp4_matmul(A._ref, *tail))
+        else:
+            _check(lib().gs_mxfp4_matmul_dense(A.data_ptr(), lda, a_code, m, *tail))
+        return C
+    return _on(stream, call, A, B, mask, out)
 
 
 def _features_dict(out: _Features) -> dict:

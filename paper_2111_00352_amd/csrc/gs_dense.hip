@@ -199,6 +199,13 @@ TnPlan tn_plan(int64_t n, int64_t a, int64_t b)
 }
 
 }  // namespace
+
+void reduce_partials(const float *part, int P, int64_t ab, float *out, hipStream_t s)
+{
+    k_tn_reduce<<<(unsigned)ceil_div(ab, 64), 1024, 0, s>>>(part, P, ab, out);
+    GS_HIP(hipGetLastError());
+}
+
 }  // namespace gs
 
 using namespace gs;
@@ -249,8 +256,7 @@ int gs_weight_grad(const float *H, int64_t ldh, const float *G, int64_t ldg, int
         GS_TN(128, 32, 4, 1) GS_TN(32, 128, 1, 4) GS_TN(64, 32, 2, 1) GS_TN(32, 64, 1, 2) GS_TN(32, 32, 1, 1)
 #undef GS_TN
         GS_HIP(hipGetLastError());
-        k_tn_reduce<<<(unsigned)ceil_div(a * b, 64), 1024, 0, s>>>(part, (int)(p.chunks * p.ks), a * b, out);
-        GS_HIP(hipGetLastError());
+        reduce_partials(part, (int)(p.chunks * p.ks), a * b, out, s);
     });
 }
 

@@ -369,6 +369,10 @@ struct WorkArea {
 // in stream order.
 void *work_for(gs_matrix_ &m, const WorkArea *fixed, size_t bytes, hipStream_t s);
 
+// out[e] = the sum of element e of P partials of ab floats each, in a fixed
+// order, enqueued on s (gs_dense).
+void reduce_partials(const float *part, int P, int64_t ab, float *out, hipStream_t s);
+
 // Records, when it goes out of scope, that work on m was enqueued on s (see
 // gs_matrix_::uses), also where an error ended the call halfway; nothing while
 // s is being captured into a graph (replays are ordered by the caller).

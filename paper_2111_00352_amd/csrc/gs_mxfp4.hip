@@ -1,0 +1,209 @@
+// MXFP4 (OCP Microscaling, e2m1 elements, blocks of 32 with a power-of-two
+// scale): quantisation along the rows or the columns of a dense matrix, and the
+// values back.  Each is one pass, bound by memory.
+#include <algorithm>
+
+#include "gs_device.h"
+#include "gs_lowbit.h"
+#include "gs_mxfp4.h"
+
+namespace gs {
+namespace {
+
+// A lane takes 8 columns, four lanes a block.
+constexpr int kLaneCols = 8;
+
+template <class T>
+__global__ __launch_bounds__(kUnitThreads) void k_mx4_rows(const T *__restrict__ X, int64_t ldx, int64_t cols,
+                                                           int64_t units, BlockDiv div, uint8_t *__restrict__ codes,
+                                                           uint8_t *__restrict__ scales)
+{
+    constexpr int E = kLaneCols, L = kMxBlock / E;
+    typename Elems<T, E>::type v[kUnitRounds];
+    for (int64_t u0 = (int64_t)blockIdx.x * kUnits; u0 < units; u0 += (int64_t)gridDim.x * kUnits) {
+        const BlockAt first = block_first(div, u0 / L);
+#pragma unroll
+        for (int i = 0; i < kUnitRounds; i++) {
+            const uint32_t t = i * kUnitThreads + threadIdx.x;
+            const BlockAt at = block_step(div, first, t / L);
+            const int32_t col = at.blk * kMxBlock + (t % L) * E;
+            if (u0 + t < units) v[i] = load_elems<T, E>(X + at.row * ldx + col, cols - col);
+        }
+#pragma unroll
+        for (int i = 0; i < kUnitRounds; i++) {
+            const int64_t u = u0 + i * kUnitThreads + threadIdx.x;
+            if (u >= units) continue;  // (whole blocks)
+            float x[E];
+            uint32_t m = 0;
+#pragma unroll
+            for (int e = 0; e < E; e++) {
+                x[e] = to_f32(v[i][e]);
+                const uint32_t b = __float_as_uint(x[e]) & 0x7fffffffu;
+                m = b > m ? b : m;
+            }
+            const int E8 = mx4_exponent(group_max<L>(m));
+            reinterpret_cast<uint32_t *>(codes)[u] = mx4_pack8(x, E8);
+            if (u % L == 0) scales[u / L] = (uint8_t)E8;
+        }
+    }
+}
+
+// Along the columns: out row c holds column c of X.  A workgroup takes 256 rows
+// x 32 columns of X: thread t loads column t % 32 of the 32 rows of block t / 32
+// and quantises them alone; the codes go out through LDS so that an out row
+// receives 128 contiguous bytes.
+constexpr int kColTile = 32;
+constexpr int kRowTile = 256;
+
+template <class T>
+__global__ __launch_bounds__(256) void k_mx4_cols(const T *__restrict__ X, int64_t ldx, int64_t rows, int64_t cols,
+                                                  int64_t row_tiles, int64_t tiles, int64_t code_pitch,
+                                                  int64_t scale_pitch, uint8_t *__restrict__ codes,
+                                                  uint8_t *__restrict__ scales)
+{
+    __shared__ uint4 tile[kColTile][kRowTile / 32 + 1];
+    __shared__ uint8_t exps[kColTile][kRowTile / 32];
+    const int c = threadIdx.x % kColTile, blk = threadIdx.x / kColTile;
+    for (int64_t t = blockIdx.x; t < tiles; t += gridDim.x) {
+        const int64_t r0 = (t % row_tiles) * kRowTile, c0 = (t / row_tiles) * kColTile;
+        float x[32];
+        uint32_t m = 0;
+        const int64_t rb = r0 + 32 * blk;
+#pragma unroll
+        for (int i = 0; i < 32; i++) {
+            x[i] = rb + i < rows && c0 + c < cols ? to_f32(X[(rb + i) * ldx + c0 + c]) : 0.0f;
+            const uint32_t b = __float_as_uint(x[i]) & 0x7fffffffu;
+            m = b > m ? b : m;
+        }
+        const int E8 = mx4_exponent(m);
+        tile[c][blk] = make_uint4(mx4_pack8(x, E8), mx4_pack8(x + 8, E8), mx4_pack8(x + 16, E8), mx4_pack8(x + 24, E8));
+        exps[c][blk] = (uint8_t)E8;
+        __syncthreads();
+        const int oc = threadIdx.x / (kRowTile / 32), ob = threadIdx.x % (kRowTile / 32);
+        const int64_t at = r0 / 32 + ob;  // block of the out row
+        if (c0 + oc < cols && at < scale_pitch) {
+            *reinterpret_cast<uint4 *>(codes + (c0 + oc) * code_pitch + at * 16) = tile[oc][ob];
+            scales[(c0 + oc) * scale_pitch + at] = exps[oc][ob];
+        }
+        __syncthreads();
+    }
+}
+
+template <class T>
+__global__ __launch_bounds__(kUnitThreads) void k_mx4_values(const uint8_t *__restrict__ codes,
+                                                             const uint8_t *__restrict__ scales, int64_t code_pitch,
+                                                             int64_t scale_pitch, int64_t cols, int64_t units,
+                                                             BlockDiv div, T *__restrict__ out, int64_t ld)
+{
+    constexpr int E = kLaneCols, L = kMxBlock / E;
+    uint32_t w[kUnitRounds];
+    int E8[kUnitRounds];
+    int64_t row[kUnitRounds];
+    int32_t col[kUnitRounds];
+    for (int64_t u0 = (int64_t)blockIdx.x * kUnits; u0 < units; u0 += (int64_t)gridDim.x * kUnits) {
+        const BlockAt first = block_first(div, u0 / L);
+#pragma unroll
+        for (int i = 0; i < kUnitRounds; i++) {
+            const uint32_t t = i * kUnitThreads + threadIdx.x;
+            const BlockAt at = block_step(div, first, t / L);
+            row[i] = at.row;
+            col[i] = at.blk * kMxBlock + (t % L) * E;
+            if (u0 + t < units) {
+                w[i] = *reinterpret_cast<const uint32_t *>(codes + row[i] * code_pitch + col[i] / 2);
+                E8[i] = scales[row[i] * scale_pitch + at.blk];
+            }
+        }
+#pragma unroll
+        for (int i = 0; i < kUnitRounds; i++) {
+            const int64_t u = u0 + i * kUnitThreads + threadIdx.x;
+            if (u >= units || col[i] >= cols) continue;
+            const float s = mx_scale(E8[i]);
+            typename Elems<T, E>::type o;
+            f32x2 p[4] = {__builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w[i], 1.0f, 0), __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w[i], 1.0f, 1),
+                          __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w[i], 1.0f, 2), __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w[i], 1.0f, 3)};
+#pragma unroll
+            for (int e = 0; e < E; e++) o[e] = from_f32<T>(p[e / 2][e % 2] * s);
+            store_elems<T, E>(out + row[i] * ld + col[i], o, cols - col[i]);
+        }
+    }
+}
+
+}  // namespace
+
+void mx4_quantize_rows(const void *X, int64_t ldx, int dtype, int64_t rows, int64_t cols, uint8_t *codes,
+                       uint8_t *scales, hipStream_t s)
+{
+    const int64_t nb = mx4_cols(cols) / kMxBlock, units = rows * nb * (kMxBlock / kLaneCols);
+    if (units == 0) return;
+    if (dtype == GS_F32)
+        k_mx4_rows<float><<<unit_grid(units), kUnitThreads, 0, s>>>((const float *)X, ldx, cols, units, block_div(nb), codes, scales);
+    else
+        k_mx4_rows<u16><<<unit_grid(units), kUnitThreads, 0, s>>>((const u16 *)X, ldx, cols, units, block_div(nb), codes, scales);
+    GS_HIP(hipGetLastError());
+}
+
+}  // namespace gs
+
+using namespace gs;
+
+extern "C" {
+
+int gs_mxfp4_layout(int64_t cols, int64_t *code_pitch, int64_t *scale_pitch)
+{
+    return guarded([&] {
+        if (!code_pitch || !scale_pitch) fail(GS_ERR_INVALID_ARG, "null output");
+        if (cols < 0) fail(GS_ERR_INVALID_ARG, "bad matrix size");
+        if (cols > kMxMaxCols) fail(GS_ERR_UNSUPPORTED, "at most 2^24 columns");
+        *code_pitch = mx4_cols(cols) / 2;
+        *scale_pitch = mx4_cols(cols) / kMxBlock;
+    });
+}
+
+int gs_mxfp4_quantize(const void *X, int64_t ldx, int dtype, int64_t rows, int64_t cols, int axis,
+                      const gs_mxfp4 *out, gs_stream stream)
+{
+    return guarded([&] {
+        check_mxfp4(out);
+        if (axis != 0 && axis != 1) fail(GS_ERR_INVALID_ARG, "axis is 0 or 1");
+        if (out->rows != (axis ? rows : cols) || out->cols != (axis ? cols : rows))
+            fail(GS_ERR_INVALID_ARG, "the MXFP4 matrix has another shape");
+        check_operand("X", X, rows, cols, ldx, dtype_size(dtype));
+        if (rows == 0 || cols == 0) return;
+        const hipStream_t s = (hipStream_t)stream;
+        if (axis == 1) {
+            mx4_quantize_rows(X, ldx, dtype, rows, cols, out->codes, out->scales, s);
+            return;
+        }
+        const int64_t padded = mx4_cols(rows), row_tiles = ceil_div(padded, kRowTile);
+        const int64_t tiles = row_tiles * ceil_div(cols, kColTile);
+        const unsigned grid = (unsigned)std::min<int64_t>(tiles, 1 << 20);
+        auto go = [&](auto type) {
+            using T = decltype(type);
+            k_mx4_cols<T><<<grid, 256, 0, s>>>((const T *)X, ldx, rows, cols, row_tiles, tiles, padded / 2,
+                                              padded / kMxBlock, out->codes, out->scales);
+        };
+        dtype == GS_F32 ? go(0.0f) : go(u16(0));
+        GS_HIP(hipGetLastError());
+    });
+}
+
+int gs_mxfp4_dequantize(const gs_mxfp4 *A, void *out, int64_t ld, int dtype, gs_stream stream)
+{
+    return guarded([&] {
+        check_mxfp4(A);
+        check_operand("out", out, A->rows, A->cols, ld, dtype_size(dtype));
+        if (A->rows == 0 || A->cols == 0) return;
+        // (blocks of the matrix, without the padding of its rows)
+        const int64_t nb = ceil_div(A->cols, kMxBlock), units = A->rows * nb * (kMxBlock / kLaneCols);
+        const int64_t padded = mx4_cols(A->cols);
+        auto go = [&](auto type) {
+            using T = decltype(type);
+            k_mx4_values<T><<<unit_grid(units), kUnitThreads, 0, (hipStream_t)stream>>>(
+                A->codes, A->scales, padded / 2, padded / kMxBlock, A->cols, units, block_div(nb), (T *)out, ld);
+        };
+        dtype == GS_F32 ? go(0.0f) : go(u16(0));
+        GS_HIP(hipGetLastError());
+    });
+}
+
+}  // extern "C"

@@ -1,0 +1,300 @@
+// Activations kept in 8 bits for the backward pass: a layer's input is read
+// twice by its gradient (the weight gradient H^T G and the mask of the ReLU
+// below it), once per step, and is otherwise the largest thing a full-batch
+// step keeps.  Blocks of 32 columns share a power-of-two step, so a value is a
+// code of at most 8 significant bits times a power of two: saving and reading
+// back are exact fp32 operations, and the matrix cores take it as bf16 without
+// rounding.
+//
+// Everything here but the weight gradient is a stream: one pass, bound by
+// memory.
+#include <algorithm>
+
+#include "gs_device.h"
+#include "gs_lowbit.h"
+
+namespace gs {
+
+int dtype_size(int dtype)
+{
+    if (dtype != GS_F32 && dtype != GS_BF16) fail(GS_ERR_INVALID_ARG, "unknown element type %d", dtype);
+    return dtype == GS_F32 ? 4 : 2;
+}
+
+void check_operand(const char *name, const void *p, int64_t rows, int64_t cols, int64_t ld, int size)
+{
+    if (rows > 0 && cols > 0 && !p) fail(GS_ERR_INVALID_ARG, "%s is null", name);
+    if (ld < cols) fail(GS_ERR_INVALID_ARG, "%s: leading dimension below the width", name);
+    if ((uintptr_t)p % size) fail(GS_ERR_INVALID_ARG, "%s is not aligned to its elements", name);
+    if (rows > 1 && ld > (((int64_t)1 << 62) / size - cols) / (rows - 1))
+        fail(GS_ERR_INVALID_ARG, "%s: span is not addressable", name);
+}
+
+static void check_shape(int64_t rows, int64_t cols)
+{
+    if (rows < 0 || cols < 0 || rows > INT32_MAX) fail(GS_ERR_INVALID_ARG, "bad matrix size");
+    if (cols > kMxMaxCols) fail(GS_ERR_UNSUPPORTED, "at most 2^24 columns");
+}
+
+void check_saved(const gs_saved *A, bool relu_only)
+{
+    if (!A) fail(GS_ERR_INVALID_ARG, "null saved activations");
+    check_shape(A->rows, A->cols);
+    if (A->act != GS_ACT_NONE && A->act != GS_ACT_RELU) fail(GS_ERR_INVALID_ARG, "unknown activation %d", A->act);
+    if (relu_only && A->act != GS_ACT_RELU) fail(GS_ERR_INVALID_ARG, "activations were not saved by a ReLU");
+    if (A->rows > 0 && A->cols > 0 && (!A->codes || !A->scales)) fail(GS_ERR_INVALID_ARG, "null saved array");
+    if ((uintptr_t)A->codes % 16) fail(GS_ERR_INVALID_ARG, "saved codes are not 16-byte aligned");
+}
+
+void check_mxfp4(const gs_mxfp4 *A)
+{
+    if (!A) fail(GS_ERR_INVALID_ARG, "null MXFP4 matrix");
+    check_shape(A->rows, A->cols);
+    if (A->rows > 0 && A->cols > 0 && (!A->codes || !A->scales)) fail(GS_ERR_INVALID_ARG, "null MXFP4 array");
+    if ((uintptr_t)A->codes % 16 || (uintptr_t)A->scales % 4)
+        fail(GS_ERR_INVALID_ARG, "MXFP4 codes are not 16-byte or scales not 4-byte aligned");
+}
+
+namespace {
+
+// Lanes of a block: 16 bytes of the dense operand each.
+template <class T> constexpr int kUnitElems = sizeof(T) == 4 ? 4 : 8;
+
+template <int E> struct Codes;
+template <> struct Codes<4> {
+    typedef uint32_t type;
+};
+template <> struct Codes<8> {
+    typedef uint2 type;
+};
+template <int E> __device__ __forceinline__ uint32_t code_word(const typename Codes<E>::type &c, int w)
+{
+    if constexpr (E == 4)
+        return c;
+    else
+        return w ? c.y : c.x;
+}
+template <int E> __device__ __forceinline__ typename Codes<E>::type code_words(const uint32_t *w)
+{
+    if constexpr (E == 4)
+        return w[0];
+    else
+        return make_uint2(w[0], w[1]);
+}
+
+// For each of this thread's units load(i, unit, row, first column, columns left in
+// the row from there), i the round, then use(...) likewise.
+template <int E, class Load, class Use>
+__device__ __forceinline__ void walk_units(int64_t units, const BlockDiv &div, int64_t cols, Load &&load, Use &&use)
+{
+    constexpr int L = kMxBlock / E;
+    for (int64_t u0 = (int64_t)blockIdx.x * kUnits; u0 < units; u0 += (int64_t)gridDim.x * kUnits) {
+        const BlockAt first = block_first(div, u0 / L);
+        int64_t row[kUnitRounds];
+        int32_t col[kUnitRounds];
+#pragma unroll
+        for (int i = 0; i < kUnitRounds; i++) {
+            const uint32_t t = i * kUnitThreads + threadIdx.x;
+            const BlockAt at = block_step(div, first, t / L);
+            row[i] = at.row;
+            col[i] = at.blk * kMxBlock + (t % L) * E;
+            if (u0 + t < units) load(i, u0 + t, row[i], col[i], cols - col[i]);
+        }
+#pragma unroll
+        for (int i = 0; i < kUnitRounds; i++) {
+            const int64_t u = u0 + i * kUnitThreads + threadIdx.x;
+            // (units are whole blocks: the lanes of a block are all inside or all outside)
+            if (u < units) use(i, u, row[i], col[i], cols - col[i]);
+        }
+    }
+}
+
+template <class T, bool RELU>
+__global__ __launch_bounds__(kUnitThreads) void k_save(const T *__restrict__ P, int64_t ldp, int64_t cols,
+                                                       int64_t units, BlockDiv div, uint8_t *__restrict__ codes,
+                                                       uint8_t *__restrict__ scales, T *__restrict__ H, int64_t ldh)
+{
+    constexpr int E = kUnitElems<T>, L = kMxBlock / E;
+    typename Elems<T, E>::type v[kUnitRounds];
+    walk_units<E>(
+        units, div, cols,
+        [&](int i, int64_t, int64_t row, int32_t col, int64_t left) { v[i] = load_elems<T, E>(P + row * ldp + col, left); },
+        [&](int i, int64_t u, int64_t row, int32_t col, int64_t left) {
+            float h[E];
+            bool on[E];
+            uint32_t m = 0;
+#pragma unroll
+            for (int e = 0; e < E; e++) {
+                const float x = to_f32(v[i][e]);
+                on[e] = !(x <= 0.0f);
+                h[e] = RELU && !on[e] ? 0.0f : x;
+                const uint32_t b = __float_as_uint(h[e]) & 0x7fffffffu;
+                m = b > m ? b : m;
+            }
+            const int k = (int)(group_max<L>(m) >> 23);
+            const int s = k - (RELU ? 7 : 6);
+            const int E8 = k == 255 ? 255 : s > 1 ? s : 1;
+            const float inv = mx_inverse(E8);
+            uint32_t w[E / 4];
+#pragma unroll
+            for (int q = 0; q < E / 4; q++) {
+                w[q] = 0;
+#pragma unroll
+                for (int e = 0; e < 4; e++) {
+                    const float r = __builtin_rintf(h[4 * q + e] * inv);
+                    if constexpr (RELU) {
+                        // (clamped to 255 by the conversion; a NaN gives 1; past the row 0)
+                        const float c = on[4 * q + e] ? fmaxf(r, 1.0f) : 0.0f;
+                        w[q] = __builtin_amdgcn_cvt_pk_u8_f32(c, e, w[q]);
+                    } else {
+                        const int c = (int)fminf(fmaxf(r, -127.0f), 127.0f);
+                        w[q] |= (uint32_t)(c & 255) << (8 * e);
+                    }
+                }
+                if (!RELU && E8 == 255) w[q] = 0;
+            }
+            *reinterpret_cast<typename Codes<E>::type *>(codes + u * E) = code_words<E>(w);
+            if (u % L == 0) scales[u / L] = (uint8_t)E8;
+            if constexpr (RELU) {
+                if (H && left > 0) {
+                    typename Elems<T, E>::type o;
+#pragma unroll
+                    for (int e = 0; e < E; e++) o[e] = on[e] ? v[i][e] : T(0);
+                    store_elems<T, E>(H + row * ldh + col, o, left);
+                }
+            } else {
+                if (H && left > 0) store_elems<T, E>(H + row * ldh + col, v[i], left);
+            }
+        });
+}
+
+template <class T>
+__global__ __launch_bounds__(kUnitThreads) void k_relu_grad(const uint8_t *__restrict__ codes, int64_t cols,
+                                                            int64_t units, BlockDiv div, const T *dH, int64_t ldh,
+                                                            T *dP, int64_t ldp)
+{
+    constexpr int E = kUnitElems<T>;
+    typename Elems<T, E>::type v[kUnitRounds];
+    typename Codes<E>::type c[kUnitRounds];
+    walk_units<E>(
+        units, div, cols,
+        [&](int i, int64_t u, int64_t row, int32_t col, int64_t left) {
+            c[i] = *reinterpret_cast<const typename Codes<E>::type *>(codes + u * E);
+            v[i] = load_elems<T, E>(dH + row * ldh + col, left);
+        },
+        [&](int i, int64_t, int64_t row, int32_t col, int64_t left) {
+            typename Elems<T, E>::type o;
+#pragma unroll
+            for (int e = 0; e < E; e++) o[e] = code_word<E>(c[i], e / 4) >> (8 * (e % 4)) & 255 ? v[i][e] : T(0);
+            if (left > 0) store_elems<T, E>(dP + row * ldp + col, o, left);
+        });
+}
+
+template <class T>
+__global__ __launch_bounds__(kUnitThreads) void k_saved_values(const uint8_t *__restrict__ codes,
+                                                               const uint8_t *__restrict__ scales, int is_signed,
+                                                               int64_t cols, int64_t units, BlockDiv div,
+                                                               T *__restrict__ out, int64_t ld)
+{
+    constexpr int E = kUnitElems<T>, L = kMxBlock / E;
+    typename Codes<E>::type c[kUnitRounds];
+    int E8[kUnitRounds];
+    walk_units<E>(
+        units, div, cols,
+        [&](int i, int64_t u, int64_t, int32_t, int64_t) {
+            c[i] = *reinterpret_cast<const typename Codes<E>::type *>(codes + u * E);
+            E8[i] = scales[u / L];
+        },
+        [&](int i, int64_t, int64_t row, int32_t col, int64_t left) {
+            typename Elems<T, E>::type o;
+            const float s = mx_scale(E8[i]);
+#pragma unroll
+            for (int e = 0; e < E; e++) {
+                const int b = code_word<E>(c[i], e / 4) >> (8 * (e % 4)) & 255;
+                o[e] = from_f32<T>((float)(is_signed ? (int)(int8_t)b : b) * s);  // (exact in bf16 too)
+            }
+            if (left > 0) store_elems<T, E>(out + row * ld + col, o, left);
+        });
+}
+
+}  // namespace
+}  // namespace gs
+
+using namespace gs;
+
+extern "C" {
+
+int gs_saved_layout(int64_t cols, int64_t *code_pitch, int64_t *scale_pitch)
+{
+    return guarded([&] {
+        if (!code_pitch || !scale_pitch) fail(GS_ERR_INVALID_ARG, "null output");
+        check_shape(0, cols);
+        *code_pitch = saved_code_pitch(cols);
+        *scale_pitch = saved_scale_pitch(cols);
+    });
+}
+
+int gs_save_activation(const void *P, int64_t ldp, int dtype, const gs_saved *out, void *H, int64_t ldh,
+                       gs_stream stream)
+{
+    return guarded([&] {
+        check_saved(out, false);
+        const int size = dtype_size(dtype);
+        check_operand("P", P, out->rows, out->cols, ldp, size);
+        if (H) check_operand("H", H, out->rows, out->cols, ldh, size);
+        if (out->rows == 0 || out->cols == 0) return;
+        const int64_t nb = saved_scale_pitch(out->cols);
+        auto go = [&](auto kernel, auto type) {
+            using T = decltype(type);
+            const int64_t units = out->rows * nb * (kMxBlock / kUnitElems<T>);
+            kernel<<<unit_grid(units), kUnitThreads, 0, (hipStream_t)stream>>>(
+                (const T *)P, ldp, out->cols, units, block_div(nb), out->codes, out->scales, (T *)H, ldh);
+        };
+        const bool relu = out->act == GS_ACT_RELU;
+        if (dtype == GS_F32)
+            relu ? go(k_save<float, true>, 0.0f) : go(k_save<float, false>, 0.0f);
+        else
+            relu ? go(k_save<u16, true>, u16(0)) : go(k_save<u16, false>, u16(0));
+        GS_HIP(hipGetLastError());
+    });
+}
+
+int gs_saved_dequantize(const gs_saved *A, void *out, int64_t ld, int dtype, gs_stream stream)
+{
+    return guarded([&] {
+        check_saved(A, false);
+        check_operand("out", out, A->rows, A->cols, ld, dtype_size(dtype));
+        if (A->rows == 0 || A->cols == 0) return;
+        const int64_t nb = saved_scale_pitch(A->cols);
+        auto go = [&](auto type) {
+            using T = decltype(type);
+            const int64_t units = A->rows * nb * (kMxBlock / kUnitElems<T>);
+            k_saved_values<T><<<unit_grid(units), kUnitThreads, 0, (hipStream_t)stream>>>(
+                A->codes, A->scales, A->act == GS_ACT_NONE, A->cols, units, block_div(nb), (T *)out, ld);
+        };
+        dtype == GS_F32 ? go(0.0f) : go(u16(0));
+        GS_HIP(hipGetLastError());
+    });
+}
+
+int gs_relu_grad(const gs_saved *A, const void *dH, int64_t ldh, int dtype, void *dP, int64_t ldp, gs_stream stream)
+{
+    return guarded([&] {
+        check_saved(A, true);
+        const int size = dtype_size(dtype);
+        check_operand("dH", dH, A->rows, A->cols, ldh, size);
+        check_operand("dP", dP, A->rows, A->cols, ldp, size);
+        if (A->rows == 0 || A->cols == 0) return;
+        const int64_t nb = saved_scale_pitch(A->cols);
+        auto go = [&](auto type) {
+            using T = decltype(type);
+            const int64_t units = A->rows * nb * (kMxBlock / kUnitElems<T>);
+            k_relu_grad<T><<<unit_grid(units), kUnitThreads, 0, (hipStream_t)stream>>>(
+                A->codes, A->cols, units, block_div(nb), (const T *)dH, ldh, (T *)dP, ldp);
+        };
+        dtype == GS_F32 ? go(0.0f) : go(u16(0));
+        GS_HIP(hipGetLastError());
+    });
+}
+
+}  // extern "C"

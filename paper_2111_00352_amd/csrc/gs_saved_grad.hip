@@ -1,0 +1,287 @@
+// Weight gradient value(A)^T . G from activations saved in 8 bits: the
+// contraction over the n rows of an n x a matrix of codes and an n x b matrix of
+// gradients.
+//
+// A value is a code of at most 8 significant bits times a power of two, which
+// bf16 holds exactly.  An fp32 gradient is the sum of three bf16 numbers of 8
+// bits each (its significand cut twice), so three bf16 products with fp32 sums
+// give the fp32 product's accuracy at several times the fp32 matrix rate
+// (V_MFMA_F32_32X32X16_BF16: 2.5 PFLOP/s against 157 TFLOP/s), and a bf16 gradient
+// needs one.  That leaves the kernel bound by reading A and G once.
+//
+// Both operands are wanted with their rows, the k index of the product, running
+// inside a lane, and they lie in memory by rows.  A lane therefore loads CA
+// neighbouring columns of A (one dword at CA = 4) and CB of G in each of eight
+// rows: as many 8-deep fragments as it loads columns, without a trip through LDS,
+// of columns CA apart.  A wave's tile is 32 CA x 32 CB of the product.
+#include <algorithm>
+#include <type_traits>
+
+#include "gs_device.h"
+#include "gs_lowbit.h"
+
+namespace gs {
+namespace {
+
+typedef float f32x16 __attribute__((ext_vector_type(16)));
+typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
+
+constexpr int kGradWaves = 8;                   // of a workgroup, all on the same tile
+constexpr int kGradStep = 16;                   // rows a wave takes at a time
+constexpr int kGradRows = kGradWaves * kGradStep;
+// Longest run of rows a wave sums before the partials are joined.
+constexpr int64_t kGradChainRows = 8192;
+
+template <int C> struct CodeBytes;
+template <> struct CodeBytes<1> {
+    typedef uint8_t type;
+};
+template <> struct CodeBytes<2> {
+    typedef u16 type;
+};
+template <> struct CodeBytes<4> {
+    typedef uint32_t type;
+};
+
+// Upper halves of a (into the low half) and b.
+__device__ __forceinline__ uint32_t high_halves(uint32_t a, uint32_t b)
+{
+    return __builtin_amdgcn_perm(b, a, 0x07060302);
+}
+
+template <class T, int CA, int CB> struct GradStage {
+    typename CodeBytes<CA>::type code[8];
+    uint8_t scale[8];
+    typename Elems<T, CB>::type g[8];
+};
+
+// T, CA, CB as above; RELU: codes are unsigned.  Workgroup (x, y): rows
+// [x * per, (x + 1) * per), tile y; its sums go to part + x * a * b.
+template <class T, int CA, int CB, bool RELU>
+__global__ __launch_bounds__(kGradWaves * kWave, 2) void k_saved_grad(
+    const uint8_t *__restrict__ codes, int64_t code_pitch, const uint8_t *__restrict__ scales, int64_t scale_pitch,
+    const T *__restrict__ G, int64_t ldg, int64_t n, int a, int b, int64_t per, float *__restrict__ part)
+{
+    constexpr int NP = sizeof(T) == 4 ? 3 : 1;  // bf16 parts of a gradient
+    __shared__ float red[2][kGradWaves][16][kWave];
+    const int wave = threadIdx.x / kWave, lane = threadIdx.x % kWave;
+    const int nbt = (b + 32 * CB - 1) / (32 * CB);
+    const int a0 = (blockIdx.y / nbt) * 32 * CA, b0 = (blockIdx.y % nbt) * 32 * CB;
+    // Columns of lane l's fragments.  Lanes past the padded codes repeat its last
+    // columns, which are not stored if they are past a; a width b that is no
+    // multiple of CB ends in columns that two lanes hold (and store alike).
+    auto col_a = [&](int l) { const int c = a0 + CA * l; return c < (int)code_pitch - CA ? c : (int)code_pitch - CA; };
+    auto col_b = [&](int l) { const int c = b0 + CB * l; return c < b - CB ? c : b - CB; };
+    const int half = lane / 32;
+    const uint8_t *pc = codes + col_a(lane % 32);
+    const uint8_t *ps = scales + col_a(lane % 32) / kMxBlock;
+    const T *pg = G + col_b(lane % 32);
+    const int64_t r0 = (int64_t)blockIdx.x * per, r1 = r0 + per < n ? r0 + per : n;
+
+    GradStage<T, CA, CB> st;
+    auto load = [&](int64_t r) {  // rows r + 8 * half + 0..7, zeros from r1 on
+        const int64_t first = r + 8 * half;
+        if (r + kGradStep <= r1) {
+#pragma unroll
+            for (int j = 0; j < 8; j++) {
+                st.code[j] = *reinterpret_cast<const typename CodeBytes<CA>::type *>(pc + (first + j) * code_pitch);
+                st.scale[j] = ps[(first + j) * scale_pitch];
+                st.g[j] = *reinterpret_cast<const typename Elems<T, CB>::type *>(pg + (first + j) * ldg);
+            }
+        } else {
+#pragma unroll
+            for (int j = 0; j < 8; j++) {
+                st.code[j] = 0;
+                st.scale[j] = 0;
+                st.g[j] = typename Elems<T, CB>::type{};
+                if (first + j < r1) {
+                    st.code[j] = *reinterpret_cast<const typename CodeBytes<CA>::type *>(pc + (first + j) * code_pitch);
+                    st.scale[j] = ps[(first + j) * scale_pitch];
+                    st.g[j] = *reinterpret_cast<const typename Elems<T, CB>::type *>(pg + (first + j) * ldg);
+                }
+            }
+        }
+    };
+
+    f32x16 acc[CA][CB];
+#pragma unroll
+    for (int i = 0; i < CA; i++)
+#pragma unroll
+        for (int j = 0; j < CB; j++) acc[i][j] = f32x16{};
+
+    int64_t r = r0 + wave * kGradStep;
+    if (r < r1) load(r);
+    for (; r < r1; r += kGradRows) {
+        uint4 fa[CA], fb[NP][CB];
+        {
+            float s[8];
+#pragma unroll
+            for (int j = 0; j < 8; j++) s[j] = mx_scale(st.scale[j]);
+#pragma unroll
+            for (int i = 0; i < CA; i++) {
+                uint32_t v[8];
+#pragma unroll
+                for (int j = 0; j < 8; j++) {
+                    const int c = (int)(st.code[j] >> (8 * i) & 255);
+                    v[j] = __float_as_uint((float)(RELU ? c : (int)(int8_t)c) * s[j]);
+                }
+                fa[i] = make_uint4(high_halves(v[0], v[1]), high_halves(v[2], v[3]), high_halves(v[4], v[5]),
+                                   high_halves(v[6], v[7]));
+            }
+        }
+        if constexpr (NP == 1) {
+#pragma unroll
+            for (int i = 0; i < CB; i++)
+                fb[0][i] = make_uint4(st.g[0][i] | (uint32_t)st.g[1][i] << 16, st.g[2][i] | (uint32_t)st.g[3][i] << 16,
+                                      st.g[4][i] | (uint32_t)st.g[5][i] << 16, st.g[6][i] | (uint32_t)st.g[7][i] << 16);
+        } else {
+            // g = hi + mid + lo, each the leading 8 bits of what is left
+            float rest[CB][8], top = 0.0f;
+#pragma unroll
+            for (int i = 0; i < CB; i++)
+#pragma unroll
+                for (int j = 0; j < 8; j++) {
+                    const float x = st.g[j][i];
+                    top = fmaxf(top, fabsf(x));
+                    rest[i][j] = x - __uint_as_float(__float_as_uint(x) & 0xffff0000u);
+                }
+            if (__any(top == __builtin_inff())) {  // (infinity less itself: it is all in hi)
+#pragma unroll
+                for (int i = 0; i < CB; i++)
+#pragma unroll
+                    for (int j = 0; j < 8; j++)
+                        if (fabsf(st.g[j][i]) == __builtin_inff()) rest[i][j] = 0.0f;
+            }
+#pragma unroll
+            for (int i = 0; i < CB; i++) {
+                uint32_t hi[8], mid[8], lo[8];
+#pragma unroll
+                for (int j = 0; j < 8; j++) {
+                    hi[j] = __float_as_uint((float)st.g[j][i]);
+                    mid[j] = __float_as_uint(rest[i][j]);
+                    lo[j] = __float_as_uint(rest[i][j] - __uint_as_float(mid[j] & 0xffff0000u));
+                }
+                fb[0][i] = make_uint4(high_halves(hi[0], hi[1]), high_halves(hi[2], hi[3]), high_halves(hi[4], hi[5]),
+                                      high_halves(hi[6], hi[7]));
+                fb[NP > 1 ? 1 : 0][i] = make_uint4(high_halves(mid[0], mid[1]), high_halves(mid[2], mid[3]),
+                                                   high_halves(mid[4], mid[5]), high_halves(mid[6], mid[7]));
+                fb[NP > 1 ? 2 : 0][i] = make_uint4(high_halves(lo[0], lo[1]), high_halves(lo[2], lo[3]),
+                                                   high_halves(lo[4], lo[5]), high_halves(lo[6], lo[7]));
+            }
+        }
+        if (r + kGradRows < r1) load(r + kGradRows);
+#pragma unroll
+        for (int p = NP - 1; p >= 0; p--)
+#pragma unroll
+            for (int i = 0; i < CA; i++)
+#pragma unroll
+                for (int j = 0; j < CB; j++)
+                    acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, fa[i]),
+                                                                        __builtin_bit_cast(bf16x8, fb[p][j]),
+                                                                        acc[i][j], 0, 0, 0);
+    }
+
+    // The waves' sums are added in LDS, one 32 x 32 tile at a time, and stored as
+    // the workgroup's partial.  Accumulator: lane l, register e hold row
+    // 8 (e / 4) + 4 (l / 32) + e % 4, column l % 32.
+    float *out = part + (int64_t)blockIdx.x * a * b;
+#pragma unroll
+    for (int t = 0; t < CA * CB; t++) {
+        const int i = t / CB, j = t % CB;
+#pragma unroll
+        for (int e = 0; e < 16; e++) red[t & 1][wave][e][lane] = acc[i][j][e];
+        __syncthreads();
+        // (the other buffer's readers are past this barrier before it is written again)
+#pragma unroll
+        for (int q = 0; q < 16 / kGradWaves; q++) {
+            const int e = wave * (16 / kGradWaves) + q;
+            float s = 0.0f;
+#pragma unroll
+            for (int w = 0; w < kGradWaves; w++) s += red[t & 1][w][e][lane];
+            const int row = col_a(8 * (e / 4) + 4 * half + e % 4) + i, col = col_b(lane % 32) + j;
+            if (row < a) out[(int64_t)row * b + col] = s;
+        }
+    }
+}
+
+struct GradPlan {
+    int ca, cb;
+    int64_t tiles, chunks, per;
+};
+
+GradPlan grad_plan(int64_t n, int64_t a, int64_t b)
+{
+    GradPlan p;
+    p.ca = a <= 32 ? 1 : a <= 64 ? 2 : 4;
+    p.cb = b <= 32 ? 1 : 2;
+    p.tiles = ceil_div(a, 32 * p.ca) * ceil_div(b, 32 * p.cb);
+    const int64_t want = std::max(std::max<int64_t>(1, 256 / p.tiles), ceil_div(n, kGradChainRows * kGradWaves));
+    p.chunks = std::max<int64_t>(1, std::min(want, ceil_div(n, kGradRows)));
+    p.per = ceil_div(ceil_div(std::max<int64_t>(n, 1), p.chunks), kGradRows) * kGradRows;
+    p.chunks = std::max<int64_t>(1, ceil_div(n, p.per));
+    return p;
+}
+
+void check_grad_sizes(int64_t n, int64_t a, int64_t b)
+{
+    if (n < 0 || a <= 0 || b <= 0) fail(GS_ERR_INVALID_ARG, "bad product size");
+    if (a > 4096 || b > 4096 || n > INT32_MAX) fail(GS_ERR_UNSUPPORTED, "a and b are at most 4096");
+}
+
+}  // namespace
+}  // namespace gs
+
+using namespace gs;
+
+extern "C" {
+
+int gs_saved_weight_grad_workspace(int64_t n, int64_t a, int64_t b, uint64_t *bytes)
+{
+    return guarded([&] {
+        if (!bytes) fail(GS_ERR_INVALID_ARG, "null output");
+        check_grad_sizes(n, a, b);
+        const GradPlan p = grad_plan(n, a, b);
+        *bytes = p.chunks > 1 ? (uint64_t)(p.chunks * a * b) * 4 : 0;
+    });
+}
+
+int gs_saved_weight_grad(const gs_saved *A, const void *G, int64_t ldg, int dtype, int64_t b, float *out,
+                         void *work, uint64_t work_bytes, gs_stream stream)
+{
+    return guarded([&] {
+        check_saved(A, false);
+        const int64_t n = A->rows, a = A->cols;
+        check_grad_sizes(n, a, b);
+        check_operand("G", G, n, b, ldg, dtype_size(dtype));
+        if (!out) fail(GS_ERR_INVALID_ARG, "null output");
+        const GradPlan p = grad_plan(n, a, b);
+        const uint64_t need = p.chunks > 1 ? (uint64_t)(p.chunks * a * b) * 4 : 0;
+        if (work_bytes < need || (need && !work))
+            fail(GS_ERR_INVALID_ARG, "workspace of %llu bytes is below the %llu needed",
+                 (unsigned long long)(work ? work_bytes : 0), (unsigned long long)need);
+        const hipStream_t s = (hipStream_t)stream;
+        float *part = p.chunks > 1 ? (float *)work : out;
+        const dim3 grid((unsigned)p.chunks, (unsigned)p.tiles);
+        auto go = [&](auto ca, auto cb, auto type, auto relu) {
+            using T = decltype(type);
+            k_saved_grad<T, decltype(ca)::value, decltype(cb)::value, decltype(relu)::value>
+                <<<grid, kGradWaves * kWave, 0, s>>>(A->codes, saved_code_pitch(a), A->scales, saved_scale_pitch(a),
+                                                    (const T *)G, ldg, n, (int)a, (int)b, p.per, part);
+        };
+        auto typed = [&](auto ca, auto cb) {
+            if (p.ca != decltype(ca)::value || p.cb != decltype(cb)::value) return;
+            if (dtype == GS_F32)
+                A->act == GS_ACT_RELU ? go(ca, cb, 0.0f, std::true_type{}) : go(ca, cb, 0.0f, std::false_type{});
+            else
+                A->act == GS_ACT_RELU ? go(ca, cb, u16(0), std::true_type{}) : go(ca, cb, u16(0), std::false_type{});
+        };
+        using C1 = std::integral_constant<int, 1>;
+        using C2 = std::integral_constant<int, 2>;
+        using C4 = std::integral_constant<int, 4>;
+        typed(C1{}, C1{}), typed(C1{}, C2{}), typed(C2{}, C1{}), typed(C2{}, C2{}), typed(C4{}, C1{}), typed(C4{}, C2{});
+        GS_HIP(hipGetLastError());
+        if (p.chunks > 1) reduce_partials(part, (int)p.chunks, a * b, out, s);
+    });
+}
+
+}  // extern "C"

@@ -16,8 +16,13 @@ the same key when the caller declares A symmetric (GCN-normalised adjacencies
 are).  The dense products H W and G W^T are PyTorch fp32 matmuls, the weight
 gradient H^T G (an n-long reduction) is the library's matrix-core kernel; ReLU and the loss are PyTorch element-wise operations.
 
+``lowbit`` trains with less memory: "saved8" keeps the hidden layer's activations in
+8 bits between forward and backward (and nothing else of them) and takes the second
+layer's weight gradient and the ReLU's mask from those; "mxfp4" also forms the dense
+products H W and G W^T in MXFP4 (weight gradients stay in fp32).
+
 Command line (end-to-end timing of one workload):
-    python -m paper_2111_00352_amd.gcn --config 2 --epochs 10
+    python -m paper_2111_00352_amd.gcn --config 2 --epochs 10 [--lowbit saved8|mxfp4]
 """
 from __future__ import annotations
 
@@ -142,14 +147,70 @@ class _Linear(torch.autograd.Function):
         return dH, dW
 
 
-class GCN2:
-    """Weights of the two layers (fp32, on the device); forward and SGD step."""
+class _LinearMx(torch.autograd.Function):
+    """H W with the product (and that of the input's gradient) in MXFP4."""
 
-    def __init__(self, W1: torch.Tensor, W2: torch.Tensor):
+    @staticmethod
+    def forward(ctx, H, W):
+        H = H.contiguous()
+        ctx.save_for_backward(H, W)
+        return gs.mxfp4_matmul(H, gs.mxfp4_quantize(W, axis=0))
+
+    @staticmethod
+    def backward(ctx, G):
+        H, W = ctx.saved_tensors
+        G = G.contiguous()
+        dH = gs.mxfp4_matmul(G, gs.mxfp4_quantize(W)) if ctx.needs_input_grad[0] else None
+        dW = weight_grad(H, G) if ctx.needs_input_grad[1] else None
+        return dH, dW
+
+
+class _ReluLinear(torch.autograd.Function):
+    """relu(P) W, of whose input only relu(P) in 8 bits is kept for the backward pass."""
+
+    @staticmethod
+    def forward(ctx, P, W, mx):
+        H, ctx.act = gs.save_activation(P.contiguous(), "relu")
+        ctx.mx = mx
+        ctx.save_for_backward(W)
+        return gs.mxfp4_matmul(H, gs.mxfp4_quantize(W, axis=0)) if mx else H @ W
+
+    @staticmethod
+    def backward(ctx, G):
+        W, = ctx.saved_tensors
+        G = G.contiguous()
+        dP = dW = None
+        if ctx.needs_input_grad[0]:
+            if ctx.mx:
+                dP = gs.mxfp4_matmul(G, gs.mxfp4_quantize(W), mask=ctx.act)
+            else:
+                dP = G @ W.t()
+                gs.relu_grad(ctx.act, dP, out=dP)
+        if ctx.needs_input_grad[1]:
+            dW = gs.saved_weight_grad(ctx.act, G)
+        return dP, dW, None
+
+
+LOWBIT = (None, "saved8", "mxfp4")
+
+
+class GCN2:
+    """Weights of the two layers (fp32, on the device); forward and SGD step.
+    lowbit: None, "saved8" or "mxfp4" (see the module's text); P1 is then not kept
+    and None takes its place."""
+
+    def __init__(self, W1: torch.Tensor, W2: torch.Tensor, lowbit: str | None = None):
+        if lowbit not in LOWBIT:
+            raise ValueError("lowbit must be None, 'saved8' or 'mxfp4'")
         self.W1 = W1.detach().clone().requires_grad_(True)
         self.W2 = W2.detach().clone().requires_grad_(True)
+        self.lowbit = lowbit
 
     def forward(self, X, adj: Adjacency):
+        if self.lowbit:
+            mx = self.lowbit == "mxfp4"
+            Z = (_LinearMx if mx else _Linear).apply(X, self.W1)
+            return aggregate(_ReluLinear.apply(aggregate(Z, adj), self.W2, mx), adj), None
         P1 = aggregate(_Linear.apply(X, self.W1), adj)
         H1 = torch.relu(P1)
         return aggregate(_Linear.apply(H1, self.W2), adj), P1
@@ -168,10 +229,11 @@ class GCN2:
         with torch.no_grad():
             self.W1 -= lr * self.W1.grad
             self.W2 -= lr * self.W2.grad
-        return loss.detach(), Out.detach(), P1.detach()
+        return loss.detach(), Out.detach(), None if P1 is None else P1.detach()
 
 
-def train(adj: Adjacency, X, T, W1, W2, epochs: int, lr: float, graph: bool = False):
+def train(adj: Adjacency, X, T, W1, W2, epochs: int, lr: float, graph: bool = False,
+          lowbit: str | None = None):
     """Trains for `epochs` steps; returns (model, per-epoch losses, seconds per epoch).
 
     graph=True: the first two epochs run eagerly (format selection, conversion
@@ -181,7 +243,7 @@ def train(adj: Adjacency, X, T, W1, W2, epochs: int, lr: float, graph: bool = Fa
     frozen in the graph, as the paper decides it once per layer across
     epochs (Sec. 5.2); every SpMM path launches kernels only once warm (no
     allocation, memset or synchronisation), so it records cleanly."""
-    model = GCN2(W1, W2)
+    model = GCN2(W1, W2, lowbit)
     losses, times = [], []
     eager = epochs if not graph else min(epochs, 2)
     for e in range(eager):
@@ -214,7 +276,7 @@ def train(adj: Adjacency, X, T, W1, W2, epochs: int, lr: float, graph: bool = Fa
 
 
 def end_to_end(row, col, val, shape, X, T, W1, W2, epochs=10, lr=0.1, symmetric=False,
-               modes=("model", "fixed:csr", "fixed:coo"), graph=False, passes=2):
+               modes=("model", "fixed:csr", "fixed:coo"), graph=False, passes=2, lowbit=None):
     """Trains once per selection mode, each with a fresh context (so every
     first-call cost -- features, prediction, conversion -- is paid inside the
     timed epochs), and reports total time and the speedups of the first mode
@@ -230,7 +292,7 @@ def end_to_end(row, col, val, shape, X, T, W1, W2, epochs=10, lr=0.1, symmetric=
         name, _, fixed = mode.partition(":")
         warm = SelectContext(name, fixed=fixed or "csr")
         train(Adjacency(row, col, val, shape, warm, key=1, symmetric=symmetric), X, T, W1, W2,
-              3 if graph else 1, lr, graph=graph)
+              3 if graph else 1, lr, graph=graph, lowbit=lowbit)
         warm.close()
     res = {}
     for _ in range(max(1, passes)):
@@ -239,7 +301,7 @@ def end_to_end(row, col, val, shape, X, T, W1, W2, epochs=10, lr=0.1, symmetric=
             ctx = SelectContext(name, fixed=fixed or "csr")
             adj = Adjacency(row, col, val, shape, ctx, key=7, symmetric=symmetric)
             torch.cuda.synchronize()
-            _, losses, times = train(adj, X, T, W1, W2, epochs, lr, graph=graph)
+            _, losses, times = train(adj, X, T, W1, W2, epochs, lr, graph=graph, lowbit=lowbit)
             res[mode] = {
                 "total_s": sum(times), "first_epoch_s": times[0],
                 "steady_epoch_s": sorted(times[1:])[len(times[1:]) // 2] if len(times) > 1 else times[0],
@@ -261,6 +323,7 @@ def main():
     ap.add_argument("--out", type=int, default=64)
     ap.add_argument("--lr", type=float, default=0.02)
     ap.add_argument("--graph", action="store_true", help="replay a captured training step after two epochs")
+    ap.add_argument("--lowbit", choices=[m for m in LOWBIT if m], help="8-bit saved activations, MXFP4 products")
     a = ap.parse_args()
     sys.path.insert(0, os.path.dirname(os.path.dirname(os.path.abspath(__file__))))
     import graphgen
@@ -274,9 +337,9 @@ def main():
     W2 = torch.from_numpy(graphgen.features_x(a.hidden, a.out, 4200 + a.config, "normal")).to(dev) / a.hidden ** 0.5
     T = torch.from_numpy(graphgen.features_x(g.R, a.out, 4300 + a.config, "normal")).to(dev)
     res = end_to_end(row, col, val, (g.R, g.C), X, T, W1, W2, a.epochs, a.lr,
-                     symmetric=bool(g.meta.get("symmetric", False)), graph=a.graph)
+                     symmetric=bool(g.meta.get("symmetric", False)), graph=a.graph, lowbit=a.lowbit)
     print(json.dumps({"workload": g.name, "epochs": a.epochs, "hidden": a.hidden, "out": a.out,
-                      "graph": a.graph, **res}))
+                      "graph": a.graph, "lowbit": a.lowbit, **res}))
 
 
 if __name__ == "__main__":

@@ -1,0 +1,110 @@
+"""Host side of the low-bit operators: the oracle's formats against hand-worked
+blocks, and the library's argument checks, none of which needs a GPU."""
+import ctypes
+
+import numpy as np
+import pytest
+
+import paper_2111_00352_amd as gs
+from oracle import lowbit
+
+
+def test_oracle_save8_by_hand():
+    x = np.zeros((1, 33))
+    x[0, :5] = [1.0, 0.004, -3.0, 0.5, 1.99609375]  # step 2^-7
+    x[0, 32] = 1e-3
+    q, E, v, h, on = lowbit.save8(x, True)
+    assert E.tolist() == [[127 - 7, 127 - 10 - 7]]
+    assert q[0, :5].tolist() == [128, 1, 0, 64, 255] and q[0, 32] == 131
+    assert v[0, 4] == 255 / 128 and on[0, :5].tolist() == [True, True, False, True, True]
+    q, E, v, _, _ = lowbit.save8(np.array([[2.0 ** 6, -127.6, 0.5, 1.5, 2.5]]), False)  # step 1
+    assert E.tolist() == [[127]] and q.tolist() == [[64, -127, 0, 2, 2]]
+    q, E, v, _, _ = lowbit.save8(np.array([[np.nan, 1.0, -1.0, 0.0]]), True)
+    assert E.tolist() == [[255]] and q.tolist() == [[1, 1, 0, 0]] and np.isnan(v).all()
+    assert lowbit.save8(np.array([[2.0 ** -149, 0.0]]), True)[0].tolist() == [[1, 0]]  # step 2^-126
+
+
+def test_oracle_quant4_by_hand():
+    code, E, v = lowbit.quant4(np.array([[4.0, 5.0, 7.9, -0.25, 0.25, 0.75, 1.75, 2.5, 3.5, -1.25, 0.2500001]]))
+    assert E.tolist() == [[127]]
+    assert v.tolist() == [[4.0, 4.0, 6.0, 0.0, 0.0, 1.0, 2.0, 2.0, 4.0, -1.0, 0.5]]
+    assert code.tolist() == [[6, 6, 7, 8, 0, 2, 4, 4, 6, 10, 1]]
+    code, E, v = lowbit.quant4(np.array([[0.0, -0.0]]))
+    assert E.tolist() == [[0]] and code.tolist() == [[0, 8]]
+    code, E, v = lowbit.quant4(np.array([[np.inf, 1.0]]))
+    assert E.tolist() == [[255]] and code.tolist() == [[0, 0]] and np.isnan(v).all()
+
+
+def test_layouts():
+    a, b = ctypes.c_int64(), ctypes.c_int64()
+    for cols, pitches in ((0, (0, 0)), (1, (32, 1)), (32, (32, 1)), (33, (64, 2)), (128, (128, 4))):
+        assert gs.lib().gs_saved_layout(cols, ctypes.byref(a), ctypes.byref(b)) == 0
+        assert (a.value, b.value) == pitches
+    for cols, pitches in ((0, (0, 0)), (1, (32, 2)), (64, (32, 2)), (65, (64, 4)), (128, (64, 4)), (129, (128, 8))):
+        assert gs.lib().gs_mxfp4_layout(cols, ctypes.byref(a), ctypes.byref(b)) == 0
+        assert (a.value, b.value) == pitches
+    for fn in (gs.lib().gs_saved_layout, gs.lib().gs_mxfp4_layout):
+        assert fn(-1, ctypes.byref(a), ctypes.byref(b)) == gs.ERR_INVALID_ARG
+        assert fn((1 << 24) + 1, ctypes.byref(a), ctypes.byref(b)) == gs.ERR_UNSUPPORTED
+        assert fn(5, None, ctypes.byref(b)) == gs.ERR_INVALID_ARG
+
+
+def _saved(rows=4, cols=8, act=1, codes=256, scales=256):
+    return ctypes.byref(gs._Saved(rows, cols, act, codes, scales))
+
+
+def _mx(rows=4, cols=8, codes=256, scales=256):
+    return ctypes.byref(gs._Mxfp4(rows, cols, codes, scales))
+
+
+def test_argument_checks():
+    # (addresses are never dereferenced: every call is refused on the host)
+    L, bad, P = gs.lib(), gs.ERR_INVALID_ARG, 512
+    need = ctypes.c_uint64()
+    assert L.gs_save_activation(None, 8, 0, _saved(), None, 0, None) == bad
+    assert L.gs_save_activation(P, 7, 0, _saved(), None, 0, None) == bad
+    assert L.gs_save_activation(P, 8, 2, _saved(), None, 0, None) == bad
+    assert L.gs_save_activation(P + 2, 8, 0, _saved(), None, 0, None) == bad
+    assert L.gs_save_activation(P, 1 << 61, 0, _saved(), None, 0, None) == bad
+    assert L.gs_save_activation(P, 8, 0, _saved(act=2), None, 0, None) == bad
+    assert L.gs_save_activation(P, 8, 0, _saved(codes=264), None, 0, None) == bad
+    assert L.gs_save_activation(P, 8, 0, _saved(scales=None), None, 0, None) == bad
+    assert L.gs_save_activation(P, 8, 0, _saved(), P, 7, None) == bad
+    assert L.gs_save_activation(P, 8, 0, None, None, 0, None) == bad
+    assert L.gs_save_activation(P, 1 << 25, 0, _saved(cols=1 << 25), None, 0, None) == gs.ERR_UNSUPPORTED
+    assert L.gs_saved_dequantize(_saved(rows=-1), P, 8, 0, None) == bad
+    assert L.gs_relu_grad(_saved(act=0), P, 8, 0, P, 8, None) == bad
+    assert L.gs_relu_grad(_saved(), P, 8, 0, None, 8, None) == bad
+    assert L.gs_saved_weight_grad_workspace(5, 0, 1, ctypes.byref(need)) == bad
+    assert L.gs_saved_weight_grad_workspace(5, 1, 4097, ctypes.byref(need)) == gs.ERR_UNSUPPORTED
+    assert L.gs_saved_weight_grad_workspace(5, 1, 1, None) == bad
+    assert L.gs_saved_weight_grad_workspace(100_000, 128, 64, ctypes.byref(need)) == 0 and need.value > 0
+    assert L.gs_saved_weight_grad(_saved(rows=100_000), P, 8, 0, 8, P, P, 16, None) == bad
+    assert L.gs_saved_weight_grad(_saved(), P, 8, 0, 8, None, P, 1 << 30, None) == bad
+    assert L.gs_mxfp4_quantize(P, 8, 0, 4, 8, 2, _mx(), None) == bad
+    assert L.gs_mxfp4_quantize(P, 8, 0, 4, 8, 0, _mx(), None) == bad
+    assert L.gs_mxfp4_quantize(P, 8, 0, 4, 8, 1, _mx(scales=258), None) == bad
+    assert L.gs_mxfp4_dequantize(_mx(), P, 7, 0, None) == bad
+    assert L.gs_mxfp4_matmul(_mx(), _mx(cols=9), None, P, 4, 0, None, 0, None) == bad
+    assert L.gs_mxfp4_matmul(_mx(), _mx(), None, P, 3, 0, None, 0, None) == bad
+    assert L.gs_mxfp4_matmul(_mx(), _mx(), _saved(rows=4, cols=5), P, 4, 0, None, 0, None) == bad
+    assert L.gs_mxfp4_matmul(_mx(), _mx(), _saved(rows=4, cols=4, act=0), P, 4, 0, None, 0, None) == bad
+    assert L.gs_mxfp4_matmul_dense(P, 7, 0, 4, _mx(), None, P, 4, 0, P, 1 << 20, None) == bad
+    assert L.gs_mxfp4_matmul_dense(P, 8, 5, 4, _mx(), None, P, 4, 0, P, 1 << 20, None) == bad
+    assert L.gs_mxfp4_matmul_workspace(-1, 4, 8, -1, ctypes.byref(need)) == bad
+    assert L.gs_mxfp4_matmul_workspace(4, 4, 8, 3, ctypes.byref(need)) == bad
+    assert b"workspace" not in L.gs_last_error()
+
+
+def test_null_stream_calls_on_empty_operands_succeed():
+    L = gs.lib()
+    assert L.gs_save_activation(None, 8, 0, _saved(rows=0, codes=None, scales=None), None, 0, None) == 0
+    assert L.gs_mxfp4_quantize(None, 8, 0, 0, 8, 1, _mx(rows=0, codes=None, scales=None), None) == 0
+
+
+def test_python_refuses_cpu_tensors():
+    import torch
+    with pytest.raises(ValueError):
+        gs.save_activation(torch.zeros(2, 2))
+    with pytest.raises(ValueError):
+        gs.mxfp4_quantize(torch.zeros(2, 2))
