@@ -28,6 +28,16 @@ __device__ __forceinline__ uint32_t mx4_pack8(const float *x, int E)
     return E == 255 ? 0 : w;
 }
 
+// Four elements likewise.
+__device__ __forceinline__ uint16_t mx4_pack4(const float *x, int E)
+{
+    const float inv = mx_inverse(E);
+    uint32_t w = 0;
+    w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, x[0] * inv, x[1] * inv, 1.0f, 0);
+    w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, x[2] * inv, x[3] * inv, 1.0f, 1);
+    return E == 255 ? 0 : (uint16_t)w;
+}
+
 // X (rows x cols of dtype) along its rows into codes and scales in the layout
 // of gs_mxfp4, enqueued on s.
 void mx4_quantize_rows(const void *X, int64_t ldx, int dtype, int64_t rows, int64_t cols, uint8_t *codes,

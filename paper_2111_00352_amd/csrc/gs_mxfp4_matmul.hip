@@ -26,62 +26,405 @@ template <int OP> __device__ __forceinline__ f32x16 mfma_fp4(u32x4 a, int sa, u3
 }
 
 // Where C goes: element (row, col) as T, 0 where the mask's code is 0.
-template <class T, bool MASK> struct Out {
+template <class T> struct Out {
+    using type = T;
     T *c;
     int64_t ld;
     const uint8_t *mask;
     int64_t mask_pitch;
-    __device__ __forceinline__ void store(int64_t row, int64_t col, float v) const
+    // Columns col .. col + E - 1 (col a multiple of E, E 4 or 8) as far as they are below n.
+    template <int E> __device__ __forceinline__ void store_row(int64_t row, int64_t col, int64_t n, typename Elems<T, E>::type v) const
     {
-        if (MASK && mask[row * mask_pitch + col] == 0) v = 0.0f;
-        c[row * ld + col] = from_f32<T>(v);
+        if (mask) {
+            const uint32_t *p = reinterpret_cast<const uint32_t *>(mask + row * mask_pitch + col);
+#pragma unroll
+            for (int e = 0; e < E; e++)
+                if ((p[e / 4] >> 8 * (e % 4) & 255) == 0) v[e] = T(0);
+        }
+        store_elems<T, E>(c + row * ld + col, v, n - col);
     }
 };
 
-// Four waves, 128 x 128 of C, a wave 64 x 64; operands straight from memory.
-template <class T, bool MASK>
-__global__ __launch_bounds__(256) void k_matmul(const uint8_t *__restrict__ ac, const uint8_t *__restrict__ as,
-                                                const uint8_t *__restrict__ bc, const uint8_t *__restrict__ bs,
-                                                int64_t m, int64_t n, int kpad, int64_t tiles_n, int64_t tiles,
-                                                Out<T, MASK> out)
-{
-    const int wave = threadIdx.x / kWave, lane = threadIdx.x % kWave;
-    const int64_t cp = kpad / 2, sp = kpad / kMxBlock;
-    for (int64_t t = blockIdx.x; t < tiles; t += gridDim.x) {
-        const int64_t m0 = (t / tiles_n) * 128 + (wave / 2) * 64, n0 = (t % tiles_n) * 128 + (wave % 2) * 64;
-        f32x16 acc[2][2] = {};
-        int64_t ra[2], rb[2];
+// A wave's 32 rows x COLS columns of C on their way through LDS: accumulators hold
+// four neighbouring columns of 32 rows, stores want whole lines.
+template <class T, int COLS> struct Staged {
+    static constexpr int E = 16 / sizeof(T);
+    static constexpr int kTiles = COLS / 32;
+    static constexpr int kPitch = COLS * sizeof(T) + 16;  // (the shift spreads rows over banks)
+    static constexpr int kBytes = 32 * kPitch;
+    static constexpr int kLanes = COLS / E, kRows = 64 / kLanes;  // lanes of a row, rows of a store
+    uint8_t *lds;
+    int lane;
+    // acc: lane l, registers 4 g .. 4 g + 3 hold columns 8 g + 4 (l / 32) .. + 3 of row l % 32
+    __device__ __forceinline__ void put(int tile, const f32x16 &acc) const
+    {
 #pragma unroll
-        for (int i = 0; i < 2; i++) {
-            ra[i] = std::min<int64_t>(m0 + 32 * i + lane % 32, m - 1);
-            rb[i] = std::min<int64_t>(n0 + 32 * i + lane % 32, n - 1);
+        for (int g = 0; g < 4; g++) {
+            typedef T quad __attribute__((ext_vector_type(4)));
+            const quad v = {from_f32<T>(acc[4 * g]), from_f32<T>(acc[4 * g + 1]), from_f32<T>(acc[4 * g + 2]),
+                            from_f32<T>(acc[4 * g + 3])};
+            *reinterpret_cast<quad *>(lds + lane % 32 * kPitch + (32 * tile + 8 * g + 4 * (lane / 32)) * sizeof(T)) = v;
         }
-        for (int k = 0; k < kpad; k += 64) {
-            u32x4 a[2], b[2];
-            int sa[2], sb[2];
+    }
+    // Rows m0 .. m0 + 31 below m, columns from col0 on below n.
+    __device__ __forceinline__ void store(const Out<T> &out, int64_t m0, int64_t m, int64_t col0, int64_t n) const
+    {
+        typedef T whole __attribute__((ext_vector_type(E)));
+        __builtin_amdgcn_wave_barrier();  // (a wave's LDS operations keep their order)
+        const int64_t col = col0 + lane % kLanes * E;
+        whole v[32 / kRows];
 #pragma unroll
-            for (int i = 0; i < 2; i++) {
-                const int blk = k / 32 + lane / 32;
-                a[i] = *reinterpret_cast<const u32x4 *>(ac + ra[i] * cp + blk * 16);
-                b[i] = *reinterpret_cast<const u32x4 *>(bc + rb[i] * cp + blk * 16);
-                sa[i] = as[ra[i] * sp + blk];
-                sb[i] = bs[rb[i] * sp + blk];
+        for (int i = 0; i < 32 / kRows; i++)
+            v[i] = *reinterpret_cast<const whole *>(lds + (kRows * i + lane / kLanes) * kPitch + lane % kLanes * 16);
+        __builtin_amdgcn_wave_barrier();
+#pragma unroll
+        for (int i = 0; i < 32 / kRows; i++) {
+            const int64_t row = m0 + kRows * i + lane / kLanes;
+            if (row < m && col < n) out.template store_row<E>(row, col, n, v[i]);
+        }
+    }
+};
+
+// ------------------------------------------- many rows, up to 512 of k (layers)
+//
+// Bound by memory: A is read and C written once, B (a layer's weights) is small.
+// A workgroup keeps a panel of B in LDS, as the fragments the instructions take;
+// each wave takes 32 rows of A at a time, holds their fragments in registers and
+// passes over the panel.  B is the instruction's first operand, so a lane ends up
+// with four neighbouring columns of one row of C.
+//
+// A dense A is quantised on the way: the wave loads its rows as they lie in memory
+// (8 or 4 lanes a block), finds each block's scale across those lanes and lets LDS
+// turn the codes into fragments (a lane a block).
+constexpr int kNarrowWaves = 4;
+constexpr int kNarrowMaxK = 512;
+constexpr int kNarrowTmp = 64 * (16 + 1);  // bytes of LDS for a wave's quantisation
+constexpr int kNarrowLine = 128;           // bytes of a row of C it stores at a time, and of LDS for that
+constexpr int kNarrowOut = 32 * (kNarrowLine + 16);
+
+// A as it is given: MXFP4 codes and scales, or dense.
+struct MxRows {
+    const uint8_t *codes, *scales;
+    int64_t code_pitch;
+    int scale_pitch;
+    int width() const { return scale_pitch * kMxBlock; }
+};
+template <class T> struct DenseRows {
+    const T *p;
+    int64_t ld;
+    int cols;
+    int width() const { return cols; }
+};
+
+// Row source of a wave: fragments of rows m0 + lane % 32, KS times 64 of k: f[ks],
+// and their scale bytes, four ks a word.  start() once with the first m0, then
+// rows(m0, the one after it) for each.  Loads are issued early, into the next rows at
+// the end of these, before this wave's stores to C (a load waits for the stores
+// issued before it).
+template <class Rows, int KS, bool FULL> struct RowSource;
+
+template <int KS, bool FULL> struct RowSource<MxRows, KS, FULL> {
+    const MxRows &A;
+    int lane;
+    u32x4 nf[KS];
+    uint32_t ns[(KS + 3) / 4];
+    __device__ __forceinline__ RowSource(const MxRows &A_, int lane_, uint8_t *) : A(A_), lane(lane_) {}
+    __device__ __forceinline__ void start(int64_t m0)
+    {
+        const int64_t row = m0 + lane % 32;
+        const uint8_t *c = A.codes + row * A.code_pitch, *s = A.scales + row * A.scale_pitch;
+#pragma unroll
+        for (int q = 0; q < (KS + 3) / 4; q++) ns[q] = 0;
+#pragma unroll
+        for (int ks = 0; ks < KS; ks++) {
+            const int blk = 2 * ks + lane / 32;
+            nf[ks] = u32x4{};
+            if (FULL || blk < A.scale_pitch) {
+                nf[ks] = *reinterpret_cast<const u32x4 *>(c + 16 * blk);
+                ns[ks / 4] |= (uint32_t)s[blk] << 8 * (ks % 4);
             }
-#pragma unroll
-            for (int i = 0; i < 2; i++)
-#pragma unroll
-                for (int j = 0; j < 2; j++) acc[i][j] = mfma_fp4<0>(a[i], sa[i], b[j], sb[j], acc[i][j]);
         }
+    }
+    __device__ __forceinline__ void rows(int64_t, int64_t next, int64_t m, u32x4 *f, uint32_t *sc)
+    {
 #pragma unroll
-        for (int i = 0; i < 2; i++)
+        for (int ks = 0; ks < KS; ks++) f[ks] = nf[ks];
 #pragma unroll
-            for (int j = 0; j < 2; j++)
+        for (int q = 0; q < (KS + 3) / 4; q++) sc[q] = ns[q];
+        if (next < m) start(std::min(next, m - 32));
+    }
+};
+
+// Dense rows.  tmp: this wave's kNarrowTmp bytes of LDS.
+template <class T, int KS, bool FULL> struct RowSource<DenseRows<T>, KS, FULL> {
+    static constexpr int E = 16 / sizeof(T), L = kMxBlock / E;  // elements a lane, lanes a block
+    static constexpr int RB = 64 / (2 * L);                     // rows of a load instruction (two blocks of each)
+    static constexpr int N = 32 / RB;                           // load instructions of a slice (64 of k)
+    static constexpr int kAhead = KS < 2 ? 1 : 2;               // slices
+    const DenseRows<T> &A;
+    int lane;
+    uint8_t *tmp;
+    int64_t off;  // of this lane's elements from the first row's of a load
+    typename Elems<T, E>::type v[kAhead][N];
+    __device__ __forceinline__ RowSource(const DenseRows<T> &A_, int lane_, uint8_t *tmp_) : A(A_), lane(lane_), tmp(tmp_)
+    {
+        off = lane / (2 * L) * A.ld + lane % (2 * L) * E;
+    }
+    __device__ __forceinline__ void load(int64_t m0, int ks)
+    {
+        const T *p = A.p + m0 * A.ld + 64 * ks;
 #pragma unroll
-                for (int e = 0; e < 16; e++) {
-                    const int64_t row = m0 + 32 * i + 8 * (e / 4) + 4 * (lane / 32) + e % 4;
-                    const int64_t col = n0 + 32 * j + lane % 32;
-                    if (row < m && col < n) out.store(row, col, acc[i][j][e]);
+        for (int i = 0; i < N; i++) {
+            const T *q = p + i * RB * A.ld + off;
+            v[ks % kAhead][i] = FULL ? *reinterpret_cast<const typename Elems<T, E>::type *>(q)
+                                     : load_elems<T, E>(q, A.cols - 64 * ks - lane % (2 * L) * E);
+        }
+    }
+    __device__ __forceinline__ void start(int64_t m0)
+    {
+#pragma unroll
+        for (int ks = 0; ks < kAhead; ks++) load(m0, ks);
+    }
+    __device__ __forceinline__ void rows(int64_t m0, int64_t next, int64_t m, u32x4 *f, uint32_t *sc)
+    {
+#pragma unroll
+        for (int q = 0; q < (KS + 3) / 4; q++) sc[q] = 0;
+#pragma unroll
+        for (int ks = 0; ks < KS; ks++) {
+#pragma unroll
+            for (int i = 0; i < N; i++) {
+                float x[E];
+                uint32_t top = 0;
+#pragma unroll
+                for (int e = 0; e < E; e++) {
+                    x[e] = to_f32(v[ks % kAhead][i][e]);
+                    const uint32_t b = __float_as_uint(x[e]) & 0x7fffffffu;
+                    top = b > top ? b : top;
                 }
+                const int E8 = mx4_exponent(group_max<L>(top));
+                // block (row, h) as lane 32 h + row of the fragment
+                const int to = lane / L % 2 * 32 + i * RB + lane / (2 * L);
+                if constexpr (E == 8)
+                    *reinterpret_cast<uint32_t *>(tmp + 16 * to + lane % L * 4) = mx4_pack8(x, E8);
+                else
+                    *reinterpret_cast<u16 *>(tmp + 16 * to + lane % L * 2) = mx4_pack4(x, E8);
+                if (lane % L == 0) tmp[1024 + to] = (uint8_t)E8;
+            }
+            if (ks + kAhead < KS)
+                load(m0, ks + kAhead);
+            else if (next < m)
+                load(std::min(next, m - 32), ks + kAhead - KS);
+            __builtin_amdgcn_wave_barrier();  // (a wave's LDS operations keep their order)
+            f[ks] = *reinterpret_cast<const u32x4 *>(tmp + 16 * lane);
+            sc[ks / 4] |= (uint32_t)tmp[1024 + lane] << 8 * (ks % 4);
+            __builtin_amdgcn_wave_barrier();
+        }
+    }
+};
+
+template <int J, int KS>
+__device__ __forceinline__ f32x16 narrow_chain(const u32x4 *b, const uint32_t *bsc, const u32x4 *f, const uint32_t *sc, f32x16 acc)
+{
+    if constexpr (J < KS) {
+        acc = mfma_fp4<J % 4>(b[64 * J], (int)bsc[64 * (J / 4)], f[J], (int)sc[J / 4], acc);
+        return narrow_chain<J + 1, KS>(b, bsc, f, sc, acc);
+    } else {
+        return acc;
+    }
+}
+
+// Workgroup b: columns [y * panel, (y + 1) * panel) of C, y = b / gx (panel a
+// multiple of 32), of the runs of 32 rows a wave the (b % gx)-th and every gx-th after it.
+// Waves of a SIMD, for the registers of the rows in flight.
+template <class Rows> constexpr int narrow_waves(int KS)
+{
+    return KS == 8 ? 2 : KS == 4 || (KS == 2 && std::is_same_v<Rows, DenseRows<float>>) ? 3 : 4;
+}
+
+// m >= 32: the last rows are taken as a full 32, some of them twice (with the same
+// results).  FULL: the rows are 64 KS wide, without padding.
+template <class Rows, class T, int KS, bool FULL>
+__global__ __launch_bounds__(kNarrowWaves * kWave, narrow_waves<Rows>(KS)) void k_narrow(Rows A, const uint8_t *__restrict__ bc,
+                                                                 const uint8_t *__restrict__ bs, int64_t m, int64_t n,
+                                                                 int kpad, int panel, int gx,
+                                                                 Out<T> out)
+{
+    constexpr int KQ = (KS + 3) / 4;
+    extern __shared__ __align__(16) uint8_t lds[];
+    const int tiles = panel / 32;
+    u32x4 *bf = reinterpret_cast<u32x4 *>(lds);                               // [tile][ks][lane]
+    uint32_t *bq = reinterpret_cast<uint32_t *>(lds + tiles * KS * 1024);     // [tile][ks / 4][lane]
+    uint8_t *tmp = lds + tiles * (KS * 1024 + KQ * 256);
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave), lane = threadIdx.x % kWave;
+    const int64_t n0 = (int64_t)(blockIdx.x / gx) * panel;
+    const int64_t cp = kpad / 2;
+    const int sp = kpad / kMxBlock;
+    for (int i = threadIdx.x; i < tiles * KS * 64; i += kNarrowWaves * kWave) {
+        const int l = i % 64, blk = 2 * (i / 64 % KS) + l / 32;
+        const int64_t row = std::min<int64_t>(n0 + i / (64 * KS) * 32 + l % 32, n - 1);
+        bf[i] = blk < sp ? *reinterpret_cast<const u32x4 *>(bc + row * cp + 16 * blk) : u32x4{};
+    }
+    for (int i = threadIdx.x; i < tiles * KQ * 64; i += kNarrowWaves * kWave) {
+        const int l = i % 64, q = i / 64 % KQ;
+        const int64_t row = std::min<int64_t>(n0 + i / (64 * KQ) * 32 + l % 32, n - 1);
+        uint32_t w = 0;
+#pragma unroll
+        for (int j = 0; j < 4; j++) {
+            const int blk = 2 * (4 * q + j) + l / 32;
+            if (4 * q + j < KS && blk < sp) w |= (uint32_t)bs[row * sp + blk] << 8 * j;
+        }
+        bq[i] = w;
+    }
+    __syncthreads();
+    const int64_t step = (int64_t)gx * kNarrowWaves * 32;
+    int64_t m0 = ((int64_t)(blockIdx.x % gx) * kNarrowWaves + wave) * 32;
+    if (m0 >= m) return;
+    uint8_t *own = tmp + wave * (kNarrowTmp + kNarrowOut);
+    RowSource<Rows, KS, FULL> src(A, lane, own);
+    const Staged<T, kNarrowLine / sizeof(T)> st{own + kNarrowTmp, lane};
+    src.start(std::min(m0, m - 32));
+    for (; m0 < m; m0 += step) {
+        const int64_t at = std::min(m0, m - 32);
+        u32x4 f[KS];
+        uint32_t sc[KQ];
+        src.rows(at, m0 + step, m, f, sc);
+        for (int j = 0; j < tiles && n0 + 32 * j < n; j += st.kTiles) {
+#pragma unroll
+            for (int i = 0; i < st.kTiles; i++)  // (a second tile past the panel is not stored)
+                if (i == 0 || j + i < tiles)
+                    st.put(i, narrow_chain<0, KS>(bf + (j + i) * KS * 64 + lane, bq + (j + i) * KQ * 64 + lane, f, sc, f32x16{}));
+            st.store(out, at, m, n0 + 32 * j, std::min<int64_t>(n, n0 + panel));
+        }
+    }
+}
+
+// --------------------------------------------------------- few rows, any k
+//
+// One row or a few against wide weights: bound by reading B once, and by latency.
+// A workgroup takes 16 rows of B (so that 4,096 of them fill the chip), its eight
+// waves 512 of k at a time each, all of a wave's loads in flight together, and the
+// waves' sums are added in LDS.  V_MFMA_SCALE_F32_16X16X128: a lane holds block
+// lane / 16 of row lane % 16, of B as it lies in memory.  A dense A
+// of at most kFewInside elements is quantised into LDS by every workgroup, after its
+// first loads of B are on their way.
+constexpr int kFewWaves = 8;
+constexpr int kFewSteps = 4;  // of 128
+constexpr int kFewRows = 64;         // of A at most, 32 where k_narrow could take them
+constexpr int64_t kFewInside = 1 << 16;
+
+typedef float f32x4 __attribute__((ext_vector_type(4)));
+
+__device__ __forceinline__ f32x4 mfma_fp4_16(u32x4 a, int sa, u32x4 b, int sb, f32x4 c)
+{
+    const i32x8 x = {(int)a[0], (int)a[1], (int)a[2], (int)a[3], 0, 0, 0, 0};
+    const i32x8 y = {(int)b[0], (int)b[1], (int)b[2], (int)b[3], 0, 0, 0, 0};
+    return __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(x, y, c, 4, 4, 0, sa, 0, sb);
+}
+
+// Blocks 4 (step + i) + lane / 16, i < kFewSteps, of a row of `blocks` blocks whose
+// codes and scales start at c and s, zeros past them; scale bytes in byte 0 of sc[i].
+__device__ __forceinline__ void load_chunk(const uint8_t *c, const uint8_t *s, int step, int blocks, int lane, u32x4 *f,
+                                           uint32_t *sc)
+{
+    const int q = lane / 16;
+    if (4 * (step + kFewSteps) <= blocks) {
+        const u32x4 w = *reinterpret_cast<const u32x4u *>(s + 4 * step);
+#pragma unroll
+        for (int i = 0; i < kFewSteps; i++) {
+            f[i] = *reinterpret_cast<const u32x4 *>(c + 64 * (step + i) + 16 * q);
+            sc[i] = w[i] >> 8 * q;
+        }
+    } else {
+#pragma unroll
+        for (int i = 0; i < kFewSteps; i++) {
+            f[i] = u32x4{};
+            sc[i] = 0;
+            if (4 * (step + i) + q < blocks) {
+                f[i] = *reinterpret_cast<const u32x4 *>(c + 64 * (step + i) + 16 * q);
+                sc[i] = s[4 * (step + i) + q];
+            }
+        }
+    }
+}
+
+// Quantises dense rows of A into LDS: rows of kpad / 2 + 16 bytes, then their scales.
+template <class T>
+__device__ __forceinline__ void few_quantise(const DenseRows<T> &A, int64_t m, int kpad, uint8_t *codes, uint8_t *scales)
+{
+    constexpr int E = 8, L = kMxBlock / E;
+    const int per = kpad / E, units = (int)m * per;
+    for (int u = threadIdx.x; u < units; u += kFewWaves * kWave) {  // (units: a multiple of 16)
+        const int row = u / per, col = u % per * E;
+        const typename Elems<T, E>::type v = load_elems<T, E>(A.p + row * A.ld + col, A.cols - col);
+        float x[E];
+        uint32_t top = 0;
+#pragma unroll
+        for (int e = 0; e < E; e++) {
+            x[e] = to_f32(v[e]);
+            const uint32_t b = __float_as_uint(x[e]) & 0x7fffffffu;
+            top = b > top ? b : top;
+        }
+        const int E8 = mx4_exponent(group_max<L>(top));
+        *reinterpret_cast<uint32_t *>(codes + row * (kpad / 2 + 16) + col / 2) = mx4_pack8(x, E8);
+        if (u % L == 0) scales[row * (kpad / kMxBlock) + col / kMxBlock] = (uint8_t)E8;
+    }
+}
+
+// MT: tiles of 16 rows of A.
+template <class Rows, class T, int MT>
+__global__ __launch_bounds__(kFewWaves * kWave) void k_few(Rows A, const uint8_t *__restrict__ bc,
+                                                          const uint8_t *__restrict__ bs, int64_t m, int64_t n, int kpad,
+                                                          Out<T> out)
+{
+    constexpr bool DENSE = !std::is_same_v<Rows, MxRows>;
+    __shared__ f32x4 sums[kFewWaves][MT][kWave];
+    extern __shared__ __align__(16) uint8_t lds[];
+    const int wave = threadIdx.x / kWave, lane = threadIdx.x % kWave;
+    const int blocks = kpad / kMxBlock, steps = (blocks + 3) / 4;
+    const int64_t n0 = (int64_t)blockIdx.x * 16;
+    const int64_t row = std::min<int64_t>(n0 + lane % 16, n - 1);
+    const uint8_t *c = bc + row * (kpad / 2), *s = bs + row * (kpad / kMxBlock);
+    const uint8_t *ac, *as;
+    int64_t ap, sp;
+    u32x4 fb[kFewSteps], fa[kFewSteps];
+    uint32_t qb[kFewSteps], qa[kFewSteps];
+    int step = kFewSteps * wave;
+    if (step < steps) load_chunk(c, s, step, blocks, lane, fb, qb);
+    if constexpr (DENSE) {
+        ac = lds;
+        as = lds + m * (kpad / 2 + 16);
+        ap = kpad / 2 + 16;
+        sp = kpad / kMxBlock;
+        few_quantise(A, m, kpad, lds, lds + m * (kpad / 2 + 16));
+        __syncthreads();
+    } else {
+        ac = A.codes;
+        as = A.scales;
+        ap = A.code_pitch;
+        sp = A.scale_pitch;
+    }
+    f32x4 acc[MT] = {};
+    for (; step < steps; step += kFewSteps * kFewWaves) {
+        if (step != kFewSteps * wave) load_chunk(c, s, step, blocks, lane, fb, qb);
+#pragma unroll
+        for (int t = 0; t < MT; t++) {
+            const int64_t i = std::min<int64_t>(16 * t + lane % 16, m - 1);
+            load_chunk(ac + i * ap, as + i * sp, step, blocks, lane, fa, qa);
+#pragma unroll
+            for (int k = 0; k < kFewSteps; k++) acc[t] = mfma_fp4_16(fb[k], (int)qb[k], fa[k], (int)qa[k], acc[t]);
+        }
+    }
+#pragma unroll
+    for (int t = 0; t < MT; t++) sums[wave][t][lane] = acc[t];
+    __syncthreads();
+    if (wave < MT) {
+        f32x4 v = sums[0][wave][lane];
+#pragma unroll
+        for (int w = 1; w < kFewWaves; w++) v += sums[w][wave][lane];
+        // accumulator: lane l holds columns 4 (l / 16) .. + 3 of row l % 16 of C
+        const int64_t i = 16 * wave + lane % 16, j = n0 + 4 * (lane / 16);
+        if (i < m && j < n)
+            out.template store_row<4>(i, j, n, typename Elems<T, 4>::type{from_f32<T>(v[0]), from_f32<T>(v[1]), from_f32<T>(v[2]), from_f32<T>(v[3])});
     }
 }
 
@@ -119,13 +462,13 @@ __device__ __forceinline__ void load_to_lds(const uint8_t *g, uint8_t *l)
 }
 
 // kpad >= 512, a multiple of 128.
-template <class T, bool MASK, int WT>
+template <class T, int WT>
 __global__ __launch_bounds__(256, WT == 4 ? 1 : 2) void k_tile(const uint8_t *__restrict__ ac,
                                                                const uint8_t *__restrict__ as,
                                                                const uint8_t *__restrict__ bc,
                                                                const uint8_t *__restrict__ bs, int64_t m, int64_t n,
                                                                int kpad, int64_t tiles_m, int64_t tiles_n,
-                                                               Out<T, MASK> out)
+                                                               Out<T> out)
 {
     constexpr int BM = 64 * WT, LD = 2 * WT, SL = 2 * BM / 256;
     __shared__ TileLds<WT> lds;
@@ -208,8 +551,8 @@ __global__ __launch_bounds__(256, WT == 4 ? 1 : 2) void k_tile(const uint8_t *__
         for (int i = 0; i < WT; i++)
 #pragma unroll
             for (int j = 0; j < WT; j++)
-                acc[i][j] = mfma_fp4<2 * (Q & 1)>(fa[Q][i], (int)(sa[Q / 2][i] >> 8 * half), fb[Q][j],
-                                                  (int)(sb[Q / 2][j] >> 8 * half), acc[i][j]);
+                acc[i][j] = mfma_fp4<2 * (Q & 1)>(fb[Q][j], (int)(sb[Q / 2][j] >> 8 * half), fa[Q][i],
+                                                  (int)(sa[Q / 2][i] >> 8 * half), acc[i][j]);
     };
     using Q0 = std::integral_constant<int, 0>;
     using Q1 = std::integral_constant<int, 1>;
@@ -280,19 +623,16 @@ __global__ __launch_bounds__(256, WT == 4 ? 1 : 2) void k_tile(const uint8_t *__
         mul(Q2{}), mul(Q3{});
     }
 
-    const int64_t row0 = m0 + 32 * wm * WT + 4 * half, col0 = n0 + 32 * wn * WT + r;
+    using St = Staged<T, 32 * WT>;
+    static_assert(4 * St::kBytes <= 2 * TileLds<WT>::kStage);
+    __syncthreads();  // every wave has read the last step
+    const St st{lds.codes[0] + wave * St::kBytes, lane};
 #pragma unroll
-    for (int i = 0; i < WT; i++)
+    for (int i = 0; i < WT; i++) {
 #pragma unroll
-        for (int e = 0; e < 16; e++) {
-            const int64_t row = row0 + 32 * i + 8 * (e / 4) + e % 4;
-            if (row < m) {
-#pragma unroll
-                for (int j = 0; j < WT; j++)
-                    if (col0 + 32 * j < n) out.store(row, col0 + 32 * j, acc[i][j][e]);
-            }
-            __builtin_amdgcn_sched_barrier(0);  // (addresses of a row at a time)
-        }
+        for (int j = 0; j < WT; j++) st.put(j, acc[i][j]);
+        st.store(out, m0 + 32 * (wm * WT + i), m, n0 + 32 * wn * WT, n);
+    }
 }
 
 uint64_t round256(uint64_t x) { return (x + 255) / 256 * 256; }
@@ -303,10 +643,33 @@ void check_sizes(int64_t m, int64_t n, int64_t k)
     if (k > kMxMaxCols) fail(GS_ERR_UNSUPPORTED, "at most 2^24 columns");
 }
 
-// Workspace: A's codes and scales when A is dense.
-uint64_t workspace(int64_t m, int64_t k, int a_dtype)
+// How a product of k > 0 is formed.
+enum class Way { kFew, kNarrow, kTile };
+Way way(int64_t m, int64_t n, int kpad)
 {
-    if (a_dtype < 0) return 0;
+    if (m < 32) return Way::kFew;
+    if (kpad <= kNarrowMaxK && (kpad < 512 || n < 512)) return Way::kNarrow;
+    return m <= kFewRows ? Way::kFew : Way::kTile;
+}
+
+// Columns of B that a workgroup of k_narrow keeps: 32 KB of it (KS times 64 of k).
+int narrow_slices(int kpad) { return kpad <= 64 ? 1 : kpad <= 128 ? 2 : kpad <= 256 ? 4 : 8; }
+int64_t narrow_columns(int kpad) { return 32 * (32 / narrow_slices(kpad)); }
+
+// Whether a dense A is quantised by the kernel that multiplies it.
+bool quantised_inside(int64_t m, int64_t n, int kpad)
+{
+    switch (way(m, n, kpad)) {
+    case Way::kFew: return m <= 32 && m * kpad <= kFewInside;
+    case Way::kNarrow: return n <= narrow_columns(kpad);
+    default: return false;
+    }
+}
+
+// Workspace: A's codes and scales when A is dense and quantised first.
+uint64_t workspace(int64_t m, int64_t n, int64_t k, int a_dtype)
+{
+    if (a_dtype < 0 || quantised_inside(m, n, (int)mx4_cols(k))) return 0;
     return round256((uint64_t)m * mx4_cols(k) / 2) + round256((uint64_t)m * mx4_cols(k) / kMxBlock);
 }
 
@@ -327,32 +690,96 @@ void check_work(const void *work, uint64_t have, uint64_t need)
     if ((uintptr_t)work % 16) fail(GS_ERR_INVALID_ARG, "workspace is not 16-byte aligned");
 }
 
-void multiply(const gs_mxfp4 &A, const gs_mxfp4 &B, const gs_saved *mask, void *C, int64_t ldc, int dtype,
-              hipStream_t s)
+struct Product {
+    int64_t m, n;
+    int kpad;
+    const gs_mxfp4 *B;
+    const gs_saved *mask;
+    void *C;
+    int64_t ldc;
+    int dtype;
+    hipStream_t s;
+};
+
+// f(Out<T>) for the product's type and mask.
+template <class F> void with_out(const Product &p, F &&f)
 {
-    const int64_t m = A.rows, n = B.rows;
-    if (m == 0 || n == 0) return;
-    const int kpad = (int)mx4_cols(A.cols);
-    auto typed = [&](auto type, auto masked) {
+    auto typed = [&](auto type) {
         using T = decltype(type);
-        constexpr bool MASK = decltype(masked)::value;
-        const Out<T, MASK> out{(T *)C, ldc, mask ? mask->codes : nullptr, mask ? saved_code_pitch(n) : 0};
+        f(Out<T>{(T *)p.C, p.ldc, p.mask ? p.mask->codes : nullptr, p.mask ? saved_code_pitch(p.n) : 0});
+    };
+    p.dtype == GS_F32 ? typed(0.0f) : typed(u16(0));
+    GS_HIP(hipGetLastError());
+}
+
+template <class Rows> void multiply_narrow(const Product &p, const Rows &A)
+{
+    // Panels of 32 KB of B (four workgroups to a compute unit), fewer columns while
+    // there are fewer workgroups than compute units.
+    const int KS = narrow_slices(p.kpad);
+    const int64_t groups = ceil_div(p.m, 32 * kNarrowWaves);
+    int64_t panel = std::min<int64_t>(ceil_div(p.n, 32) * 32, narrow_columns(p.kpad));
+    while (panel > 32 && groups * ceil_div(p.n, panel) < compute_units()) panel = ceil_div(panel / 2, 32) * 32;
+    const int64_t panels = ceil_div(p.n, panel);
+    const int64_t gx = std::min<int64_t>(groups, std::max<int64_t>(1, 8 * compute_units() / panels));
+    if (gx * panels >= 1 << 24) fail(GS_ERR_UNSUPPORTED, "the product has too many tiles");
+    with_out(p, [&](auto out) {
+        using T = typename decltype(out)::type;
+        auto go = [&](auto ks, auto full) {
+            constexpr int K = decltype(ks)::value;
+            const size_t lds = panel / 32 * (K * 1024 + (K + 3) / 4 * 256) + kNarrowWaves * (kNarrowTmp + kNarrowOut);
+            k_narrow<Rows, T, K, decltype(full)::value><<<(unsigned)(gx * panels), kNarrowWaves * kWave, lds, p.s>>>(
+                A, p.B->codes, p.B->scales, p.m, p.n, p.kpad, (int)panel, (int)gx, out);
+        };
+        auto sized = [&](auto ks) { A.width() == 64 * KS ? go(ks, std::true_type{}) : go(ks, std::false_type{}); };
+        if (KS == 1)
+            sized(std::integral_constant<int, 1>{});
+        else if (KS == 2)
+            sized(std::integral_constant<int, 2>{});
+        else if (KS == 4)
+            sized(std::integral_constant<int, 4>{});
+        else
+            sized(std::integral_constant<int, 8>{});
+    });
+}
+
+template <class Rows> void multiply_few(const Product &p, const Rows &A)
+{
+    with_out(p, [&](auto out) {
+        using T = typename decltype(out)::type;
+        auto go = [&](auto mt) {
+            const size_t lds = std::is_same_v<Rows, MxRows> ? 0 : p.m * (p.kpad / 2 + 16 + p.kpad / kMxBlock);
+            k_few<Rows, T, decltype(mt)::value>
+                <<<(unsigned)ceil_div(p.n, 16), kFewWaves * kWave, lds, p.s>>>(A, p.B->codes, p.B->scales, p.m, p.n, p.kpad, out);
+        };
+        if constexpr (std::is_same_v<Rows, MxRows>)
+            if (p.m > 32) return go(std::integral_constant<int, 4>{});
+        if (p.m > 16) return go(std::integral_constant<int, 2>{});
+        go(std::integral_constant<int, 1>{});
+    });
+}
+
+void multiply(const Product &p, const gs_mxfp4 &A)
+{
+    if (p.m == 0 || p.n == 0) return;
+    const MxRows rows{A.codes, A.scales, p.kpad / 2, p.kpad / kMxBlock};
+    const Way w = way(p.m, p.n, p.kpad);
+    if (w == Way::kNarrow) return multiply_narrow(p, rows);
+    if (w == Way::kFew) return multiply_few(p, rows);
+    with_out(p, [&](auto out) {
+        using T = typename decltype(out)::type;
         auto tiled = [&](auto wt) {
             constexpr int WT = decltype(wt)::value;
-            const int64_t tm = ceil_div(m, 64 * WT), tn = ceil_div(n, 64 * WT);
-            k_tile<T, MASK, WT><<<(unsigned)(tm * tn), 256, 0, s>>>(A.codes, A.scales, B.codes, B.scales, m, n, kpad, tm, tn, out);
+            const int64_t tm = ceil_div(p.m, 64 * WT), tn = ceil_div(p.n, 64 * WT);
+            if (tm * tn >= 1 << 24) fail(GS_ERR_UNSUPPORTED, "the product has too many tiles");
+            k_tile<T, WT>
+                <<<(unsigned)(tm * tn), 256, 0, p.s>>>(A.codes, A.scales, p.B->codes, p.B->scales, p.m, p.n, p.kpad, tm, tn, out);
         };
-        if (kpad >= 512 && ceil_div(m, 256) * ceil_div(n, 256) < (1 << 22)) {
-            ceil_div(m, 256) * ceil_div(n, 256) >= 128 ? tiled(std::integral_constant<int, 4>{}) : tiled(std::integral_constant<int, 2>{});
-            return;
-        }
-        const int64_t tiles_n = ceil_div(n, 128), tiles = ceil_div(m, 128) * tiles_n;
-        const unsigned grid = (unsigned)std::min<int64_t>(tiles, 1 << 20);
-        k_matmul<T, MASK><<<grid, 256, 0, s>>>(A.codes, A.scales, B.codes, B.scales, m, n, kpad, tiles_n, tiles, out);
-    };
-    auto go = [&](auto type) { mask ? typed(type, std::true_type{}) : typed(type, std::false_type{}); };
-    dtype == GS_F32 ? go(0.0f) : go(u16(0));
-    GS_HIP(hipGetLastError());
+        if (ceil_div(p.m, 256) * ceil_div(p.n, 256) >= 128)
+            tiled(std::integral_constant<int, 4>{});
+        else
+            tiled(std::integral_constant<int, 2>{});
+    });
 }
 
 }  // namespace
@@ -368,7 +795,7 @@ int gs_mxfp4_matmul_workspace(int64_t m, int64_t n, int64_t k, int a_dtype, uint
         if (!bytes) fail(GS_ERR_INVALID_ARG, "null output");
         check_sizes(m, n, k);
         if (a_dtype != -1) dtype_size(a_dtype);
-        *bytes = workspace(m, k, a_dtype);
+        *bytes = workspace(m, n, k, a_dtype);
     });
 }
 
@@ -380,8 +807,8 @@ int gs_mxfp4_matmul(const gs_mxfp4 *A, const gs_mxfp4 *B, const gs_saved *mask, 
         check_mxfp4(B);
         if (A->cols != B->cols) fail(GS_ERR_INVALID_ARG, "A and B have different widths");
         check_out(A->rows, B->rows, mask, C, ldc, dtype);
-        check_work(work, work_bytes, workspace(A->rows, A->cols, -1));
-        multiply(*A, *B, mask, C, ldc, dtype, (hipStream_t)stream);
+        check_work(work, work_bytes, workspace(A->rows, B->rows, A->cols, -1));
+        multiply({A->rows, B->rows, (int)mx4_cols(B->cols), B, mask, C, ldc, dtype, (hipStream_t)stream}, *A);
     });
 }
 
@@ -394,11 +821,19 @@ int gs_mxfp4_matmul_dense(const void *A, int64_t lda, int a_dtype, int64_t m, co
         check_sizes(m, B->rows, B->cols);
         check_operand("A", A, m, B->cols, lda, dtype_size(a_dtype));
         check_out(m, B->rows, mask, C, ldc, dtype);
-        check_work(work, work_bytes, workspace(m, B->cols, a_dtype));
+        check_work(work, work_bytes, workspace(m, B->rows, B->cols, a_dtype));
+        const Product p{m, B->rows, (int)mx4_cols(B->cols), B, mask, C, ldc, dtype, (hipStream_t)stream};
+        if (m == 0 || p.n == 0) return;
+        const int k = (int)B->cols;
+        if (quantised_inside(m, p.n, p.kpad)) {
+            auto rows = [&](const auto &r) { way(m, p.n, p.kpad) == Way::kNarrow ? multiply_narrow(p, r) : multiply_few(p, r); };
+            a_dtype == GS_F32 ? rows(DenseRows<float>{(const float *)A, lda, k}) : rows(DenseRows<u16>{(const u16 *)A, lda, k});
+            return;
+        }
         uint8_t *codes = (uint8_t *)work;
         const gs_mxfp4 q{m, B->cols, codes, codes + round256((uint64_t)m * mx4_cols(B->cols) / 2)};
-        mx4_quantize_rows(A, lda, a_dtype, m, B->cols, q.codes, q.scales, (hipStream_t)stream);
-        multiply(q, *B, mask, C, ldc, dtype, (hipStream_t)stream);
+        mx4_quantize_rows(A, lda, a_dtype, m, B->cols, q.codes, q.scales, p.s);
+        multiply(p, q);
     });
 }
 
