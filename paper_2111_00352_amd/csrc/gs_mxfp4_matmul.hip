@@ -431,34 +431,183 @@ __global__ __launch_bounds__(kFewWaves * kWave) void k_few(Rows A, const uint8_t
 // ------------------------------------------------------------ large products
 //
 // A workgroup of four waves makes a tile of 64 WT x 64 WT, a wave a quarter of it
-// (WT x WT instructions of 32 x 32 for every 64 of k), 256 of k a step.  Codes go
-// from memory to LDS without passing registers; two buffers hold the step that is
-// multiplied and the next one.  A row of a step is 128 bytes, whose eight 16-byte
-// pieces lie in LDS in an order that depends on the row (piece ^ row % 8), so that
-// the 32 rows an instruction reads spread over all banks; the loads put them there
-// by choosing which piece of the row each lane fetches.
+// (WT x WT instructions of 32 x 32 for every 64 of k).  k is taken in chunks of 256,
+// so that a row of a chunk is a whole line of 128 bytes (chunks of 128, half a line a
+// row, left the kernel bound by the rate of requests to L2: 8192^3 in 280 us).  Codes go
+// from memory to LDS without passing registers, a chunk ahead of the one that is
+// multiplied.  A row's eight 16-byte pieces lie in LDS in an order that depends on the
+// row (piece ^ row / 2 % 8), so that the rows LDS serves together (16 of 32: those whose
+// row / 4 is 0, 3, 5, 6 and the others) spread over all banks; the loads put them there
+// by choosing which piece each lane fetches.
 //
-// The fragments of a step are read as four quarters of 64.  The last quarter is
-// multiplied only after the next step's barrier, while that step's first quarters
-// are read: the matrix cores have work across the barrier.  The next step's loads
-// are issued after a step's last LDS read, so they have three quarters of a step
-// until the barrier waits for them.
+// A chunk is multiplied as four quarters, the fragments of each read while the one
+// before it is multiplied.  The last quarter of a chunk is multiplied after the
+// workgroup has met to start the next one, so the matrix cores have work on both
+// sides of that barrier.
 //
-// Scale words (one for 128 of k) are read four at a time (512 of k) by one thread a
-// row, a run ahead, and lie in LDS by word, so a wave reads 32 neighbouring words.
-constexpr int kStepK = 256;
+// Scales lie in LDS as 16 bytes of a row, a run of two chunks, loaded a run ahead.
+constexpr int kChunkK = 256;
 
 template <int WT> struct TileLds {
-    static constexpr int kRows = 64 * WT;
-    static constexpr int kStage = 2 * kRows * (kStepK / 2);
-    __align__(1024) uint8_t codes[2][kStage];  // A's rows, then B's
-    uint32_t scales[2][4][2 * kRows];
+    static constexpr int kRows = 64 * WT;                   // of either operand
+    static constexpr int kStage = 2 * kRows * kChunkK / 2;  // A's rows, then B's
+    __align__(1024) uint8_t codes[2 * kStage];
+    __align__(16) uint8_t scales[2][2 * kRows * 16];
+    uint8_t after[16];  // (half a chunk at the end of a row reads a word past its scales)
 };
 
-__device__ __forceinline__ void load_to_lds(const uint8_t *g, uint8_t *l)
+// 16 bytes a lane from p + lane_off + off to `to` and the 64 x 16 bytes after it.  The
+// callers mark `to` as not overlapping with what they read from LDS meanwhile: the
+// compiler then leaves the waiting to them.
+__device__ __forceinline__ void load_to_lds(const uint8_t *p, uint32_t lane_off, uint32_t off, uint8_t *to)
 {
-    __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void *)g,
-                                     (__attribute__((address_space(3))) void *)l, 16, 0, 0);
+    const __amdgpu_buffer_rsrc_t r = __builtin_amdgcn_make_buffer_rsrc((void *)p, 0, -1, 0x00020000);
+    __builtin_amdgcn_raw_ptr_buffer_load_lds(r, (__attribute__((address_space(3))) void *)to, 16, lane_off, off, 0, 0);
+}
+
+// A wave's share of the loads: 2 WT of either operand a chunk and one of the scales.
+// Load q fills rows 8 (wave 2 WT + q) .. + 7 of a stage; of the scale rows of both
+// operands, in order, a wave takes 32 WT, 64 with each chunk.  Rows past the last one
+// repeat it (their results are not stored).
+template <int WT> struct TileLoads {
+    uint32_t a[2 * WT], b[2 * WT];  // offsets from the tile's first row of A and B
+    uint32_t s[WT / 2];             // and of the scale rows (A's or B's)
+    int kpad;
+    bool upper;                     // this lane's piece for even q (the other half for odd) is
+                                    // in the upper half of a row of a chunk
+};
+template <int WT>
+__device__ __forceinline__ void tile_load(uint8_t *__restrict__ to, uint8_t *__restrict__ scales_to,
+                                          const uint8_t *__restrict__ ga, const uint8_t *__restrict__ gb,
+                                          const uint8_t *__restrict__ gs, const TileLoads<WT> &ld, int chunk, int run,
+                                          int group)
+{
+    // (a row that ends with half a chunk: the upper half, which is not read, repeats the lower)
+    const uint32_t over = (chunk + 1) * kChunkK > ld.kpad ? 64u : 0u;
+    const uint32_t back[2] = {ld.upper ? over : 0, ld.upper ? 0 : over};
+#pragma unroll
+    for (int q = 0; q < 2 * WT; q++) {
+        load_to_lds(ga, ld.a[q] - back[q % 2], chunk * (kChunkK / 2), to + 1024 * q);
+        load_to_lds(gb, ld.b[q] - back[q % 2], chunk * (kChunkK / 2), to + WT * 8192 + 1024 * q);
+    }
+    uint32_t so = ld.s[0];
+    if constexpr (WT == 4) so = group ? ld.s[1] : so;
+    load_to_lds(gs, so, std::min(16 * run, ld.kpad / kMxBlock - 16), scales_to + (WT == 4 ? group * 1024 : 0));
+}
+
+template <int WT> struct Frags {
+    u32x4 a[WT], b[WT];
+};
+template <int WT> struct ScaleWords {  // of a chunk: 128 of k each
+    uint32_t a[2][WT], b[2][WT];
+};
+template <int WT> struct TileReads {
+    int a, b;    // this lane's row of A and B in a stage
+    int sa, sb;  // and its scales in a run
+    int half, swz;
+    __device__ __forceinline__ void frags(const uint8_t *from, int q, Frags<WT> &f) const
+    {
+        const uint8_t *p = from + ((2 * q + half) ^ swz) * 16;
+#pragma unroll
+        for (int i = 0; i < WT; i++) {
+            f.a[i] = *reinterpret_cast<const u32x4 *>(p + a + i * 4096);
+            f.b[i] = *reinterpret_cast<const u32x4 *>(p + b + i * 4096);
+        }
+    }
+    __device__ __forceinline__ void scales(const uint8_t *from, ScaleWords<WT> &s) const
+    {
+#pragma unroll
+        for (int i = 0; i < WT; i++) {
+            typedef uint32_t pair __attribute__((ext_vector_type(2), aligned(4)));
+            const pair x = *reinterpret_cast<const pair *>(from + sa + i * 512);
+            const pair y = *reinterpret_cast<const pair *>(from + sb + i * 512);
+            s.a[0][i] = x[0], s.a[1][i] = x[1];
+            s.b[0][i] = y[0], s.b[1][i] = y[1];
+        }
+    }
+};
+// Quarter Q.  B is the first operand: a lane's sums are four neighbouring columns of a row of C.
+template <int Q, int WT>
+__device__ __forceinline__ void tile_mul(f32x16 (&acc)[WT][WT], const Frags<WT> &f, const ScaleWords<WT> &s, int half)
+{
+#pragma unroll
+    for (int i = 0; i < WT; i++)
+#pragma unroll
+        for (int j = 0; j < WT; j++)
+            acc[i][j] = mfma_fp4<2 * (Q & 1)>(f.b[j], (int)(s.b[Q / 2][j] >> 8 * half), f.a[i], (int)(s.a[Q / 2][i] >> 8 * half),
+                                              acc[i][j]);
+}
+
+// Of the instructions up to the next sched_barrier: COUNT groups of one
+// multiplication, R LDS reads and V loads.
+template <int COUNT, int R, int V> __device__ __forceinline__ void interleave()
+{
+#pragma unroll
+    for (int i = 0; i < COUNT; i++) {
+        __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+        if constexpr (R) __builtin_amdgcn_sched_group_barrier(0x100, R, 0);
+        if constexpr (V) __builtin_amdgcn_sched_group_barrier(0x010, V, 0);
+    }
+}
+
+// Fragments of A and the scales of a chunk's upper half, if keep is ~0.
+template <int WT> __device__ __forceinline__ void keep_rows(Frags<WT> &f, ScaleWords<WT> &s, uint32_t keep)
+{
+#pragma unroll
+    for (int i = 0; i < WT; i++) {
+        f.a[i] &= keep;
+        s.a[1][i] &= keep;
+        s.b[1][i] &= keep;
+    }
+}
+
+// One chunk, which lies in `from`.  held, s: the last quarter of the chunk before it
+// and its scales, on return this one's.  FIRST: there is none before it.  LAST: nothing
+// is loaded, and if keep is 0 instead of ~0 the chunk is half a one, whose other half
+// is taken as zeros.
+template <int WT, bool FIRST, bool LAST>
+__device__ __forceinline__ void tile_chunk(uint8_t *__restrict__ to, uint8_t *__restrict__ scales_to,
+                                           const uint8_t *__restrict__ from, const uint8_t *__restrict__ scales,
+                                           const uint8_t *__restrict__ ga, const uint8_t *__restrict__ gb,
+                                           const uint8_t *__restrict__ gs, const TileLoads<WT> &ld,
+                                           const TileReads<WT> &rd, int chunk, uint32_t keep,
+                                           f32x16 (&acc)[WT][WT], Frags<WT> &held, ScaleWords<WT> &s)
+{
+    Frags<WT> f;
+    ScaleWords<WT> sn;
+    rd.scales(scales, sn);
+    rd.frags(from, 0, f);
+    if constexpr (!LAST) tile_load<WT>(to, scales_to, ga, gb, gs, ld, chunk + 1, (chunk >> 1) + 1, chunk & 1);
+    if constexpr (!FIRST) {
+        tile_mul<3, WT>(acc, held, s, rd.half);
+        interleave<2 * WT, 2, LAST ? 0 : 1>();
+        interleave<WT == 4 ? 8 : 0, 0, LAST ? 0 : 1>();
+    }
+    __builtin_amdgcn_sched_barrier(0);
+    s = sn;
+    rd.frags(from, 1, held);
+    tile_mul<0, WT>(acc, f, s, rd.half);
+    interleave<2 * WT, 1, 0>();
+    __builtin_amdgcn_sched_barrier(0);
+    rd.frags(from, 2, f);
+    tile_mul<1, WT>(acc, held, s, rd.half);
+    interleave<2 * WT, 1, 0>();
+    __builtin_amdgcn_sched_barrier(0);
+    if constexpr (LAST) keep_rows(f, s, keep);
+    rd.frags(from, 3, held);
+    tile_mul<2, WT>(acc, f, s, rd.half);
+    interleave<2 * WT, 1, 0>();
+    if constexpr (LAST) keep_rows(held, s, keep);
+    __builtin_amdgcn_sched_barrier(0);
+}
+
+// This wave's loads have arrived and its LDS reads are done, and so are all others'.
+__device__ __forceinline__ void tile_meet()
+{
+    __builtin_amdgcn_sched_barrier(0);
+    __builtin_amdgcn_s_waitcnt(0x0070);  // vmcnt(0) lgkmcnt(0)
+    __syncthreads();
+    __builtin_amdgcn_sched_barrier(0);
 }
 
 // kpad >= 512, a multiple of 128.
@@ -467,166 +616,71 @@ __global__ __launch_bounds__(256, WT == 4 ? 1 : 2) void k_tile(const uint8_t *__
                                                                const uint8_t *__restrict__ as,
                                                                const uint8_t *__restrict__ bc,
                                                                const uint8_t *__restrict__ bs, int64_t m, int64_t n,
-                                                               int kpad, int64_t tiles_m, int64_t tiles_n,
-                                                               Out<T> out)
+                                                               int kpad, int tiles_m, int tiles_n, Out<T> out)
 {
-    constexpr int BM = 64 * WT, LD = 2 * WT, SL = 2 * BM / 256;
-    __shared__ TileLds<WT> lds;
+    constexpr int BM = 64 * WT;
+    using Lds = TileLds<WT>;
+    __shared__ Lds lds;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave), lane = threadIdx.x % kWave;
-    const int64_t cp = kpad / 2;
-    const int sp = kpad / kMxBlock;
+    const int cp = kpad / 2, sp = kpad / kMxBlock, chunks = (kpad + kChunkK - 1) / kChunkK;
     // an XCD takes a contiguous run of tiles, in panels of 8 rows of them
-    const int64_t t = xcd_tile(blockIdx.x, tiles_m * tiles_n);
-    const int64_t panel = t / (8 * tiles_n), in = t % (8 * tiles_n), ph = std::min<int64_t>(8, tiles_m - 8 * panel);
-    const int64_t m0 = (8 * panel + in % ph) * BM, n0 = (in / ph) * BM;
-    const int wm = wave / 2, wn = wave % 2, r = lane % 32, half = lane / 32;
+    const int t = (int)xcd_tile(blockIdx.x, (int64_t)tiles_m * tiles_n);
+    const int panel = t / (8 * tiles_n), in = t % (8 * tiles_n), ph = std::min(8, tiles_m - 8 * panel);
+    // (divided in vector registers: told to be the same for all lanes)
+    const int64_t m0 = (int64_t)__builtin_amdgcn_readfirstlane(8 * panel + in % ph) * BM;
+    const int64_t n0 = (int64_t)__builtin_amdgcn_readfirstlane(in / ph) * BM;
+    const int wm = wave / 2, wn = wave % 2, r = lane % 32;
+    const int last_a = (int)std::min<int64_t>(BM, m - m0) - 1, last_b = (int)std::min<int64_t>(BM, n - n0) - 1;
 
-    // Loads to LDS: a wave's load q fills rows 8 (wave LD + q) .. + 7 of a buffer.
-    // Rows past the last one repeat it (their results are not stored).
-    const int piece = (lane % 8) ^ (lane / 8);
-    uint32_t offa[LD], offb[LD];
     const uint8_t *ga = ac + m0 * cp, *gb = bc + n0 * cp;
+    const bool of_b = wave >= 2;
+    const uint8_t *gs = of_b ? bs + n0 * sp : as + m0 * sp;
+    TileLoads<WT> ld;
 #pragma unroll
-    for (int q = 0; q < LD; q++) {
-        const int row = 8 * (wave * LD + q) + lane / 8;
-        offa[q] = (uint32_t)(std::min<int64_t>(row, m - 1 - m0) * cp) + piece * 16;
-        offb[q] = (uint32_t)(std::min<int64_t>(row, n - 1 - n0) * cp) + piece * 16;
+    for (int q = 0; q < 2 * WT; q++) {
+        const int row = 8 * (wave * 2 * WT + q) + lane / 8, piece = (lane % 8) ^ (row / 2 % 8);
+        ld.a[q] = (uint32_t)std::min(row, last_a) * cp + piece * 16;
+        ld.b[q] = (uint32_t)std::min(row, last_b) * cp + piece * 16;
     }
-    auto issue = [&](int k, int buf) {
-        const uint8_t *a = ga + k / 2, *b = gb + k / 2;
-        uint8_t *to = lds.codes[buf] + 1024 * LD * wave;
-        // (half a step is left at the end of the row: its upper half is not read)
-        const uint32_t back = k + kStepK > kpad && piece >= 4 ? 64u : 0u;
 #pragma unroll
-        for (int q = 0; q < LD; q++) {
-            load_to_lds(a + (offa[q] - back), to + 1024 * q);
-            load_to_lds(b + (offb[q] - back), to + BM * 128 + 1024 * q);
-        }
-    };
-    // Scales: four words from 512 run on, moved back to the row's last four at its
-    // end; the words keep their places in a run of four.
-    const uint8_t *gs[SL];
-#pragma unroll
-    for (int i = 0; i < SL; i++) {
-        const int row = threadIdx.x + 256 * i;
-        gs[i] = row < BM ? as + (m0 + std::min<int64_t>(row, m - 1 - m0)) * sp
-                         : bs + (n0 + std::min<int64_t>(row - BM, n - 1 - n0)) * sp;
-    }
-    u32x4 sw[SL];
-    auto load_scales = [&](int run) {
-#pragma unroll
-        for (int i = 0; i < SL; i++)
-            sw[i] = *reinterpret_cast<const u32x4u *>(gs[i] + std::min(16 * run, sp - 16));
-    };
-    auto write_scales = [&](int run) {
-        const int shift = (16 * run - std::min(16 * run, sp - 16)) / 4;
-#pragma unroll
-        for (int i = 0; i < SL; i++)
-#pragma unroll
-            for (int j = 0; j < 4; j++) lds.scales[run & 1][(j - shift) & 3][threadIdx.x + 256 * i] = sw[i][j];
-    };
-    u32x4 fa[4][WT], fb[4][WT];
-    uint32_t sa[2][WT], sb[2][WT];
-    const int ra = wm * WT * 4096 + r * 128, rb = BM * 128 + wn * WT * 4096 + r * 128;
-    auto read = [&](int buf, int q) {
-        const uint8_t *p = lds.codes[buf] + ((2 * q + half) ^ (r & 7)) * 16;
-#pragma unroll
-        for (int i = 0; i < WT; i++) {
-            fa[q][i] = *reinterpret_cast<const u32x4 *>(p + ra + i * 4096);
-            fb[q][i] = *reinterpret_cast<const u32x4 *>(p + rb + i * 4096);
-        }
-    };
-    auto read_scales = [&](int step, int h) {  // of the step's half h
-        const uint32_t *p = lds.scales[step >> 1 & 1][2 * (step & 1) + h];
-#pragma unroll
-        for (int i = 0; i < WT; i++) {
-            sa[h][i] = p[wm * WT * 32 + r + 32 * i];
-            sb[h][i] = p[BM + wn * WT * 32 + r + 32 * i];
-        }
-    };
-    f32x16 acc[WT][WT] = {};
-    auto mul = [&](auto q) {
-        constexpr int Q = decltype(q)::value;
-#pragma unroll
-        for (int i = 0; i < WT; i++)
-#pragma unroll
-            for (int j = 0; j < WT; j++)
-                acc[i][j] = mfma_fp4<2 * (Q & 1)>(fb[Q][j], (int)(sb[Q / 2][j] >> 8 * half), fa[Q][i],
-                                                  (int)(sa[Q / 2][i] >> 8 * half), acc[i][j]);
-    };
-    using Q0 = std::integral_constant<int, 0>;
-    using Q1 = std::integral_constant<int, 1>;
-    using Q2 = std::integral_constant<int, 2>;
-    using Q3 = std::integral_constant<int, 3>;
+    for (int g = 0; g < WT / 2; g++)
+        ld.s[g] = (uint32_t)std::min(wave % 2 * 32 * WT + 64 * g + lane, of_b ? last_b : last_a) * sp;
+    ld.kpad = kpad;
+    ld.upper = lane % 8 >= 4;
+    TileReads<WT> rd;
+    rd.a = (wm * WT * 32 + r) * 128, rd.b = (BM + wn * WT * 32 + r) * 128;
+    rd.sa = (wm * WT * 32 + r) * 16, rd.sb = (BM + wn * WT * 32 + r) * 16;
+    rd.half = lane / 32, rd.swz = r / 2 % 8;
+    // Wave's places, and those of chunk c's scales (run c / 2 starts at byte
+    // min(16 (c / 2), sp - 16) of a scale row).
+    auto put = [&](int c) { return lds.codes + (c & 1) * Lds::kStage + 2048 * WT * wave; };
+    auto put_scales = [&](int run) { return lds.scales[run & 1] + 32 * WT * 16 * wave; };
+    auto codes_of = [&](int c) { return lds.codes + (c & 1) * Lds::kStage; };
+    auto scales_of = [&](int c) { return lds.scales[c >> 1 & 1] + 8 * c - std::min(16 * (c >> 1), sp - 16); };
 
-    auto loads_done = [] {  // every wave's loads to LDS have arrived, and its reads are over
-        __builtin_amdgcn_s_waitcnt(0x0070);  // vmcnt(0) lgkmcnt(0)
-        __syncthreads();
-    };
-    const int steps = (kpad + kStepK - 1) / kStepK;  // the last one may be half a step
-    issue(0, 0);
-    load_scales(0);
-    write_scales(0);
-    load_scales(1);
-    loads_done();
-    read(0, 0), read(0, 1), read(0, 2), read(0, 3);
-    read_scales(0, 0), read_scales(0, 1);
-    issue(kStepK, 1);
-    mul(Q0{}), mul(Q1{}), mul(Q2{});
-    // Within a step the order of the instructions is laid down: an LDS read or a load
-    // for every multiplication, which takes longer.
-    auto interleave = [](auto kind, int count) {
-#pragma unroll
-        for (int i = 0; i < count; i++) {
-            __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
-            __builtin_amdgcn_sched_group_barrier(decltype(kind)::value, 1, 0);
-        }
-    };
-    using LdsRead = std::integral_constant<int, 0x100>;
-    using Load = std::integral_constant<int, 0x010>;
-    auto full_step = [&](int s) {
-        read(s & 1, 0), read(s & 1, 1);
-        read_scales(s, 0);
-        mul(Q3{});
-        interleave(LdsRead{}, 4 * WT + WT);
-        __builtin_amdgcn_sched_barrier(0);
-        read(s & 1, 2), read(s & 1, 3);
-        read_scales(s, 1);
-        issue((s + 1) * kStepK, (s & 1) ^ 1);
-        mul(Q0{}), mul(Q1{}), mul(Q2{});
-        interleave(LdsRead{}, 4 * WT + WT);
-        interleave(Load{}, 2 * LD);
-        __builtin_amdgcn_sched_barrier(0);
-    };
-    int s = 1;
-    for (; s < steps - 2; s += 2) {
-        loads_done();
-        write_scales((s + 1) / 2);
-        load_scales((s + 3) / 2);
-        full_step(s);
-        loads_done();
-        full_step(s + 1);
+    tile_load<WT>(put(0), put_scales(0), ga, gb, gs, ld, 0, 0, 0);
+    if constexpr (WT == 4) load_to_lds(gs, ld.s[1], 0, put_scales(0) + 1024);
+    f32x16 acc[WT][WT] = {};
+    Frags<WT> held;
+    ScaleWords<WT> s;
+    tile_meet();
+    tile_chunk<WT, true, false>(put(1), put_scales(1), codes_of(0), scales_of(0), ga, gb, gs, ld, rd, 0, 0, acc, held, s);
+    int c = 1;
+#pragma unroll 1
+    for (; c < chunks - 1; c++) {
+        tile_meet();
+        tile_chunk<WT, false, false>(put(c + 1), put_scales((c >> 1) + 1), codes_of(c), scales_of(c), ga, gb, gs, ld, rd, c,
+                                     0, acc, held, s);
     }
-    if (s < steps - 1) {
-        loads_done();
-        write_scales((s + 1) / 2);
-        full_step(s++);
-    }
-    loads_done();
-    read(s & 1, 0), read(s & 1, 1);
-    read_scales(s, 0);
-    mul(Q3{});
-    mul(Q0{}), mul(Q1{});
-    if (kpad % kStepK == 0) {
-        read(s & 1, 2), read(s & 1, 3);
-        read_scales(s, 1);
-        mul(Q2{}), mul(Q3{});
-    }
+    tile_meet();
+    tile_chunk<WT, false, true>(put(0), put_scales(0), codes_of(c), scales_of(c), ga, gb, gs, ld, rd, c,
+                                kpad % kChunkK ? 0u : ~0u, acc, held, s);
+    tile_mul<3, WT>(acc, held, s, rd.half);
 
     using St = Staged<T, 32 * WT>;
-    static_assert(4 * St::kBytes <= 2 * TileLds<WT>::kStage);
+    static_assert(4 * St::kBytes <= 2 * Lds::kStage);
     __syncthreads();  // every wave has read the last step
-    const St st{lds.codes[0] + wave * St::kBytes, lane};
+    const St st{lds.codes + wave * St::kBytes, lane};
 #pragma unroll
     for (int i = 0; i < WT; i++) {
 #pragma unroll
@@ -773,7 +827,7 @@ void multiply(const Product &p, const gs_mxfp4 &A)
             const int64_t tm = ceil_div(p.m, 64 * WT), tn = ceil_div(p.n, 64 * WT);
             if (tm * tn >= 1 << 24) fail(GS_ERR_UNSUPPORTED, "the product has too many tiles");
             k_tile<T, WT>
-                <<<(unsigned)(tm * tn), 256, 0, p.s>>>(A.codes, A.scales, p.B->codes, p.B->scales, p.m, p.n, p.kpad, tm, tn, out);
+                <<<(unsigned)(tm * tn), 256, 0, p.s>>>(A.codes, A.scales, p.B->codes, p.B->scales, p.m, p.n, p.kpad, (int)tm, (int)tn, out);
         };
         if (ceil_div(p.m, 256) * ceil_div(p.n, 256) >= 128)
             tiled(std::integral_constant<int, 4>{});
