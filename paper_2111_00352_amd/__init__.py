@@ -16,6 +16,7 @@ raise.
 from __future__ import annotations
 
 import ctypes
+import functools
 import os
 
 import torch
@@ -415,27 +416,35 @@ def weight_grad(H: torch.Tensor, G: torch.Tensor, stream=None) -> torch.Tensor:
 
 
 # ------------------------------------------------- low-bit forms of dense operands
+#
+# Calls on small operands are bound by what happens here, so arguments are looked at
+# once each and nothing is made that the call does not need.
 
 ACTIVATIONS = {"none": 0, "relu": 1}
 _DTYPES = {torch.float32: 0, torch.bfloat16: 1}
 
 
-def _dense(X: torch.Tensor, name: str, device=None) -> tuple:
-    """(tensor, leading dimension, dtype code) of a 2-D fp32 or bf16 operand on the current device."""
-    if (not isinstance(X, torch.Tensor) or not X.is_cuda or X.dtype not in _DTYPES or X.layout != torch.strided
-            or X.dim() != 2):
+def _dense(X: torch.Tensor, name: str, index=None) -> tuple:
+    """(tensor, leading dimension, dtype code, shape) of a 2-D fp32 or bf16 operand on
+    the current device (and on device `index`)."""
+    code = _DTYPES.get(X.dtype) if isinstance(X, torch.Tensor) else None
+    if code is None or not X.is_cuda or X.dim() != 2 or X.layout != torch.strided:
         raise ValueError(f"{name} must be a 2-D CUDA float32 or bfloat16 tensor")
-    if X.device.index != torch._C._cuda_getDevice() or (device is not None and X.device != device):
-        raise ValueError(f"{name} is not on the current device")
+    at = X.get_device()
+    if at != torch._C._cuda_getDevice() or (index is not None and at != index):
+        raise ValueError(f"{name} is not on the current device, or not on the other operand's")
     if X.is_neg():
         X = X.resolve_neg()
-    rows, cols = X.shape
-    if cols > 1 and rows > 0 and X.stride(1) != 1:
+    shape = X.shape
+    rows, cols = shape
+    ld, step = X.stride()
+    if step != 1 and cols > 1 and rows > 0:
         raise ValueError(f"{name} must have unit column stride")
-    ld = X.stride(0) if rows > 1 else cols
-    if rows > 1 and ld < cols:
-        raise ValueError(f"{name} must have a row stride of at least its width")
-    return X, max(ld, cols), _DTYPES[X.dtype]
+    if ld < cols or rows <= 1:
+        if rows > 1:
+            raise ValueError(f"{name} must have a row stride of at least its width")
+        ld = cols
+    return X, ld, code, shape
 
 
 def _dtype_code(dtype) -> int:
@@ -444,21 +453,20 @@ def _dtype_code(dtype) -> int:
     return _DTYPES[dtype]
 
 
-def _on(stream, call, *inputs):
-    """call() with `stream` as the current stream, so that what it allocates belongs to
-    it; memory of the inputs is not given out again before it has read them."""
-    if stream is None or _stream(stream) == _stream():
-        return call()
+def _on(stream, call, *args):
+    """call(*args) with `stream` as the current stream, so that what it allocates belongs
+    to it; memory of the arguments is not given out again before it has read them."""
+    if _stream(stream) == _stream():
+        return call(*args)
     if not isinstance(stream, torch.cuda.Stream):
         raw = _stream(stream)
         stream = torch.cuda.ExternalStream(raw) if raw else torch.cuda.default_stream()
     with torch.cuda.stream(stream):
-        out = call()
-    for t in inputs:
+        out = call(*args)
+    for t in args:
         if isinstance(t, (SavedActivation, Mxfp4)):
-            t.codes.record_stream(stream)
-            t.scales.record_stream(stream)
-        elif t is not None:
+            t._buf.record_stream(stream)
+        elif isinstance(t, torch.Tensor):
             t.record_stream(stream)
     return out
 
@@ -466,136 +474,162 @@ def _on(stream, call, *inputs):
 def _out(out, shape, dtype, device):
     """`out`, or a new tensor, and its leading dimension."""
     if out is None:
-        out = torch.empty(shape, dtype=dtype, device=device)
-        return out, shape[1]
-    if out.shape != torch.Size(shape) or out.dtype != dtype or out.is_neg():
+        return torch.empty(shape, dtype=dtype, device=device), shape[1]
+    if tuple(out.shape) != tuple(shape) or out.dtype != dtype or out.is_neg():
         raise ValueError("out has the wrong shape or dtype")
-    return out, _dense(out, "out", device)[1]
+    return out, _dense(out, "out", device.index)[1]
 
 
-def _arrays(rows, code_pitch, scale_pitch, device):
-    """Uninitialised code and scale arrays, from one allocation (both start 256-byte aligned)."""
-    nc = rows * code_pitch
-    at = -(-nc // 256) * 256
-    buf = torch.empty(at + rows * scale_pitch, dtype=torch.uint8, device=device)
-    return buf[:nc].view(rows, code_pitch), buf[at:].view(rows, scale_pitch)
+class _Blocks:
+    """Codes and scale bytes of a matrix in blocks of 32 columns, in one buffer."""
 
+    def __init__(self, shape, code_pitch, scale_pitch, device):
+        rows = shape[0]
+        self.shape = (rows, shape[1])
+        self.device = device
+        self._pitches = code_pitch, scale_pitch
+        self._at = at = -(-rows * code_pitch // 256) * 256  # (the scales start 256-byte aligned)
+        self._buf = buf = torch.empty(at + rows * scale_pitch, dtype=torch.uint8, device=device)
+        self._ptr = buf.data_ptr()
 
-class SavedActivation:
-    """Activations kept in 8 bits (gs_saved): codes, one power-of-two step per 32 columns of a row."""
+    @property
+    def codes(self) -> torch.Tensor:
+        rows, pitch = self.shape[0], self._pitches[0]
+        return self._buf[:rows * pitch].view(rows, pitch)
 
-    def __init__(self, codes: torch.Tensor, scales: torch.Tensor, shape, act: str):
-        self.codes, self.scales, self.act = codes, scales, act
-        self.shape = (int(shape[0]), int(shape[1]))
-        self.device = codes.device
-        self._c = _Saved(self.shape[0], self.shape[1], ACTIVATIONS[act], codes.data_ptr(), scales.data_ptr())
-        self._ref = ctypes.byref(self._c)
+    @property
+    def scales(self) -> torch.Tensor:
+        return self._buf[self._at:].view(self.shape[0], self._pitches[1])
 
     @property
     def device_bytes(self) -> int:
-        return self.codes.numel() + self.scales.numel()
+        return self.shape[0] * sum(self._pitches)
 
     def dequantize(self, dtype=torch.float32, stream=None) -> torch.Tensor:
-        """The values the codes stand for, exact in either type (gs_saved_dequantize)."""
+        """The values the codes stand for, exact in either type."""
+        if stream is not None:
+            return _on(stream, type(self).dequantize, self, dtype)
         code = _dtype_code(dtype)
+        out = torch.empty(self.shape, dtype=dtype, device=self.device)
+        rc = self._values(lib())(self._ref, out.data_ptr(), self.shape[1], code, _stream())
+        if rc:
+            _check(rc)
+        return out
 
-        def call():
-            out = torch.empty(self.shape, dtype=dtype, device=self.device)
-            _check(lib().gs_saved_dequantize(self._ref, out.data_ptr(), self.shape[1], code, _stream()))
-            return out
-        return _on(stream, call, self)
+
+class SavedActivation(_Blocks):
+    """Activations kept in 8 bits (gs_saved): codes, one power-of-two step per 32 columns of a row."""
+
+    def __init__(self, shape, act: str, device):
+        blocks = -(-shape[1] // 32)
+        super().__init__(shape, 32 * blocks, blocks, device)
+        self.act = act
+        self._c = _Saved(shape[0], shape[1], ACTIVATIONS[act], self._ptr, self._ptr + self._at)
+        self._ref = ctypes.byref(self._c)
+
+    @staticmethod
+    def _values(L):
+        return L.gs_saved_dequantize
+
+
+class Mxfp4(_Blocks):
+    """A matrix in MXFP4 (gs_mxfp4): e2m1 codes, one power-of-two scale per 32 columns of a row."""
+
+    def __init__(self, shape, device):
+        step = 64 if shape[1] <= 64 else 128
+        padded = -(-shape[1] // step) * step
+        super().__init__(shape, padded // 2, padded // 32, device)
+        self._c = _Mxfp4(shape[0], shape[1], self._ptr, self._ptr + self._at)
+        self._ref = ctypes.byref(self._c)
+
+    @staticmethod
+    def _values(L):
+        return L.gs_mxfp4_dequantize
 
 
 def save_activation(P: torch.Tensor, act: str = "relu", stream=None) -> tuple:
     """(H, saved): H = relu(P) (act "relu") or P itself (act "none"), and H in 8 bits
     for the backward pass (gs_save_activation)."""
+    if stream is not None:
+        return _on(stream, save_activation, P, act)
     if act not in ACTIVATIONS:
         raise ValueError("act must be 'relu' or 'none'")
-    P, ld, code = _dense(P, "P")
-    n, a = P.shape
-
-    def call():
-        saved = SavedActivation(*_arrays(n, -(-a // 32) * 32, -(-a // 32), P.device), (n, a), act)
-        H = torch.empty((n, a), dtype=P.dtype, device=P.device) if act == "relu" else None
-        _check(lib().gs_save_activation(P.data_ptr(), ld, code, saved._ref, None if H is None else H.data_ptr(), a,
-                                        _stream()))
-        return (P if H is None else H), saved
-    return _on(stream, call, P)
+    P, ld, code, shape = _dense(P, "P")
+    saved = SavedActivation(shape, act, P.device)
+    if act == "relu":
+        H = torch.empty_like(P) if ld == shape[1] else torch.empty(shape, dtype=P.dtype, device=P.device)
+        rc = lib().gs_save_activation(P.data_ptr(), ld, code, saved._ref, H.data_ptr(), shape[1], _stream())
+    else:
+        H = P
+        rc = lib().gs_save_activation(P.data_ptr(), ld, code, saved._ref, None, 0, _stream())
+    if rc:
+        _check(rc)
+    return H, saved
 
 
 def relu_grad(saved: SavedActivation, dH: torch.Tensor, out: torch.Tensor | None = None, stream=None) -> torch.Tensor:
     """dH where the saved ReLU was active, else 0 (gs_relu_grad); out may be dH."""
-    dH, ld, code = _dense(dH, "dH", saved.device)
-    if tuple(dH.shape) != saved.shape:
+    if stream is not None:
+        return _on(stream, relu_grad, saved, dH, out)
+    dH, ld, code, shape = _dense(dH, "dH", saved.device.index)
+    if shape != saved.shape:
         raise ValueError("dH and the saved activations have different shapes")
+    if out is None and ld == shape[1]:
+        dP, ldp = torch.empty_like(dH), ld  # (the quickest way to a tensor of this shape)
+    else:
+        dP, ldp = _out(out, shape, dH.dtype, dH.device)
+    rc = lib().gs_relu_grad(saved._ref, dH.data_ptr(), ld, code, dP.data_ptr(), ldp, _stream())
+    if rc:
+        _check(rc)
+    return dP
 
-    def call():
-        dP, ldp = _out(out, saved.shape, dH.dtype, dH.device)
-        _check(lib().gs_relu_grad(saved._ref, dH.data_ptr(), ld, code, dP.data_ptr(), ldp, _stream()))
-        return dP
-    return _on(stream, call, saved, dH, out)
+
+@functools.lru_cache(maxsize=1024)
+def _grad_work(n: int, a: int, b: int) -> int:
+    need = _u64()
+    _check(lib().gs_saved_weight_grad_workspace(n, a, b, ctypes.byref(need)))
+    return need.value
 
 
 def saved_weight_grad(saved: SavedActivation, G: torch.Tensor, stream=None) -> torch.Tensor:
     """H^T G in fp32 from saved activations H (n x a) and G (n x b) (gs_saved_weight_grad)."""
-    G, ld, code = _dense(G, "G", saved.device)
-    (n, a), b = saved.shape, G.shape[1]
-    if G.shape[0] != n:
+    if stream is not None:
+        return _on(stream, saved_weight_grad, saved, G)
+    G, ld, code, shape = _dense(G, "G", saved.device.index)
+    (n, a), b = saved.shape, shape[1]
+    if shape[0] != n:
         raise ValueError("G and the saved activations must have the same number of rows")
-
-    def call():
-        need = _u64()
-        _check(lib().gs_saved_weight_grad_workspace(n, a, b, ctypes.byref(need)))
-        out = torch.empty((a, b), dtype=torch.float32, device=G.device)
-        work = torch.empty(need.value, dtype=torch.uint8, device=G.device) if need.value else None
-        _check(lib().gs_saved_weight_grad(saved._ref, G.data_ptr(), ld, code, b, out.data_ptr(),
-                                          None if work is None else work.data_ptr(), need.value, _stream()))
-        return out
-    return _on(stream, call, saved, G)
-
-
-class Mxfp4:
-    """A matrix in MXFP4 (gs_mxfp4): e2m1 codes, one power-of-two scale per 32 columns of a row."""
-
-    def __init__(self, codes: torch.Tensor, scales: torch.Tensor, shape):
-        self.codes, self.scales = codes, scales
-        self.shape = (int(shape[0]), int(shape[1]))
-        self.device = codes.device
-        self._c = _Mxfp4(self.shape[0], self.shape[1], codes.data_ptr(), scales.data_ptr())
-        self._ref = ctypes.byref(self._c)
-
-    @property
-    def device_bytes(self) -> int:
-        return self.codes.numel() + self.scales.numel()
-
-    def dequantize(self, dtype=torch.float32, stream=None) -> torch.Tensor:
-        """The values the codes stand for, exact in either type (gs_mxfp4_dequantize)."""
-        code = _dtype_code(dtype)
-
-        def call():
-            out = torch.empty(self.shape, dtype=dtype, device=self.device)
-            _check(lib().gs_mxfp4_dequantize(self._ref, out.data_ptr(), self.shape[1], code, _stream()))
-            return out
-        return _on(stream, call, self)
+    need = _grad_work(n, a, b)
+    out = torch.empty((a, b), dtype=torch.float32, device=G.device)
+    work = torch.empty(need, dtype=torch.uint8, device=G.device) if need else None
+    rc = lib().gs_saved_weight_grad(saved._ref, G.data_ptr(), ld, code, b, out.data_ptr(),
+                                    None if work is None else work.data_ptr(), need, _stream())
+    if rc:
+        _check(rc)
+    return out
 
 
 def mxfp4_quantize(X: torch.Tensor, axis: int = 1, stream=None) -> Mxfp4:
     """X in MXFP4, with blocks of 32 along its rows (axis 1), or X^T with blocks along
     X's columns (axis 0): the operands of mxfp4_matmul for X W are X and W with axis 0
     (gs_mxfp4_quantize)."""
+    if stream is not None:
+        return _on(stream, mxfp4_quantize, X, axis)
     if axis not in (0, 1):
         raise ValueError("axis must be 0 or 1")
-    X, ld, code = _dense(X, "X")
-    rows, cols = X.shape
-    shape = (rows, cols) if axis == 1 else (cols, rows)
+    X, ld, code, (rows, cols) = _dense(X, "X")
+    q = Mxfp4((rows, cols) if axis == 1 else (cols, rows), X.device)
+    rc = lib().gs_mxfp4_quantize(X.data_ptr(), ld, code, rows, cols, axis, q._ref, _stream())
+    if rc:
+        _check(rc)
+    return q
 
-    def call():
-        step = 64 if shape[1] <= 64 else 128
-        padded = -(-shape[1] // step) * step
-        q = Mxfp4(*_arrays(shape[0], padded // 2, padded // 32, X.device), shape)
-        _check(lib().gs_mxfp4_quantize(X.data_ptr(), ld, code, rows, cols, axis, q._ref, _stream()))
-        return q
-    return _on(stream, call, X)
+
+@functools.lru_cache(maxsize=1024)
+def _matmul_work(m: int, n: int, k: int, a_code: int) -> int:
+    need = _u64()
+    _check(lib().gs_mxfp4_matmul_workspace(m, n, k, a_code, ctypes.byref(need)))
+    return need.value
 
 
 def mxfp4_matmul(A, B: Mxfp4, mask: SavedActivation | None = None, dtype=torch.float32,
@@ -603,35 +637,36 @@ def mxfp4_matmul(A, B: Mxfp4, mask: SavedActivation | None = None, dtype=torch.f
     """A B^T for A (m x k: an Mxfp4, or a dense tensor that is quantised along its rows
     within the call) and B (n x k, an Mxfp4), as fp32 or bf16 (gs_mxfp4_matmul).  mask:
     activations saved by a ReLU (m x n); the product is 0 where they are."""
+    if stream is not None:
+        return _on(stream, mxfp4_matmul, A, B, mask, dtype, out)
     code = _dtype_code(dtype)
     if not isinstance(B, Mxfp4):
         raise ValueError("B must be an Mxfp4")
+    device = B.device
     quantised = isinstance(A, Mxfp4)
     if quantised:
-        if A.device != B.device:
-            raise ValueError("A and B must be on the same device")
-        a_code = -1
+        if A.device != device or device.index != torch._C._cuda_getDevice():
+            raise ValueError("A and B must be on the current device")
+        a_code, (m, k) = -1, A.shape
     else:
-        A, lda, a_code = _dense(A, "A", B.device)
-    (m, k), n = A.shape, B.shape[0]
-    if k != B.shape[1]:
-        raise ValueError(f"A has {k} columns, B has {B.shape[1]}")
-    if mask is not None and (mask.shape != (m, n) or mask.device != B.device):
+        A, lda, a_code, (m, k) = _dense(A, "A", device.index)
+    n, kb = B.shape
+    if k != kb:
+        raise ValueError(f"A has {k} columns, B has {kb}")
+    if mask is not None and (mask.shape != (m, n) or mask.device != device):
         raise ValueError("the mask's shape or device is not the product's")
-
-    def call():
-        C, ldc = _out(out, (m, n), dtype, B.device)
-        need = _u64()
-        _check(lib().gs_mxfp4_matmul_workspace(m, n, k, a_code, ctypes.byref(need)))
-        work = torch.empty(need.value, dtype=torch.uint8, device=B.device) if need.value else None
-        tail = (B._ref, None if mask is None else mask._ref, C.data_ptr(), ldc, code,
-                None if work is None else work.data_ptr(), need.value, _stream())
-        if quantised:
-            _check(lib().gs_mxfp4_matmul(A._ref, *tail))
-        else:
-            _check(lib().gs_mxfp4_matmul_dense(A.data_ptr(), lda, a_code, m, *tail))
-        return C
-    return _on(stream, call, A, B, mask, out)
+    C, ldc = _out(out, (m, n), dtype, device)
+    need = _matmul_work(m, n, k, a_code)
+    work = torch.empty(need, dtype=torch.uint8, device=device) if need else None
+    mask_ref, at = None if mask is None else mask._ref, None if work is None else work.data_ptr()
+    if quantised:
+        rc = lib().gs_mxfp4_matmul(A._ref, B._ref, mask_ref, C.data_ptr(), ldc, code, at, need, _stream())
+    else:
+        rc = lib().gs_mxfp4_matmul_dense(A.data_ptr(), lda, a_code, m, B._ref, mask_ref, C.data_ptr(), ldc, code, at, need,
+                                         _stream())
+    if rc:
+        _check(rc)
+    return C
 
 
 def _features_dict(out: _Features) -> dict:

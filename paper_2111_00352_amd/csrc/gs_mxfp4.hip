@@ -48,12 +48,26 @@ __global__ __launch_bounds__(kUnitThreads) void k_mx4_rows(const T *__restrict__
     }
 }
 
-// Along the columns: out row c holds column c of X.  A workgroup takes 256 rows
-// x 32 columns of X: thread t loads column t % 32 of the 32 rows of block t / 32
-// and quantises them alone; the codes go out through LDS so that an out row
-// receives 128 contiguous bytes.
-constexpr int kColTile = 32;
+// Along the columns: out row c holds column c of X.  A workgroup takes 256 rows x 64
+// columns of X, a wave a block of 32 rows at a time: lane (g, j) = (lane / 8, lane % 8)
+// loads eight neighbouring columns (8 j on) of rows 4 g .. 4 g + 3, so that a load
+// reads whole lines, finds the columns' largest magnitudes across the eight g and
+// packs its four rows of each column into two bytes.  The codes go out through LDS,
+// where they meet those of the other blocks, as 128 contiguous bytes of an out row.
+constexpr int kColTile = 64;
 constexpr int kRowTile = 256;
+constexpr int kColBlocks = kRowTile / kMxBlock;
+
+// The larger of v in this lane and the lanes 8, 16, 32 away (by xor).
+__device__ __forceinline__ uint32_t max_over_rows(uint32_t v)
+{
+    uint32_t w = (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0x128, 0xf, 0xf, true);  // row_ror:8
+    v = w > v ? w : v;
+    w = (uint32_t)__shfl_xor((int)v, 16, kWave);
+    v = w > v ? w : v;
+    w = (uint32_t)__shfl_xor((int)v, 32, kWave);
+    return w > v ? w : v;
+}
 
 template <class T>
 __global__ __launch_bounds__(256) void k_mx4_cols(const T *__restrict__ X, int64_t ldx, int64_t rows, int64_t cols,
@@ -61,29 +75,46 @@ __global__ __launch_bounds__(256) void k_mx4_cols(const T *__restrict__ X, int64
                                                   int64_t scale_pitch, uint8_t *__restrict__ codes,
                                                   uint8_t *__restrict__ scales)
 {
-    __shared__ uint4 tile[kColTile][kRowTile / 32 + 1];
-    __shared__ uint8_t exps[kColTile][kRowTile / 32];
-    const int c = threadIdx.x % kColTile, blk = threadIdx.x / kColTile;
+    constexpr int kPitch = kColBlocks * 16 + 16;  // (the shift spreads columns over banks)
+    __shared__ __align__(16) uint8_t tile[kColTile * kPitch];
+    __shared__ uint8_t exps[kColTile][kColBlocks];
+    const int wave = threadIdx.x / kWave, g = threadIdx.x % kWave / 8, j = threadIdx.x % 8;
     for (int64_t t = blockIdx.x; t < tiles; t += gridDim.x) {
-        const int64_t r0 = (t % row_tiles) * kRowTile, c0 = (t / row_tiles) * kColTile;
-        float x[32];
-        uint32_t m = 0;
-        const int64_t rb = r0 + 32 * blk;
+        const int64_t r0 = (t % row_tiles) * kRowTile, c0 = (t / row_tiles) * kColTile, left = cols - c0 - 8 * j;
 #pragma unroll
-        for (int i = 0; i < 32; i++) {
-            x[i] = rb + i < rows && c0 + c < cols ? to_f32(X[(rb + i) * ldx + c0 + c]) : 0.0f;
-            const uint32_t b = __float_as_uint(x[i]) & 0x7fffffffu;
-            m = b > m ? b : m;
+        for (int h = 0; h < kColBlocks / 4; h++) {
+            const int blk = 4 * h + wave;
+            float x[8][4];
+            uint32_t m[8] = {};
+#pragma unroll
+            for (int i = 0; i < 4; i++) {
+                const int64_t row = r0 + 32 * blk + 4 * g + i;
+                typename Elems<T, 8>::type v = {};
+                if (row < rows) v = load_elems<T, 8>(X + row * ldx + c0 + 8 * j, left);
+#pragma unroll
+                for (int c = 0; c < 8; c++) {
+                    x[c][i] = to_f32((T)v[c]);
+                    const uint32_t b = __float_as_uint(x[c][i]) & 0x7fffffffu;
+                    m[c] = b > m[c] ? b : m[c];
+                }
+            }
+#pragma unroll
+            for (int c = 0; c < 8; c++) {
+                const int E8 = mx4_exponent(max_over_rows(m[c]));
+                *reinterpret_cast<u16 *>(tile + (8 * j + c) * kPitch + 16 * blk + 2 * g) = mx4_pack4(x[c], E8);
+                if (g == c) exps[8 * j + c][blk] = (uint8_t)E8;
+            }
         }
-        const int E8 = mx4_exponent(m);
-        tile[c][blk] = make_uint4(mx4_pack8(x, E8), mx4_pack8(x + 8, E8), mx4_pack8(x + 16, E8), mx4_pack8(x + 24, E8));
-        exps[c][blk] = (uint8_t)E8;
         __syncthreads();
-        const int oc = threadIdx.x / (kRowTile / 32), ob = threadIdx.x % (kRowTile / 32);
-        const int64_t at = r0 / 32 + ob;  // block of the out row
-        if (c0 + oc < cols && at < scale_pitch) {
-            *reinterpret_cast<uint4 *>(codes + (c0 + oc) * code_pitch + at * 16) = tile[oc][ob];
-            scales[(c0 + oc) * scale_pitch + at] = exps[oc][ob];
+#pragma unroll
+        for (int q = 0; q < kColTile * kColBlocks / 256; q++) {
+            const int e = q * 256 + threadIdx.x, c = e / kColBlocks, blk = e % kColBlocks;
+            const int64_t at = r0 / kMxBlock + blk;  // block of the out row
+            if (c0 + c < cols && at < scale_pitch) {
+                *reinterpret_cast<uint4 *>(codes + (c0 + c) * code_pitch + at * 16) =
+                    *reinterpret_cast<const uint4 *>(tile + c * kPitch + 16 * blk);
+                scales[(c0 + c) * scale_pitch + at] = exps[c][blk];
+            }
         }
         __syncthreads();
     }

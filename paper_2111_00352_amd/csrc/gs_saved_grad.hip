@@ -11,9 +11,11 @@
 //
 // Both operands are wanted with their rows, the k index of the product, running
 // inside a lane, and they lie in memory by rows.  A lane therefore loads CA
-// neighbouring columns of A (one dword at CA = 4) and CB of G in each of eight
-// rows: as many 8-deep fragments as it loads columns, without a trip through LDS,
-// of columns CA apart.  A wave's tile is 32 CA x 32 CB of the product.
+// neighbouring columns of A (one dword at CA = 4) and CB of G in each of eight rows:
+// as many 8-deep fragments as it loads columns, without a trip through LDS, of columns
+// CA (CB) apart.  A wave's tile is 32 CA x 32 CB of the product; a workgroup's eight
+// waves share it and split the rows, 16 at a time each, with the loads of the next
+// two steps in flight.
 #include <algorithm>
 #include <type_traits>
 
@@ -26,11 +28,12 @@ namespace {
 typedef float f32x16 __attribute__((ext_vector_type(16)));
 typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 
-constexpr int kGradWaves = 8;                   // of a workgroup, all on the same tile
-constexpr int kGradStep = 16;                   // rows a wave takes at a time
+constexpr int kGradWaves = 8;   // of a workgroup
+constexpr int kGradStep = 16;   // rows a wave takes at a time
 constexpr int kGradRows = kGradWaves * kGradStep;
 // Longest run of rows a wave sums before the partials are joined.
 constexpr int64_t kGradChainRows = 8192;
+constexpr int64_t kGradMaxLd = 1 << 26;  // (a lane's offset from its step's row has 32 bits)
 
 template <int C> struct CodeBytes;
 template <> struct CodeBytes<1> {
@@ -55,8 +58,8 @@ template <class T, int CA, int CB> struct GradStage {
     typename Elems<T, CB>::type g[8];
 };
 
-// T, CA, CB as above; RELU: codes are unsigned.  Workgroup (x, y): rows
-// [x * per, (x + 1) * per), tile y; its sums go to part + x * a * b.
+// Workgroup (x, y): rows [x * per, (x + 1) * per), columns of tile y; its sums go to
+// part + x * a * b.  RELU: codes are unsigned.
 template <class T, int CA, int CB, bool RELU>
 __global__ __launch_bounds__(kGradWaves * kWave, 2) void k_saved_grad(
     const uint8_t *__restrict__ codes, int64_t code_pitch, const uint8_t *__restrict__ scales, int64_t scale_pitch,
@@ -64,7 +67,7 @@ __global__ __launch_bounds__(kGradWaves * kWave, 2) void k_saved_grad(
 {
     constexpr int NP = sizeof(T) == 4 ? 3 : 1;  // bf16 parts of a gradient
     __shared__ float red[2][kGradWaves][16][kWave];
-    const int wave = threadIdx.x / kWave, lane = threadIdx.x % kWave;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave), lane = threadIdx.x % kWave;
     const int nbt = (b + 32 * CB - 1) / (32 * CB);
     const int a0 = (blockIdx.y / nbt) * 32 * CA, b0 = (blockIdx.y % nbt) * 32 * CB;
     // Columns of lane l's fragments.  Lanes past the padded codes repeat its last
@@ -73,103 +76,100 @@ __global__ __launch_bounds__(kGradWaves * kWave, 2) void k_saved_grad(
     auto col_a = [&](int l) { const int c = a0 + CA * l; return c < (int)code_pitch - CA ? c : (int)code_pitch - CA; };
     auto col_b = [&](int l) { const int c = b0 + CB * l; return c < b - CB ? c : b - CB; };
     const int half = lane / 32;
-    const uint8_t *pc = codes + col_a(lane % 32);
-    const uint8_t *ps = scales + col_a(lane % 32) / kMxBlock;
-    const T *pg = G + col_b(lane % 32);
     const int64_t r0 = (int64_t)blockIdx.x * per, r1 = r0 + per < n ? r0 + per : n;
+    int64_t r = r0 + wave * kGradStep;
+    // Addresses are a row's, the same for all lanes, and this lane's offset from it.
+    const uint32_t oc = 8 * half * (uint32_t)code_pitch + col_a(lane % 32);
+    const uint32_t os = 8 * half * (uint32_t)scale_pitch + col_a(lane % 32) / kMxBlock;
+    const uint32_t og = 8 * half * (uint32_t)ldg + col_b(lane % 32);
 
-    GradStage<T, CA, CB> st;
-    auto load = [&](int64_t r) {  // rows r + 8 * half + 0..7, zeros from r1 on
-        const int64_t first = r + 8 * half;
-        if (r + kGradStep <= r1) {
+    GradStage<T, CA, CB> st[2];
+    auto load = [&](GradStage<T, CA, CB> &st, int64_t row) {  // rows row + 8 * half + 0..7
+        const uint8_t *pc = codes + row * code_pitch, *ps = scales + row * scale_pitch;
+        const T *pg = G + row * ldg;
+        asm("" : "+s"(pc), "+s"(ps), "+s"(pg));  // (or every load would keep a pointer of its own)
 #pragma unroll
-            for (int j = 0; j < 8; j++) {
-                st.code[j] = *reinterpret_cast<const typename CodeBytes<CA>::type *>(pc + (first + j) * code_pitch);
-                st.scale[j] = ps[(first + j) * scale_pitch];
-                st.g[j] = *reinterpret_cast<const typename Elems<T, CB>::type *>(pg + (first + j) * ldg);
-            }
-        } else {
+        for (int j = 0; j < 8; j++) {
+            st.code[j] = *reinterpret_cast<const typename CodeBytes<CA>::type *>(pc + j * code_pitch + oc);
+            st.scale[j] = *(ps + j * scale_pitch + os);
+            st.g[j] = *reinterpret_cast<const typename Elems<T, CB>::type *>(pg + j * ldg + og);
+        }
+    };
+    auto load_end = [&](GradStage<T, CA, CB> &st, int64_t row) {  // the same with zeros from r1 on
 #pragma unroll
-            for (int j = 0; j < 8; j++) {
-                st.code[j] = 0;
-                st.scale[j] = 0;
-                st.g[j] = typename Elems<T, CB>::type{};
-                if (first + j < r1) {
-                    st.code[j] = *reinterpret_cast<const typename CodeBytes<CA>::type *>(pc + (first + j) * code_pitch);
-                    st.scale[j] = ps[(first + j) * scale_pitch];
-                    st.g[j] = *reinterpret_cast<const typename Elems<T, CB>::type *>(pg + (first + j) * ldg);
-                }
+        for (int j = 0; j < 8; j++) {
+            const int64_t at = row + 8 * half + j;
+            st.code[j] = 0;
+            st.scale[j] = 0;
+            st.g[j] = typename Elems<T, CB>::type{};
+            if (at < r1) {
+                st.code[j] = *reinterpret_cast<const typename CodeBytes<CA>::type *>(codes + at * code_pitch + col_a(lane % 32));
+                st.scale[j] = scales[at * scale_pitch + col_a(lane % 32) / kMxBlock];
+                st.g[j] = *reinterpret_cast<const typename Elems<T, CB>::type *>(G + at * ldg + col_b(lane % 32));
             }
         }
     };
-
+    uint4 fa[CA], fb[NP][CB];
+    auto fragments = [&](const GradStage<T, CA, CB> &st) {
+        auto pack = [](const uint32_t *v) {
+            return make_uint4(high_halves(v[0], v[1]), high_halves(v[2], v[3]), high_halves(v[4], v[5]),
+                              high_halves(v[6], v[7]));
+        };
+        float s[8];
+#pragma unroll
+        for (int j = 0; j < 8; j++) s[j] = mx_scale(st.scale[j]);
+#pragma unroll
+        for (int i = 0; i < CA; i++) {
+            uint32_t v[8];
+#pragma unroll
+            for (int j = 0; j < 8; j++) {
+                const int c = (int)(st.code[j] >> (8 * i) & 255);
+                v[j] = __float_as_uint((float)(RELU ? c : (int)(int8_t)c) * s[j]);
+            }
+            fa[i] = pack(v);
+            __builtin_amdgcn_sched_barrier(0);
+        }
+#pragma unroll
+        for (int i = 0; i < CB; i++) {
+            if constexpr (NP == 1) {
+                fb[0][i] = make_uint4(st.g[0][i] | (uint32_t)st.g[1][i] << 16, st.g[2][i] | (uint32_t)st.g[3][i] << 16,
+                                      st.g[4][i] | (uint32_t)st.g[5][i] << 16, st.g[6][i] | (uint32_t)st.g[7][i] << 16);
+            } else {
+                // g = hi + mid + lo, each the leading 8 bits of what is left
+                float rest[8], top = 0.0f;
+                uint32_t v[8];
+#pragma unroll
+                for (int j = 0; j < 8; j++) {
+                    const float g = st.g[j][i];
+                    v[j] = __float_as_uint(g);
+                    top = fmaxf(top, fabsf(g));
+                    rest[j] = g - __uint_as_float(v[j] & 0xffff0000u);
+                }
+                fb[0][i] = pack(v);
+                if (__any(top == __builtin_inff())) {  // (infinity less itself: it is all in hi)
+#pragma unroll
+                    for (int j = 0; j < 8; j++)
+                        if (fabsf((float)st.g[j][i]) == __builtin_inff()) rest[j] = 0.0f;
+                }
+#pragma unroll
+                for (int j = 0; j < 8; j++) {
+                    v[j] = __float_as_uint(rest[j]);
+                    rest[j] -= __uint_as_float(v[j] & 0xffff0000u);
+                }
+                fb[NP > 1 ? 1 : 0][i] = pack(v);
+#pragma unroll
+                for (int j = 0; j < 8; j++) v[j] = __float_as_uint(rest[j]);
+                fb[NP > 1 ? 2 : 0][i] = pack(v);
+            }
+            __builtin_amdgcn_sched_barrier(0);
+        }
+    };
     f32x16 acc[CA][CB];
 #pragma unroll
     for (int i = 0; i < CA; i++)
 #pragma unroll
         for (int j = 0; j < CB; j++) acc[i][j] = f32x16{};
-
-    int64_t r = r0 + wave * kGradStep;
-    if (r < r1) load(r);
-    for (; r < r1; r += kGradRows) {
-        uint4 fa[CA], fb[NP][CB];
-        {
-            float s[8];
-#pragma unroll
-            for (int j = 0; j < 8; j++) s[j] = mx_scale(st.scale[j]);
-#pragma unroll
-            for (int i = 0; i < CA; i++) {
-                uint32_t v[8];
-#pragma unroll
-                for (int j = 0; j < 8; j++) {
-                    const int c = (int)(st.code[j] >> (8 * i) & 255);
-                    v[j] = __float_as_uint((float)(RELU ? c : (int)(int8_t)c) * s[j]);
-                }
-                fa[i] = make_uint4(high_halves(v[0], v[1]), high_halves(v[2], v[3]), high_halves(v[4], v[5]),
-                                   high_halves(v[6], v[7]));
-            }
-        }
-        if constexpr (NP == 1) {
-#pragma unroll
-            for (int i = 0; i < CB; i++)
-                fb[0][i] = make_uint4(st.g[0][i] | (uint32_t)st.g[1][i] << 16, st.g[2][i] | (uint32_t)st.g[3][i] << 16,
-                                      st.g[4][i] | (uint32_t)st.g[5][i] << 16, st.g[6][i] | (uint32_t)st.g[7][i] << 16);
-        } else {
-            // g = hi + mid + lo, each the leading 8 bits of what is left
-            float rest[CB][8], top = 0.0f;
-#pragma unroll
-            for (int i = 0; i < CB; i++)
-#pragma unroll
-                for (int j = 0; j < 8; j++) {
-                    const float x = st.g[j][i];
-                    top = fmaxf(top, fabsf(x));
-                    rest[i][j] = x - __uint_as_float(__float_as_uint(x) & 0xffff0000u);
-                }
-            if (__any(top == __builtin_inff())) {  // (infinity less itself: it is all in hi)
-#pragma unroll
-                for (int i = 0; i < CB; i++)
-#pragma unroll
-                    for (int j = 0; j < 8; j++)
-                        if (fabsf(st.g[j][i]) == __builtin_inff()) rest[i][j] = 0.0f;
-            }
-#pragma unroll
-            for (int i = 0; i < CB; i++) {
-                uint32_t hi[8], mid[8], lo[8];
-#pragma unroll
-                for (int j = 0; j < 8; j++) {
-                    hi[j] = __float_as_uint((float)st.g[j][i]);
-                    mid[j] = __float_as_uint(rest[i][j]);
-                    lo[j] = __float_as_uint(rest[i][j] - __uint_as_float(mid[j] & 0xffff0000u));
-                }
-                fb[0][i] = make_uint4(high_halves(hi[0], hi[1]), high_halves(hi[2], hi[3]), high_halves(hi[4], hi[5]),
-                                      high_halves(hi[6], hi[7]));
-                fb[NP > 1 ? 1 : 0][i] = make_uint4(high_halves(mid[0], mid[1]), high_halves(mid[2], mid[3]),
-                                                   high_halves(mid[4], mid[5]), high_halves(mid[6], mid[7]));
-                fb[NP > 1 ? 2 : 0][i] = make_uint4(high_halves(lo[0], lo[1]), high_halves(lo[2], lo[3]),
-                                                   high_halves(lo[4], lo[5]), high_halves(lo[6], lo[7]));
-            }
-        }
-        if (r + kGradRows < r1) load(r + kGradRows);
+    auto multiply = [&] {
 #pragma unroll
         for (int p = NP - 1; p >= 0; p--)
 #pragma unroll
@@ -179,10 +179,40 @@ __global__ __launch_bounds__(kGradWaves * kWave, 2) void k_saved_grad(
                     acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, fa[i]),
                                                                         __builtin_bit_cast(bf16x8, fb[p][j]),
                                                                         acc[i][j], 0, 0, 0);
+    };
+    // Whole steps two at a time; the registers of one are loaded for the step after the
+    // next as soon as its fragments are made.
+    const int64_t whole = r1 - kGradStep;  // last row a whole step can start at
+    if (r <= whole) {
+        load(st[0], r);
+        if (r + kGradRows <= whole) load(st[1], r + kGradRows);
+#pragma unroll 1
+        for (; r + kGradRows <= whole; r += 2 * kGradRows) {
+            __builtin_amdgcn_sched_barrier(0);
+            fragments(st[0]);
+            if (r + 2 * kGradRows <= whole) load(st[0], r + 2 * kGradRows);
+            __builtin_amdgcn_sched_barrier(0);
+            multiply();
+            __builtin_amdgcn_sched_barrier(0);
+            fragments(st[1]);
+            if (r + 3 * kGradRows <= whole) load(st[1], r + 3 * kGradRows);
+            __builtin_amdgcn_sched_barrier(0);
+            multiply();
+        }
+        if (r <= whole) {
+            fragments(st[0]);
+            multiply();
+            r += kGradRows;
+        }
+    }
+    if (r < r1) {
+        load_end(st[0], r);
+        fragments(st[0]);
+        multiply();
     }
 
-    // The waves' sums are added in LDS, one 32 x 32 tile at a time, and stored as
-    // the workgroup's partial.  Accumulator: lane l, register e hold row
+    // The waves' sums are added in LDS, one 32 x 32 tile at a time, and stored as the
+    // workgroup's partial.  Accumulator: lane l, register e hold row
     // 8 (e / 4) + 4 (l / 32) + e % 4, column l % 32.
     float *out = part + (int64_t)blockIdx.x * a * b;
 #pragma unroll
@@ -209,6 +239,7 @@ struct GradPlan {
     int64_t tiles, chunks, per;
 };
 
+// One workgroup to a compute unit.
 GradPlan grad_plan(int64_t n, int64_t a, int64_t b)
 {
     GradPlan p;
@@ -217,7 +248,7 @@ GradPlan grad_plan(int64_t n, int64_t a, int64_t b)
     p.tiles = ceil_div(a, 32 * p.ca) * ceil_div(b, 32 * p.cb);
     const int64_t want = std::max(std::max<int64_t>(1, 256 / p.tiles), ceil_div(n, kGradChainRows * kGradWaves));
     p.chunks = std::max<int64_t>(1, std::min(want, ceil_div(n, kGradRows)));
-    p.per = ceil_div(ceil_div(std::max<int64_t>(n, 1), p.chunks), kGradRows) * kGradRows;
+    p.per = ceil_div(ceil_div(std::max<int64_t>(n, 1), p.chunks), kGradStep) * kGradStep;
     p.chunks = std::max<int64_t>(1, ceil_div(n, p.per));
     return p;
 }
@@ -253,6 +284,7 @@ int gs_saved_weight_grad(const gs_saved *A, const void *G, int64_t ldg, int dtyp
         const int64_t n = A->rows, a = A->cols;
         check_grad_sizes(n, a, b);
         check_operand("G", G, n, b, ldg, dtype_size(dtype));
+        if (n > 1 && ldg > kGradMaxLd) fail(GS_ERR_UNSUPPORTED, "G's leading dimension is at most 2^26");
         if (!out) fail(GS_ERR_INVALID_ARG, "null output");
         const GradPlan p = grad_plan(n, a, b);
         const uint64_t need = p.chunks > 1 ? (uint64_t)(p.chunks * a * b) * 4 : 0;
