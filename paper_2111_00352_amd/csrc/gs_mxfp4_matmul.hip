@@ -610,19 +610,23 @@ __device__ __forceinline__ void tile_meet()
     __builtin_amdgcn_sched_barrier(0);
 }
 
-// kpad >= 512, a multiple of 128.
+// Chunks [slice * per, (slice + 1) * per) of k (the last slice: to the end), slice =
+// blockIdx.y, per even, at least two of them; slice i's product goes to out i * m * n
+// elements on.  kpad >= 512, a multiple of 128.
 template <class T, int WT>
 __global__ __launch_bounds__(256, WT == 4 ? 1 : 2) void k_tile(const uint8_t *__restrict__ ac,
                                                                const uint8_t *__restrict__ as,
                                                                const uint8_t *__restrict__ bc,
                                                                const uint8_t *__restrict__ bs, int64_t m, int64_t n,
-                                                               int kpad, int tiles_m, int tiles_n, Out<T> out)
+                                                               int kpad, int per, int tiles_m, int tiles_n,
+                                                               Out<T> out)
 {
     constexpr int BM = 64 * WT;
     using Lds = TileLds<WT>;
     __shared__ Lds lds;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave), lane = threadIdx.x % kWave;
-    const int cp = kpad / 2, sp = kpad / kMxBlock, chunks = (kpad + kChunkK - 1) / kChunkK;
+    const int cp = kpad / 2, sp = kpad / kMxBlock, all = (kpad + kChunkK - 1) / kChunkK;
+    const int first = (int)blockIdx.y * per, chunks = blockIdx.y + 1 == gridDim.y ? all : first + per;  // the end
     // an XCD takes a contiguous run of tiles, in panels of 8 rows of them
     const int t = (int)xcd_tile(blockIdx.x, (int64_t)tiles_m * tiles_n);
     const int panel = t / (8 * tiles_n), in = t % (8 * tiles_n), ph = std::min(8, tiles_m - 8 * panel);
@@ -658,14 +662,15 @@ __global__ __launch_bounds__(256, WT == 4 ? 1 : 2) void k_tile(const uint8_t *__
     auto codes_of = [&](int c) { return lds.codes + (c & 1) * Lds::kStage; };
     auto scales_of = [&](int c) { return lds.scales[c >> 1 & 1] + 8 * c - std::min(16 * (c >> 1), sp - 16); };
 
-    tile_load<WT>(put(0), put_scales(0), ga, gb, gs, ld, 0, 0, 0);
-    if constexpr (WT == 4) load_to_lds(gs, ld.s[1], 0, put_scales(0) + 1024);
+    tile_load<WT>(put(0), put_scales(first / 2), ga, gb, gs, ld, first, first / 2, 0);
+    if constexpr (WT == 4) load_to_lds(gs, ld.s[1], std::min(8 * first, sp - 16), put_scales(first / 2) + 1024);
     f32x16 acc[WT][WT] = {};
     Frags<WT> held;
     ScaleWords<WT> s;
     tile_meet();
-    tile_chunk<WT, true, false>(put(1), put_scales(1), codes_of(0), scales_of(0), ga, gb, gs, ld, rd, 0, 0, acc, held, s);
-    int c = 1;
+    tile_chunk<WT, true, false>(put(1), put_scales(first / 2 + 1), codes_of(0), scales_of(first), ga, gb, gs, ld, rd, first,
+                                0, acc, held, s);
+    int c = first + 1;
 #pragma unroll 1
     for (; c < chunks - 1; c++) {
         tile_meet();
@@ -674,19 +679,39 @@ __global__ __launch_bounds__(256, WT == 4 ? 1 : 2) void k_tile(const uint8_t *__
     }
     tile_meet();
     tile_chunk<WT, false, true>(put(0), put_scales(0), codes_of(c), scales_of(c), ga, gb, gs, ld, rd, c,
-                                kpad % kChunkK ? 0u : ~0u, acc, held, s);
+                                chunks == all && kpad % kChunkK ? 0u : ~0u, acc, held, s);
     tile_mul<3, WT>(acc, held, s, rd.half);
 
     using St = Staged<T, 32 * WT>;
     static_assert(4 * St::kBytes <= 2 * Lds::kStage);
     __syncthreads();  // every wave has read the last step
     const St st{lds.codes + wave * St::kBytes, lane};
+    out.c += (int64_t)blockIdx.y * m * n;
 #pragma unroll
     for (int i = 0; i < WT; i++) {
 #pragma unroll
         for (int j = 0; j < WT; j++) st.put(j, acc[i][j]);
         st.store(out, m0 + 32 * (wm * WT + i), m, n0 + 32 * wn * WT, n);
     }
+}
+
+// C from `split` partial products of m x n, added in order.
+template <class T>
+__global__ __launch_bounds__(256) void k_join(const float *__restrict__ part, int split, int64_t m, int64_t n, Out<T> out)
+{
+    const int64_t col = ((int64_t)blockIdx.x * 256 + threadIdx.x) * 4, row = blockIdx.y;
+    if (col >= n) return;
+    Elems<float, 4>::type s = {};
+    constexpr int U = 4;  // partials in flight
+    for (int p = 0; p < split; p += U) {
+        Elems<float, 4>::type v[U] = {};
+#pragma unroll
+        for (int u = 0; u < U; u++)
+            if (p + u < split) v[u] = load_elems<float, 4>(part + ((int64_t)(p + u) * m + row) * n + col, n - col);
+#pragma unroll
+        for (int u = 0; u < U; u++) s += v[u];
+    }
+    out.template store_row<4>(row, col, n, typename Elems<T, 4>::type{from_f32<T>(s[0]), from_f32<T>(s[1]), from_f32<T>(s[2]), from_f32<T>(s[3])});
 }
 
 uint64_t round256(uint64_t x) { return (x + 255) / 256 * 256; }
@@ -720,11 +745,50 @@ bool quantised_inside(int64_t m, int64_t n, int kpad)
     }
 }
 
-// Workspace: A's codes and scales when A is dense and quantised first.
+// Tiles of a large product, and how many slices of k they are made in.
+struct TilePlan {
+    int wt, split, per;
+    int64_t tiles_m, tiles_n;
+};
+TilePlan tile_plan(int64_t m, int64_t n, int kpad)
+{
+    TilePlan p;
+    p.wt = ceil_div(m, 256) * ceil_div(n, 256) >= 128 ? 4 : 2;
+    p.tiles_m = ceil_div(m, 64 * p.wt);
+    p.tiles_n = ceil_div(n, 64 * p.wt);
+    // Slices of k are for products with fewer tiles than compute units.  A chunk takes a
+    // workgroup about 0.55 us; the second launch costs 4 us, and partial products are
+    // written and read at about 5 TB/s: 224 x 310 x 8192 20.1 us in one, 10.1 us in eight;
+    // 256 x 4096 x 4096 12.0 us in one, 19.7 us in four.
+    const int chunks = (kpad + kChunkK - 1) / kChunkK;
+    const int64_t idle = compute_units() / (p.tiles_m * p.tiles_n);
+    p.per = chunks;
+    p.split = 1;
+    double best = 0;
+    for (int per = 2; per < chunks; per += 2) {
+        const int split = chunks / per, longest = chunks - (split - 1) * per;
+        if (split < 2 || split > idle) continue;
+        const double gain = 0.55 * (chunks - longest) - 4.0 - (double)split * m * n * 8 / 5e6;
+        if (gain > best) {
+            best = gain;
+            p.per = per;
+            p.split = split;
+        }
+    }
+    return p;
+}
+
+uint64_t dense_bytes(int64_t m, int kpad) { return round256((uint64_t)m * kpad / 2) + round256((uint64_t)m * kpad / kMxBlock); }
+
+// Workspace: A's codes and scales when A is dense and quantised first, and the
+// partial products of slices of k.
 uint64_t workspace(int64_t m, int64_t n, int64_t k, int a_dtype)
 {
-    if (a_dtype < 0 || quantised_inside(m, n, (int)mx4_cols(k))) return 0;
-    return round256((uint64_t)m * mx4_cols(k) / 2) + round256((uint64_t)m * mx4_cols(k) / kMxBlock);
+    const int kpad = (int)mx4_cols(k);
+    uint64_t bytes = a_dtype < 0 || quantised_inside(m, n, kpad) ? 0 : dense_bytes(m, kpad);
+    if (way(m, n, kpad) == Way::kTile)
+        if (const TilePlan p = tile_plan(m, n, kpad); p.split > 1) bytes += (uint64_t)p.split * m * n * 4;
+    return bytes;
 }
 
 void check_out(int64_t m, int64_t n, const gs_saved *mask, void *C, int64_t ldc, int dtype)
@@ -753,6 +817,7 @@ struct Product {
     int64_t ldc;
     int dtype;
     hipStream_t s;
+    float *part;  // for slices of k
 };
 
 // f(Out<T>) for the product's type and mask.
@@ -820,19 +885,22 @@ void multiply(const Product &p, const gs_mxfp4 &A)
     const Way w = way(p.m, p.n, p.kpad);
     if (w == Way::kNarrow) return multiply_narrow(p, rows);
     if (w == Way::kFew) return multiply_few(p, rows);
-    with_out(p, [&](auto out) {
+    const TilePlan t = tile_plan(p.m, p.n, p.kpad);
+    if (t.tiles_m * t.tiles_n >= 1 << 24) fail(GS_ERR_UNSUPPORTED, "the product has too many tiles");
+    auto tiled = [&](auto wt, auto out) {
         using T = typename decltype(out)::type;
-        auto tiled = [&](auto wt) {
-            constexpr int WT = decltype(wt)::value;
-            const int64_t tm = ceil_div(p.m, 64 * WT), tn = ceil_div(p.n, 64 * WT);
-            if (tm * tn >= 1 << 24) fail(GS_ERR_UNSUPPORTED, "the product has too many tiles");
-            k_tile<T, WT>
-                <<<(unsigned)(tm * tn), 256, 0, p.s>>>(A.codes, A.scales, p.B->codes, p.B->scales, p.m, p.n, p.kpad, (int)tm, (int)tn, out);
-        };
-        if (ceil_div(p.m, 256) * ceil_div(p.n, 256) >= 128)
-            tiled(std::integral_constant<int, 4>{});
-        else
-            tiled(std::integral_constant<int, 2>{});
+        const dim3 grid((unsigned)(t.tiles_m * t.tiles_n), (unsigned)t.split);
+        k_tile<T, decltype(wt)::value><<<grid, 256, 0, p.s>>>(A.codes, A.scales, p.B->codes, p.B->scales, p.m, p.n, p.kpad, t.per,
+                                                              (int)t.tiles_m, (int)t.tiles_n, out);
+    };
+    auto sized = [&](auto out) {
+        t.wt == 4 ? tiled(std::integral_constant<int, 4>{}, out) : tiled(std::integral_constant<int, 2>{}, out);
+    };
+    if (t.split == 1) return with_out(p, sized);
+    sized(Out<float>{p.part, p.n, nullptr, 0});
+    GS_HIP(hipGetLastError());
+    with_out(p, [&](auto out) {
+        k_join<<<dim3((unsigned)ceil_div(p.n, 1024), (unsigned)p.m), 256, 0, p.s>>>(p.part, t.split, p.m, p.n, out);
     });
 }
 
@@ -862,7 +930,7 @@ int gs_mxfp4_matmul(const gs_mxfp4 *A, const gs_mxfp4 *B, const gs_saved *mask, 
         if (A->cols != B->cols) fail(GS_ERR_INVALID_ARG, "A and B have different widths");
         check_out(A->rows, B->rows, mask, C, ldc, dtype);
         check_work(work, work_bytes, workspace(A->rows, B->rows, A->cols, -1));
-        multiply({A->rows, B->rows, (int)mx4_cols(B->cols), B, mask, C, ldc, dtype, (hipStream_t)stream}, *A);
+        multiply({A->rows, B->rows, (int)mx4_cols(B->cols), B, mask, C, ldc, dtype, (hipStream_t)stream, (float *)work}, *A);
     });
 }
 
@@ -876,7 +944,7 @@ int gs_mxfp4_matmul_dense(const void *A, int64_t lda, int a_dtype, int64_t m, co
         check_operand("A", A, m, B->cols, lda, dtype_size(a_dtype));
         check_out(m, B->rows, mask, C, ldc, dtype);
         check_work(work, work_bytes, workspace(m, B->rows, B->cols, a_dtype));
-        const Product p{m, B->rows, (int)mx4_cols(B->cols), B, mask, C, ldc, dtype, (hipStream_t)stream};
+        Product p{m, B->rows, (int)mx4_cols(B->cols), B, mask, C, ldc, dtype, (hipStream_t)stream, nullptr};
         if (m == 0 || p.n == 0) return;
         const int k = (int)B->cols;
         if (quantised_inside(m, p.n, p.kpad)) {
@@ -885,7 +953,8 @@ int gs_mxfp4_matmul_dense(const void *A, int64_t lda, int a_dtype, int64_t m, co
             return;
         }
         uint8_t *codes = (uint8_t *)work;
-        const gs_mxfp4 q{m, B->cols, codes, codes + round256((uint64_t)m * mx4_cols(B->cols) / 2)};
+        p.part = (float *)(codes + dense_bytes(m, p.kpad));
+        const gs_mxfp4 q{m, B->cols, codes, codes + round256((uint64_t)m * p.kpad / 2)};
         mx4_quantize_rows(A, lda, a_dtype, m, B->cols, q.codes, q.scales, p.s);
         multiply(p, q);
     });

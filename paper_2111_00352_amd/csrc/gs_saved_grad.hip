@@ -33,7 +33,10 @@ constexpr int kGradStep = 16;   // rows a wave takes at a time
 constexpr int kGradRows = kGradWaves * kGradStep;
 // Longest run of rows a wave sums before the partials are joined.
 constexpr int64_t kGradChainRows = 8192;
+constexpr int64_t kGradOne = 1024;
 constexpr int64_t kGradMaxLd = 1 << 26;  // (a lane's offset from its step's row has 32 bits)
+
+#define GLOBAL __attribute__((address_space(1)))
 
 template <int C> struct CodeBytes;
 template <> struct CodeBytes<1> {
@@ -81,18 +84,18 @@ __global__ __launch_bounds__(kGradWaves * kWave, 2) void k_saved_grad(
     // Addresses are a row's, the same for all lanes, and this lane's offset from it.
     const uint32_t oc = 8 * half * (uint32_t)code_pitch + col_a(lane % 32);
     const uint32_t os = 8 * half * (uint32_t)scale_pitch + col_a(lane % 32) / kMxBlock;
-    const uint32_t og = 8 * half * (uint32_t)ldg + col_b(lane % 32);
+    const uint32_t og = (8 * half * (uint32_t)ldg + col_b(lane % 32)) * (uint32_t)sizeof(T);
 
     GradStage<T, CA, CB> st[2];
     auto load = [&](GradStage<T, CA, CB> &st, int64_t row) {  // rows row + 8 * half + 0..7
-        const uint8_t *pc = codes + row * code_pitch, *ps = scales + row * scale_pitch;
-        const T *pg = G + row * ldg;
+        uint64_t pc = (uint64_t)(codes + row * code_pitch), ps = (uint64_t)(scales + row * scale_pitch);
+        uint64_t pg = (uint64_t)(G + row * ldg);
         asm("" : "+s"(pc), "+s"(ps), "+s"(pg));  // (or every load would keep a pointer of its own)
 #pragma unroll
         for (int j = 0; j < 8; j++) {
-            st.code[j] = *reinterpret_cast<const typename CodeBytes<CA>::type *>(pc + j * code_pitch + oc);
-            st.scale[j] = *(ps + j * scale_pitch + os);
-            st.g[j] = *reinterpret_cast<const typename Elems<T, CB>::type *>(pg + j * ldg + og);
+            st.code[j] = *(const GLOBAL typename CodeBytes<CA>::type *)((const GLOBAL uint8_t *)(pc + j * code_pitch) + oc);
+            st.scale[j] = *((const GLOBAL uint8_t *)(ps + j * scale_pitch) + os);
+            st.g[j] = *(const GLOBAL typename Elems<T, CB>::type *)((const GLOBAL uint8_t *)(pg + j * ldg * sizeof(T)) + og);
         }
     };
     auto load_end = [&](GradStage<T, CA, CB> &st, int64_t row) {  // the same with zeros from r1 on
@@ -109,31 +112,44 @@ __global__ __launch_bounds__(kGradWaves * kWave, 2) void k_saved_grad(
             }
         }
     };
-    uint4 fa[CA], fb[NP][CB];
-    auto fragments = [&](const GradStage<T, CA, CB> &st) {
-        auto pack = [](const uint32_t *v) {
-            return make_uint4(high_halves(v[0], v[1]), high_halves(v[2], v[3]), high_halves(v[4], v[5]),
-                              high_halves(v[6], v[7]));
-        };
-        float s[8];
+    f32x16 acc[CA][CB];
 #pragma unroll
-        for (int j = 0; j < 8; j++) s[j] = mx_scale(st.scale[j]);
+    for (int i = 0; i < CA; i++)
 #pragma unroll
-        for (int i = 0; i < CA; i++) {
-            uint32_t v[8];
+        for (int j = 0; j < CB; j++) acc[i][j] = f32x16{};
+    auto pack = [](const uint32_t *v) {
+        return make_uint4(high_halves(v[0], v[1]), high_halves(v[2], v[3]), high_halves(v[4], v[5]),
+                          high_halves(v[6], v[7]));
+    };
+    // Multiplies the rows in st, then_load() once their registers are free.
+    auto multiply = [&](const GradStage<T, CA, CB> &st, auto &&then_load) {
+        uint4 fa[CA];
+        {
+            // 2^(E - 127), E > 0 here (0 beside codes of 0); E = 255 gives infinity, and z NaN
+            float s[8], z[8];
 #pragma unroll
             for (int j = 0; j < 8; j++) {
-                const int c = (int)(st.code[j] >> (8 * i) & 255);
-                v[j] = __float_as_uint((float)(RELU ? c : (int)(int8_t)c) * s[j]);
+                s[j] = __uint_as_float((uint32_t)st.scale[j] << 23);
+                z[j] = s[j] * 0.0f;
             }
-            fa[i] = pack(v);
-            __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+            for (int i = 0; i < CA; i++) {
+                uint32_t v[8];
+#pragma unroll
+                for (int j = 0; j < 8; j++) {
+                    const int c = (int)(st.code[j] >> (8 * i) & 255);
+                    v[j] = __float_as_uint(__builtin_fmaf((float)(RELU ? c : (int)(int8_t)c), s[j], z[j]));
+                }
+                fa[i] = pack(v);
+                __builtin_amdgcn_sched_barrier(0);
+            }
         }
 #pragma unroll
         for (int i = 0; i < CB; i++) {
+            uint4 fb[NP];
             if constexpr (NP == 1) {
-                fb[0][i] = make_uint4(st.g[0][i] | (uint32_t)st.g[1][i] << 16, st.g[2][i] | (uint32_t)st.g[3][i] << 16,
-                                      st.g[4][i] | (uint32_t)st.g[5][i] << 16, st.g[6][i] | (uint32_t)st.g[7][i] << 16);
+                fb[0] = make_uint4(st.g[0][i] | (uint32_t)st.g[1][i] << 16, st.g[2][i] | (uint32_t)st.g[3][i] << 16,
+                                   st.g[4][i] | (uint32_t)st.g[5][i] << 16, st.g[6][i] | (uint32_t)st.g[7][i] << 16);
             } else {
                 // g = hi + mid + lo, each the leading 8 bits of what is left
                 float rest[8], top = 0.0f;
@@ -145,8 +161,9 @@ __global__ __launch_bounds__(kGradWaves * kWave, 2) void k_saved_grad(
                     top = fmaxf(top, fabsf(g));
                     rest[j] = g - __uint_as_float(v[j] & 0xffff0000u);
                 }
-                fb[0][i] = pack(v);
+                fb[0] = pack(v);
                 if (__any(top == __builtin_inff())) {  // (infinity less itself: it is all in hi)
+                    asm volatile("");                  // (rare: not worth selects in every step)
 #pragma unroll
                     for (int j = 0; j < 8; j++)
                         if (fabsf((float)st.g[j][i]) == __builtin_inff()) rest[j] = 0.0f;
@@ -156,29 +173,23 @@ __global__ __launch_bounds__(kGradWaves * kWave, 2) void k_saved_grad(
                     v[j] = __float_as_uint(rest[j]);
                     rest[j] -= __uint_as_float(v[j] & 0xffff0000u);
                 }
-                fb[NP > 1 ? 1 : 0][i] = pack(v);
+                fb[NP > 1 ? 1 : 0] = pack(v);
 #pragma unroll
                 for (int j = 0; j < 8; j++) v[j] = __float_as_uint(rest[j]);
-                fb[NP > 1 ? 2 : 0][i] = pack(v);
+                fb[NP > 1 ? 2 : 0] = pack(v);
             }
-            __builtin_amdgcn_sched_barrier(0);
+            if (i == CB - 1) {
+                __builtin_amdgcn_sched_barrier(0);
+                then_load();
+                __builtin_amdgcn_sched_barrier(0);
+            }
+#pragma unroll
+            for (int p = NP - 1; p >= 0; p--)
+#pragma unroll
+                for (int k = 0; k < CA; k++)
+                    acc[k][i] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, fa[k]),
+                                                                        __builtin_bit_cast(bf16x8, fb[p]), acc[k][i], 0, 0, 0);
         }
-    };
-    f32x16 acc[CA][CB];
-#pragma unroll
-    for (int i = 0; i < CA; i++)
-#pragma unroll
-        for (int j = 0; j < CB; j++) acc[i][j] = f32x16{};
-    auto multiply = [&] {
-#pragma unroll
-        for (int p = NP - 1; p >= 0; p--)
-#pragma unroll
-            for (int i = 0; i < CA; i++)
-#pragma unroll
-                for (int j = 0; j < CB; j++)
-                    acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, fa[i]),
-                                                                        __builtin_bit_cast(bf16x8, fb[p][j]),
-                                                                        acc[i][j], 0, 0, 0);
     };
     // Whole steps two at a time; the registers of one are loaded for the step after the
     // next as soon as its fragments are made.
@@ -188,27 +199,17 @@ __global__ __launch_bounds__(kGradWaves * kWave, 2) void k_saved_grad(
         if (r + kGradRows <= whole) load(st[1], r + kGradRows);
 #pragma unroll 1
         for (; r + kGradRows <= whole; r += 2 * kGradRows) {
-            __builtin_amdgcn_sched_barrier(0);
-            fragments(st[0]);
-            if (r + 2 * kGradRows <= whole) load(st[0], r + 2 * kGradRows);
-            __builtin_amdgcn_sched_barrier(0);
-            multiply();
-            __builtin_amdgcn_sched_barrier(0);
-            fragments(st[1]);
-            if (r + 3 * kGradRows <= whole) load(st[1], r + 3 * kGradRows);
-            __builtin_amdgcn_sched_barrier(0);
-            multiply();
+            multiply(st[0], [&] { if (r + 2 * kGradRows <= whole) load(st[0], r + 2 * kGradRows); });
+            multiply(st[1], [&] { if (r + 3 * kGradRows <= whole) load(st[1], r + 3 * kGradRows); });
         }
         if (r <= whole) {
-            fragments(st[0]);
-            multiply();
+            multiply(st[0], [] {});
             r += kGradRows;
         }
     }
     if (r < r1) {
         load_end(st[0], r);
-        fragments(st[0]);
-        multiply();
+        multiply(st[0], [] {});
     }
 
     // The waves' sums are added in LDS, one 32 x 32 tile at a time, and stored as the
@@ -239,14 +240,17 @@ struct GradPlan {
     int64_t tiles, chunks, per;
 };
 
-// One workgroup to a compute unit.
+// A compute unit's share of the workgroups is one, or two where a wave's tile is a
+// single instruction's (its registers allow two).  Up to kGradOne rows one workgroup
+// sums them all, which saves the launch that joins partials.
 GradPlan grad_plan(int64_t n, int64_t a, int64_t b)
 {
     GradPlan p;
     p.ca = a <= 32 ? 1 : a <= 64 ? 2 : 4;
     p.cb = b <= 32 ? 1 : 2;
     p.tiles = ceil_div(a, 32 * p.ca) * ceil_div(b, 32 * p.cb);
-    const int64_t want = std::max(std::max<int64_t>(1, 256 / p.tiles), ceil_div(n, kGradChainRows * kGradWaves));
+    const int64_t fill = (p.ca * p.cb == 1 ? 512 : 256) / p.tiles;
+    const int64_t want = n <= kGradOne ? 1 : std::max(std::max<int64_t>(1, fill), ceil_div(n, kGradChainRows * kGradWaves));
     p.chunks = std::max<int64_t>(1, std::min(want, ceil_div(n, kGradRows)));
     p.per = ceil_div(ceil_div(std::max<int64_t>(n, 1), p.chunks), kGradStep) * kGradStep;
     p.chunks = std::max<int64_t>(1, ceil_div(n, p.per));
