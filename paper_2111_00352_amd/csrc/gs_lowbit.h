@@ -78,23 +78,30 @@ template <class T> __device__ __forceinline__ T from_f32(float x)
 }
 
 // E elements from p, of which the first `valid` are in the row; zeros after them.
-template <class T, int E>
+// NT: past the caches' replacement (as data that no one reads again soon).
+template <class T, int E, bool NT = false>
 __device__ __forceinline__ typename Elems<T, E>::type load_elems(const T *p, int64_t valid)
 {
     typename Elems<T, E>::type v;
     if (valid >= E) {
-        v = *reinterpret_cast<const typename Elems<T, E>::type *>(p);
+        if constexpr (NT)
+            v = __builtin_nontemporal_load(reinterpret_cast<const typename Elems<T, E>::type *>(p));
+        else
+            v = *reinterpret_cast<const typename Elems<T, E>::type *>(p);
     } else {
 #pragma unroll
         for (int i = 0; i < E; i++) v[i] = i < valid ? p[i] : T(0);
     }
     return v;
 }
-template <class T, int E>
+template <class T, int E, bool NT = false>
 __device__ __forceinline__ void store_elems(T *p, typename Elems<T, E>::type v, int64_t valid)
 {
     if (valid >= E) {
-        *reinterpret_cast<typename Elems<T, E>::type *>(p) = v;
+        if constexpr (NT)
+            __builtin_nontemporal_store(v, reinterpret_cast<typename Elems<T, E>::type *>(p));
+        else
+            *reinterpret_cast<typename Elems<T, E>::type *>(p) = v;
     } else {
 #pragma unroll
         for (int i = 0; i < E; i++)

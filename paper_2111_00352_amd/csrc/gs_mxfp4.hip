@@ -10,15 +10,23 @@
 namespace gs {
 namespace {
 
-// A lane takes 8 columns, four lanes a block.
-constexpr int kLaneCols = 8;
+// A lane takes 16 bytes of the dense operand: four or eight columns, so that a load
+// or store of a wave is contiguous.
+template <class T> constexpr int kLaneCols = 16 / sizeof(T);
+template <int E> struct Nibbles;
+template <> struct Nibbles<4> {
+    typedef u16 type;
+};
+template <> struct Nibbles<8> {
+    typedef uint32_t type;
+};
 
 template <class T>
 __global__ __launch_bounds__(kUnitThreads) void k_mx4_rows(const T *__restrict__ X, int64_t ldx, int64_t cols,
                                                            int64_t units, BlockDiv div, uint8_t *__restrict__ codes,
                                                            uint8_t *__restrict__ scales)
 {
-    constexpr int E = kLaneCols, L = kMxBlock / E;
+    constexpr int E = kLaneCols<T>, L = kMxBlock / E;
     typename Elems<T, E>::type v[kUnitRounds];
     for (int64_t u0 = (int64_t)blockIdx.x * kUnits; u0 < units; u0 += (int64_t)gridDim.x * kUnits) {
         const BlockAt first = block_first(div, u0 / L);
@@ -42,7 +50,10 @@ __global__ __launch_bounds__(kUnitThreads) void k_mx4_rows(const T *__restrict__
                 m = b > m ? b : m;
             }
             const int E8 = mx4_exponent(group_max<L>(m));
-            reinterpret_cast<uint32_t *>(codes)[u] = mx4_pack8(x, E8);
+            if constexpr (E == 8)
+                reinterpret_cast<uint32_t *>(codes)[u] = mx4_pack8(x, E8);
+            else
+                reinterpret_cast<u16 *>(codes)[u] = mx4_pack4(x, E8);
             if (u % L == 0) scales[u / L] = (uint8_t)E8;
         }
     }
@@ -126,8 +137,8 @@ __global__ __launch_bounds__(kUnitThreads) void k_mx4_values(const uint8_t *__re
                                                              int64_t scale_pitch, int64_t cols, int64_t units,
                                                              BlockDiv div, T *__restrict__ out, int64_t ld)
 {
-    constexpr int E = kLaneCols, L = kMxBlock / E;
-    uint32_t w[kUnitRounds];
+    constexpr int E = kLaneCols<T>, L = kMxBlock / E;
+    typename Nibbles<E>::type w[kUnitRounds];
     int E8[kUnitRounds];
     int64_t row[kUnitRounds];
     int32_t col[kUnitRounds];
@@ -140,7 +151,7 @@ __global__ __launch_bounds__(kUnitThreads) void k_mx4_values(const uint8_t *__re
             row[i] = at.row;
             col[i] = at.blk * kMxBlock + (t % L) * E;
             if (u0 + t < units) {
-                w[i] = *reinterpret_cast<const uint32_t *>(codes + row[i] * code_pitch + col[i] / 2);
+                w[i] = *reinterpret_cast<const typename Nibbles<E>::type *>(codes + row[i] * code_pitch + col[i] / 2);
                 E8[i] = scales[row[i] * scale_pitch + at.blk];
             }
         }
@@ -150,8 +161,11 @@ __global__ __launch_bounds__(kUnitThreads) void k_mx4_values(const uint8_t *__re
             if (u >= units || col[i] >= cols) continue;
             const float s = mx_scale(E8[i]);
             typename Elems<T, E>::type o;
-            f32x2 p[4] = {__builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w[i], 1.0f, 0), __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w[i], 1.0f, 1),
-                          __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w[i], 1.0f, 2), __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w[i], 1.0f, 3)};
+            f32x2 p[4] = {__builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w[i], 1.0f, 0), __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w[i], 1.0f, 1)};
+            if constexpr (E == 8) {
+                p[2] = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w[i], 1.0f, 2);
+                p[3] = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w[i], 1.0f, 3);
+            }
 #pragma unroll
             for (int e = 0; e < E; e++) o[e] = from_f32<T>(p[e / 2][e % 2] * s);
             store_elems<T, E>(out + row[i] * ld + col[i], o, cols - col[i]);
@@ -164,12 +178,14 @@ __global__ __launch_bounds__(kUnitThreads) void k_mx4_values(const uint8_t *__re
 void mx4_quantize_rows(const void *X, int64_t ldx, int dtype, int64_t rows, int64_t cols, uint8_t *codes,
                        uint8_t *scales, hipStream_t s)
 {
-    const int64_t nb = mx4_cols(cols) / kMxBlock, units = rows * nb * (kMxBlock / kLaneCols);
-    if (units == 0) return;
-    if (dtype == GS_F32)
-        k_mx4_rows<float><<<unit_grid(units), kUnitThreads, 0, s>>>((const float *)X, ldx, cols, units, block_div(nb), codes, scales);
-    else
-        k_mx4_rows<u16><<<unit_grid(units), kUnitThreads, 0, s>>>((const u16 *)X, ldx, cols, units, block_div(nb), codes, scales);
+    const int64_t nb = mx4_cols(cols) / kMxBlock;
+    if (rows * nb == 0) return;
+    auto go = [&](auto type) {
+        using T = decltype(type);
+        const int64_t units = rows * nb * (kMxBlock / kLaneCols<T>);
+        k_mx4_rows<T><<<unit_grid(units), kUnitThreads, 0, s>>>((const T *)X, ldx, cols, units, block_div(nb), codes, scales);
+    };
+    dtype == GS_F32 ? go(0.0f) : go(u16(0));
     GS_HIP(hipGetLastError());
 }
 
@@ -225,10 +241,10 @@ int gs_mxfp4_dequantize(const gs_mxfp4 *A, void *out, int64_t ld, int dtype, gs_
         check_operand("out", out, A->rows, A->cols, ld, dtype_size(dtype));
         if (A->rows == 0 || A->cols == 0) return;
         // (blocks of the matrix, without the padding of its rows)
-        const int64_t nb = ceil_div(A->cols, kMxBlock), units = A->rows * nb * (kMxBlock / kLaneCols);
-        const int64_t padded = mx4_cols(A->cols);
+        const int64_t nb = ceil_div(A->cols, kMxBlock), padded = mx4_cols(A->cols);
         auto go = [&](auto type) {
             using T = decltype(type);
+            const int64_t units = A->rows * nb * (kMxBlock / kLaneCols<T>);
             k_mx4_values<T><<<unit_grid(units), kUnitThreads, 0, (hipStream_t)stream>>>(
                 A->codes, A->scales, padded / 2, padded / kMxBlock, A->cols, units, block_div(nb), (T *)out, ld);
         };

@@ -32,6 +32,7 @@ template <class T> struct Out {
     int64_t ld;
     const uint8_t *mask;
     int64_t mask_pitch;
+    bool stream = false;  // stores past the caches' replacement
     // Columns col .. col + E - 1 (col a multiple of E, E 4 or 8) as far as they are below n.
     template <int E> __device__ __forceinline__ void store_row(int64_t row, int64_t col, int64_t n, typename Elems<T, E>::type v) const
     {
@@ -41,7 +42,10 @@ template <class T> struct Out {
             for (int e = 0; e < E; e++)
                 if ((p[e / 4] >> 8 * (e % 4) & 255) == 0) v[e] = T(0);
         }
-        store_elems<T, E>(c + row * ld + col, v, n - col);
+        if (stream)
+            store_elems<T, E, true>(c + row * ld + col, v, n - col);
+        else
+            store_elems<T, E>(c + row * ld + col, v, n - col);
     }
 };
 
@@ -107,12 +111,14 @@ struct MxRows {
     const uint8_t *codes, *scales;
     int64_t code_pitch;
     int scale_pitch;
+    static constexpr double kSize = 0.5;
     int width() const { return scale_pitch * kMxBlock; }
 };
 template <class T> struct DenseRows {
     const T *p;
     int64_t ld;
     int cols;
+    static constexpr double kSize = sizeof(T);
     int width() const { return cols; }
 };
 
@@ -121,9 +127,12 @@ template <class T> struct DenseRows {
 // rows(m0, the one after it) for each.  Loads are issued early, into the next rows at
 // the end of these, before this wave's stores to C (a load waits for the stores
 // issued before it).
-template <class Rows, int KS, bool FULL> struct RowSource;
+// FIT: kPadded rows, kFull ones (64 KS wide), or full ones that are loaded past the
+// caches' replacement.
+enum Fit { kPadded, kFull, kFullStream };
+template <class Rows, int KS, Fit FIT> struct RowSource;
 
-template <int KS, bool FULL> struct RowSource<MxRows, KS, FULL> {
+template <int KS, Fit FIT> struct RowSource<MxRows, KS, FIT> {
     const MxRows &A;
     int lane;
     u32x4 nf[KS];
@@ -139,7 +148,7 @@ template <int KS, bool FULL> struct RowSource<MxRows, KS, FULL> {
         for (int ks = 0; ks < KS; ks++) {
             const int blk = 2 * ks + lane / 32;
             nf[ks] = u32x4{};
-            if (FULL || blk < A.scale_pitch) {
+            if (FIT != kPadded || blk < A.scale_pitch) {
                 nf[ks] = *reinterpret_cast<const u32x4 *>(c + 16 * blk);
                 ns[ks / 4] |= (uint32_t)s[blk] << 8 * (ks % 4);
             }
@@ -156,7 +165,7 @@ template <int KS, bool FULL> struct RowSource<MxRows, KS, FULL> {
 };
 
 // Dense rows.  tmp: this wave's kNarrowTmp bytes of LDS.
-template <class T, int KS, bool FULL> struct RowSource<DenseRows<T>, KS, FULL> {
+template <class T, int KS, Fit FIT> struct RowSource<DenseRows<T>, KS, FIT> {
     static constexpr int E = 16 / sizeof(T), L = kMxBlock / E;  // elements a lane, lanes a block
     static constexpr int RB = 64 / (2 * L);                     // rows of a load instruction (two blocks of each)
     static constexpr int N = 32 / RB;                           // load instructions of a slice (64 of k)
@@ -176,8 +185,7 @@ template <class T, int KS, bool FULL> struct RowSource<DenseRows<T>, KS, FULL> {
 #pragma unroll
         for (int i = 0; i < N; i++) {
             const T *q = p + i * RB * A.ld + off;
-            v[ks % kAhead][i] = FULL ? *reinterpret_cast<const typename Elems<T, E>::type *>(q)
-                                     : load_elems<T, E>(q, A.cols - 64 * ks - lane % (2 * L) * E);
+            v[ks % kAhead][i] = load_elems<T, E, FIT == kFullStream>(q, FIT == kPadded ? A.cols - 64 * ks - lane % (2 * L) * E : E);
         }
     }
     __device__ __forceinline__ void start(int64_t m0)
@@ -242,8 +250,8 @@ template <class Rows> constexpr int narrow_waves(int KS)
 }
 
 // m >= 32: the last rows are taken as a full 32, some of them twice (with the same
-// results).  FULL: the rows are 64 KS wide, without padding.
-template <class Rows, class T, int KS, bool FULL>
+// results).
+template <class Rows, class T, int KS, Fit FIT>
 __global__ __launch_bounds__(kNarrowWaves * kWave, narrow_waves<Rows>(KS)) void k_narrow(Rows A, const uint8_t *__restrict__ bc,
                                                                  const uint8_t *__restrict__ bs, int64_t m, int64_t n,
                                                                  int kpad, int panel, int gx,
@@ -280,7 +288,7 @@ __global__ __launch_bounds__(kNarrowWaves * kWave, narrow_waves<Rows>(KS)) void 
     int64_t m0 = ((int64_t)(blockIdx.x % gx) * kNarrowWaves + wave) * 32;
     if (m0 >= m) return;
     uint8_t *own = tmp + wave * (kNarrowTmp + kNarrowOut);
-    RowSource<Rows, KS, FULL> src(A, lane, own);
+    RowSource<Rows, KS, FIT> src(A, lane, own);
     const Staged<T, kNarrowLine / sizeof(T)> st{own + kNarrowTmp, lane};
     src.start(std::min(m0, m - 32));
     for (; m0 < m; m0 += step) {
@@ -844,13 +852,22 @@ template <class Rows> void multiply_narrow(const Product &p, const Rows &A)
     if (gx * panels >= 1 << 24) fail(GS_ERR_UNSUPPORTED, "the product has too many tiles");
     with_out(p, [&](auto out) {
         using T = typename decltype(out)::type;
-        auto go = [&](auto ks, auto full) {
+        // C past the caches: 500,000 x 128 x 128 fp32 105 -> 81 us; and A where both are
+        // far larger than these: 1,000,000 x 64 x 128 175 -> 152 us (the former: 96 us).
+        out.stream = true;
+        const double bytes = (double)p.m * (A.width() * Rows::kSize + p.n * sizeof(T));
+        auto go = [&](auto ks, auto fit) {
             constexpr int K = decltype(ks)::value;
             const size_t lds = panel / 32 * (K * 1024 + (K + 3) / 4 * 256) + kNarrowWaves * (kNarrowTmp + kNarrowOut);
-            k_narrow<Rows, T, K, decltype(full)::value><<<(unsigned)(gx * panels), kNarrowWaves * kWave, lds, p.s>>>(
+            k_narrow<Rows, T, K, decltype(fit)::value><<<(unsigned)(gx * panels), kNarrowWaves * kWave, lds, p.s>>>(
                 A, p.B->codes, p.B->scales, p.m, p.n, p.kpad, (int)panel, (int)gx, out);
         };
-        auto sized = [&](auto ks) { A.width() == 64 * KS ? go(ks, std::true_type{}) : go(ks, std::false_type{}); };
+        auto sized = [&](auto ks) {
+            if (A.width() != 64 * KS) return go(ks, std::integral_constant<Fit, kPadded>{});
+            if constexpr (!std::is_same_v<Rows, MxRows>)
+                if (bytes > 700e6) return go(ks, std::integral_constant<Fit, kFullStream>{});
+            go(ks, std::integral_constant<Fit, kFull>{});
+        };
         if (KS == 1)
             sized(std::integral_constant<int, 1>{});
         else if (KS == 2)
@@ -896,7 +913,11 @@ void multiply(const Product &p, const gs_mxfp4 &A)
     auto sized = [&](auto out) {
         t.wt == 4 ? tiled(std::integral_constant<int, 4>{}, out) : tiled(std::integral_constant<int, 2>{}, out);
     };
-    if (t.split == 1) return with_out(p, sized);
+    if (t.split == 1)
+        return with_out(p, [&](auto out) {
+            out.stream = true;  // (4096^3 to bf16: 38.3 us, 40.4 us without; 2048^3 to fp32 10.5 and 11.4)
+            sized(out);
+        });
     sized(Out<float>{p.part, p.n, nullptr, 0});
     GS_HIP(hipGetLastError());
     with_out(p, [&](auto out) {
