@@ -232,6 +232,9 @@ MATMULS = [(1, 1, 1), (1, 64, 4096), (1, 1000, 100), (2, 33, 64), (5, 4096, 256)
            (32, 257, 2048), (33, 64, 128), (64, 48, 7000), (65, 2, 16), (100, 129, 130), (128, 128, 128), (129, 256, 512),
            (200, 300, 64), (257, 511, 384), (513, 65, 96), (1000, 128, 128), (3000, 47, 257), (20_011, 64, 100),
            (256, 256, 5000), (520, 776, 1024)]
+# products in slices of k (few tiles, long k), and of enough tiles for the larger ones:
+# ragged, and whole with half a chunk of k at the end
+MATMULS += [(150, 300, 4500), (129, 66, 8064), (700, 513, 2100), (4096, 2100, 700), (2816, 3328, 1152)]
 
 
 @pytest.mark.parametrize("m,n,k", MATMULS)
@@ -311,6 +314,35 @@ def test_empty_operands():
     assert torch.equal(gs.mxfp4_matmul(torch.empty(4, 0, device=DEV), B), torch.zeros(4, 7, device=DEV))
     assert gs.mxfp4_matmul(torch.empty(0, 64, device=DEV), gs.mxfp4_quantize(torch.ones(7, 64, device=DEV))).shape == (0, 7)
     assert gs.mxfp4_matmul(torch.ones(4, 64, device=DEV), gs.mxfp4_quantize(torch.empty(0, 64, device=DEV))).shape == (4, 0)
+
+
+@pytest.mark.parametrize("a", [128, 100, 64])
+def test_calls_larger_than_the_caches(a):
+    # more than 700 MB of operands, where loads and stores go past the caches: any rows
+    # are those of a call with these rows alone
+    n, b = 1_800_001 if a == 64 else 1_000_003, 70
+    gen = torch.Generator(device=DEV).manual_seed(a)
+    P = torch.randn(n, a, device=DEV, generator=gen)
+    W = gs.mxfp4_quantize(torch.randn(b, a, device=DEV, generator=gen))
+    H, saved = gs.save_activation(P)
+    grad, values = gs.relu_grad(saved, P), saved.dequantize()
+    q, cols, C = gs.mxfp4_quantize(P), gs.mxfp4_quantize(P, axis=0), gs.mxfp4_matmul(P, W)
+    Cq, back = gs.mxfp4_matmul(q, W), q.dequantize()
+    for at in (0, 31 * 32, n // 64 * 32, n // 32 * 32 - 256, n - 100):
+        rows = slice(at, min(at + 256, n))
+        p = P[rows].contiguous()
+        h, s = gs.save_activation(p)
+        assert torch.equal(H[rows], h) and torch.equal(saved.codes[rows], s.codes) and torch.equal(saved.scales[rows], s.scales)
+        assert torch.equal(values[rows], s.dequantize()) and torch.equal(grad[rows], gs.relu_grad(s, p))
+        x = gs.mxfp4_quantize(p)
+        assert torch.equal(q.codes[rows], x.codes) and torch.equal(q.scales[rows], x.scales)
+        assert torch.equal(back[rows], x.dequantize())
+        c = gs.mxfp4_matmul(p, W)
+        assert torch.equal(C[rows], c) and torch.equal(Cq[rows], c)
+        if at % 32 == 0 and len(p) == 256:
+            y = gs.mxfp4_quantize(p, axis=0)
+            assert torch.equal(cols.codes[:, at // 2:at // 2 + 128], y.codes)
+            assert torch.equal(cols.scales[:, at // 32:at // 32 + 8], y.scales)
 
 
 def test_offsets_past_32_bits():
