@@ -65,6 +65,9 @@ __global__ __launch_bounds__(kUnitThreads) void k_mx4_rows(const T *__restrict__
 // reads whole lines, finds the columns' largest magnitudes across the eight g and
 // packs its four rows of each column into two bytes.  The codes go out through LDS,
 // where they meet those of the other blocks, as 128 contiguous bytes of an out row.
+// Neighbouring workgroups take neighbouring columns, the rest of the same rows of X:
+// 4096 x 4096 bf16 11.0 us, 13.6 us with neighbours along the rows; 8192 x 8192 37 and
+// 48 us.
 constexpr int kColTile = 64;
 constexpr int kRowTile = 256;
 constexpr int kColBlocks = kRowTile / kMxBlock;
@@ -82,7 +85,7 @@ __device__ __forceinline__ uint32_t max_over_rows(uint32_t v)
 
 template <class T>
 __global__ __launch_bounds__(256) void k_mx4_cols(const T *__restrict__ X, int64_t ldx, int64_t rows, int64_t cols,
-                                                  int64_t row_tiles, int64_t tiles, int64_t code_pitch,
+                                                  int64_t col_tiles, int64_t tiles, int64_t code_pitch,
                                                   int64_t scale_pitch, uint8_t *__restrict__ codes,
                                                   uint8_t *__restrict__ scales)
 {
@@ -91,7 +94,7 @@ __global__ __launch_bounds__(256) void k_mx4_cols(const T *__restrict__ X, int64
     __shared__ uint8_t exps[kColTile][kColBlocks];
     const int wave = threadIdx.x / kWave, g = threadIdx.x % kWave / 8, j = threadIdx.x % 8;
     for (int64_t t = blockIdx.x; t < tiles; t += gridDim.x) {
-        const int64_t r0 = (t % row_tiles) * kRowTile, c0 = (t / row_tiles) * kColTile, left = cols - c0 - 8 * j;
+        const int64_t r0 = (t / col_tiles) * kRowTile, c0 = (t % col_tiles) * kColTile, left = cols - c0 - 8 * j;
 #pragma unroll
         for (int h = 0; h < kColBlocks / 4; h++) {
             const int blk = 4 * h + wave;
@@ -221,12 +224,12 @@ int gs_mxfp4_quantize(const void *X, int64_t ldx, int dtype, int64_t rows, int64
             mx4_quantize_rows(X, ldx, dtype, rows, cols, out->codes, out->scales, s);
             return;
         }
-        const int64_t padded = mx4_cols(rows), row_tiles = ceil_div(padded, kRowTile);
-        const int64_t tiles = row_tiles * ceil_div(cols, kColTile);
+        const int64_t padded = mx4_cols(rows), col_tiles = ceil_div(cols, kColTile);
+        const int64_t tiles = ceil_div(padded, kRowTile) * col_tiles;
         const unsigned grid = (unsigned)std::min<int64_t>(tiles, 1 << 20);
         auto go = [&](auto type) {
             using T = decltype(type);
-            k_mx4_cols<T><<<grid, 256, 0, s>>>((const T *)X, ldx, rows, cols, row_tiles, tiles, padded / 2,
+            k_mx4_cols<T><<<grid, 256, 0, s>>>((const T *)X, ldx, rows, cols, col_tiles, tiles, padded / 2,
                                               padded / kMxBlock, out->codes, out->scales);
         };
         dtype == GS_F32 ? go(0.0f) : go(u16(0));

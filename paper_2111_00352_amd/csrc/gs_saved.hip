@@ -111,6 +111,10 @@ __device__ __forceinline__ void walk_units(int64_t units, const BlockDiv &div, i
     }
 }
 
+// 1.5 * 2^23: the sum with a number below 2^22 is rounded to a whole one, whose low bits
+// are those of the sum.
+constexpr float kWhole = 12582912.0f;
+
 template <class T, bool RELU, bool NT>
 __global__ __launch_bounds__(kUnitThreads) void k_save(const T *__restrict__ P, int64_t ldp, int64_t cols,
                                                        int64_t units, BlockDiv div, uint8_t *__restrict__ codes,
@@ -140,19 +144,16 @@ __global__ __launch_bounds__(kUnitThreads) void k_save(const T *__restrict__ P, 
             uint32_t w[E / 4];
 #pragma unroll
             for (int q = 0; q < E / 4; q++) {
-                w[q] = 0;
+                uint32_t c[4];
 #pragma unroll
                 for (int e = 0; e < 4; e++) {
-                    const float r = __builtin_rintf(h[4 * q + e] * inv);
-                    if constexpr (RELU) {
-                        // (clamped to 255 by the conversion; a NaN gives 1; past the row 0)
-                        const float c = on[4 * q + e] ? fmaxf(r, 1.0f) : 0.0f;
-                        w[q] = __builtin_amdgcn_cvt_pk_u8_f32(c, e, w[q]);
-                    } else {
-                        const int c = (int)fminf(fmaxf(r, -127.0f), 127.0f);
-                        w[q] |= (uint32_t)(c & 255) << (8 * e);
-                    }
+                    // (nearest whole number, ties to even, in the low byte; a NaN gives the lower bound)
+                    const float r = __builtin_amdgcn_fmed3f(__builtin_fmaf(h[4 * q + e], inv, kWhole), kWhole + (RELU ? 1 : -127),
+                                                            kWhole + (RELU ? 255 : 127));
+                    c[e] = __float_as_uint(r);
+                    if (RELU) c[e] = on[4 * q + e] ? c[e] : 0;
                 }
+                w[q] = __builtin_amdgcn_perm(c[1], c[0], 0x0c0c0400) | __builtin_amdgcn_perm(c[3], c[2], 0x04000c0c);
                 if (!RELU && E8 == 255) w[q] = 0;
             }
             *reinterpret_cast<typename Codes<E>::type *>(codes + u * E) = code_words<E>(w);
