@@ -72,16 +72,111 @@ constexpr int kColTile = 64;
 constexpr int kRowTile = 256;
 constexpr int kColBlocks = kRowTile / kMxBlock;
 
-// The larger of v in this lane and the lanes 8, 16, 32 away (by xor).
-__device__ __forceinline__ uint32_t max_over_rows(uint32_t v)
+// Swaps a's lanes 32 .. 63 with b's lanes 0 .. 31, and a's lanes 16 .. 31 and 48 .. 63
+// with b's 0 .. 15 and 32 .. 47.
+__device__ __forceinline__ void swap_halves(uint32_t &a, uint32_t &b)
 {
-    uint32_t w = (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0x128, 0xf, 0xf, true);  // row_ror:8
-    v = w > v ? w : v;
-    w = (uint32_t)__shfl_xor((int)v, 16, kWave);
-    v = w > v ? w : v;
-    w = (uint32_t)__shfl_xor((int)v, 32, kWave);
-    return w > v ? w : v;
+    const auto r = __builtin_amdgcn_permlane32_swap(a, b, false, false);
+    a = r[0];
+    b = r[1];
 }
+__device__ __forceinline__ void swap_rows(uint32_t &a, uint32_t &b)
+{
+    const auto r = __builtin_amdgcn_permlane16_swap(a, b, false, false);
+    a = r[0];
+    b = r[1];
+}
+__device__ __forceinline__ uint32_t larger(uint32_t a, uint32_t b) { return a > b ? a : b; }
+
+// The largest m[c] over the eight lanes with this lane's j, for two of the eight columns c:
+// 2 (lane / 16) and the next one.  Each swap folds two columns at once.
+__device__ __forceinline__ void max_over_rows(uint32_t (&m)[8], uint32_t (&top)[2])
+{
+#pragma unroll
+    for (int c = 0; c < 4; c++) {
+        swap_halves(m[c], m[c + 4]);
+        m[c] = larger(m[c], m[c + 4]);
+    }
+#pragma unroll
+    for (int c = 0; c < 2; c++) {
+        swap_rows(m[c], m[c + 2]);
+        const uint32_t v = larger(m[c], m[c + 2]);
+        top[c] = larger(v, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0x128, 0xf, 0xf, true));  // row_ror:8
+    }
+}
+
+// All eight columns' values in every lane, from that distribution.
+__device__ __forceinline__ void to_all_rows(const uint32_t (&v)[2], uint32_t (&all)[8])
+{
+#pragma unroll
+    for (int c = 0; c < 2; c++) {
+        all[c] = all[c + 2] = v[c];
+        swap_rows(all[c], all[c + 2]);
+    }
+#pragma unroll
+    for (int c = 0; c < 4; c++) {
+        all[c + 4] = all[c];
+        swap_halves(all[c], all[c + 4]);
+    }
+}
+
+// Four rows of eight columns in a lane.
+template <class T> struct ColLane;
+template <> struct ColLane<float> {
+    float x[8][4];
+    __device__ __forceinline__ void set(int i, typename Elems<float, 8>::type v)
+    {
+#pragma unroll
+        for (int c = 0; c < 8; c++) x[c][i] = v[c];
+    }
+    __device__ __forceinline__ void magnitudes(uint32_t (&m)[8]) const
+    {
+#pragma unroll
+        for (int c = 0; c < 8; c++) {
+            m[c] = 0;
+#pragma unroll
+            for (int i = 0; i < 4; i++) m[c] = larger(m[c], __float_as_uint(x[c][i]) & 0x7fffffffu);
+        }
+    }
+    // What pack() takes of a scale byte.
+    static __device__ __forceinline__ uint32_t factor(int E8) { return __float_as_uint(mx_inverse(E8)); }
+    __device__ __forceinline__ u16 pack(int c, uint32_t f) const
+    {
+        const float inv = __uint_as_float(f);
+        uint32_t w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(0, x[c][0] * inv, x[c][1] * inv, 1.0f, 0);
+        w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, x[c][2] * inv, x[c][3] * inv, 1.0f, 1);
+        return f ? (u16)w : 0;
+    }
+};
+template <> struct ColLane<u16> {
+    typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+    typedef u16 u16x2 __attribute__((ext_vector_type(2)));
+    typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+    u32x4 x[4];  // two columns a word
+    __device__ __forceinline__ void set(int i, typename Elems<u16, 8>::type v) { x[i] = __builtin_bit_cast(u32x4, v); }
+    __device__ __forceinline__ void magnitudes(uint32_t (&m)[8]) const
+    {
+#pragma unroll
+        for (int p = 0; p < 4; p++) {
+            u16x2 top = {};
+#pragma unroll
+            for (int i = 0; i < 4; i++)
+                top = __builtin_elementwise_max(top, __builtin_bit_cast(u16x2, x[i][p] & 0x7fff7fffu));
+            const uint32_t t = __builtin_bit_cast(uint32_t, top);
+            m[2 * p] = t << 16;
+            m[2 * p + 1] = t & 0xffff0000u;
+        }
+    }
+    static __device__ __forceinline__ uint32_t factor(int E8) { return E8 ? (uint32_t)E8 << 23 : 0x00400000u; }
+    __device__ __forceinline__ u16 pack(int c, uint32_t f) const
+    {
+        const uint32_t pick = c % 2 ? 0x07060302 : 0x05040100;
+        auto rows = [&](int i) { return __builtin_bit_cast(bf16x2, __builtin_amdgcn_perm(x[i + 1][c / 2], x[i][c / 2], pick)); };
+        uint32_t w = __builtin_amdgcn_cvt_scalef32_pk_fp4_bf16(0, rows(0), __uint_as_float(f), 0);
+        w = __builtin_amdgcn_cvt_scalef32_pk_fp4_bf16(w, rows(2), __uint_as_float(f), 1);
+        return f < 0x7f800000u ? (u16)w : 0;
+    }
+};
 
 template <class T>
 __global__ __launch_bounds__(256) void k_mx4_cols(const T *__restrict__ X, int64_t ldx, int64_t rows, int64_t cols,
@@ -98,26 +193,27 @@ __global__ __launch_bounds__(256) void k_mx4_cols(const T *__restrict__ X, int64
 #pragma unroll
         for (int h = 0; h < kColBlocks / 4; h++) {
             const int blk = 4 * h + wave;
-            float x[8][4];
-            uint32_t m[8] = {};
+            ColLane<T> x;
 #pragma unroll
             for (int i = 0; i < 4; i++) {
                 const int64_t row = r0 + 32 * blk + 4 * g + i;
                 typename Elems<T, 8>::type v = {};
                 if (row < rows) v = load_elems<T, 8>(X + row * ldx + c0 + 8 * j, left);
-#pragma unroll
-                for (int c = 0; c < 8; c++) {
-                    x[c][i] = to_f32((T)v[c]);
-                    const uint32_t b = __float_as_uint(x[c][i]) & 0x7fffffffu;
-                    m[c] = b > m[c] ? b : m[c];
-                }
+                x.set(i, v);
             }
+            uint32_t m[8], top[2], f[2], factors[8];
+            x.magnitudes(m);
+            max_over_rows(m, top);
 #pragma unroll
-            for (int c = 0; c < 8; c++) {
-                const int E8 = mx4_exponent(max_over_rows(m[c]));
-                *reinterpret_cast<u16 *>(tile + (8 * j + c) * kPitch + 16 * blk + 2 * g) = mx4_pack4(x[c], E8);
-                if (g == c) exps[8 * j + c][blk] = (uint8_t)E8;
+            for (int c = 0; c < 2; c++) {
+                const int E8 = mx4_exponent(top[c]);
+                if (g % 2 == 0) exps[8 * j + g + c][blk] = (uint8_t)E8;
+                f[c] = ColLane<T>::factor(E8);
             }
+            to_all_rows(f, factors);
+#pragma unroll
+            for (int c = 0; c < 8; c++)
+                *reinterpret_cast<u16 *>(tile + (8 * j + c) * kPitch + 16 * blk + 2 * g) = x.pack(c, factors[c]);
         }
         __syncthreads();
 #pragma unroll

@@ -202,6 +202,8 @@ __global__ __launch_bounds__(kUnitThreads) void k_saved_values(const uint8_t *__
     constexpr int E = kUnitElems<T>, L = kMxBlock / E;
     typename Codes<E>::type c[kUnitRounds];
     int E8[kUnitRounds];
+    const uint32_t flip = is_signed ? 0x80808080u : 0;
+    const float zero = is_signed ? 128.0f : 0.0f;
     walk_units<E>(
         units, div, cols,
         [&](int i, int64_t u, int64_t, int32_t, int64_t) {
@@ -213,8 +215,9 @@ __global__ __launch_bounds__(kUnitThreads) void k_saved_values(const uint8_t *__
             const float s = mx_scale(E8[i]);
 #pragma unroll
             for (int e = 0; e < E; e++) {
-                const int b = code_word<E>(c[i], e / 4) >> (8 * (e % 4)) & 255;
-                o[e] = from_f32<T>((float)(is_signed ? (int)(int8_t)b : b) * s);  // (exact in bf16 too)
+                // (signed codes as unsigned ones 128 above)
+                const uint32_t b = (code_word<E>(c[i], e / 4) ^ flip) >> (8 * (e % 4)) & 255;
+                o[e] = from_f32<T>(((float)b - zero) * s);  // (exact in bf16 too)
             }
             if (left > 0) store_elems<T, E, NT>(out + row * ld + col, o, left);
         });
