@@ -79,7 +79,7 @@ template <class T> __device__ __forceinline__ T from_f32(float x)
 
 // E elements from p, of which the first `valid` are in the row; zeros after them.
 // NT: past the caches' replacement (as data that no one reads again soon).
-// The end of a row is stored in up to three pieces of 4, 2 and 1 elements (100,000 x 257
+// The end of a row is stored in up to three PIECES of 4, 2 and 1 elements (100,000 x 257
 // bf16 values of saved codes 15.3 us, element by element 16.1), but loaded by elements
 // (pieces, put together afterwards: quantising these rows 20.8 us instead of 18.5).
 template <class T, int E, bool NT = false>
@@ -97,7 +97,7 @@ __device__ __forceinline__ typename Elems<T, E>::type load_elems(const T *p, int
     }
     return v;
 }
-template <class T, int E, bool NT = false>
+template <class T, int E, bool NT = false, bool PIECES = true>
 __device__ __forceinline__ void store_elems(T *p, typename Elems<T, E>::type v, int64_t valid)
 {
     if (valid >= E) {
@@ -105,6 +105,10 @@ __device__ __forceinline__ void store_elems(T *p, typename Elems<T, E>::type v, 
             __builtin_nontemporal_store(v, reinterpret_cast<typename Elems<T, E>::type *>(p));
         else
             *reinterpret_cast<typename Elems<T, E>::type *>(p) = v;
+    } else if constexpr (!PIECES) {
+#pragma unroll
+        for (int i = 0; i < E; i++)
+            if (i < valid) p[i] = v[i];
     } else {
         static_assert(E == 4 || E == 8);
         const int n = valid > 0 ? (int)valid : 0;

@@ -14,29 +14,69 @@ __device__ __forceinline__ int mx4_exponent(uint32_t m)
     return k == 255 ? 255 : k > 2 ? k - 2 : 0;
 }
 
-// Eight elements under scale byte E as e2m1, the first in the low bits (round to
-// nearest even and clamped by the conversion); zeros for E = 255.  The scaling is
-// exact but for numbers far below the smallest e2m1 step.
-__device__ __forceinline__ uint32_t mx4_pack8(const float *x, int E)
+typedef u16 u16x2 __attribute__((ext_vector_type(2)));
+typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+
+__device__ __forceinline__ uint32_t larger(uint32_t a, uint32_t b) { return a > b ? a : b; }
+
+// Two bf16 numbers a word: the larger magnitudes, which order as their bits do.
+__device__ __forceinline__ u16x2 larger_magnitudes(u16x2 top, uint32_t w)
 {
-    const float inv = mx_inverse(E);
-    uint32_t w = 0;
-    w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, x[0] * inv, x[1] * inv, 1.0f, 0);
-    w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, x[2] * inv, x[3] * inv, 1.0f, 1);
-    w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, x[4] * inv, x[5] * inv, 1.0f, 2);
-    w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, x[6] * inv, x[7] * inv, 1.0f, 3);
-    return E == 255 ? 0 : w;
+    return __builtin_elementwise_max(top, __builtin_bit_cast(u16x2, w & 0x7fff7fffu));
 }
 
-// Four elements likewise.
-__device__ __forceinline__ uint16_t mx4_pack4(const float *x, int E)
+// Elements 2 PAIR and 2 PAIR + 1 (two floats, or two bf16 in a word) under scale s =
+// mx_scale() of their block, as e2m1 in byte PAIR of w: one rounding, to nearest even,
+// and clamped, all by the conversion.
+template <int PAIR> __device__ __forceinline__ uint32_t mx4_pair(uint32_t w, float a, float b, float s)
 {
-    const float inv = mx_inverse(E);
-    uint32_t w = 0;
-    w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, x[0] * inv, x[1] * inv, 1.0f, 0);
-    w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, x[2] * inv, x[3] * inv, 1.0f, 1);
-    return E == 255 ? 0 : (uint16_t)w;
+    return __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, a, b, s, PAIR);
 }
+template <int PAIR> __device__ __forceinline__ uint32_t mx4_pair(uint32_t w, uint32_t ab, float s)
+{
+    return __builtin_amdgcn_cvt_scalef32_pk_fp4_bf16(w, __builtin_bit_cast(bf16x2, ab), s, PAIR);
+}
+
+// A lane's E elements of a block (4 or 8, of bf16 8).
+template <class T, int E> struct Mx4Lane;
+template <int E> struct Mx4Lane<float, E> {
+    typename Elems<float, E>::type x;
+    // Bit pattern (of fp32) of the largest magnitude.
+    __device__ __forceinline__ uint32_t magnitude() const
+    {
+        uint32_t m = 0;
+#pragma unroll
+        for (int e = 0; e < E; e++) m = larger(m, __float_as_uint(x[e]) & 0x7fffffffu);
+        return m;
+    }
+    // As e2m1, the first in the low bits; zeros for E8 = 255.
+    __device__ __forceinline__ uint32_t codes(int E8) const
+    {
+        const float s = mx_scale(E8);
+        uint32_t w = mx4_pair<1>(mx4_pair<0>(0, x[0], x[1], s), x[2], x[3], s);
+        if constexpr (E == 8) w = mx4_pair<3>(mx4_pair<2>(w, x[4], x[5], s), x[6], x[7], s);
+        return E8 == 255 ? 0 : w;
+    }
+};
+template <> struct Mx4Lane<u16, 8> {
+    typedef uint32_t words __attribute__((ext_vector_type(4)));
+    words x;
+    __device__ __forceinline__ Mx4Lane(const typename Elems<u16, 8>::type &v) : x(__builtin_bit_cast(words, v)) {}
+    __device__ __forceinline__ uint32_t magnitude() const
+    {
+        u16x2 top = {};
+#pragma unroll
+        for (int p = 0; p < 4; p++) top = larger_magnitudes(top, x[p]);
+        const uint32_t t = __builtin_bit_cast(uint32_t, top);
+        return larger(t << 16, t & 0xffff0000u);
+    }
+    __device__ __forceinline__ uint32_t codes(int E8) const
+    {
+        const float s = mx_scale(E8);
+        const uint32_t w = mx4_pair<3>(mx4_pair<2>(mx4_pair<1>(mx4_pair<0>(0, x[0], s), x[1], s), x[2], s), x[3], s);
+        return E8 == 255 ? 0 : w;
+    }
+};
 
 // X (rows x cols of dtype) along its rows into codes and scales in the layout
 // of gs_mxfp4, enqueued on s.

@@ -41,19 +41,9 @@ __global__ __launch_bounds__(kUnitThreads) void k_mx4_rows(const T *__restrict__
         for (int i = 0; i < kUnitRounds; i++) {
             const int64_t u = u0 + i * kUnitThreads + threadIdx.x;
             if (u >= units) continue;  // (whole blocks)
-            float x[E];
-            uint32_t m = 0;
-#pragma unroll
-            for (int e = 0; e < E; e++) {
-                x[e] = to_f32(v[i][e]);
-                const uint32_t b = __float_as_uint(x[e]) & 0x7fffffffu;
-                m = b > m ? b : m;
-            }
-            const int E8 = mx4_exponent(group_max<L>(m));
-            if constexpr (E == 8)
-                reinterpret_cast<uint32_t *>(codes)[u] = mx4_pack8(x, E8);
-            else
-                reinterpret_cast<u16 *>(codes)[u] = mx4_pack4(x, E8);
+            const Mx4Lane<T, E> x{v[i]};
+            const int E8 = mx4_exponent(group_max<L>(x.magnitude()));
+            reinterpret_cast<typename Nibbles<E>::type *>(codes)[u] = (typename Nibbles<E>::type)x.codes(E8);
             if (u % L == 0) scales[u / L] = (uint8_t)E8;
         }
     }
@@ -86,8 +76,6 @@ __device__ __forceinline__ void swap_rows(uint32_t &a, uint32_t &b)
     a = r[0];
     b = r[1];
 }
-__device__ __forceinline__ uint32_t larger(uint32_t a, uint32_t b) { return a > b ? a : b; }
-
 // The largest m[c] over the eight lanes with this lane's j, for two of the eight columns c:
 // 2 (lane / 16) and the next one.  Each swap folds two columns at once.
 __device__ __forceinline__ void max_over_rows(uint32_t (&m)[8], uint32_t (&top)[2])
@@ -138,20 +126,13 @@ template <> struct ColLane<float> {
             for (int i = 0; i < 4; i++) m[c] = larger(m[c], __float_as_uint(x[c][i]) & 0x7fffffffu);
         }
     }
-    // What pack() takes of a scale byte.
-    static __device__ __forceinline__ uint32_t factor(int E8) { return __float_as_uint(mx_inverse(E8)); }
-    __device__ __forceinline__ u16 pack(int c, uint32_t f) const
+    __device__ __forceinline__ u16 pack(int c, float s) const
     {
-        const float inv = __uint_as_float(f);
-        uint32_t w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(0, x[c][0] * inv, x[c][1] * inv, 1.0f, 0);
-        w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, x[c][2] * inv, x[c][3] * inv, 1.0f, 1);
-        return f ? (u16)w : 0;
+        return (u16)mx4_pair<1>(mx4_pair<0>(0, x[c][0], x[c][1], s), x[c][2], x[c][3], s);
     }
 };
 template <> struct ColLane<u16> {
     typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
-    typedef u16 u16x2 __attribute__((ext_vector_type(2)));
-    typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
     u32x4 x[4];  // two columns a word
     __device__ __forceinline__ void set(int i, typename Elems<u16, 8>::type v) { x[i] = __builtin_bit_cast(u32x4, v); }
     __device__ __forceinline__ void magnitudes(uint32_t (&m)[8]) const
@@ -161,20 +142,17 @@ template <> struct ColLane<u16> {
             u16x2 top = {};
 #pragma unroll
             for (int i = 0; i < 4; i++)
-                top = __builtin_elementwise_max(top, __builtin_bit_cast(u16x2, x[i][p] & 0x7fff7fffu));
+                top = larger_magnitudes(top, x[i][p]);
             const uint32_t t = __builtin_bit_cast(uint32_t, top);
             m[2 * p] = t << 16;
             m[2 * p + 1] = t & 0xffff0000u;
         }
     }
-    static __device__ __forceinline__ uint32_t factor(int E8) { return E8 ? (uint32_t)E8 << 23 : 0x00400000u; }
-    __device__ __forceinline__ u16 pack(int c, uint32_t f) const
+    __device__ __forceinline__ u16 pack(int c, float s) const
     {
         const uint32_t pick = c % 2 ? 0x07060302 : 0x05040100;
-        auto rows = [&](int i) { return __builtin_bit_cast(bf16x2, __builtin_amdgcn_perm(x[i + 1][c / 2], x[i][c / 2], pick)); };
-        uint32_t w = __builtin_amdgcn_cvt_scalef32_pk_fp4_bf16(0, rows(0), __uint_as_float(f), 0);
-        w = __builtin_amdgcn_cvt_scalef32_pk_fp4_bf16(w, rows(2), __uint_as_float(f), 1);
-        return f < 0x7f800000u ? (u16)w : 0;
+        auto rows = [&](int i) { return __builtin_amdgcn_perm(x[i + 1][c / 2], x[i][c / 2], pick); };
+        return (u16)mx4_pair<1>(mx4_pair<0>(0, rows(0), s), rows(2), s);
     }
 };
 
@@ -201,19 +179,20 @@ __global__ __launch_bounds__(256) void k_mx4_cols(const T *__restrict__ X, int64
                 if (row < rows) v = load_elems<T, 8>(X + row * ldx + c0 + 8 * j, left);
                 x.set(i, v);
             }
-            uint32_t m[8], top[2], f[2], factors[8];
+            uint32_t m[8], top[2], s[2], scale[8];
             x.magnitudes(m);
             max_over_rows(m, top);
 #pragma unroll
             for (int c = 0; c < 2; c++) {
                 const int E8 = mx4_exponent(top[c]);
                 if (g % 2 == 0) exps[8 * j + g + c][blk] = (uint8_t)E8;
-                f[c] = ColLane<T>::factor(E8);
+                s[c] = __float_as_uint(mx_scale(E8));
             }
-            to_all_rows(f, factors);
+            to_all_rows(s, scale);
 #pragma unroll
-            for (int c = 0; c < 8; c++)
-                *reinterpret_cast<u16 *>(tile + (8 * j + c) * kPitch + 16 * blk + 2 * g) = x.pack(c, factors[c]);
+            for (int c = 0; c < 8; c++)  // (a block with a NaN or an infinity has zeros)
+                *reinterpret_cast<u16 *>(tile + (8 * j + c) * kPitch + 16 * blk + 2 * g) =
+                    scale[c] < 0x7f800000u ? x.pack(c, __uint_as_float(scale[c])) : 0;
         }
         __syncthreads();
 #pragma unroll
@@ -228,6 +207,12 @@ __global__ __launch_bounds__(256) void k_mx4_cols(const T *__restrict__ X, int64
         }
         __syncthreads();
     }
+}
+
+// Codes 2 PAIR and 2 PAIR + 1 of w under scale s as two bf16 (exactly).
+template <int PAIR> __device__ __forceinline__ uint32_t mx4_values2(uint32_t w, float s)
+{
+    return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, s, PAIR));
 }
 
 template <class T>
@@ -260,13 +245,15 @@ __global__ __launch_bounds__(kUnitThreads) void k_mx4_values(const uint8_t *__re
             if (u >= units || col[i] >= cols) continue;
             const float s = mx_scale(E8[i]);
             typename Elems<T, E>::type o;
-            f32x2 p[4] = {__builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w[i], 1.0f, 0), __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w[i], 1.0f, 1)};
             if constexpr (E == 8) {
-                p[2] = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w[i], 1.0f, 2);
-                p[3] = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w[i], 1.0f, 3);
+                uint4 p = make_uint4(mx4_values2<0>(w[i], s), mx4_values2<1>(w[i], s), mx4_values2<2>(w[i], s), mx4_values2<3>(w[i], s));
+                if (E8[i] == 255) p = make_uint4(0x7fc07fc0, 0x7fc07fc0, 0x7fc07fc0, 0x7fc07fc0);
+                o = __builtin_bit_cast(typename Elems<T, E>::type, p);
+            } else {
+                const f32x2 p0 = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w[i], 1.0f, 0);
+                const f32x2 p1 = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w[i], 1.0f, 1);
+                o = typename Elems<T, E>::type{p0[0] * s, p0[1] * s, p1[0] * s, p1[1] * s};
             }
-#pragma unroll
-            for (int e = 0; e < E; e++) o[e] = from_f32<T>(p[e / 2][e % 2] * s);
             store_elems<T, E>(out + row[i] * ld + col[i], o, cols - col[i]);
         }
     }

@@ -42,10 +42,11 @@ template <class T> struct Out {
             for (int e = 0; e < E; e++)
                 if ((p[e / 4] >> 8 * (e % 4) & 255) == 0) v[e] = T(0);
         }
+        // (row ends by elements: k_narrow would spill for the pieces)
         if (stream)
-            store_elems<T, E, true>(c + row * ld + col, v, n - col);
+            store_elems<T, E, true, false>(c + row * ld + col, v, n - col);
         else
-            store_elems<T, E>(c + row * ld + col, v, n - col);
+            store_elems<T, E, false, false>(c + row * ld + col, v, n - col);
     }
 };
 
@@ -206,21 +207,14 @@ template <class T, int KS, Fit FIT> struct RowSource<DenseRows<T>, KS, FIT> {
         for (int ks = 0; ks < KS; ks++) {
 #pragma unroll
             for (int i = 0; i < N; i++) {
-                float x[E];
-                uint32_t top = 0;
-#pragma unroll
-                for (int e = 0; e < E; e++) {
-                    x[e] = to_f32(v[ks % kAhead][i][e]);
-                    const uint32_t b = __float_as_uint(x[e]) & 0x7fffffffu;
-                    top = b > top ? b : top;
-                }
-                const int E8 = mx4_exponent(group_max<L>(top));
+                const Mx4Lane<T, E> x{v[ks % kAhead][i]};
+                const int E8 = mx4_exponent(group_max<L>(x.magnitude()));
                 // block (row, h) as lane 32 h + row of the fragment
                 const int to = lane / L % 2 * 32 + i * RB + lane / (2 * L);
                 if constexpr (E == 8)
-                    *reinterpret_cast<uint32_t *>(tmp + 16 * to + lane % L * 4) = mx4_pack8(x, E8);
+                    *reinterpret_cast<uint32_t *>(tmp + 16 * to + lane % L * 4) = x.codes(E8);
                 else
-                    *reinterpret_cast<u16 *>(tmp + 16 * to + lane % L * 2) = mx4_pack4(x, E8);
+                    *reinterpret_cast<u16 *>(tmp + 16 * to + lane % L * 2) = (u16)x.codes(E8);
                 if (lane % L == 0) tmp[1024 + to] = (uint8_t)E8;
             }
             if (ks + kAhead < KS)
@@ -368,17 +362,9 @@ __device__ __forceinline__ void few_quantise(const DenseRows<T> &A, int64_t m, i
     const int per = kpad / E, units = (int)m * per;
     for (int u = threadIdx.x; u < units; u += kFewWaves * kWave) {  // (units: a multiple of 16)
         const int row = u / per, col = u % per * E;
-        const typename Elems<T, E>::type v = load_elems<T, E>(A.p + row * A.ld + col, A.cols - col);
-        float x[E];
-        uint32_t top = 0;
-#pragma unroll
-        for (int e = 0; e < E; e++) {
-            x[e] = to_f32(v[e]);
-            const uint32_t b = __float_as_uint(x[e]) & 0x7fffffffu;
-            top = b > top ? b : top;
-        }
-        const int E8 = mx4_exponent(group_max<L>(top));
-        *reinterpret_cast<uint32_t *>(codes + row * (kpad / 2 + 16) + col / 2) = mx4_pack8(x, E8);
+        const Mx4Lane<T, E> x{load_elems<T, E>(A.p + row * A.ld + col, A.cols - col)};
+        const int E8 = mx4_exponent(group_max<L>(x.magnitude()));
+        *reinterpret_cast<uint32_t *>(codes + row * (kpad / 2 + 16) + col / 2) = x.codes(E8);
         if (u % L == 0) scales[row * (kpad / kMxBlock) + col / kMxBlock] = (uint8_t)E8;
     }
 }

@@ -214,6 +214,23 @@ def test_mxfp4_quantize_is_exact(n, a, dtype, axis):
         assert _same(q.dequantize(t2), v)
 
 
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("step", [-140, -133, -131, -130, -129, -128, -127, -126, -125, 122])
+def test_mxfp4_ends_of_the_range(dtype, step):
+    # blocks around the smallest scale (2^-127) and near the largest, with every code and
+    # every tie between two in them: inputs, scales and values may be subnormal
+    ramp = torch.arange(-32, 32, dtype=torch.float64) / 4
+    x = torch.stack([ramp * 2.0 ** step, ramp.flip(0) * 2.0 ** (step - 1), ramp * 2.0 ** (step - 2)]).to(TYPES[dtype])
+    code, E, v = lowbit.quant4(_np(x))
+    for axis, X in ((1, x), (0, x.T.contiguous())):
+        q = gs.mxfp4_quantize(X.to(DEV), axis=axis)
+        codes = q.codes.cpu().numpy().astype(np.int64)
+        assert np.array_equal(codes[:, :32], code[:, 0::2] | code[:, 1::2] << 4)
+        assert np.array_equal(q.scales[:, :2].cpu().numpy().astype(np.int64), E)
+        for t2 in TYPES.values():
+            assert _same(q.dequantize(t2), v)
+
+
 def _check_product(A, B, mask_on, dtype, got):
     """got against value(A) value(B)^T: k / 64 instructions and, where the sum is
     split, fewer than 64 parts more; one rounding to bf16."""
