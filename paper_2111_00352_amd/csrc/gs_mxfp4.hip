@@ -1,6 +1,9 @@
 // MXFP4 (OCP Microscaling, e2m1 elements, blocks of 32 with a power-of-two
 // scale): quantisation along the rows or the columns of a dense matrix, and the
-// values back.  Each is one pass, bound by memory.
+// values back.  Each is one pass, bound by memory: 100,000 x 128 fp32 in 12.7 us (4.6
+// TB/s), their values in 12 us; 2 to 3 us of each are the launch's start and drain.  The
+// element conversions of gfx950 take the block's scale, so an element costs little more
+// than its share of the largest magnitude.
 #include <algorithm>
 
 #include "gs_device.h"
@@ -56,8 +59,9 @@ __global__ __launch_bounds__(kUnitThreads) void k_mx4_rows(const T *__restrict__
 // packs its four rows of each column into two bytes.  The codes go out through LDS,
 // where they meet those of the other blocks, as 128 contiguous bytes of an out row.
 // Neighbouring workgroups take neighbouring columns, the rest of the same rows of X:
-// 4096 x 4096 bf16 11.0 us, 13.6 us with neighbours along the rows; 8192 x 8192 37 and
-// 48 us.
+// 4096 x 4096 bf16 11.0 us, 13.6 us with neighbours along the rows; 8192 x 8192 38.5 and
+// 49 us.  Finding maxima by lane swaps, which fold two columns at once, instead of through
+// LDS made that 9.5 us (4.5 TB/s; 128 x 128 fp32 5.2 -> 3.6 us).
 constexpr int kColTile = 64;
 constexpr int kRowTile = 256;
 constexpr int kColBlocks = kRowTile / kMxBlock;

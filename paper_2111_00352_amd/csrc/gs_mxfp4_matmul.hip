@@ -106,6 +106,10 @@ template <class T, int COLS> struct Staged {
 // A dense A is quantised on the way: the wave loads its rows as they lie in memory
 // (8 or 4 lanes a block), finds each block's scale across those lanes and lets LDS
 // turn the codes into fragments (a lane a block).
+//
+// 2,000,000 x 128 x 128 fp32 390 us (5.3 TB/s; reading and writing in equal parts, a
+// copy of 8 GB reaches 4.8), 100,000 x 128 x 64 with fp32 operands and a mask 16.5 us (5.3
+// TB/s); bf16 100,000 x 128 x 128 8.6 us, of which 2 to 3 are the launch.
 constexpr int kNarrowWaves = 4;
 constexpr int kNarrowMaxK = 512;
 constexpr int kNarrowTmp = 64 * (16 + 1);  // bytes of LDS for a wave's quantisation
@@ -314,6 +318,9 @@ __global__ __launch_bounds__(kNarrowWaves * kWave, narrow_waves<Rows>(KS)) void 
 // lane / 16 of row lane % 16, of B as it lies in memory.  A dense A
 // of at most kFewInside elements is quantised into LDS by every workgroup, after its
 // first loads of B are on their way.
+//
+// 1 x 4096 x 4096 4.4 us (9 MB, 2.0 TB/s): about 1.3 us of reading at the rate of a copy,
+// the rest the launch, one round trip to memory and the join.
 constexpr int kFewWaves = 8;
 constexpr int kFewSteps = 4;  // of 128
 constexpr int kFewRows = 64;         // of A at most, 32 where k_narrow could take them
@@ -432,7 +439,7 @@ __global__ __launch_bounds__(kFewWaves * kWave) void k_few(Rows A, const uint8_t
 // A workgroup of four waves makes a tile of 64 WT x 64 WT, a wave a quarter of it
 // (WT x WT instructions of 32 x 32 for every 64 of k).  k is taken in chunks of 256,
 // so that a row of a chunk is a whole line of 128 bytes (chunks of 128, half a line a
-// row, left the kernel bound by the rate of requests to L2: 8192^3 in 280 us).  Codes go
+// row, left the kernel bound by the rate of requests to L2).  Codes go
 // from memory to LDS without passing registers, a chunk ahead of the one that is
 // multiplied.  A row's eight 16-byte pieces lie in LDS in an order that depends on the
 // row (piece ^ row / 2 % 8), so that the rows LDS serves together (16 of 32: those whose
@@ -445,6 +452,14 @@ __global__ __launch_bounds__(kFewWaves * kWave) void k_few(Rows A, const uint8_t
 // sides of that barrier.
 //
 // Scales lie in LDS as 16 bytes of a row, a run of two chunks, loaded a run ahead.
+//
+// 8192^3 to bf16 255 us, 4.3 PFLOP/s: 113 us for every 4,096 of k (4.9 PFLOP/s) and 25 us
+// around them, 16 of which are the stores.  The instructions alone, on random operands
+// in registers, reach 7.0 PFLOP/s (clocks fall under that load); with operands that are
+// not loaded anew the loop takes 210 us, with ones that are not read from LDS 250.
+// Tiles of 256 x 256 leave a compute unit one workgroup, whose stores nothing covers; a
+// workgroup that goes on to its next tile meanwhile was slower (261 us: what it keeps
+// across the stores spills).
 constexpr int kChunkK = 256;
 
 template <int WT> struct TileLds {
