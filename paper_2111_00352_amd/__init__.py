@@ -510,6 +510,8 @@ class _Blocks:
         if stream is not None:
             return _on(stream, type(self).dequantize, self, dtype)
         code = _dtype_code(dtype)
+        if self.device.index != torch._C._cuda_getDevice():
+            raise ValueError("the codes are not on the current device")
         out = torch.empty(self.shape, dtype=dtype, device=self.device)
         rc = self._values(lib())(self._ref, out.data_ptr(), self.shape[1], code, _stream())
         if rc:

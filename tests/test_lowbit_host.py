@@ -108,3 +108,31 @@ def test_python_refuses_cpu_tensors():
         gs.save_activation(torch.zeros(2, 2))
     with pytest.raises(ValueError):
         gs.mxfp4_quantize(torch.zeros(2, 2))
+
+
+class _Launches:
+    """In the library's place: records the calls, all of which succeed."""
+
+    def __init__(self):
+        self.calls = []
+
+    def __getattr__(self, name):
+        return lambda *args: self.calls.append((name, args)) or 0
+
+
+@pytest.mark.parametrize("make", [lambda: gs.SavedActivation((3, 40), "relu", "cpu"), lambda: gs.Mxfp4((3, 40), "cpu")])
+def test_values_of_codes_on_another_device_are_refused(make, monkeypatch):
+    # a kernel launched there would be given the other device's addresses
+    import torch
+    library, empty = _Launches(), torch.empty
+    monkeypatch.setattr(gs, "lib", lambda: library)
+    monkeypatch.setattr(gs, "_stream", lambda stream=None: 0)
+    monkeypatch.setattr(torch._C, "_cuda_getDevice", lambda: 0, raising=False)
+    monkeypatch.setattr(torch, "empty", lambda shape, dtype=None, device=None: empty(shape, dtype=dtype))
+    q = make()
+    q.device = torch.device("cuda", 1)
+    with pytest.raises(ValueError):
+        q.dequantize()
+    assert not library.calls
+    q.device = torch.device("cuda", 0)
+    assert q.dequantize().shape == (3, 40) and len(library.calls) == 1
