@@ -394,7 +394,8 @@ int gs_mxfp4_dequantize(const gs_mxfp4 *A, void *out, int64_t ld, int dtype, gs_
 /* C = A . B^T on the matrix cores: A m x k, B n x k in MXFP4, exact products,
  * fp32 sums, C [dev] m x n of dtype with leading dimension ldc.  mask may be
  * NULL, or m x n activations saved with GS_ACT_RELU: C is then 0 where their
- * code is 0 (the gradient of the layer below, masked on the way out).  work
+ * code is 0 (the gradient of the layer below, masked on the way out).  m and n
+ * are below 2^31 (with a mask n is at most 2^24), k is at most 2^24.  work
  * [dev] holds at least the bytes that gs_mxfp4_matmul_workspace reports for
  * a_dtype = -1 (it may be NULL if that is 0). */
 int gs_mxfp4_matmul(const gs_mxfp4 *A, const gs_mxfp4 *B, const gs_saved *mask, void *C, int64_t ldc, int dtype,

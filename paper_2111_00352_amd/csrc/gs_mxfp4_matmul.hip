@@ -325,6 +325,7 @@ constexpr int kFewWaves = 8;
 constexpr int kFewSteps = 4;  // of 128
 constexpr int kFewRows = 64;         // of A at most, 32 where k_narrow could take them
 constexpr int64_t kFewInside = 1 << 16;
+constexpr int64_t kFewColumns = 1 << 26;  // of C in a launch, which holds fewer than 2^32 threads
 
 typedef float f32x4 __attribute__((ext_vector_type(4)));
 
@@ -899,8 +900,13 @@ template <class Rows> void multiply_few(const Product &p, const Rows &A)
         using T = typename decltype(out)::type;
         auto go = [&](auto mt) {
             const size_t lds = std::is_same_v<Rows, MxRows> ? 0 : p.m * (p.kpad / 2 + 16 + p.kpad / kMxBlock);
-            k_few<Rows, T, decltype(mt)::value>
-                <<<(unsigned)ceil_div(p.n, 16), kFewWaves * kWave, lds, p.s>>>(A, p.B->codes, p.B->scales, p.m, p.n, p.kpad, out);
+            for (int64_t n0 = 0; n0 < p.n; n0 += kFewColumns) {
+                const int64_t n = std::min(p.n - n0, kFewColumns);
+                auto at = out;  // (a mask has 2^24 columns at most: it is read in the first launch only)
+                at.c += n0;
+                k_few<Rows, T, decltype(mt)::value><<<(unsigned)ceil_div(n, 16), kFewWaves * kWave, lds, p.s>>>(
+                    A, p.B->codes + n0 * (p.kpad / 2), p.B->scales + n0 * (p.kpad / kMxBlock), p.m, n, p.kpad, at);
+            }
         };
         if constexpr (std::is_same_v<Rows, MxRows>)
             if (p.m > 32) return go(std::integral_constant<int, 4>{});

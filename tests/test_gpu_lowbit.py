@@ -309,6 +309,19 @@ def test_mxfp4_matmul_nan_blocks_and_masked_nan(m):
         assert torch.equal(got.isnan(), want & on) and bool((got[~on] == 0).all())
 
 
+@pytest.mark.parametrize("how", ["mxfp4", "f32"])
+def test_mxfp4_matmul_of_few_rows_and_very_many_columns(how):
+    # more columns than one launch has workgroups for; whole numbers that e2m1 holds, so
+    # products and sums are exact
+    n = 2 ** 27 + 33
+    vals = torch.tensor([0, 1, 2, 3, 4, 6, -1, -2, -3, -4, -6], dtype=torch.bfloat16, device=DEV)
+    X = vals[torch.randint(len(vals), (n, 3), device=DEV, dtype=torch.int32)]
+    A = torch.tensor([[1.0, 2.0, -3.0], [6.0, 0.0, 4.0]], device=DEV)
+    C = gs.mxfp4_matmul(gs.mxfp4_quantize(A) if how == "mxfp4" else A, gs.mxfp4_quantize(X))
+    for i in range(2):
+        assert torch.equal(C[i], (X[:, 0] * A[i, 0] + X[:, 1] * A[i, 1] + X[:, 2] * A[i, 2]).float())
+
+
 def test_mxfp4_matmul_extreme_scales():
     # scale bytes at both ends of the range meet in one product
     a = torch.zeros(40, 128)
