@@ -147,6 +147,15 @@ class _Linear(torch.autograd.Function):
         return dH, dW
 
 
+def _first_order_only():
+    """Refuses create_graph=True in the backward pass of a low-bit layer: what autograd
+    would record of it lacks the mask and the operators' part of the derivative, and an
+    error put off until that is used is passed over by gradients that reach their input
+    another way too."""
+    if torch.is_grad_enabled():
+        raise RuntimeError("low-bit layers cannot be differentiated twice (create_graph=True)")
+
+
 class _LinearMx(torch.autograd.Function):
     """H W with the product (and that of the input's gradient) in MXFP4."""
 
@@ -158,6 +167,7 @@ class _LinearMx(torch.autograd.Function):
 
     @staticmethod
     def backward(ctx, G):
+        _first_order_only()
         H, W = ctx.saved_tensors
         G = G.contiguous()
         dH = gs.mxfp4_matmul(G, gs.mxfp4_quantize(W)) if ctx.needs_input_grad[0] else None
@@ -177,6 +187,7 @@ class _ReluLinear(torch.autograd.Function):
 
     @staticmethod
     def backward(ctx, G):
+        _first_order_only()
         W, = ctx.saved_tensors
         G = G.contiguous()
         dP = dW = None

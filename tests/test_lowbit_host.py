@@ -136,3 +136,65 @@ def test_values_of_codes_on_another_device_are_refused(make, monkeypatch):
     assert not library.calls
     q.device = torch.device("cuda", 0)
     assert q.dequantize().shape == (3, 40) and len(library.calls) == 1
+
+
+def _operators_on_the_cpu(monkeypatch):
+    """The operators that the GCN's layers call, in plain torch: like the kernels, they see
+    values only, and autograd does not see what they write."""
+    import torch
+
+    def save_activation(P, act="relu"):
+        H = torch.relu(P.detach())
+        saved = gs.SavedActivation(P.shape, act, "cpu")
+        q, E = lowbit.save8(H.double().numpy(), True)[:2]
+        saved.codes[:, :P.shape[1]] = torch.from_numpy(q.astype(np.uint8))
+        saved.scales[:] = torch.from_numpy(E.astype(np.uint8))
+        return H, saved
+
+    def values(saved):
+        cols = saved.shape[1]
+        step = torch.exp2(saved.scales.float() - 127).repeat_interleave(32, 1)[:, :cols]
+        return saved.codes[:, :cols].float() * step
+
+    def relu_grad(saved, dH, out=None):
+        assert out is None or out is dH
+        dP = (dH if out is not None else dH.clone()).detach()
+        dP.numpy()[(saved.codes[:, :dH.shape[1]] == 0).numpy()] = 0.0
+        return dP
+
+    def matmul(A, B, mask=None):
+        C = A.detach() @ B.t()
+        return C if mask is None else relu_grad(mask, C)
+
+    monkeypatch.setattr(gs, "save_activation", save_activation)
+    monkeypatch.setattr(gs, "relu_grad", relu_grad)
+    monkeypatch.setattr(gs, "saved_weight_grad", lambda saved, G: values(saved).t() @ G.detach())
+    monkeypatch.setattr(gs, "mxfp4_quantize", lambda W, axis=1: (W.detach() if axis else W.detach().t()).contiguous())
+    monkeypatch.setattr(gs, "mxfp4_matmul", matmul)
+
+
+def _layers():
+    from paper_2111_00352_amd import gcn
+    return {"saved8": lambda P, W: gcn._ReluLinear.apply(P, W, False),
+            "mxfp4": lambda P, W: gcn._ReluLinear.apply(P, W, True),
+            "linear": gcn._LinearMx.apply}
+
+
+@pytest.mark.parametrize("layer", ["saved8", "mxfp4", "linear"])
+def test_second_derivatives_of_low_bit_layers_are_refused(layer, monkeypatch):
+    # what autograd records of their backward passes would lack the mask and whatever
+    # the operators computed
+    import torch
+    _operators_on_the_cpu(monkeypatch)
+    gen = torch.Generator().manual_seed(3)
+    P, W, G = (torch.randn(s, generator=gen).requires_grad_(True) for s in ((20, 40), (40, 7), (20, 7)))
+    grads = torch.autograd.grad(_layers()[layer](P, W), (P, W), G)
+    H = torch.relu(P) if layer != "linear" else P
+    want = torch.autograd.grad(H @ W, (P, W), G)
+    assert torch.allclose(grads[0], want[0], atol=1e-5)
+    # a saved value is within a step, 2^-7 of its block's largest, of its activation
+    slack = 2.0 ** -7 * H.detach().max() * G.detach().abs().sum(0) + 1e-4
+    assert bool(((grads[1] - want[1]).abs() <= slack).all())
+    for x in (P, W):
+        with pytest.raises(RuntimeError, match="twice"):
+            torch.autograd.grad(_layers()[layer](P, W), x, G, create_graph=True)
