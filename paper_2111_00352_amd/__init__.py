@@ -24,7 +24,7 @@ import torch
 __all__ = [
     "FORMATS", "FORMAT_NAMES", "GnnSpmmError", "Matrix", "SelectContext", "build_format",
     "extract_features", "lib", "library_path", "FEATURE_NAMES", "set_allocator",
-    "SavedActivation", "save_activation", "relu_grad", "saved_weight_grad",
+    "SavedActivation", "save_activation", "relu_grad", "saved_weight_grad", "SAVED_GRAD_WIDTH",
     "Mxfp4", "mxfp4_quantize", "mxfp4_matmul",
 ]
 
@@ -421,6 +421,7 @@ def weight_grad(H: torch.Tensor, G: torch.Tensor, stream=None) -> torch.Tensor:
 # once each and nothing is made that the call does not need.
 
 ACTIVATIONS = {"none": 0, "relu": 1}
+SAVED_GRAD_WIDTH = 4096  # columns of either operand of saved_weight_grad at most
 _DTYPES = {torch.float32: 0, torch.bfloat16: 1}
 
 
@@ -594,7 +595,8 @@ def _grad_work(n: int, a: int, b: int) -> int:
 
 
 def saved_weight_grad(saved: SavedActivation, G: torch.Tensor, stream=None) -> torch.Tensor:
-    """H^T G in fp32 from saved activations H (n x a) and G (n x b) (gs_saved_weight_grad)."""
+    """H^T G in fp32 from saved activations H (n x a) and G (n x b), a and b at most
+    SAVED_GRAD_WIDTH (gs_saved_weight_grad)."""
     if stream is not None:
         return _on(stream, saved_weight_grad, saved, G)
     G, ld, code, shape = _dense(G, "G", saved.device.index)

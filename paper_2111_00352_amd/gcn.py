@@ -175,6 +175,14 @@ class _LinearMx(torch.autograd.Function):
         return dH, dW
 
 
+def _saved_weight_grad(act: gs.SavedActivation, G: torch.Tensor) -> torch.Tensor:
+    """H^T G for saved activations H; of layers wider than the library's kernel takes, from
+    H's values as ``weight_grad`` forms it (which leaves wide products to PyTorch)."""
+    if max(act.shape[1], G.shape[1]) > gs.SAVED_GRAD_WIDTH:
+        return weight_grad(act.dequantize(G.dtype), G)
+    return gs.saved_weight_grad(act, G)
+
+
 class _ReluLinear(torch.autograd.Function):
     """relu(P) W, of whose input only relu(P) in 8 bits is kept for the backward pass."""
 
@@ -198,7 +206,7 @@ class _ReluLinear(torch.autograd.Function):
                 dP = G @ W.t()
                 gs.relu_grad(ctx.act, dP, out=dP)
         if ctx.needs_input_grad[1]:
-            dW = gs.saved_weight_grad(ctx.act, G)
+            dW = _saved_weight_grad(ctx.act, G)
         return dP, dW, None
 
 

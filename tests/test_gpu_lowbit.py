@@ -464,6 +464,20 @@ def test_relu_linear_in_mxfp4_matches_its_formula():
     assert np.all(np.abs(_np(W.grad) - q8[2].T @ g) <= 2 * 100 * U * (q8[2].T @ np.abs(g)))
 
 
+@pytest.mark.parametrize("a,b", [(4130, 9), (9, 4130)])
+@pytest.mark.parametrize("mx", [False, True])
+def test_relu_linear_wider_than_the_weight_gradient_kernel(a, b, mx):
+    rng = np.random.default_rng(a)
+    n = 300
+    P, W, G = (torch.from_numpy(rng.standard_normal(s).astype(np.float32)).to(DEV) for s in ((n, a), (a, b), (n, b)))
+    P.requires_grad_(True)
+    W.requires_grad_(True)
+    gcn._ReluLinear.apply(P, W, mx).backward(G)
+    v, g = lowbit.save8(_np(P), True)[2], _np(G)
+    assert np.all(np.abs(_np(W.grad) - v.T @ g) <= 2 * n * U * (v.T @ np.abs(g)))
+    assert P.grad.shape == (n, a)
+
+
 def _problem(k, H, O, seed):
     g = graphgen.scaled(k)
     F = g.X.shape[1]

@@ -168,7 +168,13 @@ def _operators_on_the_cpu(monkeypatch):
 
     monkeypatch.setattr(gs, "save_activation", save_activation)
     monkeypatch.setattr(gs, "relu_grad", relu_grad)
-    monkeypatch.setattr(gs, "saved_weight_grad", lambda saved, G: values(saved).t() @ G.detach())
+    def saved_weight_grad(saved, G):
+        need = ctypes.c_uint64()
+        gs._check(gs.lib().gs_saved_weight_grad_workspace(*saved.shape, G.shape[1], ctypes.byref(need)))
+        return values(saved).t() @ G.detach()
+
+    monkeypatch.setattr(gs, "saved_weight_grad", saved_weight_grad)
+    monkeypatch.setattr(gs.SavedActivation, "dequantize", lambda saved, dtype=torch.float32: values(saved).to(dtype))
     monkeypatch.setattr(gs, "mxfp4_quantize", lambda W, axis=1: (W.detach() if axis else W.detach().t()).contiguous())
     monkeypatch.setattr(gs, "mxfp4_matmul", matmul)
 
@@ -198,3 +204,19 @@ def test_second_derivatives_of_low_bit_layers_are_refused(layer, monkeypatch):
     for x in (P, W):
         with pytest.raises(RuntimeError, match="twice"):
             torch.autograd.grad(_layers()[layer](P, W), x, G, create_graph=True)
+
+
+@pytest.mark.parametrize("layer", ["saved8", "mxfp4"])
+@pytest.mark.parametrize("a,b", [(4096, 5), (4097, 5), (5, 4096), (5, 4097)])
+def test_low_bit_layers_of_any_width_have_a_backward_pass(layer, a, b, monkeypatch):
+    # wider than the weight gradient's kernel takes: the values go to PyTorch's product, as
+    # those of wide fp32 layers do
+    import torch
+    _operators_on_the_cpu(monkeypatch)
+    gen = torch.Generator().manual_seed(4)
+    P, W = (torch.randn(s, generator=gen).requires_grad_(True) for s in ((6, a), (a, b)))
+    G = torch.randn(6, b, generator=gen)
+    _layers()[layer](P, W).backward(G)
+    v = lowbit.save8(P.detach().double().numpy(), True)[2]
+    mag = np.abs(v).T @ np.abs(G.double().numpy())
+    assert np.all(np.abs(W.grad.double().numpy() - v.T @ G.double().numpy()) <= 2 * 6 * 2.0 ** -24 * mag)
