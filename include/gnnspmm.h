@@ -364,8 +364,9 @@ int gs_relu_grad(const gs_saved *A, const void *dH, int64_t ldh, int dtype, void
 /* Weight gradient from saved activations: out = value(A)^T . G, A.cols x b fp32
  * row-major (leading dimension b), G [dev] rows x b with leading dimension ldg.
  * The values of A are exact on the matrix cores and G is taken in three parts
- * that add up to it, so products and sums are those of fp32.  A.cols and b at
- * most 4096, ldg at most 2^26 (GS_ERR_UNSUPPORTED beyond).  work [dev] holds at least the bytes that
+ * that add up to it, so products and sums are those of fp32.  A.cols and b are
+ * at least 1 (GS_ERR_INVALID_ARG) and at most 4096, ldg at most 2^26
+ * (GS_ERR_UNSUPPORTED).  work [dev] holds at least the bytes that
  * gs_saved_weight_grad_workspace reports. */
 int gs_saved_weight_grad_workspace(int64_t n, int64_t a, int64_t b, uint64_t *bytes);
 int gs_saved_weight_grad(const gs_saved *A, const void *G, int64_t ldg, int dtype, int64_t b, float *out,

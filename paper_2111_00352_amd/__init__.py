@@ -603,8 +603,10 @@ def saved_weight_grad(saved: SavedActivation, G: torch.Tensor, stream=None) -> t
     (n, a), b = saved.shape, shape[1]
     if shape[0] != n:
         raise ValueError("G and the saved activations must have the same number of rows")
-    need = _grad_work(n, a, b)
     out = torch.empty((a, b), dtype=torch.float32, device=G.device)
+    if not a or not b:
+        return out
+    need = _grad_work(n, a, b)
     work = torch.empty(need, dtype=torch.uint8, device=G.device) if need else None
     rc = lib().gs_saved_weight_grad(saved._ref, G.data_ptr(), ld, code, b, out.data_ptr(),
                                     None if work is None else work.data_ptr(), need, _stream())

@@ -346,6 +346,13 @@ def test_empty_operands():
     assert gs.mxfp4_matmul(torch.ones(4, 64, device=DEV), gs.mxfp4_quantize(torch.empty(0, 64, device=DEV))).shape == (4, 0)
 
 
+@pytest.mark.parametrize("n,a,b", [(6, 0, 4), (6, 4, 0), (0, 0, 0), (0, 4, 0), (0, 3, 4)])
+def test_empty_weight_gradients(n, a, b):
+    _, saved = gs.save_activation(torch.ones(n, a, device=DEV))
+    got = gs.saved_weight_grad(saved, torch.ones(n, b, device=DEV))
+    assert got.dtype == torch.float32 and torch.equal(got, torch.zeros(a, b, device=DEV))
+
+
 @pytest.mark.parametrize("a", [128, 100, 64])
 def test_calls_larger_than_the_caches(a):
     # more than 700 MB of operands, where loads and stores go past the caches: any rows
