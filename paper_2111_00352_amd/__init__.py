@@ -425,14 +425,14 @@ SAVED_GRAD_WIDTH = 4096  # columns of either operand of saved_weight_grad at mos
 _DTYPES = {torch.float32: 0, torch.bfloat16: 1}
 
 
-def _dense(X: torch.Tensor, name: str, index=None) -> tuple:
+def _dense(X: torch.Tensor, name: str, index: int | None = -1) -> tuple:
     """(tensor, leading dimension, dtype code, shape) of a 2-D fp32 or bf16 operand on
-    the current device (and on device `index`)."""
+    the current device, and on the GPU `index` of another operand (None: it is on none)."""
     code = _DTYPES.get(X.dtype) if isinstance(X, torch.Tensor) else None
     if code is None or not X.is_cuda or X.dim() != 2 or X.layout != torch.strided:
         raise ValueError(f"{name} must be a 2-D CUDA float32 or bfloat16 tensor")
     at = X.get_device()
-    if at != torch._C._cuda_getDevice() or (index is not None and at != index):
+    if at != torch._C._cuda_getDevice() or (index != -1 and at != index):
         raise ValueError(f"{name} is not on the current device, or not on the other operand's")
     if X.is_neg():
         X = X.resolve_neg()
@@ -484,14 +484,24 @@ def _out(out, shape, dtype, device):
 class _Blocks:
     """Codes and scale bytes of a matrix in blocks of 32 columns, in one buffer."""
 
-    def __init__(self, shape, code_pitch, scale_pitch, device):
+    def __init__(self, shape, code_pitch, scale_pitch, device, buffer=None):
         rows = shape[0]
         self.shape = (rows, shape[1])
-        self.device = device
         self._pitches = code_pitch, scale_pitch
         self._at = at = -(-rows * code_pitch // 256) * 256  # (the scales start 256-byte aligned)
-        self._buf = buf = torch.empty(at + rows * scale_pitch, dtype=torch.uint8, device=device)
-        self._ptr = buf.data_ptr()
+        size = at + rows * scale_pitch
+        if buffer is None:
+            buffer = torch.empty(size, dtype=torch.uint8, device=device)
+        elif buffer.shape != (size,) or buffer.dtype != torch.uint8 or not buffer.is_contiguous():
+            raise ValueError("the buffer is not that of a matrix of this shape")
+        self._buf = buffer
+        self.device = buffer.device
+        self._ptr = buffer.data_ptr()
+
+    @property
+    def buffer(self) -> torch.Tensor:
+        """Codes and scale bytes as one tensor: what a save_for_backward is given."""
+        return self._buf
 
     @property
     def codes(self) -> torch.Tensor:
@@ -521,11 +531,12 @@ class _Blocks:
 
 
 class SavedActivation(_Blocks):
-    """Activations kept in 8 bits (gs_saved): codes, one power-of-two step per 32 columns of a row."""
+    """Activations kept in 8 bits (gs_saved): codes, one power-of-two step per 32 columns of a row.
+    buffer: that of other saved activations of this shape, or a copy of it."""
 
-    def __init__(self, shape, act: str, device):
+    def __init__(self, shape, act: str, device, buffer: torch.Tensor | None = None):
         blocks = -(-shape[1] // 32)
-        super().__init__(shape, 32 * blocks, blocks, device)
+        super().__init__(shape, 32 * blocks, blocks, device, buffer)
         self.act = act
         self._c = _Saved(shape[0], shape[1], ACTIVATIONS[act], self._ptr, self._ptr + self._at)
         self._ref = ctypes.byref(self._c)

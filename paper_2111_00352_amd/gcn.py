@@ -188,25 +188,26 @@ class _ReluLinear(torch.autograd.Function):
 
     @staticmethod
     def forward(ctx, P, W, mx):
-        H, ctx.act = gs.save_activation(P.contiguous(), "relu")
-        ctx.mx = mx
-        ctx.save_for_backward(W)
+        H, act = gs.save_activation(P.contiguous(), "relu")
+        ctx.mx, ctx.shape = mx, act.shape
+        ctx.save_for_backward(W, act.buffer)
         return gs.mxfp4_matmul(H, gs.mxfp4_quantize(W, axis=0)) if mx else H @ W
 
     @staticmethod
     def backward(ctx, G):
         _first_order_only()
-        W, = ctx.saved_tensors
+        W, codes = ctx.saved_tensors
+        act = gs.SavedActivation(ctx.shape, "relu", codes.device, codes)
         G = G.contiguous()
         dP = dW = None
         if ctx.needs_input_grad[0]:
             if ctx.mx:
-                dP = gs.mxfp4_matmul(G, gs.mxfp4_quantize(W), mask=ctx.act)
+                dP = gs.mxfp4_matmul(G, gs.mxfp4_quantize(W), mask=act)
             else:
                 dP = G @ W.t()
-                gs.relu_grad(ctx.act, dP, out=dP)
+                gs.relu_grad(act, dP, out=dP)
         if ctx.needs_input_grad[1]:
-            dW = _saved_weight_grad(ctx.act, G)
+            dW = _saved_weight_grad(act, G)
         return dP, dW, None
 
 

@@ -523,6 +523,34 @@ def test_gcn_lowbit_training(k, mode):
         assert np.all(np.abs(got - want) <= 2.0 ** -7 * want)
 
 
+@pytest.mark.parametrize("mode", ["saved8", "mxfp4"])
+def test_gcn_lowbit_keeps_the_codes_and_nothing_else(mode):
+    # between the passes: the output and the hidden layer's codes and scales; after them
+    # the output and the gradients, though the output still holds its graph.  An
+    # allocation is a multiple of 512 bytes.
+    H, O = 64, 32
+    g, coo, X, W1, W2, T = _problem(2, H, O, 5200)
+    ctx = gs.SelectContext("fixed", fixed="csr")
+    adj = gcn.Adjacency(*coo, (g.R, g.C), ctx, key=6, symmetric=g.meta["symmetric"])
+    model = gcn.GCN2(W1, W2, mode)
+    model.step(X, T, adj, lr=0.0)  # (formats and workspaces are made)
+    model.W1.grad = model.W2.grad = None
+    torch.cuda.synchronize()
+    before = torch.cuda.memory_allocated()
+    Out, P1 = model.forward(X, adj)
+    between = torch.cuda.memory_allocated() - before
+    loss = model.loss(Out, T)
+    loss.backward()
+    del loss
+    after = torch.cuda.memory_allocated() - before
+    ctx.close()
+    out, codes = g.R * O * 4, g.R * H * 33 // 32
+    grads = W1.numel() * 4 + W2.numel() * 4
+    assert P1 is None
+    assert between <= out + codes + 256 + 2 * 511
+    assert after <= out + grads + 3 * 511
+
+
 @pytest.mark.parametrize("k", [2, 3])
 def test_gcn_mxfp4_forward_matches_oracle(k):
     # the forward pass with its 4-bit products against the same chain in fp64.  X and

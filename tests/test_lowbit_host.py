@@ -220,3 +220,78 @@ def test_low_bit_layers_of_any_width_have_a_backward_pass(layer, a, b, monkeypat
     v = lowbit.save8(P.detach().double().numpy(), True)[2]
     mag = np.abs(v).T @ np.abs(G.double().numpy())
     assert np.all(np.abs(W.grad.double().numpy() - v.T @ G.double().numpy()) <= 2 * 6 * 2.0 ** -24 * mag)
+
+
+@pytest.mark.parametrize("layer", ["saved8", "mxfp4"])
+def test_codes_of_a_layer_are_saved_tensors(layer, monkeypatch):
+    # hooks on saved tensors see them (and may give back another tensor), and they go
+    # with the graph's other saved tensors once the backward pass has run
+    import torch
+    _operators_on_the_cpu(monkeypatch)
+    made, save = [], gs.save_activation
+
+    def save_activation(P, act="relu"):
+        H, saved = save(P, act)
+        made.append(saved._buf)
+        return H, saved
+
+    monkeypatch.setattr(gs, "save_activation", save_activation)
+    gen = torch.Generator().manual_seed(5)
+    P, W = (torch.randn(s, generator=gen).requires_grad_(True) for s in ((30, 70), (70, 9)))
+    G = torch.randn(30, 9, generator=gen)
+    want = torch.autograd.grad(_layers()[layer](P, W), (P, W), G)
+    size = made[0].numel()
+    assert size == 256 * -(-30 * 96 // 256) + 30 * 3
+
+    def pack(t):
+        return t.clone() if t.dtype == torch.uint8 else t
+
+    packed = []
+    with torch.autograd.graph.saved_tensors_hooks(lambda t: packed.append(t.dtype) or pack(t), lambda t: t):
+        Z = _layers()[layer](P, W)
+    assert packed.count(torch.uint8) == 1
+    made[1].zero_()  # (the layer reads what the hook kept)
+    got = torch.autograd.grad(Z, (P, W), G)
+    assert all(torch.equal(x, y) for x, y in zip(got, want))
+    with pytest.raises(RuntimeError, match="second time"):
+        torch.autograd.grad(Z, (P, W), G)
+
+
+def test_saved_activation_of_another_buffer():
+    import torch
+    saved = gs.SavedActivation((5, 40), "relu", "cpu")
+    saved.codes[:] = 3
+    saved.scales[:] = 127
+    again = gs.SavedActivation((5, 40), "relu", "cpu", saved.buffer.clone())
+    assert torch.equal(again.codes, saved.codes) and torch.equal(again.scales, saved.scales)
+    for buffer in (saved.buffer[:-1], saved.buffer.view(torch.int8), torch.zeros(2 * saved.buffer.numel(), dtype=torch.uint8)[::2],
+                   saved.buffer[None]):
+        with pytest.raises(ValueError):
+            gs.SavedActivation((5, 40), "relu", "cpu", buffer)
+
+
+def test_codes_in_host_memory_are_refused(monkeypatch):
+    # as a hook on saved tensors may leave them: no kernel is given their address
+    import torch
+    library = _Launches()
+    monkeypatch.setattr(gs, "lib", lambda: library)
+    monkeypatch.setattr(gs, "_stream", lambda stream=None: 0)
+    monkeypatch.setattr(torch._C, "_cuda_getDevice", lambda: 0, raising=False)
+
+    class OnTheGpu(torch.Tensor):  # (says so: this test needs none)
+        is_cuda = True
+
+        def get_device(self):
+            return 0
+
+    def dense(*shape):
+        return torch.zeros(shape).as_subclass(OnTheGpu)
+
+    saved, q = gs.SavedActivation((3, 40), "relu", "cpu"), gs.Mxfp4((7, 40), "cpu")
+    mask = gs.SavedActivation((3, 7), "relu", "cpu")
+    for call in (lambda: gs.relu_grad(saved, dense(3, 40)), lambda: gs.saved_weight_grad(saved, dense(3, 7)),
+                 lambda: gs.mxfp4_matmul(dense(3, 40), q), lambda: gs.mxfp4_matmul(dense(3, 40), q, mask=mask),
+                 lambda: gs.mxfp4_matmul(q, q), saved.dequantize, q.dequantize):
+        with pytest.raises(ValueError):
+            call()
+    assert not library.calls
