@@ -419,24 +419,33 @@ def weight_grad(H: torch.Tensor, G: torch.Tensor, stream=None) -> torch.Tensor:
 #
 # Calls on small operands are bound by what happens here, so arguments are looked at
 # once each and nothing is made that the call does not need.
+#
+# The calls have no derivatives (the layers in gcn define theirs), and codes carry none:
+# a backward pass that reaches a result computed from a tensor that requires a gradient
+# fails there, rather than going on without that part.
 
 ACTIVATIONS = {"none": 0, "relu": 1}
 SAVED_GRAD_WIDTH = 4096  # columns of either operand of saved_weight_grad at most
 _DTYPES = {torch.float32: 0, torch.bfloat16: 1}
+_STRIDED = torch.strided
+_tracing, _forward_ad = torch._C._get_tracing_state, torch.autograd.forward_ad
 
 
 def _dense(X: torch.Tensor, name: str, index: int | None = -1) -> tuple:
-    """(tensor, leading dimension, dtype code, shape) of a 2-D fp32 or bf16 operand on
-    the current device, and on the GPU `index` of another operand (None: it is on none)."""
+    """(tensor, leading dimension, dtype code, shape, current stream) of a 2-D fp32 or bf16
+    operand on the current device, and on the GPU `index` of another operand (None: it is
+    on none)."""
     code = _DTYPES.get(X.dtype) if isinstance(X, torch.Tensor) else None
-    if code is None or not X.is_cuda or X.dim() != 2 or X.layout != torch.strided:
+    if code is None or X.layout != _STRIDED or len(shape := X.shape) != 2 or (at := X.get_device()) < 0:
         raise ValueError(f"{name} must be a 2-D CUDA float32 or bfloat16 tensor")
-    at = X.get_device()
+    if _tracing() is not None:
+        raise RuntimeError("the low-bit operators cannot be traced: a trace would keep their results as constants")
+    if _forward_ad._current_level >= 0 and _forward_ad.unpack_dual(X).tangent is not None:
+        raise RuntimeError("the low-bit operators have no forward-mode derivative")
     if at != torch._C._cuda_getDevice() or (index != -1 and at != index):
         raise ValueError(f"{name} is not on the current device, or not on the other operand's")
     if X.is_neg():
         X = X.resolve_neg()
-    shape = X.shape
     rows, cols = shape
     ld, step = X.stride()
     if step != 1 and cols > 1 and rows > 0:
@@ -445,7 +454,31 @@ def _dense(X: torch.Tensor, name: str, index: int | None = -1) -> tuple:
         if rows > 1:
             raise ValueError(f"{name} must have a row stride of at least its width")
         ld = cols
-    return X, ld, code, shape
+    return X, ld, code, shape, torch._C._cuda_getCurrentRawStream(at)
+
+
+class _NoGradient(torch.autograd.Function):
+    """The result of a call, in the place of its operands' derivatives."""
+
+    @staticmethod
+    def forward(ctx, result, *operands):
+        return result
+
+    @staticmethod
+    def backward(ctx, *_):
+        raise RuntimeError("the low-bit operators have no gradient: detach their operands, or use the layers of gcn")
+
+
+def _result(t: torch.Tensor, X: torch.Tensor) -> torch.Tensor:
+    """t, a new tensor computed from X that requires a gradient, as autograd is to see it."""
+    return _NoGradient.apply(t, X) if torch.is_grad_enabled() else t
+
+
+def _written(out: torch.Tensor) -> torch.Tensor:
+    """`out`, whose change a graph that keeps it for a backward pass is to find."""
+    if not out.is_inference():
+        torch.autograd.graph.increment_version(out)
+    return out
 
 
 def _dtype_code(dtype) -> int:
@@ -472,12 +505,14 @@ def _on(stream, call, *args):
     return out
 
 
-def _out(out, shape, dtype, device):
-    """`out`, or a new tensor, and its leading dimension."""
+def _out(out, shape, dtype, device, operand=None):
+    """`out`, or a new tensor, and its leading dimension; `operand`: what is computed from."""
     if out is None:
         return torch.empty(shape, dtype=dtype, device=device), shape[1]
     if tuple(out.shape) != tuple(shape) or out.dtype != dtype or out.is_neg():
         raise ValueError("out has the wrong shape or dtype")
+    if torch.is_grad_enabled() and (out.requires_grad or (operand is not None and operand.requires_grad)):
+        raise ValueError("out cannot be given where an argument requires a gradient")
     return out, _dense(out, "out", device.index)[1]
 
 
@@ -494,8 +529,10 @@ class _Blocks:
             buffer = torch.empty(size, dtype=torch.uint8, device=device)
         elif buffer.shape != (size,) or buffer.dtype != torch.uint8 or not buffer.is_contiguous():
             raise ValueError("the buffer is not that of a matrix of this shape")
+        else:
+            device = None
         self._buf = buffer
-        self.device = buffer.device
+        self.device = device if type(device) is torch.device and device.index is not None else buffer.device
         self._ptr = buffer.data_ptr()
 
     @property
@@ -521,10 +558,11 @@ class _Blocks:
         if stream is not None:
             return _on(stream, type(self).dequantize, self, dtype)
         code = _dtype_code(dtype)
-        if self.device.index != torch._C._cuda_getDevice():
+        at = torch._C._cuda_getDevice()
+        if self.device.index != at:
             raise ValueError("the codes are not on the current device")
         out = torch.empty(self.shape, dtype=dtype, device=self.device)
-        rc = self._values(lib())(self._ref, out.data_ptr(), self.shape[1], code, _stream())
+        rc = self._values(lib())(self._ref, out.data_ptr(), self.shape[1], code, torch._C._cuda_getCurrentRawStream(at))
         if rc:
             _check(rc)
         return out
@@ -568,16 +606,19 @@ def save_activation(P: torch.Tensor, act: str = "relu", stream=None) -> tuple:
         return _on(stream, save_activation, P, act)
     if act not in ACTIVATIONS:
         raise ValueError("act must be 'relu' or 'none'")
-    P, ld, code, shape = _dense(P, "P")
+    P, ld, code, shape, s = _dense(P, "P")
     saved = SavedActivation(shape, act, P.device)
     if act == "relu":
         H = torch.empty_like(P) if ld == shape[1] else torch.empty(shape, dtype=P.dtype, device=P.device)
-        rc = lib().gs_save_activation(P.data_ptr(), ld, code, saved._ref, H.data_ptr(), shape[1], _stream())
+        rc = lib().gs_save_activation(P.data_ptr(), ld, code, saved._ref, H.data_ptr(), shape[1], s)
     else:
-        H = P
-        rc = lib().gs_save_activation(P.data_ptr(), ld, code, saved._ref, None, 0, _stream())
+        rc = lib().gs_save_activation(P.data_ptr(), ld, code, saved._ref, None, 0, s)
     if rc:
         _check(rc)
+    if act != "relu":
+        H = P
+    elif P.requires_grad:
+        H = _result(H, P)
     return H, saved
 
 
@@ -585,17 +626,19 @@ def relu_grad(saved: SavedActivation, dH: torch.Tensor, out: torch.Tensor | None
     """dH where the saved ReLU was active, else 0 (gs_relu_grad); out may be dH."""
     if stream is not None:
         return _on(stream, relu_grad, saved, dH, out)
-    dH, ld, code, shape = _dense(dH, "dH", saved.device.index)
+    dH, ld, code, shape, s = _dense(dH, "dH", saved.device.index)
     if shape != saved.shape:
         raise ValueError("dH and the saved activations have different shapes")
     if out is None and ld == shape[1]:
         dP, ldp = torch.empty_like(dH), ld  # (the quickest way to a tensor of this shape)
     else:
-        dP, ldp = _out(out, shape, dH.dtype, dH.device)
-    rc = lib().gs_relu_grad(saved._ref, dH.data_ptr(), ld, code, dP.data_ptr(), ldp, _stream())
+        dP, ldp = _out(out, shape, dH.dtype, dH.device, dH)
+    rc = lib().gs_relu_grad(saved._ref, dH.data_ptr(), ld, code, dP.data_ptr(), ldp, s)
     if rc:
         _check(rc)
-    return dP
+    if out is not None:
+        return _written(dP)
+    return _result(dP, dH) if dH.requires_grad else dP
 
 
 @functools.lru_cache(maxsize=1024)
@@ -610,7 +653,7 @@ def saved_weight_grad(saved: SavedActivation, G: torch.Tensor, stream=None) -> t
     SAVED_GRAD_WIDTH (gs_saved_weight_grad)."""
     if stream is not None:
         return _on(stream, saved_weight_grad, saved, G)
-    G, ld, code, shape = _dense(G, "G", saved.device.index)
+    G, ld, code, shape, s = _dense(G, "G", saved.device.index)
     (n, a), b = saved.shape, shape[1]
     if shape[0] != n:
         raise ValueError("G and the saved activations must have the same number of rows")
@@ -620,10 +663,10 @@ def saved_weight_grad(saved: SavedActivation, G: torch.Tensor, stream=None) -> t
     need = _grad_work(n, a, b)
     work = torch.empty(need, dtype=torch.uint8, device=G.device) if need else None
     rc = lib().gs_saved_weight_grad(saved._ref, G.data_ptr(), ld, code, b, out.data_ptr(),
-                                    None if work is None else work.data_ptr(), need, _stream())
+                                    None if work is None else work.data_ptr(), need, s)
     if rc:
         _check(rc)
-    return out
+    return _result(out, G) if G.requires_grad else out
 
 
 def mxfp4_quantize(X: torch.Tensor, axis: int = 1, stream=None) -> Mxfp4:
@@ -634,9 +677,9 @@ def mxfp4_quantize(X: torch.Tensor, axis: int = 1, stream=None) -> Mxfp4:
         return _on(stream, mxfp4_quantize, X, axis)
     if axis not in (0, 1):
         raise ValueError("axis must be 0 or 1")
-    X, ld, code, (rows, cols) = _dense(X, "X")
+    X, ld, code, (rows, cols), s = _dense(X, "X")
     q = Mxfp4((rows, cols) if axis == 1 else (cols, rows), X.device)
-    rc = lib().gs_mxfp4_quantize(X.data_ptr(), ld, code, rows, cols, axis, q._ref, _stream())
+    rc = lib().gs_mxfp4_quantize(X.data_ptr(), ld, code, rows, cols, axis, q._ref, s)
     if rc:
         _check(rc)
     return q
@@ -664,26 +707,28 @@ def mxfp4_matmul(A, B: Mxfp4, mask: SavedActivation | None = None, dtype=torch.f
     if quantised:
         if A.device != device or device.index != torch._C._cuda_getDevice():
             raise ValueError("A and B must be on the current device")
-        a_code, (m, k) = -1, A.shape
+        a_code, (m, k), s = -1, A.shape, _stream()
     else:
-        A, lda, a_code, (m, k) = _dense(A, "A", device.index)
+        A, lda, a_code, (m, k), s = _dense(A, "A", device.index)
     n, kb = B.shape
     if k != kb:
         raise ValueError(f"A has {k} columns, B has {kb}")
     if mask is not None and (mask.shape != (m, n) or mask.device != device):
         raise ValueError("the mask's shape or device is not the product's")
-    C, ldc = _out(out, (m, n), dtype, device)
+    C, ldc = _out(out, (m, n), dtype, device, None if quantised else A)
     need = _matmul_work(m, n, k, a_code)
     work = torch.empty(need, dtype=torch.uint8, device=device) if need else None
     mask_ref, at = None if mask is None else mask._ref, None if work is None else work.data_ptr()
     if quantised:
-        rc = lib().gs_mxfp4_matmul(A._ref, B._ref, mask_ref, C.data_ptr(), ldc, code, at, need, _stream())
+        rc = lib().gs_mxfp4_matmul(A._ref, B._ref, mask_ref, C.data_ptr(), ldc, code, at, need, s)
     else:
         rc = lib().gs_mxfp4_matmul_dense(A.data_ptr(), lda, a_code, m, B._ref, mask_ref, C.data_ptr(), ldc, code, at, need,
-                                         _stream())
+                                         s)
     if rc:
         _check(rc)
-    return C
+    if out is not None:
+        return _written(C)
+    return C if quantised or not A.requires_grad else _result(C, A)
 
 
 def _features_dict(out: _Features) -> dict:

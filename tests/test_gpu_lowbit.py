@@ -681,3 +681,59 @@ def test_views_with_other_strides():
     assert torch.equal(gs.save_activation(col)[0], torch.relu(col))
     row = torch.randn(7, 1, device=DEV).t()  # one row whose row stride is below its width
     assert torch.equal(gs.save_activation(row)[0], torch.relu(row))
+
+
+def test_no_gradient_is_dropped_unseen():
+    # the operators have no derivatives: a backward pass that reaches one of their results
+    # fails, as do traces, forward-mode derivatives and out= beside a gradient
+    P, G = torch.randn(10, 40, device=DEV), torch.randn(10, 8, device=DEV)
+    _, saved = gs.save_activation(P)
+    W = gs.mxfp4_quantize(torch.randn(8, 40, device=DEV))
+    calls = {"save": (lambda x: gs.save_activation(x)[0], P), "mask": (lambda x: gs.relu_grad(saved, x), P),
+             "wgrad": (lambda x: gs.saved_weight_grad(saved, x), G), "matmul": (lambda x: gs.mxfp4_matmul(x, W), P)}
+    for call, x in calls.values():
+        want = call(x)
+        assert not want.requires_grad
+        p = x.clone().requires_grad_(True)
+        got = call(p)
+        assert torch.equal(got, want)
+        with pytest.raises(RuntimeError, match="no gradient"):
+            (got.sum() + p.sum()).backward()
+        got = call(p.detach())
+        assert torch.equal(got, want) and not got.requires_grad
+        with torch.no_grad():
+            got = call(p)
+        assert torch.equal(got, want) and not got.requires_grad
+        with pytest.raises(RuntimeError, match="traced"):
+            torch.jit.trace(call, x)
+        with torch.autograd.forward_ad.dual_level():
+            assert torch.equal(call(x), want)
+            with pytest.raises(RuntimeError, match="forward-mode"):
+                call(torch.autograd.forward_ad.make_dual(x, torch.ones_like(x)))
+        with torch.inference_mode():
+            assert torch.equal(call(x), want)
+    p = P.clone().requires_grad_(True)
+    assert gs.save_activation(p, "none")[0] is p  # (the identity passes its gradient on)
+    for call in (lambda: gs.relu_grad(saved, p, out=torch.empty_like(P)), lambda: gs.relu_grad(saved, P, out=p),
+                 lambda: gs.mxfp4_matmul(p, W, out=torch.empty(10, 8, device=DEV)),
+                 lambda: gs.mxfp4_matmul(P, W, out=torch.empty(10, 8, device=DEV, requires_grad=True))):
+        with pytest.raises(ValueError):
+            call()
+
+
+def test_outputs_in_place_are_seen_by_autograd():
+    # a tensor that a graph keeps is found changed, as by PyTorch's own in-place operations
+    P = torch.randn(10, 40, device=DEV)
+    _, saved = gs.save_activation(P)
+    W = gs.mxfp4_quantize(torch.randn(8, 40, device=DEV))
+    for shape, write in (((10, 40), lambda t: gs.relu_grad(saved, t, out=t)), ((10, 8), lambda t: gs.mxfp4_matmul(P, W, out=t)),
+                         ((10, 8), lambda t: gs.mxfp4_matmul(gs.mxfp4_quantize(P), W, out=t))):
+        w = torch.ones(shape, device=DEV, requires_grad=True)
+        t = torch.randn(shape, device=DEV)
+        loss = (w * t).sum()
+        assert write(t) is t
+        with pytest.raises(RuntimeError, match="modified by an inplace operation"):
+            loss.backward()
+    with torch.inference_mode():
+        t = torch.randn(10, 40, device=DEV)
+        assert gs.relu_grad(saved, t, out=t) is t

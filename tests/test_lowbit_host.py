@@ -126,7 +126,7 @@ def test_values_of_codes_on_another_device_are_refused(make, monkeypatch):
     import torch
     library, empty = _Launches(), torch.empty
     monkeypatch.setattr(gs, "lib", lambda: library)
-    monkeypatch.setattr(gs, "_stream", lambda stream=None: 0)
+    monkeypatch.setattr(torch._C, "_cuda_getCurrentRawStream", lambda at: 0, raising=False)
     monkeypatch.setattr(torch._C, "_cuda_getDevice", lambda: 0, raising=False)
     monkeypatch.setattr(torch, "empty", lambda shape, dtype=None, device=None: empty(shape, dtype=dtype))
     q = make()
@@ -275,7 +275,7 @@ def test_codes_in_host_memory_are_refused(monkeypatch):
     import torch
     library = _Launches()
     monkeypatch.setattr(gs, "lib", lambda: library)
-    monkeypatch.setattr(gs, "_stream", lambda stream=None: 0)
+    monkeypatch.setattr(torch._C, "_cuda_getCurrentRawStream", lambda at: 0, raising=False)
     monkeypatch.setattr(torch._C, "_cuda_getDevice", lambda: 0, raising=False)
 
     class OnTheGpu(torch.Tensor):  # (says so: this test needs none)
