@@ -289,6 +289,37 @@ def test_mxfp4_matmul_integers_are_exact(m, n, k):
     assert torch.equal(gs.mxfp4_matmul(a.to(DEV), B).cpu().double(), want)
 
 
+# products in slices of k: of 2 chunks of 256 and more, even ones and a last one that is longer,
+# with half a chunk at the end or not, of small tiles and (from 128 of them, k > 30,000) of large
+# ones; and the shortest k that is made of tiles at all, in one slice of two chunks
+SLICES = [(256, 256, 5000), (512, 512, 8192), (512, 512, 8500), (300, 700, 8500), (500, 520, 9100), (1000, 1000, 16000),
+          (2047, 4001, 32600), (2048, 4096, 32768), (200, 600, 512), (200, 600, 450), (65, 512, 512)]
+
+
+@pytest.mark.parametrize("m,n,k", SLICES)
+def test_mxfp4_matmul_in_slices_of_k_is_exact(m, n, k):
+    # small whole numbers under different scales: products are multiples of 2^-6 and their
+    # sums' standard deviation is at most 51 sqrt(k) < 2^14, far below 2^24 of those steps, so
+    # every partial sum is exact and a misplaced chunk, slice or run of scales shows
+    gen = torch.Generator(device=DEV).manual_seed(m + n + k)
+    vals = torch.tensor([0.0, 1, 2, 3, 4, 6, -1, -2, -3, -4, -6], device=DEV)
+
+    def operand(rows):
+        x = vals[torch.randint(len(vals), (rows, k), device=DEV, generator=gen)]
+        scale = torch.exp2(torch.randint(-2, 3, (rows, -(-k // 32)), device=DEV, generator=gen).float())
+        return x * scale.repeat_interleave(32, 1)[:, :k]
+
+    a, B = operand(m), gs.mxfp4_quantize(operand(n))
+    A = gs.mxfp4_quantize(a)
+    want = (A.dequantize().double() @ B.dequantize().double().t()).float()
+    _, saved = gs.save_activation(torch.randn(m, n, device=DEV, generator=gen))
+    on = saved.codes[:, :n] > 0
+    for operand in (A, a):
+        assert torch.equal(gs.mxfp4_matmul(operand, B), want)
+        assert torch.equal(gs.mxfp4_matmul(operand, B, mask=saved), torch.where(on, want, 0.0))
+        assert torch.equal(gs.mxfp4_matmul(operand, B, dtype=torch.bfloat16), want.bfloat16())
+
+
 @pytest.mark.parametrize("m", [1, 40, 300])
 def test_mxfp4_matmul_nan_blocks_and_masked_nan(m):
     # a block that is not finite makes its row (A) or column (B) of the product NaN,
