@@ -502,6 +502,58 @@ def test_relu_linear_in_mxfp4_matches_its_formula():
     assert np.all(np.abs(_np(W.grad) - q8[2].T @ g) <= 2 * 100 * U * (q8[2].T @ np.abs(g)))
 
 
+def test_linear_in_mxfp4_matches_its_formula():
+    rng = np.random.default_rng(12)
+    n, a, b = 300, 100, 45
+    H, W, G = (torch.from_numpy(rng.standard_normal(s).astype(np.float32)).to(DEV) for s in ((n, a), (a, b), (n, b)))
+    H.requires_grad_(True)
+    W.requires_grad_(True)
+    Z = gcn._LinearMx.apply(H, W)
+    Z.backward(G)
+    h, w, g = _np(H), _np(W), _np(G)
+    hv, wt, wr, gv = lowbit.quant4(h)[2], lowbit.quant4(w.T)[2], lowbit.quant4(w)[2], lowbit.quant4(g)[2]
+    assert np.all(np.abs(_np(Z) - hv @ wt.T) <= 2 * 70 * U * (np.abs(hv) @ np.abs(wt).T))
+    assert np.all(np.abs(_np(H.grad) - gv @ wr.T) <= 2 * 70 * U * (np.abs(gv) @ np.abs(wr).T))
+    assert np.all(np.abs(_np(W.grad) - h.T @ g) <= 2 * n * U * (np.abs(h).T @ np.abs(g)))
+
+
+@pytest.mark.parametrize("k", [2, 3])
+def test_gcn_mxfp4_step_stage_by_stage(k):
+    # each gradient of one step against its formula in fp64 from the gradient above it, and
+    # the same step through GCN2, which runs the same kernels, bit for bit
+    g, coo, X, W1, W2, T = _problem(k, 64, 32, 5400 + k)
+    ctx = gs.SelectContext("fixed", fixed="csr")
+    adj = gcn.Adjacency(*coo, (g.R, g.C), ctx, key=8, symmetric=g.meta["symmetric"])
+    model = gcn.GCN2(W1, W2, "mxfp4")
+    Z1 = gcn._LinearMx.apply(X, model.W1)
+    P1 = gcn.aggregate(Z1, adj)
+    Z2 = gcn._ReluLinear.apply(P1, model.W2, True)
+    Out = gcn.aggregate(Z2, adj)
+    for t in (Z1, P1, Z2, Out):
+        t.retain_grad()
+    model.loss(Out, T).backward()
+    og = ogcn.Graph(g.R, g.C, g.row, g.col, g.val)
+    terms = int(np.bincount(g.col, minlength=g.C).max()) + 1  # of a sum of the aggregation
+
+    def near(got, want, mag, terms):
+        assert np.all(np.abs(_np(got) - want) <= 2 * terms * U * mag)
+
+    d = (_np(Out) - _np(T)) / g.R
+    near(Out.grad, d, np.abs(d) + np.abs(_np(T)) / g.R, 4)  # (the difference, the square, the mean)
+    near(Z2.grad, og.agg_t(_np(Out.grad)), og.agg_t(np.abs(_np(Out.grad)), absolute=True), terms)
+    dz, p, w = _np(Z2.grad), _np(P1), _np(W2)
+    gv, wv = lowbit.quant4(dz)[2], lowbit.quant4(w)[2]
+    _, _, hv, _, on = lowbit.save8(p, True)
+    near(P1.grad, np.where(on, gv @ wv.T, 0), np.where(on, np.abs(gv) @ np.abs(wv).T, 0), 70)
+    near(model.W2.grad, hv.T @ dz, hv.T @ np.abs(dz), 3 * -(-g.R // 128) + 16 + 64)
+    near(Z1.grad, og.agg_t(_np(P1.grad)), og.agg_t(np.abs(_np(P1.grad)), absolute=True), terms)
+    near(model.W1.grad, _np(X).T @ _np(Z1.grad), np.abs(_np(X)).T @ np.abs(_np(Z1.grad)), g.R)
+    again = gcn.GCN2(W1, W2, "mxfp4")
+    again.step(X, T, adj, lr=0.0)
+    ctx.close()
+    assert torch.equal(again.W1.grad, model.W1.grad) and torch.equal(again.W2.grad, model.W2.grad)
+
+
 @pytest.mark.parametrize("a,b", [(4130, 9), (9, 4130)])
 @pytest.mark.parametrize("mx", [False, True])
 def test_relu_linear_wider_than_the_weight_gradient_kernel(a, b, mx):
