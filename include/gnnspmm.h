@@ -363,8 +363,10 @@ int gs_relu_grad(const gs_saved *A, const void *dH, int64_t ldh, int dtype, void
 
 /* Weight gradient from saved activations: out = value(A)^T . G, A.cols x b fp32
  * row-major (leading dimension b), G [dev] rows x b with leading dimension ldg.
- * The values of A are exact on the matrix cores and G is taken in three parts
- * that add up to it, so products and sums are those of fp32.  A.cols and b are
+ * The values of A are exact on the matrix cores.  bf16 gradients are too; fp32
+ * ones are taken in three bf16 parts that add up to them from 2^-110 on and miss
+ * less than 2^-133 below, so a sum is that of fp32 products and sums within
+ * 2^-133 of the values that meet such gradients.  A.cols and b are
  * at least 1 (GS_ERR_INVALID_ARG) and at most 4096, ldg at most 2^26
  * (GS_ERR_UNSUPPORTED).  work [dev] holds at least the bytes that
  * gs_saved_weight_grad_workspace reports. */

@@ -7,7 +7,9 @@
 // bits each (its significand cut twice), so three bf16 products with fp32 sums
 // give the fp32 product's accuracy at several times the fp32 matrix rate
 // (V_MFMA_F32_32X32X16_BF16: 2.5 PFLOP/s against 157 TFLOP/s), and a bf16 gradient
-// needs one.  That leaves the kernel bound by reading A and G once.
+// needs one.  That leaves the kernel bound by reading A and G once.  Gradients below
+// 2^-110 end under bf16's smallest subnormal, 2^-133 (the instruction takes subnormals
+// as they are): what lies below it, less than 2^-133 of a gradient, is cut off.
 //
 // Both operands are wanted with their rows, the k index of the product, running
 // inside a lane, and they lie in memory by rows.  A lane therefore loads CA

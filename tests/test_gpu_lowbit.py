@@ -160,6 +160,25 @@ def test_saved_weight_grad_is_deterministic_and_takes_wide_ranges():
     assert np.all(np.abs(_np(first) - v.T @ g) <= bound)
 
 
+def test_saved_weight_grad_of_subnormal_parts():
+    # a gradient from 2^-110 on is the sum of its three bf16 parts; below that its last part
+    # loses what lies under bf16's smallest subnormal, 2^-133, which large values bring back
+    # into range: column j holds gradients around 2^-(105 + 2 j), values are 2^60 and more
+    rng = np.random.default_rng(8)
+    n, a, b = 500, 40, 23
+    P = torch.from_numpy((rng.uniform(1, 2, (n, a)) * 2.0 ** rng.integers(60, 120, (1, a))).astype(np.float32))
+    G = torch.from_numpy((rng.standard_normal((n, b)) * 2.0 ** -(105 + 2 * np.arange(b)))).float()
+    _, saved = gs.save_activation(P.to(DEV))
+    v, g = lowbit.save8(_np(P), True)[2], _np(G)
+    terms = 3 * -(-n // 128) + 16 + 64
+    lost = np.where(np.abs(g) < 2.0 ** -110, 2.0 ** -133, 0.0)
+    got, mag = _np(gs.saved_weight_grad(saved, G.to(DEV))), v.T @ np.abs(g)
+    assert np.all(np.abs(got - v.T @ g) <= 2 * terms * U * mag + v.T @ lost)
+    got = _np(gs.saved_weight_grad(saved, G.bfloat16().to(DEV)))  # (one part: nothing is lost)
+    g = _np(G.bfloat16())
+    assert np.all(np.abs(got - v.T @ g) <= 2 * terms * U * (v.T @ np.abs(g)))
+
+
 def test_saved_weight_grad_infinities_and_nan():
     # an infinite gradient gives infinity where the value is not 0 and NaN where it
     # is, as the fp32 product does; a NaN block makes its 32 columns NaN; no other
