@@ -368,7 +368,7 @@ __device__ __forceinline__ void few_quantise(const DenseRows<T> &A, int64_t m, i
 {
     constexpr int E = 8, L = kMxBlock / E;
     const int per = kpad / E, units = (int)m * per;
-    for (int u = threadIdx.x; u < units; u += kFewWaves * kWave) {  // (units: a multiple of 16)
+    for (int u = threadIdx.x; u < units; u += kFewWaves * kWave) {  // (whole blocks: a multiple of 4)
         const int row = u / per, col = u % per * E;
         const Mx4Lane<T, E> x{load_elems<T, E>(A.p + row * A.ld + col, A.cols - col)};
         const int E8 = mx4_exponent(group_max<L>(x.magnitude()));
@@ -454,10 +454,11 @@ __global__ __launch_bounds__(kFewWaves * kWave) void k_few(Rows A, const uint8_t
 //
 // Scales lie in LDS as 16 bytes of a row, a run of two chunks, loaded a run ahead.
 //
-// 8192^3 to bf16 255 us, 4.3 PFLOP/s: 113 us for every 4,096 of k (4.9 PFLOP/s) and 25 us
-// around them, 16 of which are the stores.  The instructions alone, on random operands
-// in registers, reach 7.0 PFLOP/s (clocks fall under that load); with operands that are
-// not loaded anew the loop takes 210 us, with ones that are not read from LDS 250.
+// 8192^3 to bf16 255 to 264 us, 4.2 to 4.3 PFLOP/s: 113 us for every 4,096 of k (4.9
+// PFLOP/s) and 25 us around them, 16 of which are the stores.  The instructions alone,
+// on random operands in registers, reach 6.5 to 7.0 PFLOP/s, at clocks that have fallen
+// under that load; with operands that are not loaded anew the loop takes 210 us, with ones
+// that are not read from LDS 250.
 // Tiles of 256 x 256 leave a compute unit one workgroup, whose stores nothing covers; a
 // workgroup that goes on to its next tile meanwhile was slower (261 us: what it keeps
 // across the stores spills).
@@ -745,7 +746,17 @@ void check_sizes(int64_t m, int64_t n, int64_t k)
     if (k > kMxMaxCols) fail(GS_ERR_UNSUPPORTED, "at most 2^24 columns");
 }
 
-// How a product of k > 0 is formed.
+// How a product of k > 0 is formed.  Measured on both sides of each limit (us in a graph, A in
+// MXFP4, C in fp32; n x k of B):
+// - Under 32 rows only k_few can (k_narrow takes 32 at a time).  32 rows, k_few and k_narrow: 4096 x
+//   64 3.2 and 3.0, 4096 x 256 3.4 and 3.5, 128 x 512 2.9 and 3.8; 64 rows 3.8 and 3.1, 4.2 and 3.7,
+//   3.5 and 4.2.  A dense A of 32 rows is quicker by k_few: 4096 x 256 from bf16 4.0 and 6.6.
+// - At a padded k of 512 both k_narrow (512 at most) and k_tile (512 at least) can: 1,000 rows, n = 500 5.2
+//   and 6.0; 8,192 rows, n = 512 9.3 and 6.1; 100,000 rows, n = 128 20.8 and 26.5, n = 512 58.5 and
+//   50.7.  The limit in n is right at both ends only: from 8,192 rows on tiles are quicker at n = 256
+//   (6.5 and 4.9; 100,000 rows 38.5 and 27.6), at 1,000 rows k_narrow still is at n = 1024 (5.3 and 5.8).
+// - Up to 64 rows and a longer k, k_few and k_tile: 64 rows, 512 x 1024 3.8 and 6.3, 4096 x 4096 8.1 and
+//   11.0; with much of B the tiles are quicker already (8192 x 8192 25.7 and 16.5, 300 x 8192 12.9 and 9.5).
 enum class Way { kFew, kNarrow, kTile };
 Way way(int64_t m, int64_t n, int kpad)
 {
@@ -754,11 +765,18 @@ Way way(int64_t m, int64_t n, int kpad)
     return m <= kFewRows ? Way::kFew : Way::kTile;
 }
 
-// Columns of B that a workgroup of k_narrow keeps: 32 KB of it (KS times 64 of k).
+// Columns of B that a workgroup of k_narrow keeps: 32 KB of it (KS times 64 of k).  With 32 KB
+// and with 16 (us in a graph, MXFP4 to fp32): 100,000 x 1024 x 64 107 and 121, 100,000 x 300 x 384 88 and 93,
+// 500,000 x 512 x 128 207 and 207, 100,000 x 512 x 256 49 and 45.  Two workgroups
+// of 32 KB fit a compute unit's LDS, one of 64 KB would.
 int narrow_slices(int kpad) { return kpad <= 64 ? 1 : kpad <= 128 ? 2 : kpad <= 256 ? 4 : 8; }
 int64_t narrow_columns(int kpad) { return 32 * (32 / narrow_slices(kpad)); }
 
-// Whether a dense A is quantised by the kernel that multiplies it.
+// Whether a dense A is quantised by the kernel that multiplies it: by k_few up to kFewInside elements,
+// by k_narrow while one panel holds all of B.  Inside and in a launch before it (us in a graph, where a
+// launch costs 2 us instead of the host's 3): k_few, bf16, 1 x 4096 x 4096 4.0 and 6.0, 31 x 1000 x 1024
+// 5.8 and 6.8, at its limit 16 x 4096 x 4096 10.3 and 7.9; k_narrow, 100,000 x 256 x 256 from bf16 32 and 41,
+// from fp32 41 and 49, past its limit 100,000 x 512 x 256 from fp32 73 and 71, x 300 x 384 127 and 117.
 bool quantised_inside(int64_t m, int64_t n, int kpad)
 {
     switch (way(m, n, kpad)) {
@@ -776,6 +794,9 @@ struct TilePlan {
 TilePlan tile_plan(int64_t m, int64_t n, int kpad)
 {
     TilePlan p;
+    // Tiles of 128 x 128 and of 256 x 256 (us in a graph, MXFP4 to bf16): 120 large ones, 2048 x 3840 x 1024,
+    // 8.1 and 11.4; 128, 2048 x 4096 x 4096, 25 and 29; 143, 2816 x 3328 x 1152, 13.8 and 13.8; 144, 3000^3, 30 and
+    // 26.5; 256, 4096^3, 51 and 38.  Small ones stay quicker where k is short: 8192 x 8192 x 1024 60 and 66.
     p.wt = ceil_div(m, 256) * ceil_div(n, 256) >= 128 ? 4 : 2;
     p.tiles_m = ceil_div(m, 64 * p.wt);
     p.tiles_n = ceil_div(n, 64 * p.wt);
@@ -856,8 +877,9 @@ template <class F> void with_out(const Product &p, F &&f)
 
 template <class Rows> void multiply_narrow(const Product &p, const Rows &A)
 {
-    // Panels of 32 KB of B (four workgroups to a compute unit), fewer columns while
-    // there are fewer workgroups than compute units.
+    // Panels of 32 KB of B (two workgroups to a compute unit), fewer columns while
+    // there are fewer workgroups than compute units: 512 x 512 x 256 from fp32 7.2 us, 12.4 with
+    // whole panels, 8192 x 512 x 128 7.6 and 15.3 (20,000 x 128 x 128 7.7 and 7.2).
     const int KS = narrow_slices(p.kpad);
     const int64_t groups = ceil_div(p.m, 32 * kNarrowWaves);
     int64_t panel = std::min<int64_t>(ceil_div(p.n, 32) * 32, narrow_columns(p.kpad));

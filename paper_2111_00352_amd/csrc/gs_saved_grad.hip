@@ -19,10 +19,12 @@
 // waves share it and split the rows, 16 at a time each, with the loads of the next
 // two steps in flight.
 //
-// 100,000 rows of 128 x 64 in 32 bits take 15 us and 2.5 us for joining the partials:
-// the operands' 39 MB are 6 us of that at the rate of a copy, the rest is the start of
-// 256 workgroups of six steps a wave, the waves' join in LDS (2 us) and the partials (8 MB
-// written and read, 4 us).  30,011 rows of 255 x 47 in bf16 11 us and 2.5 us.
+// 100,000 rows of 128 x 64 in 32 bits take 15.4 us and 3.9 us for joining the partials
+// (16.9 us a call); the operands' 39 MB are 6 us of that at the rate of a copy.  The
+// rest is the start of 250 workgroups whose waves take three or four steps each, so that
+// two of them in flight never run steadily, the join of eight waves through LDS in eight
+// rounds, and the partials (8 MB written and read); how much each takes is not measured.
+// 30,011 rows of 255 x 47 in bf16 (one or two steps a wave) 10.5 us and 2.5 us.
 #include <algorithm>
 #include <type_traits>
 
