@@ -19,7 +19,8 @@ gradient H^T G (an n-long reduction) is the library's matrix-core kernel; ReLU a
 ``lowbit`` trains with less memory: "saved8" keeps the hidden layer's activations in
 8 bits between forward and backward (and nothing else of them) and takes the second
 layer's weight gradient and the ReLU's mask from those; "mxfp4" also forms the dense
-products H W and G W^T in MXFP4 (weight gradients stay in fp32).
+products H W and G W^T in MXFP4 (weight gradients stay in fp32).  These layers have first
+derivatives only.
 
 Command line (end-to-end timing of one workload):
     python -m paper_2111_00352_amd.gcn --config 2 --epochs 10 [--lowbit saved8|mxfp4]
