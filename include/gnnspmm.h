@@ -411,6 +411,104 @@ int gs_mxfp4_matmul_dense(const void *A, int64_t lda, int a_dtype, int64_t m, co
                           gs_stream s);
 int gs_mxfp4_matmul_workspace(int64_t m, int64_t n, int64_t k, int a_dtype, uint64_t *bytes);
 
+/* ---- norm, products by group, scores and distillation ----
+ *
+ * The operators of a deep layer whose weights depend on a row's type, and of the
+ * head that answers and is trained.  Dense operands are fp32 or bf16 (a gs_dtype)
+ * with any leading dimension >= their width; columns are at most 2^24, rows below
+ * 2^31.  Sums, statistics and partial sums are fp32 or fp64, a result is rounded
+ * once to its type.  Outputs must not overlap inputs except where a call says so.
+ * All calls are deterministic, asynchronous on s and allocate nothing.
+ */
+
+/* Root-mean-square norm of H = X + R (rows x cols of dtype, cols >= 1), H rounded
+ * to its type: r = (mean of a row's H^2 + eps)^(-1/2), Y = H r w.  R may be NULL:
+ * H is then X and is not written, else it goes to H [dev], which may be X or R
+ * itself.  w [dev]: cols numbers of w_dtype, or NULL for ones.  Y goes to Y [dev]
+ * in dtype, or, if `saved` is given, there as gs_save_activation with GS_ACT_NONE
+ * writes it.  rstd [dev]: r of each row.  eps is at least 0. */
+int gs_rms_norm(const void *X, int64_t ldx, const void *R, int64_t ldr, int dtype, int64_t rows, int64_t cols, const void *w,
+                int w_dtype, double eps, void *H, int64_t ldh, void *Y, int64_t ldy, const gs_saved *saved, float *rstd,
+                gs_stream s);
+
+/* Its gradient: with x = H r and u = dY w, dX = dH + r (u - x mean(u x)), the
+ * gradient of X and of R, and dw = sum over rows of dY x (fp32).  dH: the gradient that
+ * reaches H otherwise, or NULL; dX may be dH itself.  dw may be NULL.  work [dev]
+ * holds at least the bytes that gs_rms_norm_grad_workspace reports. */
+int gs_rms_norm_grad_workspace(int64_t rows, int64_t cols, int dtype, uint64_t *bytes);
+int gs_rms_norm_grad(const void *H, int64_t ldh, const float *rstd, const void *dY, int64_t ldy, int dtype, int64_t rows,
+                     int64_t cols, const void *w, int w_dtype, const void *dH, int64_t ldd, void *dX, int64_t ldx, float *dw,
+                     void *work, uint64_t work_bytes, gs_stream s);
+
+/* Products by group on the matrix cores: rows offsets[g] .. offsets[g+1] - 1 of A
+ * belong to group g, 0 <= g < groups <= 65535, offsets [dev] groups + 1 numbers of
+ * offset_bytes (4 or 8) that do not descend.  W [dev]: a k x n matrix of dtype for
+ * each group, leading dimension ldw, w_step >= 0 elements from one to the next (0:
+ * one matrix for all).
+ *   transpose 0: C = A W_g    (A rows x k, C rows x n)
+ *   transpose 1: C = A W_g^T  (A rows x n, C rows x k), the gradient of A
+ * fp32 operands are multiplied in fp32, bf16 ones exactly, both summed in fp32.
+ * C is of c_dtype.  Rows of C that no group has become 0 if fill is not 0, else
+ * they are not written.  Offsets outside 0 .. rows count as the nearer end; where
+ * they descend, rows may be missed or written by several groups, but nothing outside C. */
+int gs_grouped_matmul(const void *A, int64_t lda, int dtype, int64_t rows, const void *W, int64_t ldw, int64_t w_step, int64_t groups,
+                      int64_t k, int64_t n, int transpose, const void *offsets, int offset_bytes, int fill, void *C, int64_t ldc,
+                      int c_dtype, gs_stream s);
+
+/* The same with A in 8 bits (gs_rms_norm, gs_save_activation), whose values are exact in
+ * the product; dtype is W's. */
+int gs_grouped_matmul_saved(const gs_saved *A, const void *W, int dtype, int64_t ldw, int64_t w_step, int64_t groups, int64_t k,
+                            int64_t n, int transpose, const void *offsets, int offset_bytes, int fill, void *C, int64_t ldc,
+                            int c_dtype, gs_stream s);
+
+/* Weight gradients by group: out [dev] groups x a x b fp32, out_g = A_g^T . G_g (zeros for
+ * a group without rows), A rows x a, G rows x b of dtype.  work [dev] holds at
+ * least the bytes that gs_grouped_weight_grad_workspace reports. */
+int gs_grouped_weight_grad_workspace(int64_t rows, int64_t groups, int64_t a, int64_t b, uint64_t *bytes);
+int gs_grouped_weight_grad(const void *A, int64_t lda, const void *G, int64_t ldg, int dtype, int64_t rows, int64_t a, int64_t b,
+                           int64_t groups, const void *offsets, int offset_bytes, float *out, void *work, uint64_t work_bytes,
+                           gs_stream s);
+int gs_grouped_weight_grad_saved(const gs_saved *A, const void *G, int64_t ldg, int dtype, int64_t b, int64_t groups,
+                                 const void *offsets, int offset_bytes, float *out, void *work, uint64_t work_bytes, gs_stream s);
+
+/* Scores of the rows of s (n x v logits of dtype, v >= 1): with m a row's largest
+ * logit and S the sum of exp(s_j - m), log p_j = s_j - m - log S.
+ *   logp     log p of the row's class ids[i] (id_bytes 4 or 8); 0 for a negative id
+ *            (no class), NaN for one of v or more
+ *   entropy  -sum p log p
+ *   stats    m and S (n x 2), 8-byte aligned: what the gradient takes
+ *   top_ids, top_logp  the `top` largest logits' classes (n x top, ties to the
+ *            lower class, NaN above +inf) and their log p; top is at most 128 and v
+ * All [dev] fp32 (top_ids int32); logp (with ids), entropy and stats may be NULL.
+ * Logits of -inf are classes left out; a row of nothing else, or with a NaN or
+ * +inf, has log probabilities and an entropy of NaN. */
+int gs_log_probs(const void *s, int64_t ld, int dtype, int64_t n, int64_t v, const void *ids, int id_bytes, float *logp,
+                 float *entropy, float *stats, int64_t top, int32_t *top_ids, float *top_logp, gs_stream stream);
+
+/* Gradient of dlogp[i] logp[i] + dentropy[i] entropy[i] by the logits, in their type:
+ * dlogp (1 - p) at the given class, else -dlogp p, and -dentropy p (log p + entropy).
+ * Rows without a class take no part in dlogp; dlogp (with ids) and dentropy (with
+ * entropy) may be NULL.  out may be s itself with the same leading dimension. */
+int gs_log_probs_grad(const void *s, int64_t ld, int dtype, int64_t n, int64_t v, const void *ids, int id_bytes, const float *stats,
+                      const float *dlogp, const float *dentropy, const float *entropy, void *out, int64_t ldo, gs_stream stream);
+
+/* Distillation from a teacher's k best classes (1 <= k <= 128): top_ids (n x k of
+ * id_bytes) and top_logits (n x k of t_dtype), logits or log probabilities.  A negative id or a logit of
+ * -inf is no alternative.  With T the temperature (0.001 to 1000), q the softmax of
+ * top_logits / T over a row's alternatives and p that of s / T over all classes,
+ *   loss = T^2 sum q (log q - log p)
+ * and 0 for a row without an alternative; NaN where an id is v or more.  stats (n
+ * x 2): the largest logit and the sum of exp((s_j - m) / T). */
+int gs_distill_loss(const void *s, int64_t ld, int dtype, int64_t n, int64_t v, const void *top_ids, int id_bytes,
+                    const void *top_logits, int t_dtype, int64_t k, double temperature, float *loss, float *stats, gs_stream stream);
+
+/* Its gradient dloss T (p - q) by the logits, in their type; a class that a row's
+ * alternatives name more than once has the sum of their q.  out may be s itself with the same leading
+ * dimension. */
+int gs_distill_grad(const void *s, int64_t ld, int dtype, int64_t n, int64_t v, const void *top_ids, int id_bytes,
+                    const void *top_logits, int t_dtype, int64_t k, double temperature, const float *stats, const float *dloss,
+                    void *out, int64_t ldo, gs_stream stream);
+
 /* Thread-local description of the last error (never NULL). */
 const char *gs_last_error(void);
 

@@ -26,6 +26,8 @@ __all__ = [
     "extract_features", "lib", "library_path", "FEATURE_NAMES", "set_allocator",
     "SavedActivation", "save_activation", "relu_grad", "saved_weight_grad", "SAVED_GRAD_WIDTH",
     "Mxfp4", "mxfp4_quantize", "mxfp4_matmul",
+    "rms_norm", "rms_norm_grad", "grouped_matmul", "grouped_weight_grad",
+    "LogProbs", "log_probs", "log_probs_grad", "distill_loss", "distill_grad", "TOP_MAX",
 ]
 
 _HERE = os.path.dirname(os.path.abspath(__file__))
@@ -157,6 +159,21 @@ def lib() -> ctypes.CDLL:
         "gs_mxfp4_matmul": (c_int, [P(_Mxfp4), P(_Mxfp4), P(_Saved), _p, _i64, c_int, _p, _u64, _p]),
         "gs_mxfp4_matmul_dense": (c_int, [_p, _i64, c_int, _i64, P(_Mxfp4), P(_Saved), _p, _i64, c_int, _p, _u64, _p]),
         "gs_mxfp4_matmul_workspace": (c_int, [_i64, _i64, _i64, c_int, P(_u64)]),
+        "gs_rms_norm": (c_int, [_p, _i64, _p, _i64, c_int, _i64, _i64, _p, c_int, ctypes.c_double, _p, _i64, _p, _i64, P(_Saved), _p,
+                                _p]),
+        "gs_rms_norm_grad_workspace": (c_int, [_i64, _i64, c_int, P(_u64)]),
+        "gs_rms_norm_grad": (c_int, [_p, _i64, _p, _p, _i64, c_int, _i64, _i64, _p, c_int, _p, _i64, _p, _i64, _p, _p, _u64, _p]),
+        "gs_grouped_matmul": (c_int, [_p, _i64, c_int, _i64, _p, _i64, _i64, _i64, _i64, _i64, c_int, _p, c_int, c_int, _p, _i64,
+                                      c_int, _p]),
+        "gs_grouped_matmul_saved": (c_int, [P(_Saved), _p, c_int, _i64, _i64, _i64, _i64, _i64, c_int, _p, c_int, c_int, _p, _i64,
+                                            c_int, _p]),
+        "gs_grouped_weight_grad_workspace": (c_int, [_i64, _i64, _i64, _i64, P(_u64)]),
+        "gs_grouped_weight_grad": (c_int, [_p, _i64, _p, _i64, c_int, _i64, _i64, _i64, _i64, _p, c_int, _p, _p, _u64, _p]),
+        "gs_grouped_weight_grad_saved": (c_int, [P(_Saved), _p, _i64, c_int, _i64, _i64, _p, c_int, _p, _p, _u64, _p]),
+        "gs_log_probs": (c_int, [_p, _i64, c_int, _i64, _i64, _p, c_int, _p, _p, _p, _i64, _p, _p, _p]),
+        "gs_log_probs_grad": (c_int, [_p, _i64, c_int, _i64, _i64, _p, c_int, _p, _p, _p, _p, _p, _i64, _p]),
+        "gs_distill_loss": (c_int, [_p, _i64, c_int, _i64, _i64, _p, c_int, _p, c_int, _i64, ctypes.c_double, _p, _p, _p]),
+        "gs_distill_grad": (c_int, [_p, _i64, c_int, _i64, _i64, _p, c_int, _p, c_int, _i64, ctypes.c_double, _p, _p, _p, _i64, _p]),
         "gs_last_error": (ctypes.c_char_p, []),
         "gs_abi_version": (c_int, []),
     }
@@ -439,9 +456,9 @@ def _dense(X: torch.Tensor, name: str, index: int | None = -1) -> tuple:
     if code is None or X.layout != _STRIDED or len(shape := X.shape) != 2 or (at := X.get_device()) < 0:
         raise ValueError(f"{name} must be a 2-D CUDA float32 or bfloat16 tensor")
     if _tracing() is not None:
-        raise RuntimeError("the low-bit operators cannot be traced: a trace would keep their results as constants")
+        raise RuntimeError("the library's operators cannot be traced: a trace would keep their results as constants")
     if _forward_ad._current_level >= 0 and _forward_ad.unpack_dual(X).tangent is not None:
-        raise RuntimeError("the low-bit operators have no forward-mode derivative")
+        raise RuntimeError("the library's operators have no forward-mode derivative")
     if at != torch._C._cuda_getDevice() or (index != -1 and at != index):
         raise ValueError(f"{name} is not on the current device, or not on the other operand's")
     if X.is_neg():
@@ -466,7 +483,7 @@ class _NoGradient(torch.autograd.Function):
 
     @staticmethod
     def backward(ctx, *_):
-        raise RuntimeError("the low-bit operators have no gradient: detach their operands, or use the layers of gcn")
+        raise RuntimeError("the library's operators have no gradient: detach their operands, or use the layers of gcn and layers")
 
 
 def _result(t: torch.Tensor, X: torch.Tensor) -> torch.Tensor:
@@ -819,3 +836,8 @@ class SelectContext:
         return dict(t_features=st.t_features, t_predict=st.t_predict, t_convert=st.t_convert,
                     chosen=FORMAT_NAMES.get(st.chosen, "?"), feasible_mask=st.feasible_mask,
                     scores={FORMAT_NAMES[i]: st.scores[i] for i in range(len(FORMATS))})
+
+
+from paper_2111_00352_amd.operators import (  # noqa: E402  (they are made of what stands above)
+    TOP_MAX, LogProbs, distill_grad, distill_loss, grouped_matmul, grouped_weight_grad, log_probs, log_probs_grad, rms_norm,
+    rms_norm_grad)

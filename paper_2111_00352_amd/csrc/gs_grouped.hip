@@ -1,0 +1,638 @@
+// Products of rows sorted by group (a node's type, a relation, an expert), each group with a
+// matrix of its own: rows offsets[g] .. offsets[g + 1] - 1 belong to group g.
+//
+//   C = A W_g        gs_grouped_matmul
+//   C = A W_g^T      the same, transposed: the gradient of A
+//   dW_g = A_g^T G_g gs_grouped_weight_grad
+//
+// The offsets stay on the device: a launch has as many workgroups as there can be tiles, and
+// each finds its group and rows itself, from a prefix sum over the groups' tiles that a wave
+// makes with its lanes.
+//
+// All three are one tile kernel.  A tile's operands lie in LDS by rows of 128 bytes along the
+// summed index, 64 elements in bf16, 32 in fp32, so that a lane's fragment of a matrix
+// instruction is 16 bytes there.  Operands whose summed index is not the one that is
+// contiguous in memory are turned on their way through registers.  Activations in the 8 bits
+// of a norm or a saved activation are exact in bf16 and become the product's type there too.
+// fp32 operands are multiplied in fp32 (V_MFMA_F32_32X32X2_F32).
+#include <algorithm>
+#include <type_traits>
+
+#include "gs_rows.h"
+
+namespace gs {
+namespace {
+
+typedef float f32x16 __attribute__((ext_vector_type(16)));
+typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+typedef float f32x4v __attribute__((ext_vector_type(4)));
+
+constexpr int kLine = 128;                                  // bytes of a row of a tile in LDS
+template <class T> constexpr int kChunk = kLine / sizeof(T);  // elements along the summed index
+
+// ------------------------------------------------------------- where a tile is
+
+struct Offsets {
+    const void *p;
+    bool wide;
+    int groups;
+    int64_t rows;
+    __device__ __forceinline__ int64_t at(int g) const
+    {
+        const int64_t o = wide ? ((const int64_t *)p)[g] : ((const int32_t *)p)[g];
+        return o < 0 ? 0 : o < rows ? o : rows;  // (whatever they hold, rows are those there are)
+    }
+};
+
+// Of the segments "rows before the first group" (0), the groups (1 ..) and "rows behind the
+// last" (groups + 1), the one in which the id-th of `per` x ceil(rows / step) items lies.
+struct Segment {
+    int index;        // -1: there are fewer items
+    int64_t r0, r1;   // its rows
+    int64_t local;    // the item's number in it
+    int64_t first;    // number of its first item
+};
+__device__ __forceinline__ int64_t lane_value(int64_t v, int lane)
+{
+    const uint32_t lo = __builtin_amdgcn_readlane((int)(uint32_t)v, lane), hi = __builtin_amdgcn_readlane((int)(v >> 32), lane);
+    return (int64_t)((uint64_t)hi << 32 | lo);
+}
+// ends: whether the segments without a group count.  EMPTY: a group without rows has `per` items too.
+template <bool EMPTY>
+__device__ __forceinline__ Segment find_segment(const Offsets &o, int64_t step, int64_t per, bool ends, int64_t id)
+{
+    int64_t base = 0;
+    for (int j0 = 0; j0 < o.groups + 2; j0 += kWave) {
+        const int j = j0 + lane_id();
+        int64_t r0 = 0, r1 = 0;
+        if (j <= o.groups + 1) {
+            r0 = j == 0 ? 0 : o.at(j - 1);
+            r1 = j == o.groups + 1 ? o.rows : o.at(j);
+            if (r1 < r0) r1 = r0;
+        }
+        const bool group = j >= 1 && j <= o.groups;
+        int64_t items = (r1 - r0 + step - 1) / step;
+        if (EMPTY && items == 0) items = 1;
+        if (!(group || (ends && j <= o.groups + 1))) items = 0;
+        int64_t inc = items * per;
+#pragma unroll
+        for (int d = 1; d < kWave; d <<= 1) {
+            const int64_t up = __shfl_up(inc, d, kWave);
+            if (lane_id() >= d) inc += up;
+        }
+        inc += base;
+        const unsigned long long past = __ballot(inc > id);
+        if (past) {
+            const int l = __ffsll(past) - 1;
+            const int64_t first = lane_value(inc - items * per, l);
+            return {j0 + l, lane_value(r0, l), lane_value(r1, l), id - first, first};
+        }
+        base = lane_value(inc, kWave - 1);
+    }
+    return {-1, 0, 0, 0, 0};
+}
+
+// ------------------------------------------------------------------ operands
+//
+// An operand of a tile: ROWS rows of the tile, chunk by chunk along the summed index k.  256
+// threads load a chunk into registers (load) and put it into LDS (store), where piece p of
+// row r lies at r * 128 + (p ^ r / 2 % 8) * 16: the rows that LDS serves together then spread
+// over its banks.
+
+__device__ __forceinline__ uint8_t *piece_at(uint8_t *lds, int row, int piece)
+{
+    return lds + row * kLine + ((piece ^ (row >> 1 & 7)) << 4);
+}
+
+// k contiguous: element (r, k) at p[r * ld + k].
+template <class T> struct AlongRows {
+    typedef T type;
+    const T *p;
+    int64_t ld;
+    template <int ROWS> struct Held {
+        typename Elems<T, kPiece<T>>::type v[ROWS / 32];
+    };
+    // Rows r0 .. below r1, k from k0 below k1.
+    template <int ROWS> __device__ __forceinline__ void load(Held<ROWS> &h, int64_t r0, int64_t r1, int64_t k0, int64_t k1) const
+    {
+        constexpr int E = kPiece<T>;
+        const int64_t k = k0 + threadIdx.x % 8 * E;
+#pragma unroll
+        for (int i = 0; i < ROWS / 32; i++) {
+            const int64_t r = r0 + threadIdx.x / 8 + 32 * i;
+            h.v[i] = load_elems<T, E>(p + r * ld + k, r < r1 ? k1 - k : 0);
+        }
+    }
+    template <int ROWS> __device__ __forceinline__ void store(const Held<ROWS> &h, uint8_t *lds) const
+    {
+#pragma unroll
+        for (int i = 0; i < ROWS / 32; i++)
+            *reinterpret_cast<u32x4 *>(piece_at(lds, threadIdx.x / 8 + 32 * i, threadIdx.x % 8)) = __builtin_bit_cast(u32x4, h.v[i]);
+    }
+};
+
+// The number of a signed code, and of codes of activations saved by a ReLU.
+struct CodeValue {
+    bool relu;
+    __device__ __forceinline__ float operator()(uint32_t word, int byte) const
+    {
+        const int c = (int)(word >> (8 * byte) & 255);
+        return (float)(relu ? c : (int)(int8_t)c);
+    }
+};
+
+// A row of 8-bit activations, as T.
+template <class T> struct SavedAlongRows {
+    typedef T type;
+    const uint8_t *codes, *scales;
+    int64_t code_pitch, scale_pitch;
+    CodeValue value;
+    template <int ROWS> struct Held {
+        typename Codes<kPiece<T>>::type c[ROWS / 32];
+        uint8_t s[ROWS / 32];
+    };
+    template <int ROWS> __device__ __forceinline__ void load(Held<ROWS> &h, int64_t r0, int64_t r1, int64_t k0, int64_t k1) const
+    {
+        constexpr int E = kPiece<T>;
+        const int64_t k = k0 + threadIdx.x % 8 * E;
+#pragma unroll
+        for (int i = 0; i < ROWS / 32; i++) {
+            const int64_t r = r0 + threadIdx.x / 8 + 32 * i;
+            h.c[i] = {};
+            h.s[i] = 0;
+            if (r < r1 && k < k1) {  // (codes behind the last column are 0)
+                h.c[i] = *reinterpret_cast<const typename Codes<E>::type *>(codes + r * code_pitch + k);
+                h.s[i] = scales[r * scale_pitch + k / kMxBlock];
+            }
+        }
+    }
+    template <int ROWS> __device__ __forceinline__ void store(const Held<ROWS> &h, uint8_t *lds) const
+    {
+        constexpr int E = kPiece<T>;
+#pragma unroll
+        for (int i = 0; i < ROWS / 32; i++) {
+            typename Elems<T, E>::type v;
+            const float s = mx_scale(h.s[i]);
+#pragma unroll
+            for (int e = 0; e < E; e++) v[e] = from_f32<T>(value(code_word<E>(h.c[i], e / 4), e % 4) * s);
+            *reinterpret_cast<u32x4 *>(piece_at(lds, threadIdx.x / 8 + 32 * i, threadIdx.x % 8)) = __builtin_bit_cast(u32x4, v);
+        }
+    }
+};
+
+// 16 bytes of column c of E rows of `N` columns.
+template <class T, int N> __device__ __forceinline__ u32x4 turned(const typename Elems<T, N>::type (&v)[kPiece<T>], int c)
+{
+    typename Elems<T, kPiece<T>>::type o;
+#pragma unroll
+    for (int e = 0; e < kPiece<T>; e++) o[e] = v[e][c];
+    return __builtin_bit_cast(u32x4, o);
+}
+
+// k is the matrix's row: element (r, k) at p[k * ld + r].  A thread takes E neighbouring k of
+// ROWS / 32 neighbouring r.
+template <class T> struct AcrossRows {
+    typedef T type;
+    const T *p;
+    int64_t ld;
+    template <int ROWS> struct Held {
+        typename Elems<T, ROWS / 32>::type v[kPiece<T>];
+    };
+    template <int ROWS> __device__ __forceinline__ void load(Held<ROWS> &h, int64_t r0, int64_t r1, int64_t k0, int64_t k1) const
+    {
+        constexpr int E = kPiece<T>, N = ROWS / 32;
+        const int64_t k = k0 + threadIdx.x % 8 * E, r = r0 + threadIdx.x / 8 * N;
+#pragma unroll
+        for (int e = 0; e < E; e++) h.v[e] = load_elems<T, N>(p + (k + e) * ld + r, k + e < k1 ? r1 - r : 0);
+    }
+    template <int ROWS> __device__ __forceinline__ void store(const Held<ROWS> &h, uint8_t *lds) const
+    {
+        constexpr int N = ROWS / 32;
+#pragma unroll
+        for (int i = 0; i < N; i++)
+            *reinterpret_cast<u32x4 *>(piece_at(lds, threadIdx.x / 8 * N + i, threadIdx.x % 8)) = turned<T, N>(h.v, i);
+    }
+};
+
+// The same from 8-bit activations.
+template <class T> struct SavedAcrossRows {
+    typedef T type;
+    const uint8_t *codes, *scales;
+    int64_t code_pitch, scale_pitch;
+    CodeValue value;
+    template <int N> struct Bytes {
+        typedef std::conditional_t<N == 2, u16, uint32_t> type;
+    };
+    template <int ROWS> struct Held {
+        typename Bytes<ROWS / 32>::type c[kPiece<T>];
+        uint8_t s[kPiece<T>];
+    };
+    template <int ROWS> __device__ __forceinline__ void load(Held<ROWS> &h, int64_t r0, int64_t r1, int64_t k0, int64_t k1) const
+    {
+        constexpr int E = kPiece<T>, N = ROWS / 32;
+        static_assert(N == 2 || N == 4);
+        const int64_t k = k0 + threadIdx.x % 8 * E, r = r0 + threadIdx.x / 8 * N;
+#pragma unroll
+        for (int e = 0; e < E; e++) {
+            h.c[e] = 0;
+            h.s[e] = 0;
+            if (k + e < k1 && r < r1) {
+                h.c[e] = *reinterpret_cast<const typename Bytes<N>::type *>(codes + (k + e) * code_pitch + r);
+                h.s[e] = scales[(k + e) * scale_pitch + r / kMxBlock];
+            }
+        }
+    }
+    template <int ROWS> __device__ __forceinline__ void store(const Held<ROWS> &h, uint8_t *lds) const
+    {
+        constexpr int E = kPiece<T>, N = ROWS / 32;
+#pragma unroll
+        for (int i = 0; i < N; i++) {
+            typename Elems<T, E>::type v;
+#pragma unroll
+            for (int e = 0; e < E; e++) v[e] = from_f32<T>(value(h.c[e], i) * mx_scale(h.s[e]));
+            *reinterpret_cast<u32x4 *>(piece_at(lds, threadIdx.x / 8 * N + i, threadIdx.x % 8)) = __builtin_bit_cast(u32x4, v);
+        }
+    }
+};
+
+// --------------------------------------------------------------------- tile
+
+// c + b a^T over 32 bytes of k of 32 rows of either: a lane holds 16 bytes of row lane % 32.
+// Its sums are columns 8 g + 4 (lane / 32) .. + 3 (register 4 g ..) of A's row lane % 32.
+template <class T> __device__ __forceinline__ f32x16 multiply(u32x4 b, u32x4 a, f32x16 c)
+{
+    if constexpr (sizeof(T) == 2) {
+        return __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, b), __builtin_bit_cast(bf16x8, a), c, 0, 0, 0);
+    } else {
+        const f32x4v x = __builtin_bit_cast(f32x4v, b), y = __builtin_bit_cast(f32x4v, a);
+#pragma unroll
+        for (int i = 0; i < 4; i++) c = __builtin_amdgcn_mfma_f32_32x32x2f32(x[i], y[i], c, 0, 0, 0);
+        return c;
+    }
+}
+
+// The sums of a tile of 64 WT x 64 WT, over k from k0 below k1: waves 2 x 2, each WT x WT
+// times 32 x 32.  Two chunks in LDS, the next one in registers.
+template <class LA, class LB, int WT>
+__device__ __forceinline__ void tile_sums(const LA &A, const LB &B, int64_t a0, int64_t a1, int64_t b0, int64_t b1, int64_t k0,
+                                          int64_t k1, uint8_t *lds, f32x16 (&acc)[WT][WT])
+{
+    using T = typename LA::type;
+    constexpr int ROWS = 64 * WT, STAGE = 2 * ROWS * kLine;
+    const int wave = threadIdx.x / kWave, lane = threadIdx.x % kWave;
+    const int ra = wave / 2 * 32 * WT + lane % 32, rb = wave % 2 * 32 * WT + lane % 32, half = lane / 32;
+    typename LA::template Held<ROWS> ha;
+    typename LB::template Held<ROWS> hb;
+    A.template load<ROWS>(ha, a0, a1, k0, k1);
+    B.template load<ROWS>(hb, b0, b1, k0, k1);
+    A.template store<ROWS>(ha, lds);
+    B.template store<ROWS>(hb, lds + STAGE / 2);
+    __syncthreads();
+    int at = 0;
+    for (int64_t k = k0; k < k1; k += kChunk<T>, at ^= 1) {
+        const bool more = k + kChunk<T> < k1;
+        if (more) {
+            A.template load<ROWS>(ha, a0, a1, k + kChunk<T>, k1);
+            B.template load<ROWS>(hb, b0, b1, k + kChunk<T>, k1);
+        }
+        uint8_t *from = lds + at * STAGE;
+#pragma unroll
+        for (int q = 0; q < 4; q++) {
+            u32x4 fa[WT], fb[WT];
+#pragma unroll
+            for (int i = 0; i < WT; i++) {
+                fa[i] = *reinterpret_cast<const u32x4 *>(piece_at(from, ra + 32 * i, 2 * q + half));
+                fb[i] = *reinterpret_cast<const u32x4 *>(piece_at(from + STAGE / 2, rb + 32 * i, 2 * q + half));
+            }
+#pragma unroll
+            for (int i = 0; i < WT; i++)
+#pragma unroll
+                for (int j = 0; j < WT; j++) acc[i][j] = multiply<T>(fb[j], fa[i], acc[i][j]);
+        }
+        if (more) {
+            A.template store<ROWS>(ha, lds + (at ^ 1) * STAGE);
+            B.template store<ROWS>(hb, lds + (at ^ 1) * STAGE + STAGE / 2);
+        }
+        __syncthreads();
+    }
+}
+
+// Stores a wave's WT x WT sums at (r0, c0), as far as rows are below r1 and columns below c1,
+// through LDS: a lane has four neighbouring columns, a store wants whole lines.
+template <class T, int WT>
+__device__ __forceinline__ void tile_store(const f32x16 (&acc)[WT][WT], uint8_t *lds, T *out, int64_t ld, int64_t r0, int64_t r1,
+                                           int64_t c0, int64_t c1)
+{
+    constexpr int E = kPiece<T>, PITCH = 32 * WT * sizeof(T) + 16, LANES = 32 * WT / E, ROWS = kWave / LANES;
+    const int wave = threadIdx.x / kWave, lane = threadIdx.x % kWave;
+    uint8_t *mine = lds + wave * 32 * PITCH;
+    r0 += wave / 2 * 32 * WT;
+    c0 += wave % 2 * 32 * WT;
+#pragma unroll
+    for (int i = 0; i < WT; i++) {
+#pragma unroll
+        for (int j = 0; j < WT; j++)
+#pragma unroll
+            for (int g = 0; g < 4; g++) {
+                typedef T quad __attribute__((ext_vector_type(4)));
+                const quad v = {from_f32<T>(acc[i][j][4 * g]), from_f32<T>(acc[i][j][4 * g + 1]), from_f32<T>(acc[i][j][4 * g + 2]),
+                                from_f32<T>(acc[i][j][4 * g + 3])};
+                *reinterpret_cast<quad *>(mine + lane % 32 * PITCH + (32 * j + 8 * g + 4 * (lane / 32)) * sizeof(T)) = v;
+            }
+        __syncthreads();
+#pragma unroll
+        for (int q = 0; q < 32 / ROWS; q++) {
+            const int r = ROWS * q + lane / LANES, c = lane % LANES * E;
+            const auto v = *reinterpret_cast<const typename Elems<T, E>::type *>(mine + r * PITCH + c * sizeof(T));
+            const int64_t row = r0 + 32 * i + r;
+            if (row < r1 && c0 + c < c1) store_elems<T, E>(out + row * ld + c0 + c, v, c1 - c0 - c);
+        }
+        __syncthreads();
+    }
+}
+
+template <int WT> constexpr int kTileLds = 2 * 2 * 64 * WT * kLine;
+
+// C's tiles.  Tiles of a group go in blocks of eight along its rows, all of the columns for
+// each, so that operands are met again in a cache.
+template <class LA, class LB, class TO, int WT>
+__global__ __launch_bounds__(256, WT == 1 ? 4 : 2) void k_grouped(LA A, LB W, int64_t w_step, Offsets off, int64_t k, int64_t n, bool fill,
+                                                                  int tiles_n, TO *__restrict__ C, int64_t ldc)
+{
+    __shared__ __align__(1024) uint8_t lds[kTileLds<WT>];
+    constexpr int SIDE = 64 * WT;
+    const Segment s = find_segment<false>(off, SIDE, tiles_n, fill, xcd_tile(blockIdx.x, gridDim.x));
+    if (s.index < 0) return;
+    const int64_t tiles = (s.r1 - s.r0 + SIDE - 1) / SIDE, block = s.local / (8 * tiles_n), rest = s.local - block * 8 * tiles_n;
+    const int64_t high = std::min<int64_t>(8, tiles - block * 8);
+    const int64_t r0 = s.r0 + (block * 8 + rest % high) * SIDE, c0 = rest / high * SIDE;
+    f32x16 acc[WT][WT];
+#pragma unroll
+    for (int i = 0; i < WT; i++)
+#pragma unroll
+        for (int j = 0; j < WT; j++) acc[i][j] = f32x16{};
+    if (s.index >= 1 && s.index <= off.groups) {
+        LB B = W;
+        B.p += (s.index - 1) * w_step;
+        tile_sums<LA, LB, WT>(A, B, r0, s.r1, c0, n, 0, k, lds, acc);
+    }
+    tile_store<TO, WT>(acc, lds, C, ldc, r0, s.r1, c0, n);
+}
+
+// dW: chunks of `per` rows of a group, a tile of it each; out is the chunk's a x b, or the
+// group's if a chunk is all of a group (per past the rows).
+template <class LA, class LG, int WT>
+__global__ __launch_bounds__(256, WT == 1 ? 3 : 2) void k_grouped_grad(LA A, LG G, Offsets off, int64_t a, int64_t b, int64_t per,
+                                                                       int tiles_b, float *__restrict__ out)
+{
+    __shared__ __align__(1024) uint8_t lds[kTileLds<WT>];
+    constexpr int SIDE = 64 * WT;
+    const Segment s = find_segment<true>(off, per, 1, false, blockIdx.x);
+    if (s.index < 0) return;
+    const int64_t k0 = s.r0 + s.local * per, k1 = std::min(k0 + per, s.r1);
+    const int64_t a0 = (int64_t)(blockIdx.y / tiles_b) * SIDE, b0 = (int64_t)(blockIdx.y % tiles_b) * SIDE;
+    f32x16 acc[WT][WT];
+#pragma unroll
+    for (int i = 0; i < WT; i++)
+#pragma unroll
+        for (int j = 0; j < WT; j++) acc[i][j] = f32x16{};
+    tile_sums<LA, LG, WT>(A, G, a0, a, b0, b, k0, k1, lds, acc);
+    tile_store<float, WT>(acc, lds, out + (int64_t)blockIdx.x * a * b, b, a0, a, b0, b);
+}
+// The chunks of a group added in order: 256 threads, four elements each; blockIdx.y the group.
+__global__ __launch_bounds__(256) void k_grouped_join(const float *__restrict__ part, Offsets off, int64_t ab, int64_t per,
+                                                      int64_t all, float *__restrict__ out)
+{
+    // number of the group's first chunk: chunks of the groups before it
+    int64_t first = 0, mine = 1;
+    for (int j0 = 0; j0 <= (int)blockIdx.y; j0 += kWave) {
+        const int j = j0 + lane_id();
+        int64_t chunks = 0;
+        if (j <= (int)blockIdx.y) {
+            const int64_t r0 = off.at(j), r1 = off.at(j + 1);
+            chunks = r1 > r0 ? (r1 - r0 + per - 1) / per : 1;
+        }
+        if ((int)blockIdx.y < j0 + kWave) mine = lane_value(chunks, blockIdx.y - j0);
+        first += (int64_t)wave_sum_u64((unsigned long long)chunks);
+    }
+    first -= mine;
+    const int64_t e = ((int64_t)blockIdx.x * 256 + threadIdx.x) * 4;
+    if (e >= ab) return;
+    float4 s = make_float4(0, 0, 0, 0);
+    const int64_t end = std::min(first + mine, all);  // (offsets that descend: no more than there are)
+    for (int64_t c = first; c < end; c++) {
+        const auto v = load_elems<float, 4>(part + c * ab + e, ab - e);
+        s.x += v[0], s.y += v[1], s.z += v[2], s.w += v[3];
+    }
+    store_elems<float, 4>(out + blockIdx.y * ab + e, typename Elems<float, 4>::type{s.x, s.y, s.z, s.w}, ab - e);
+}
+
+// ------------------------------------------------------------------- launch
+
+Offsets check_offsets(const void *offsets, int bytes, int64_t groups, int64_t rows)
+{
+    if (bytes != 4 && bytes != 8) fail(GS_ERR_INVALID_ARG, "offsets have 4 or 8 bytes");
+    if (groups < 1) fail(GS_ERR_INVALID_ARG, "there must be at least one group");
+    if (groups > 65535) fail(GS_ERR_UNSUPPORTED, "at most 65535 groups");
+    if (rows < 0 || rows > INT32_MAX) fail(GS_ERR_INVALID_ARG, "bad matrix size");
+    if (!offsets) fail(GS_ERR_INVALID_ARG, "offsets are null");
+    if ((uintptr_t)offsets % bytes) fail(GS_ERR_INVALID_ARG, "offsets are not aligned");
+    return {offsets, bytes == 8, (int)groups, rows};
+}
+
+struct Operand {  // dense, or saved
+    const void *p;
+    int64_t ld;
+    const gs_saved *saved;
+};
+
+// Rows of a chunk, and how many chunks there can be: enough workgroups to fill the chip
+// twice, chains of at most 8,192 rows.
+struct GroupedGradPlan {
+    int64_t per, chunks, tiles_a, tiles_b;
+    bool direct;
+    int wt;
+};
+GroupedGradPlan grouped_grad_plan(int64_t rows, int64_t groups, int64_t a, int64_t b)
+{
+    GroupedGradPlan p;
+    p.wt = a <= 64 && b <= 64 ? 1 : 2;
+    p.tiles_a = ceil_div(a, 64 * p.wt);
+    p.tiles_b = ceil_div(b, 64 * p.wt);
+    const int64_t tiles = p.tiles_a * p.tiles_b, want = std::max<int64_t>(1, 1024 / tiles);
+    p.per = std::min<int64_t>(8192, std::max<int64_t>(256, ceil_div(ceil_div(rows, want), 64) * 64));
+    // (what partial sums would take: at most 1 GB of them)
+    const int64_t most = std::max<int64_t>(1, ((int64_t)1 << 28) / (a * b));
+    if (ceil_div(rows, p.per) + groups > most) p.per = ceil_div(ceil_div(rows, std::max<int64_t>(1, most - groups)), 64) * 64;
+    p.direct = rows <= p.per || most <= groups;
+    if (p.direct) p.per = std::max<int64_t>(1, rows);
+    p.chunks = p.direct ? groups : ceil_div(rows, p.per) + groups;
+    return p;
+}
+
+void check_product(int64_t k, int64_t n)
+{
+    if (k < 1 || n < 1) fail(GS_ERR_INVALID_ARG, "bad matrix size");
+    if (k > kMxMaxCols || n > kMxMaxCols) fail(GS_ERR_UNSUPPORTED, "at most 2^24 columns");
+}
+
+}  // namespace
+}  // namespace gs
+
+using namespace gs;
+
+static int grouped_matmul(const Operand &A, int a_dtype, int64_t rows, const void *W, int w_dtype, int64_t ldw, int64_t w_step,
+                          int64_t groups, int64_t k, int64_t n, int transpose, const void *offsets, int offset_bytes, int fill,
+                          void *C, int64_t ldc, int c_dtype, gs_stream stream)
+{
+    return guarded([&] {
+        check_product(k, n);
+        const Offsets off = check_offsets(offsets, offset_bytes, groups, rows);
+        const int wsize = dtype_size(w_dtype), csize = dtype_size(c_dtype);
+        const int64_t in = transpose ? n : k, outw = transpose ? k : n;
+        if (A.saved) {
+            check_saved(A.saved, false);
+            if (A.saved->rows != rows || A.saved->cols != in) fail(GS_ERR_INVALID_ARG, "A has another shape");
+        } else {
+            check_operand("A", A.p, rows, in, A.ld, dtype_size(a_dtype));
+            if (a_dtype != w_dtype) fail(GS_ERR_INVALID_ARG, "A and W have different types");
+        }
+        check_operand("W", W, k, n, ldw, wsize);
+        if (w_step < 0) fail(GS_ERR_INVALID_ARG, "negative step from group to group");
+        if (groups > 1 && w_step > (((int64_t)1 << 62) / wsize - k * ldw) / (groups - 1))
+            fail(GS_ERR_INVALID_ARG, "W: span is not addressable");
+        check_operand("C", C, rows, outw, ldc, csize);
+        if (rows == 0) return;
+        const hipStream_t s = (hipStream_t)stream;
+        const int wt = rows <= 64 * groups || outw <= 64 ? 1 : 2;
+        const int64_t tiles_n = ceil_div(outw, 64 * wt), grid = (ceil_div(rows, 64 * wt) + groups + 2) * tiles_n;
+        if (grid > INT32_MAX / 256) fail(GS_ERR_UNSUPPORTED, "the product has too many tiles");
+        auto go = [&](auto la, auto lb, auto out) {
+            using LA = decltype(la);
+            using LB = decltype(lb);
+            using TO = decltype(out);
+            auto run = [&](auto kernel) {
+                kernel<<<(unsigned)grid, 256, 0, s>>>(la, lb, w_step, off, in, outw, fill != 0, (int)tiles_n, (TO *)C, ldc);
+            };
+            wt == 1 ? run(k_grouped<LA, LB, TO, 1>) : run(k_grouped<LA, LB, TO, 2>);
+        };
+        auto with_out = [&](auto la, auto lb) { c_dtype == GS_F32 ? go(la, lb, 0.0f) : go(la, lb, u16(0)); };
+        auto with_w = [&](auto la, auto type) {
+            using T = decltype(type);
+            transpose ? with_out(la, AlongRows<T>{(const T *)W, ldw}) : with_out(la, AcrossRows<T>{(const T *)W, ldw});
+        };
+        auto with_type = [&](auto type) {
+            using T = decltype(type);
+            if (A.saved)
+                with_w(SavedAlongRows<T>{A.saved->codes, A.saved->scales, saved_code_pitch(in), saved_scale_pitch(in),
+                                         {A.saved->act == GS_ACT_RELU}},
+                       type);
+            else
+                with_w(AlongRows<T>{(const T *)A.p, A.ld}, type);
+        };
+        w_dtype == GS_F32 ? with_type(0.0f) : with_type(u16(0));
+        GS_HIP(hipGetLastError());
+    });
+}
+
+static int grouped_weight_grad(const Operand &A, int a_dtype, int64_t rows, int64_t a, const void *G, int64_t ldg, int dtype, int64_t b,
+                               int64_t groups, const void *offsets, int offset_bytes, float *out, void *work, uint64_t work_bytes,
+                               gs_stream stream)
+{
+    return guarded([&] {
+        check_product(a, b);
+        const Offsets off = check_offsets(offsets, offset_bytes, groups, rows);
+        if (A.saved) {
+            check_saved(A.saved, false);
+            if (A.saved->rows != rows || A.saved->cols != a) fail(GS_ERR_INVALID_ARG, "A has another shape");
+        } else {
+            check_operand("A", A.p, rows, a, A.ld, dtype_size(a_dtype));
+            if (a_dtype != dtype) fail(GS_ERR_INVALID_ARG, "A and G have different types");
+        }
+        check_operand("G", G, rows, b, ldg, dtype_size(dtype));
+        if (!out) fail(GS_ERR_INVALID_ARG, "null output");
+        const GroupedGradPlan p = grouped_grad_plan(rows, groups, a, b);
+        const uint64_t need = p.direct ? 0 : (uint64_t)(p.chunks * a * b) * 4;
+        if (work_bytes < need || (need && !work))
+            fail(GS_ERR_INVALID_ARG, "workspace of %llu bytes is below the %llu needed",
+                 (unsigned long long)(work ? work_bytes : 0), (unsigned long long)need);
+        if (p.tiles_a * p.tiles_b > 65535) fail(GS_ERR_UNSUPPORTED, "the product has too many tiles");
+        const hipStream_t s = (hipStream_t)stream;
+        float *part = p.direct ? out : (float *)work;
+        auto go = [&](auto la, auto lg) {
+            using LA = decltype(la);
+            using LG = decltype(lg);
+            auto run = [&](auto kernel) {
+                kernel<<<dim3((unsigned)p.chunks, (unsigned)(p.tiles_a * p.tiles_b)), 256, 0, s>>>(la, lg, off, a, b, p.per,
+                                                                                                 (int)p.tiles_b, part);
+            };
+            p.wt == 1 ? run(k_grouped_grad<LA, LG, 1>) : run(k_grouped_grad<LA, LG, 2>);
+        };
+        auto with_type = [&](auto type) {
+            using T = decltype(type);
+            const AcrossRows<T> g{(const T *)G, ldg};
+            if (A.saved)
+                go(SavedAcrossRows<T>{A.saved->codes, A.saved->scales, saved_code_pitch(a), saved_scale_pitch(a),
+                                      {A.saved->act == GS_ACT_RELU}},
+                   g);
+            else
+                go(AcrossRows<T>{(const T *)A.p, A.ld}, g);
+        };
+        dtype == GS_F32 ? with_type(0.0f) : with_type(u16(0));
+        GS_HIP(hipGetLastError());
+        if (!p.direct) {
+            k_grouped_join<<<dim3((unsigned)ceil_div(a * b, 1024), (unsigned)groups), 256, 0, s>>>(part, off, a * b, p.per, p.chunks, out);
+            GS_HIP(hipGetLastError());
+        }
+    });
+}
+
+extern "C" {
+
+int gs_grouped_matmul(const void *A, int64_t lda, int dtype, int64_t rows, const void *W, int64_t ldw, int64_t w_step, int64_t groups,
+                      int64_t k, int64_t n, int transpose, const void *offsets, int offset_bytes, int fill, void *C, int64_t ldc,
+                      int c_dtype, gs_stream stream)
+{
+    return grouped_matmul({A, lda, nullptr}, dtype, rows, W, dtype, ldw, w_step, groups, k, n, transpose, offsets, offset_bytes, fill, C,
+                          ldc, c_dtype, stream);
+}
+
+int gs_grouped_matmul_saved(const gs_saved *A, const void *W, int dtype, int64_t ldw, int64_t w_step, int64_t groups, int64_t k,
+                            int64_t n, int transpose, const void *offsets, int offset_bytes, int fill, void *C, int64_t ldc,
+                            int c_dtype, gs_stream stream)
+{
+    if (!A) return guarded([] { fail(GS_ERR_INVALID_ARG, "null saved activations"); });
+    return grouped_matmul({nullptr, 0, A}, dtype, A->rows, W, dtype, ldw, w_step, groups, k, n, transpose, offsets, offset_bytes, fill,
+                          C, ldc, c_dtype, stream);
+}
+
+int gs_grouped_weight_grad_workspace(int64_t rows, int64_t groups, int64_t a, int64_t b, uint64_t *bytes)
+{
+    return guarded([&] {
+        if (!bytes) fail(GS_ERR_INVALID_ARG, "null output");
+        check_product(a, b);
+        if (rows < 0 || rows > INT32_MAX || groups < 1) fail(GS_ERR_INVALID_ARG, "bad matrix size");
+        if (groups > 65535) fail(GS_ERR_UNSUPPORTED, "at most 65535 groups");
+        const GroupedGradPlan p = grouped_grad_plan(rows, groups, a, b);
+        *bytes = p.direct ? 0 : (uint64_t)(p.chunks * a * b) * 4;
+    });
+}
+
+int gs_grouped_weight_grad(const void *A, int64_t lda, const void *G, int64_t ldg, int dtype, int64_t rows, int64_t a, int64_t b,
+                           int64_t groups, const void *offsets, int offset_bytes, float *out, void *work, uint64_t work_bytes,
+                           gs_stream stream)
+{
+    return grouped_weight_grad({A, lda, nullptr}, dtype, rows, a, G, ldg, dtype, b, groups, offsets, offset_bytes, out, work, work_bytes,
+                               stream);
+}
+
+int gs_grouped_weight_grad_saved(const gs_saved *A, const void *G, int64_t ldg, int dtype, int64_t b, int64_t groups,
+                                 const void *offsets, int offset_bytes, float *out, void *work, uint64_t work_bytes, gs_stream stream)
+{
+    if (!A) return guarded([] { fail(GS_ERR_INVALID_ARG, "null saved activations"); });
+    return grouped_weight_grad({nullptr, 0, A}, dtype, A->rows, A->cols, G, ldg, dtype, b, groups, offsets, offset_bytes, out, work,
+                               work_bytes, stream);
+}
+
+}  // extern "C"

@@ -6,6 +6,8 @@
 #include <hip/hip_runtime.h>
 
 #include <cstdint>
+#include <initializer_list>
+#include <utility>
 
 #include "gs_internal.h"
 
@@ -27,6 +29,8 @@ void check_operand(const char *name, const void *p, int64_t rows, int64_t cols, 
 void check_saved(const gs_saved *A, bool relu_only);
 void check_mxfp4(const gs_mxfp4 *A);
 int dtype_size(int dtype);  // bytes of a gs_dtype, throws for others
+// Whether a call that moves `bytes` goes past the caches; operands with their leading dimensions.
+bool streams(double bytes, int64_t cols, int size, std::initializer_list<std::pair<const void *, int64_t>> operands);
 
 // --------------------------------------------------------------- scale bytes
 
@@ -123,6 +127,65 @@ __device__ __forceinline__ void store_elems(T *p, typename Elems<T, E>::type v, 
         if (n & 2) *reinterpret_cast<typename Elems<T, 2>::type *>(p + (n & 4)) = q2;
         if (n & 1) p[n & 6] = E == 8 && n & 4 ? high : low;
     }
+}
+
+// ------------------------------------------------------------------ 8-bit codes
+
+// Codes of E neighbouring elements.
+template <int E> struct Codes;
+template <> struct Codes<4> {
+    typedef uint32_t type;
+};
+template <> struct Codes<8> {
+    typedef uint2 type;
+};
+template <int E> __device__ __forceinline__ uint32_t code_word(const typename Codes<E>::type &c, int w)
+{
+    if constexpr (E == 4)
+        return c;
+    else
+        return w ? c.y : c.x;
+}
+template <int E> __device__ __forceinline__ typename Codes<E>::type code_words(const uint32_t *w)
+{
+    if constexpr (E == 4)
+        return w[0];
+    else
+        return make_uint2(w[0], w[1]);
+}
+
+// 1.5 * 2^23: the sum with a number below 2^22 is rounded to a whole one, whose low bits
+// are those of the sum.
+constexpr float kWhole = 12582912.0f;
+
+// Signed codes of E elements of a block of 32, whose other elements the neighbouring lanes
+// (an aligned group of 32 / E) hold, and the block's scale byte.
+template <int E> struct Saved8 {
+    typename Codes<E>::type codes;
+    uint8_t scale;
+};
+template <int E> __device__ __forceinline__ Saved8<E> save8_signed(const float (&y)[E])
+{
+    uint32_t m = 0;
+#pragma unroll
+    for (int e = 0; e < E; e++) {
+        const uint32_t b = __float_as_uint(y[e]) & 0x7fffffffu;
+        m = b > m ? b : m;
+    }
+    const int k = (int)(group_max<kMxBlock / E>(m) >> 23);
+    const int E8 = k == 255 ? 255 : k > 7 ? k - 6 : 1;
+    const float inv = mx_inverse(E8);
+    uint32_t w[E / 4];
+#pragma unroll
+    for (int q = 0; q < E / 4; q++) {
+        uint32_t c[4];
+#pragma unroll
+        for (int e = 0; e < 4; e++)
+            c[e] = __float_as_uint(__builtin_amdgcn_fmed3f(__builtin_fmaf(y[4 * q + e], inv, kWhole), kWhole - 127, kWhole + 127));
+        w[q] = __builtin_amdgcn_perm(c[1], c[0], 0x0c0c0400) | __builtin_amdgcn_perm(c[3], c[2], 0x04000c0c);
+        if (E8 == 255) w[q] = 0;
+    }
+    return {code_words<E>(w), (uint8_t)E8};
 }
 
 // ------------------------------------------------------------- block walk

@@ -1,0 +1,150 @@
+// Rows of a dense matrix held by groups of lanes: how many lanes and 16-byte pieces a row
+// takes, sums and maxima over a group, and tensors whose type a call names.
+#pragma once
+
+#include <hip/hip_runtime.h>
+
+#include <cstdint>
+#include <type_traits>
+
+#include "gs_device.h"
+#include "gs_lowbit.h"
+
+namespace gs {
+
+// Elements of 16 bytes.
+template <class T> constexpr int kPiece = sizeof(T) == 4 ? 4 : 8;
+
+// ------------------------------------------------------- sums over lanes
+
+template <int CTRL> __device__ __forceinline__ uint32_t dpp32(uint32_t v)
+{
+    return (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, CTRL, 0xf, 0xf, true);
+}
+template <int CTRL> __device__ __forceinline__ float dpp(float v) { return __uint_as_float(dpp32<CTRL>(__float_as_uint(v))); }
+template <int CTRL> __device__ __forceinline__ double dpp(double v)
+{
+    const uint64_t b = __double_as_longlong(v);
+    return __longlong_as_double((long long)((uint64_t)dpp32<CTRL>((uint32_t)(b >> 32)) << 32 | dpp32<CTRL>((uint32_t)b)));
+}
+
+// v of the two halves of the wave (of neighbouring rows of 16 lanes), both in every lane.
+template <class V> struct Both {
+    V low, high;
+};
+__device__ __forceinline__ Both<float> halves(float v)
+{
+    const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+    return {__uint_as_float(r[0]), __uint_as_float(r[1])};
+}
+__device__ __forceinline__ Both<float> rows16(float v)
+{
+    const auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+    return {__uint_as_float(r[0]), __uint_as_float(r[1])};
+}
+template <class F> __device__ __forceinline__ Both<double> both64(double v, F &&swap)
+{
+    const uint64_t b = __double_as_longlong(v);
+    const Both<float> lo = swap(__uint_as_float((uint32_t)b)), hi = swap(__uint_as_float((uint32_t)(b >> 32)));
+    auto join = [](float h, float l) {
+        return __longlong_as_double((long long)((uint64_t)__float_as_uint(h) << 32 | __float_as_uint(l)));
+    };
+    return {join(hi.low, lo.low), join(hi.high, lo.high)};
+}
+__device__ __forceinline__ Both<double> halves(double v) { return both64(v, [](float x) { return halves(x); }); }
+__device__ __forceinline__ Both<double> rows16(double v) { return both64(v, [](float x) { return rows16(x); }); }
+
+// op over aligned groups of L lanes (a power of two up to 64), the same bits in each of
+// them: every step combines two lanes' values, and op is commutative.
+template <int L, class V, class Op> __device__ __forceinline__ V group_fold(V v, Op &&op)
+{
+    if constexpr (L > 1) v = op(v, dpp<0xB1>(v));    // lanes 1 0 3 2
+    if constexpr (L > 2) v = op(v, dpp<0x4E>(v));    // lanes 2 3 0 1
+    if constexpr (L > 4) v = op(v, dpp<0x141>(v));   // lanes 7 .. 0
+    if constexpr (L > 8) v = op(v, dpp<0x140>(v));   // lanes 15 .. 0
+    if constexpr (L > 16) {
+        const Both<V> b = rows16(v);
+        v = op(b.low, b.high);
+    }
+    if constexpr (L > 32) {
+        const Both<V> b = halves(v);
+        v = op(b.low, b.high);
+    }
+    return v;
+}
+// The same for whole numbers.
+template <int L, class Op> __device__ __forceinline__ uint32_t group_fold_u(uint32_t v, Op &&op)
+{
+    return __float_as_uint(group_fold<L>(__uint_as_float(v), [&](float a, float b) {
+        return __uint_as_float(op(__float_as_uint(a), __float_as_uint(b)));
+    }));
+}
+template <int L, class V> __device__ __forceinline__ V group_sum(V v)
+{
+    return group_fold<L>(v, [](V a, V b) { return a + b; });
+}
+
+// The same over a row that L lanes hold, or all waves of a workgroup of L > 64 threads: tmp is
+// L / 64 values in LDS; ends with a barrier then.
+template <int L, class V, class Op> __device__ __forceinline__ V row_fold(V v, V *tmp, Op &&op)
+{
+    if constexpr (L <= kWave) {
+        return group_fold<L>(v, op);
+    } else {
+        v = group_fold<kWave>(v, op);
+        if (threadIdx.x % kWave == 0) tmp[threadIdx.x / kWave] = v;
+        __syncthreads();
+        V t = tmp[0];
+#pragma unroll
+        for (int w = 1; w < L / kWave; w++) t = op(t, tmp[w]);
+        __syncthreads();
+        return t;
+    }
+}
+template <int L, class V> __device__ __forceinline__ V row_sum(V v, V *tmp)
+{
+    return row_fold<L>(v, tmp, [](V a, V b) { return a + b; });
+}
+
+// -------------------------------------------------------------- held rows
+
+constexpr int kRowThreads = 256;
+
+// A row is held by L lanes (a wave's, or all of a workgroup's), R pieces of 16 bytes in each.
+// Neighbouring lanes hold neighbouring pieces.
+template <class T, int L, int R> struct RowAt {
+    static constexpr int E = kPiece<T>;
+    static constexpr int kRows = L <= kRowThreads ? kRowThreads / L : 1;  // of a workgroup
+    static constexpr int kThreads = L <= kRowThreads ? kRowThreads : L;
+    __device__ __forceinline__ static int lane() { return threadIdx.x % L; }
+    __device__ __forceinline__ static int64_t first_row() { return (int64_t)blockIdx.x * kRows + threadIdx.x / L; }
+    __device__ __forceinline__ static int64_t row_step() { return (int64_t)gridDim.x * kRows; }
+    __device__ __forceinline__ static int col(int i) { return (i * L + lane()) * E; }
+};
+
+// (L, R) that hold a row of `pieces` 16-byte pieces; go(L, R) as integral constants.  False:
+// the row is wider than any holds.
+template <class Go> bool with_row(int64_t pieces, Go &&go)
+{
+    auto is = [&](auto l, auto r) {
+        if (pieces > (int64_t)decltype(l)::value * decltype(r)::value) return false;
+        go(l, r);
+        return true;
+    };
+    using std::integral_constant;
+    integral_constant<int, 8> l8;
+    integral_constant<int, 64> l64;
+    integral_constant<int, 256> l256;
+    return is(l8, integral_constant<int, 1>{}) || is(l8, integral_constant<int, 2>{}) || is(l8, integral_constant<int, 3>{}) ||
+           is(l8, integral_constant<int, 4>{}) || is(l8, integral_constant<int, 6>{}) || is(l8, integral_constant<int, 8>{}) ||
+           is(l64, integral_constant<int, 2>{}) || is(l64, integral_constant<int, 4>{}) || is(l64, integral_constant<int, 8>{}) ||
+           is(l256, integral_constant<int, 4>{}) || is(l256, integral_constant<int, 8>{});
+}
+
+// Element i of an fp32 or bf16 array (wide: fp32).
+__device__ __forceinline__ float load_either(const void *p, bool wide, int64_t i)
+{
+    return wide ? ((const float *)p)[i] : to_f32(((const u16 *)p)[i]);
+}
+
+}  // namespace gs

@@ -64,32 +64,24 @@ void check_mxfp4(const gs_mxfp4 *A)
         fail(GS_ERR_INVALID_ARG, "MXFP4 codes are not 16-byte or scales not 4-byte aligned");
 }
 
+// Whether a call streams past the caches: when what it moves is more than the
+// memory-side cache holds for its next reader, and rows are whole 16-byte pieces
+// (others share lines between accesses).  Saving and reading back n x 128 fp32:
+// 100,000 rows 30.5 us in the caches, 32.0 us past them; 200,000 68.4 and 61.8;
+// 2,000,000 631 and 530.
+static constexpr double kStreamBytes = 200e6;
+bool streams(double bytes, int64_t cols, int size, std::initializer_list<std::pair<const void *, int64_t>> operands)
+{
+    if (bytes < kStreamBytes || cols * size % 16) return false;
+    for (const auto &[p, ld] : operands)
+        if ((uintptr_t)p % 16 || ld * size % 16) return false;
+    return true;
+}
+
 namespace {
 
 // Lanes of a block: 16 bytes of the dense operand each.
 template <class T> constexpr int kUnitElems = sizeof(T) == 4 ? 4 : 8;
-
-template <int E> struct Codes;
-template <> struct Codes<4> {
-    typedef uint32_t type;
-};
-template <> struct Codes<8> {
-    typedef uint2 type;
-};
-template <int E> __device__ __forceinline__ uint32_t code_word(const typename Codes<E>::type &c, int w)
-{
-    if constexpr (E == 4)
-        return c;
-    else
-        return w ? c.y : c.x;
-}
-template <int E> __device__ __forceinline__ typename Codes<E>::type code_words(const uint32_t *w)
-{
-    if constexpr (E == 4)
-        return w[0];
-    else
-        return make_uint2(w[0], w[1]);
-}
 
 // For each of this thread's units load(i, unit, row, first column, columns left in
 // the row from there), i the round, then use(...) likewise.
@@ -117,10 +109,6 @@ __device__ __forceinline__ void walk_units(int64_t units, const BlockDiv &div, i
         }
     }
 }
-
-// 1.5 * 2^23: the sum with a number below 2^22 is rounded to a whole one, whose low bits
-// are those of the sum.
-constexpr float kWhole = 12582912.0f;
 
 template <class T, bool RELU, bool NT>
 __global__ __launch_bounds__(kUnitThreads) void k_save(const T *__restrict__ P, int64_t ldp, int64_t cols,
@@ -228,20 +216,6 @@ __global__ __launch_bounds__(kUnitThreads) void k_saved_values(const uint8_t *__
             }
             if (left > 0) store_elems<T, E, NT>(out + row * ld + col, o, left);
         });
-}
-
-// Whether a call streams past the caches: when what it moves is more than the
-// memory-side cache holds for its next reader, and rows are whole 16-byte pieces
-// (others share lines between accesses).  Saving and reading back n x 128 fp32:
-// 100,000 rows 30.5 us in the caches, 32.0 us past them; 200,000 68.4 and 61.8;
-// 2,000,000 631 and 530.
-constexpr double kStreamBytes = 200e6;
-bool streams(double bytes, int64_t cols, int size, std::initializer_list<std::pair<const void *, int64_t>> operands)
-{
-    if (bytes < kStreamBytes || cols * size % 16) return false;
-    for (const auto &[p, ld] : operands)
-        if ((uintptr_t)p % 16 || ld * size % 16) return false;
-    return true;
 }
 
 }  // namespace

@@ -1,0 +1,446 @@
+"""GPU parity of the norm, the products by group, the scores and the distillation against
+the fp64 formulas in oracle/operators.py.
+
+U = 2^-24 is half a step of fp32.  Bounds count roundings: a product or a sum of c terms one
+after another is off by at most (c + 1) U of its terms' magnitudes (matrix instructions may
+round twice a term), exp(x) by (2|x| + 4) U of its value (its argument is scaled and
+rounded), a logarithm by 4 U of its value, and an output by half a step of its own type.  The
+exponential's instruction gives 0 for what is below 2^-126, the smallest normal number: a
+probability p = exp(x) / S <= exp(x) may come out smaller by as much, so FLUSH = 2^-126 goes with it.
+"""
+import numpy as np
+import pytest
+import torch
+
+import paper_2111_00352_amd as gs
+from oracle import lowbit
+from oracle import operators as oracle
+
+pytestmark = pytest.mark.gpu
+
+U = 2.0 ** -24
+FLUSH = 2.0 ** -126
+DEV = "cuda"
+TYPES = {"f32": torch.float32, "bf16": torch.bfloat16}
+HALF = {"f32": U, "bf16": 2.0 ** -8}
+
+
+def _np(t):
+    return t.detach().cpu().double().numpy()
+
+
+def _inside(t, left=1, right=2, above=1):
+    """t as a view into a larger tensor full of NaN, at an odd element offset, and the larger one."""
+    wide = torch.full((t.shape[0] + 2 * above, t.shape[1] + left + right), float("nan"), dtype=t.dtype, device=DEV)
+    view = wide[above:above + t.shape[0], left:left + t.shape[1]]
+    view.copy_(t)
+    return view, wide
+
+
+def _around_is_nan(view, wide):
+    keep = view.clone()
+    view.fill_(float("nan"))
+    ok = bool(wide.isnan().all())
+    view.copy_(keep)
+    return ok
+
+
+def _close(got, want, tol, what=""):
+    got = _np(got) if isinstance(got, torch.Tensor) else got
+    assert got.shape == want.shape, what
+    assert np.array_equal(np.isnan(got), np.isnan(want)), what
+    inf = np.isinf(want)
+    assert np.array_equal(got[inf], want[inf]), what
+    ok = np.isfinite(want)
+    err = np.abs(got - want)[ok]
+    tol = np.broadcast_to(tol, want.shape)[ok] + 2.0 ** -140
+    bad = err > tol
+    assert not bad.any(), f"{what}: {bad.sum()} of {bad.size} off, worst {np.max(err / tol):.3g} of the bound"
+
+
+def _hidden(n, a, seed, dtype):
+    rng = np.random.default_rng(seed)
+    x = rng.standard_normal((n, a)) * np.exp(rng.standard_normal((n, 1)))
+    if n > 3:
+        x[1] = 0.0
+        x[2] *= 1e-18
+        x[3] *= 1e17
+    return torch.from_numpy(x.astype(np.float32)).to(TYPES[dtype])
+
+
+# ------------------------------------------------------------------------ norm
+
+NORM_SHAPES = [(1, 1), (5, 1), (70, 31), (33, 32), (17, 33), (300, 64), (41, 100), (65, 129), (37, 257), (9, 500), (7, 1000),
+               (6, 2047), (5, 4100), (5, 9001), (4, 20011)]
+
+
+@pytest.mark.parametrize("n,a", NORM_SHAPES)
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("residual", [False, True])
+def test_rms_norm(n, a, dtype, residual):
+    rng = np.random.default_rng(n + a)
+    X, wide = _inside(_hidden(n, a, 3 * a + n, dtype).to(DEV))
+    R = _inside(_hidden(n, a, 3 * a + n + 1, dtype).to(DEV), left=2, right=1)[0] if residual else None
+    w = torch.from_numpy((1 + 0.3 * rng.standard_normal(a)).astype(np.float32)).to(DEV)
+    if a % 2:
+        w = w.bfloat16()
+    Y, H, r = gs.rms_norm(X, w, R, eps=1e-5)
+    if residual:
+        assert torch.equal(H, (X.float() + R.float()).to(X.dtype))
+    else:
+        assert H is X
+    want, wr = oracle.rms_norm(_np(H), _np(w), 1e-5)
+    _close(r, wr, 2 * U * wr, "rstd")
+    _close(Y, want, (4 * U + HALF[dtype]) * np.abs(want), "Y")
+    assert _around_is_nan(X, wide)
+    S, H2, r2 = gs.rms_norm(X, w, R, eps=1e-5, save=True)
+    assert torch.equal(r, r2) and torch.equal(H, H2) and S.act == "none" and S.shape == (n, a)
+    if dtype == "f32":  # the same numbers, into 8 bits by the format's rule
+        q, E, v, _, _ = lowbit.save8(_np(Y), False)
+        assert np.array_equal(_np(S.codes.view(torch.int8)[:, :a]), q) and np.array_equal(_np(S.scales), E)
+        assert np.array_equal(_np(S.dequantize()), v)
+    else:
+        m = np.abs(want)
+        top = np.stack([m[:, c:c + 32].max(1) for c in range(0, a, 32)], 1).repeat(32, 1)[:, :a]
+        step = np.exp2(np.maximum(np.floor(np.log2(np.maximum(top, 1e-300))) - 6, -126))
+        _close(S.dequantize(), want, step * np.where(m > 127 * step, 1.0, 0.5) + 8 * U * m + 1e-5 * step, "8 bits")
+    assert (S.codes[:, a:] == 0).all()  # columns behind the last
+
+
+def test_rms_norm_of_extremes():
+    X = torch.zeros(6, 40)
+    X[0] = 1e30
+    X[1] = 1e-30
+    X[2] = 2.0 ** -140
+    X[3, 5] = float("inf")
+    X[4, 7] = float("nan")
+    Y, _, r = gs.rms_norm(X.to(DEV), eps=0.0)
+    want = 1 / np.sqrt((_np(X) ** 2).mean(1))
+    _close(r[:2], want[:2], 2 * U * want[:2])
+    assert torch.isinf(r[2]) and r[3] == 0 and torch.isnan(r[4]) and torch.isinf(r[5])  # 2^140 is past fp32
+    _close(Y[:2], np.ones((2, 40)), 6 * U)
+    assert torch.isnan(Y[4]).all() and torch.isnan(Y[5]).all() and torch.isnan(Y[3, 5]) and (Y[3, :5] == 0).all()
+    S, _, _ = gs.rms_norm(X.to(DEV), eps=0.0, save=True)
+    v = S.dequantize()
+    assert torch.isnan(v[4]).all() and torch.isnan(v[3, :32]).all() and (v[3, 32:] == 0).all()
+    assert gs.rms_norm(torch.zeros(0, 7, device=DEV))[0].shape == (0, 7)
+
+
+@pytest.mark.parametrize("n,a", NORM_SHAPES + [(3000, 48), (1, 6000)])
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("other", [False, True])
+def test_rms_norm_grad(n, a, dtype, other):
+    rng = np.random.default_rng(n + 7 * a)
+    H = _inside(_hidden(n, a, a + n, dtype).to(DEV))[0]
+    dY, wide = _inside(_hidden(n, a, a + n + 1, dtype).to(DEV), left=3)
+    dH = _inside(_hidden(n, a, a + n + 2, dtype).to(DEV), left=2, right=1)[0] if other else None
+    w = torch.from_numpy((1 + 0.3 * rng.standard_normal(a)).astype(np.float32)).to(DEV)
+    r = gs.rms_norm(H, w, eps=1e-5)[2]
+    dX, dw = gs.rms_norm_grad(H, r, dY, w, dH)
+    want, wdw, size, dsize = oracle.rms_norm_grad(_np(H), _np(r), _np(dY), _np(w), None if dH is None else _np(dH))
+    # a lane adds at most 64 products (or 20 folds of 64), its row's lanes 10 pairs
+    _close(dX, want, 110 * U * size + HALF[dtype] * np.abs(want), "dX")
+    _close(dw, wdw, (n + 20) * U * dsize, "dw")
+    assert _around_is_nan(dY, wide)
+    dX2, none = gs.rms_norm_grad(H, r, dY, None, dH)
+    assert none is None
+    want = oracle.rms_norm_grad(_np(H), _np(r), _np(dY), np.ones(a), None if dH is None else _np(dH))
+    _close(dX2, want[0], 110 * U * want[2] + HALF[dtype] * np.abs(want[0]), "without weight")
+
+
+def test_rms_norm_grad_is_the_norms_derivative():
+    """Central differences of the fp64 formula, whose own gradient the kernel is held to above."""
+    rng = np.random.default_rng(5)
+    H, w, dY = rng.standard_normal((3, 7)), rng.standard_normal(7), rng.standard_normal((3, 7))
+    r = oracle.rms_norm(H, w, 1e-3)[1]
+    dX, dw, _, _ = oracle.rms_norm_grad(H, r, dY, w)
+    h = 1e-6
+    for i in range(3):
+        for j in range(7):
+            P = [H.copy(), H.copy()]
+            P[0][i, j] += h
+            P[1][i, j] -= h
+            d = ((oracle.rms_norm(P[0], w, 1e-3)[0] - oracle.rms_norm(P[1], w, 1e-3)[0]) * dY).sum() / (2 * h)
+            assert abs(d - dX[i, j]) < 1e-7
+    Ht, wt, dYt = (torch.from_numpy(a.astype(np.float32)).to(DEV) for a in (H, w, dY))
+    rt = gs.rms_norm(Ht, wt, eps=1e-3)[2]
+    got = gs.rms_norm_grad(Ht, rt, dYt, wt)
+    # the inputs were rounded to fp32, which moves results by some U of their terms
+    _close(got[0], dX, 60 * U * 20, "dX")
+    _close(got[1], dw, 60 * U * 20, "dw")
+
+
+# ----------------------------------------------------------- products by group
+
+GROUPED = [  # rows, k, n, offsets
+    (1, 1, 1, [0, 1]), (3, 5, 7, [0, 0, 2, 2, 3]), (65, 33, 31, [0, 64, 65]), (200, 47, 255, [0, 1, 130, 130, 200]),
+    (130, 128, 128, [0, 130]), (300, 64, 100, [7, 100, 100, 290]), (16, 300, 200, list(range(17))),
+    (5, 1000, 33, [0, 2, 5]), (520, 96, 72, [0, 256, 512, 520]), (40, 17, 300, [40, 40, 40]), (700, 129, 257, [0] * 70 + [350] * 30 + [700])]
+
+
+def _grouped_inputs(rows, k, n, offsets, dtype, seed, back):
+    A = _hidden(rows, n if back else k, seed, dtype).clamp(-1e6, 1e6)
+    rng = np.random.default_rng(seed + 1)
+    W = torch.from_numpy(rng.standard_normal((len(offsets) - 1, k, n)).astype(np.float32)).to(TYPES[dtype]).to(DEV)
+    return A, W
+
+
+@pytest.mark.parametrize("rows,k,n,offsets", GROUPED)
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("back", [False, True])
+@pytest.mark.parametrize("a8", [False, True])
+def test_grouped_matmul(rows, k, n, offsets, dtype, back, a8):
+    A, W = _grouped_inputs(rows, k, n, offsets, dtype, rows + k, back)
+    off = torch.tensor(offsets, dtype=torch.int64 if k % 2 else torch.int32, device=DEV)
+    if a8:
+        Ad = gs.save_activation(A.to(DEV), "relu" if n % 2 else "none")[1]
+        Av = _np(Ad.dequantize())
+    else:
+        Ad, wide = _inside(A.to(DEV))
+        Av = _np(A)
+    want, M = oracle.grouped(Av, _np(W), offsets, back)
+    got = gs.grouped_matmul(Ad, W, off, transpose=back)
+    assert got.dtype == W.dtype
+    c = 2 * (n if back else k) + 4
+    _close(got, want, c * U * M + HALF[dtype] * np.abs(want))
+    other = torch.float32 if dtype == "bf16" else torch.bfloat16
+    _close(gs.grouped_matmul(Ad, W, off, transpose=back, dtype=other), want, c * U * M + HALF["f32" if dtype == "bf16" else "bf16"] * np.abs(want))
+    # into rows of a larger matrix, around which and in whose rows without a group nothing changes
+    out, wide_out = _inside(torch.full(want.shape, float("nan"), device=DEV).to(W.dtype), left=3)
+    # W with rows and matrices further apart than their sizes
+    Wv = torch.full((W.shape[0], k + 2, n + 3), float("nan"), dtype=W.dtype, device=DEV)[:, 1:1 + k, 2:2 + n]
+    Wv.copy_(W)
+    assert gs.grouped_matmul(Ad, Wv, off, transpose=back, out=out) is out
+    inner = np.zeros(rows, dtype=bool)
+    inner[offsets[0]:offsets[-1]] = True
+    assert torch.isnan(out[torch.from_numpy(~inner).to(DEV)]).all()
+    assert torch.equal(out[torch.from_numpy(inner).to(DEV)], got[torch.from_numpy(inner).to(DEV)])
+    assert _around_is_nan(out, wide_out)
+
+
+@pytest.mark.parametrize("rows,k,n,offsets", GROUPED + [(9000, 40, 24, [0, 3000, 3000, 8999, 9000]), (20000, 33, 65, [0, 20000])])
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("a8", [False, True])
+def test_grouped_weight_grad(rows, k, n, offsets, dtype, a8):
+    A = _hidden(rows, k, rows + k, dtype).clamp(-1e6, 1e6)
+    G, _ = _inside(_hidden(rows, n, rows + k + 1, dtype).clamp(-1e6, 1e6).to(DEV), left=3)
+    off = torch.tensor(offsets, dtype=torch.int32 if k % 2 else torch.int64, device=DEV)
+    if a8:
+        Ad = gs.save_activation(A.to(DEV), "none" if n % 2 else "relu")[1]
+        Av = _np(Ad.dequantize())
+    else:
+        Ad, Av = _inside(A.to(DEV))[0], _np(A)
+    want, M = oracle.grouped_grad(Av, _np(G), offsets)
+    got = gs.grouped_weight_grad(Ad, G, off)
+    assert got.dtype == torch.float32
+    longest = max(b - a for a, b in zip(offsets, offsets[1:]))
+    _close(got, want, (2 * longest + 4) * U * M)
+    assert torch.equal(got, gs.grouped_weight_grad(Ad, G, off))
+
+
+def test_grouped_rows_without_a_group_may_hold_anything():
+    A = torch.full((100, 40), float("nan"), device=DEV)
+    A[10:30] = 1.0
+    W = torch.ones(2, 40, 24, device=DEV)
+    off = torch.tensor([10, 20, 30], device=DEV)
+    C = gs.grouped_matmul(A, W, off)
+    assert (C[10:30] == 40).all() and (C[:10] == 0).all() and (C[30:] == 0).all()
+    G = torch.full((100, 8), float("inf"), device=DEV)
+    G[10:30] = 2.0
+    assert (gs.grouped_weight_grad(A, G, off) == 20).all()
+
+
+def test_grouped_offsets_that_do_not_fit_stay_inside():
+    """Offsets past the rows count as the end; descending ones give some of the rows twice or not at all."""
+    A, W = torch.ones(64, 16, device=DEV), torch.ones(3, 16, 16, device=DEV)
+    C = gs.grouped_matmul(A, W, torch.tensor([-5, 10, 1 << 40, 1 << 41], device=DEV))
+    assert (C == 16).all()
+    out, wide = _inside(torch.zeros(64, 16, device=DEV))
+    gs.grouped_matmul(A, W, torch.tensor([60, 10, 50, 20], device=DEV), out=out)
+    assert _around_is_nan(out, wide) and (out[10:50] == 16).all()
+    dW = gs.grouped_weight_grad(A, A, torch.tensor([0, 64, 0, 64], device=DEV))
+    assert dW.shape == (3, 16, 16) and (dW[0] == 64).all()
+
+
+def test_grouped_one_matrix_for_all_groups_and_no_rows():
+    W = torch.randn(1, 16, 8, device=DEV).expand(5, 16, 8)
+    A = torch.randn(50, 16, device=DEV)
+    off = torch.arange(0, 51, 10, device=DEV)
+    _close(gs.grouped_matmul(A, W, off), _np(A) @ _np(W[0]), 40 * U * (np.abs(_np(A)) @ np.abs(_np(W[0]))))
+    zero = torch.zeros(6, dtype=torch.int32, device=DEV)
+    assert gs.grouped_matmul(A[:0], W, zero).shape == (0, 8)
+    assert (gs.grouped_weight_grad(A[:0], A[:0], zero) == 0).all()
+
+
+# ---------------------------------------------------------------------- scores
+
+SCORE_SHAPES = [(1, 1), (3, 2), (70, 47), (33, 256), (9, 257), (11, 349), (5, 1024), (4, 2500), (3, 5000), (2, 20011), (2, 70000)]
+
+
+def _logits(n, v, seed, dtype, masked=True):
+    rng = np.random.default_rng(seed)
+    s = 3 * rng.standard_normal((n, v))
+    if masked and v > 4:
+        s[rng.random((n, v)) < 0.1] = -np.inf
+        s[:, 0] = np.where(np.isinf(s[:, 0]), 0.5, s[:, 0])
+    if n > 2:
+        s[1] = np.round(s[1])          # ties
+        s[2] = -1e30 if v < 5 else 40 * s[2]
+    return torch.from_numpy(s.astype(np.float32)).to(TYPES[dtype])
+
+
+def _parts(s, T=1.0):
+    """Per row: (x, log S, E|x|, E x^2) with x = (s - max) / T, all with the masked classes left out."""
+    s = s / T
+    x = s - s.max(1, keepdims=True)
+    x0 = np.where(np.isfinite(x), x, 0.0)
+    e = np.where(np.isfinite(x), np.exp(x), 0.0)
+    S = e.sum(1)
+    return x0, np.log(S), (e * -x0).sum(1) / S, (e * x0 * x0).sum(1) / S
+
+
+def _sum_terms(v):
+    return v / 256 + 100
+
+
+@pytest.mark.parametrize("n,v", SCORE_SHAPES)
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_log_probs(n, v, dtype):
+    s, wide = _inside(_logits(n, v, n + v, dtype).to(DEV))
+    rng = np.random.default_rng(v)
+    ids = rng.integers(0, v, n)
+    ids[0] = 0
+    if n > 2:
+        ids[2] = -1
+    top = min(v, 1 + n % 40 + (60 if v > 3000 else 0))
+    it = torch.from_numpy(ids).to(DEV)
+    got = gs.log_probs(s, it if n % 2 else it.int(), top=top)
+    lp, H, every = oracle.scores(_np(s), ids)
+    x, logS, ax, xx = _parts(_np(s))
+    tol = U * (4 * np.abs(np.where(ids >= 0, x[np.arange(n), ids], 0)) + 4 * logS + 2 * ax + _sum_terms(v))
+    _close(got.logp, lp, tol, "logp")
+    tolH = U * (4 * logS + 2 * xx + (ax + 1) * (8 + _sum_terms(v)))
+    _close(got.entropy, H, tolH, "entropy")
+    want = oracle.best(_np(s), top)
+    assert np.array_equal(_np(got.top_ids), want)
+    rows = np.arange(n)[:, None]
+    _close(got.top_logp, every[rows, want], U * (4 * np.abs(x[rows, want]) + (4 * logS + 2 * ax + _sum_terms(v))[:, None]), "top")
+    plain = gs.log_probs(s, it)
+    assert torch.equal(plain.logp, got.logp) and plain.top_ids.shape == (n, 0)
+    g = torch.from_numpy(rng.standard_normal(n).astype(np.float32)).to(DEV)
+    e = torch.from_numpy(rng.standard_normal(n).astype(np.float32)).to(DEV)
+    p = np.exp(every)
+    rp = U * (2 * np.abs(x) + 12 + (2 * ax + _sum_terms(v))[:, None])
+    inner = np.where(np.isinf(every), 0, np.abs(np.where(np.isfinite(every), every, 0) + H[:, None]))
+    for gg, ee in ((g, None), (None, e), (g, e)):
+        d = gs.log_probs_grad(s, it, got, gg, ee)
+        w = oracle.scores_grad(every, H, ids, None if gg is None else _np(gg), None if ee is None else _np(ee))
+        tol = np.zeros((n, v))
+        if gg is not None:
+            tol += np.where(ids >= 0, np.abs(_np(gg)), 0)[:, None] * (p * rp + FLUSH + 2 * U)
+        if ee is not None:
+            tol += np.abs(_np(ee))[:, None] * ((p * rp + FLUSH) * inner + p * (tolH[:, None] + 4 * U * (np.abs(x) + logS[:, None] + inner)))
+        _close(d, w, tol + HALF[dtype] * np.abs(w), "gradient")
+    assert _around_is_nan(s, wide)
+    flat = s.contiguous()
+    first = gs.log_probs_grad(flat, it, got, g, e)
+    assert gs.log_probs_grad(flat, it, got, g, e, out=flat) is flat and torch.equal(flat, first)  # in place
+
+
+@pytest.mark.parametrize("v", [5, 300, 3000, 40000])
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_log_probs_of_rows_without_a_distribution(v, dtype):
+    s = torch.zeros(9, v)
+    s[0] = -float("inf")
+    s[1, v - 1] = float("nan")
+    s[2, 3] = float("inf")
+    s[3] = -float("inf")
+    s[3, 2] = -5.0                       # one class left
+    s[4] = torch.arange(v) % 7           # long runs of ties
+    s[5] = torch.arange(v).float()       # ascending: the best come last
+    s[6, ::2] = -0.0                     # the same as 0
+    s[7] = torch.finfo(torch.float32).min
+    s = s.to(TYPES[dtype])
+    ids = torch.tensor([1, 1, 1, 2, v, -1, 0, 1, 1 << 40])
+    top = min(v, 128)
+    got = gs.log_probs(s.to(DEV), ids.to(DEV), top=top)
+    lp, H, every = oracle.scores(_np(s), ids.numpy())
+    _close(got.logp, lp, 1e-4 * (1 + np.abs(np.nan_to_num(lp))))
+    _close(got.entropy, H, 1e-4 * (1 + np.abs(np.nan_to_num(H))))
+    assert got.logp[3] == 0 and got.entropy[3] == 0
+    want = oracle.best(_np(s), top)
+    assert np.array_equal(_np(got.top_ids), want)
+    with np.errstate(invalid="ignore"):
+        _close(got.top_logp, every[np.arange(9)[:, None], want], 1e-4 * (1 + np.abs(np.nan_to_num(every[np.arange(9)[:, None], want]))))
+    d = gs.log_probs_grad(s.to(DEV), ids.to(DEV), got, torch.ones(9, device=DEV), None)
+    nan = torch.isnan(d).all(1).cpu()
+    gone = dtype == "bf16"  # (the least fp32 number is -inf in bf16: a row of masked classes)
+    assert nan.tolist() == [True, True, True, False, True, False, False, gone, True]
+    assert (d[3] == 0).all() and (d[5] == 0).all() and not torch.isnan(d[[3, 5, 6]]).any()
+
+
+# ---------------------------------------------------------------- distillation
+
+
+@pytest.mark.parametrize("n,v", SCORE_SHAPES)
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("T", [1.0, 2.5])
+def test_distill(n, v, dtype, T):
+    rng = np.random.default_rng(n * v)
+    s, wide = _inside(_logits(n, v, n + v, dtype, masked=False).to(DEV))
+    k = min(v, 1 + (n * 7 + v) % 128)
+    ids = np.stack([rng.permutation(v)[:k] for _ in range(n)])
+    t = 3 * rng.standard_normal((n, k)).astype(np.float32)
+    if k > 3:
+        ids[:, 1] = ids[:, 0]               # a class twice
+        t[:, 2] = -np.inf
+        ids[-1, 3] = -1
+    if n > 3:
+        ids[1] = -1                         # no alternative
+        t[2] = -np.inf
+        t[3, 0] = 60.0                      # all but certain
+    tt = torch.from_numpy(t).to(DEV)
+    if v % 2:
+        tt = tt.bfloat16()
+    it = torch.from_numpy(ids).to(DEV)
+    it = it.int() if n % 2 else it
+    loss, stats = gs.distill_loss(s, it, tt, T)
+    want, d, q, at, lp = oracle.distill(_np(s), ids, _np(tt), T)
+    x, logS, ax, xx = _parts(_np(s), T)
+    on = (ids >= 0) & np.isfinite(_np(tt))
+    tf = np.where(on, _np(tt), 0.0)
+    dd = np.where(on, np.abs(tf - np.where(on.any(1), np.max(np.where(on, tf, -np.inf), 1), 0)[:, None]), 0) / T
+    xa = np.abs(x[np.arange(n)[:, None], np.where(on, ids, 0)])
+    rS = 4 * ax + _sum_terms(v)
+    tol = T * T * U * ((q * (dd + xa) * (4 * dd + 2 * k + 20)).sum(1) + (q * 4 * xa).sum(1) + 6 * logS + 6 * np.log(k + 1) + rS)
+    _close(loss, want, tol, "loss")
+    g = rng.standard_normal(n).astype(np.float32)
+    gt = torch.from_numpy(g).to(DEV)
+    got = gs.distill_grad(s, it, tt, stats, gt, T)
+    p = np.exp(lp)
+    tol = p * U * (4 * np.abs(x) + 16 + rS[:, None]) + FLUSH
+    rows = np.repeat(np.arange(n), k)[on.ravel()]
+    np.add.at(tol, (rows, ids.ravel()[on.ravel()]), (q * U * (4 * dd + 2 * k + 20)).ravel()[on.ravel()])
+    w = d * g[:, None]
+    _close(got, w, np.abs(g)[:, None] * T * tol + (HALF[dtype] + 4 * U) * np.abs(w), "gradient")
+    assert _around_is_nan(s, wide)
+    flat = s.contiguous()
+    assert gs.distill_grad(flat, it, tt, stats, gt, T, out=flat) is flat and torch.equal(flat, got)
+
+
+def test_distill_masked_and_bad():
+    s = torch.randn(6, 50)
+    s[0, 3] = -float("inf")  # the student leaves out a class that the teacher names
+    s[1, 7] = float("nan")
+    ids = torch.tensor([[3, 4], [1, 2], [50, 1], [1, 2], [1, 2], [5, 5]])
+    t = torch.zeros(6, 2)
+    t[3, 0] = float("nan")
+    t[4, 0] = float("inf")
+    loss, stats = gs.distill_loss(s.to(DEV), ids.to(DEV), t.to(DEV))
+    assert torch.isinf(loss[0]) and torch.isnan(loss[1:5]).all() and torch.isfinite(loss[5])
+    d = gs.distill_grad(s.to(DEV), ids.to(DEV), t.to(DEV), stats, torch.ones(6, device=DEV))
+    assert torch.isfinite(d[[0, 5]]).all() and torch.isnan(d[1:5]).all()
+    assert d[0, 3] == -0.5
+    want = oracle.distill(_np(s), ids.numpy(), _np(t), 1.0)
+    _close(loss[5], want[0][5], 1e-5)
+    _close(d[5], want[1][5], 1e-5)
