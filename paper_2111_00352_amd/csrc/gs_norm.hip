@@ -51,16 +51,20 @@ __global__ __launch_bounds__((RowAt<T, L, R>::kThreads)) void k_norm(const T *__
     for (int64_t row = At::first_row(), at = (int64_t)blockIdx.x * At::kRows; at < n; row += At::row_step(), at += At::row_step()) {
         const bool in = row < n;
         V v[R];
+        RowPiece<T> x[R], q[R];
 #pragma unroll
-        for (int i = 0; i < R; i++) v[i] = load_elems<T, E, NT>(X + row * ldx + At::col(i), in ? cols - At::col(i) : 0);
+        for (int i = 0; i < R; i++) x[i].template load<NT>(X + row * ldx, At::col(i), cols, in);
+        if (Res)
+#pragma unroll
+            for (int i = 0; i < R; i++) q[i].template load<NT>(Res + row * ldr, At::col(i), cols, in);
+#pragma unroll
+        for (int i = 0; i < R; i++) v[i] = x[i].get(At::col(i), cols);
         if (Res) {
-            V q[R];
-#pragma unroll
-            for (int i = 0; i < R; i++) q[i] = load_elems<T, E, NT>(Res + row * ldr + At::col(i), in ? cols - At::col(i) : 0);
 #pragma unroll
             for (int i = 0; i < R; i++) {
+                const V t = q[i].get(At::col(i), cols);
 #pragma unroll
-                for (int e = 0; e < E; e++) v[i][e] = from_f32<T>(to_f32(v[i][e]) + to_f32(q[i][e]));
+                for (int e = 0; e < E; e++) v[i][e] = from_f32<T>(to_f32(v[i][e]) + to_f32(t[e]));
                 store_elems<T, E, NT>(H + row * ldh + At::col(i), v[i], in ? cols - At::col(i) : 0);
             }
         }
@@ -74,6 +78,8 @@ __global__ __launch_bounds__((RowAt<T, L, R>::kThreads)) void k_norm(const T *__
             }
         ss = row_sum<L>(ss, tmp);
         const float r = inverse_root(ss * inv + eps);
+#pragma unroll
+        for (int i = 0; i < R; i++) as_they_lie(v[i]);
         if (in && At::lane() == 0) rstd[row] = r;
 #pragma unroll
         for (int i = 0; i < R; i++) {
@@ -119,18 +125,31 @@ __global__ __launch_bounds__((RowAt<T, L, R>::kThreads)) void k_norm_grad(const 
             dw[i][e] = 0.0f;
         }
     const float inv = 1.0f / (float)cols;
+    // the next row is loaded while this one is worked on
+    RowPiece<T> hp[R], gp[R], dp[R];
+    float r_next;
+    auto load = [&](int64_t row) {
+        const bool in = row < n;
+        r_next = in ? rstd[row] : 0.0f;
+#pragma unroll
+        for (int i = 0; i < R; i++) {
+            hp[i].template load<NT>(H + row * ldh, At::col(i), cols, in);
+            gp[i].template load<NT>(dY + row * ldy, At::col(i), cols, in);
+            if (dH) dp[i].template load<NT>(dH + row * ldd, At::col(i), cols, in);
+        }
+    };
+    load(At::first_row());
     for (int64_t row = At::first_row(), at = (int64_t)blockIdx.x * At::kRows; at < n; row += At::row_step(), at += At::row_step()) {
         const bool in = row < n;
         V h[R], g[R], d[R];
+        const float r = r_next;
 #pragma unroll
         for (int i = 0; i < R; i++) {
-            h[i] = load_elems<T, E, NT>(H + row * ldh + At::col(i), in ? cols - At::col(i) : 0);
-            g[i] = load_elems<T, E, NT>(dY + row * ldy + At::col(i), in ? cols - At::col(i) : 0);
+            h[i] = hp[i].get(At::col(i), cols);
+            g[i] = gp[i].get(At::col(i), cols);
+            if (dH) d[i] = dp[i].get(At::col(i), cols);
         }
-        if (dH)
-#pragma unroll
-            for (int i = 0; i < R; i++) d[i] = load_elems<T, E, NT>(dH + row * ldd + At::col(i), in ? cols - At::col(i) : 0);
-        const float r = in ? rstd[row] : 0.0f;
+        load(row + At::row_step());
         float dot = 0.0f;
 #pragma unroll
         for (int i = 0; i < R; i++)
@@ -143,6 +162,8 @@ __global__ __launch_bounds__((RowAt<T, L, R>::kThreads)) void k_norm_grad(const 
         dot = row_sum<L>(dot, tmp) * inv;
 #pragma unroll
         for (int i = 0; i < R; i++) {
+            as_they_lie(h[i]);
+            as_they_lie(g[i]);
             V o;
 #pragma unroll
             for (int e = 0; e < E; e++) {
@@ -305,6 +326,7 @@ __global__ __launch_bounds__(kRowThreads) void k_norm_grad_wide(const T *__restr
 
 // Partial rows of dw: a workgroup's share of the rows is summed in its registers, so a few
 // workgroups a compute unit, and no more than 32 MB of partials.
+template <class T> constexpr int kGradPieces = sizeof(T) == 4 ? 4 : 2;  // of a lane (bf16 takes 50 registers for each)
 struct NormGradPlan {
     int64_t blocks;
     bool wide;
@@ -313,9 +335,10 @@ template <class T> NormGradPlan norm_grad_plan(int64_t n, int64_t cols)
 {
     NormGradPlan p{0, false};
     const int64_t most = std::max<int64_t>(1, (32 << 20) / 4 / std::max<int64_t>(1, cols));
-    const bool held = with_row(ceil_div(cols, kPiece<T>), [&](auto l, auto r) {
+    const bool held = with_row<8, 512, kGradPieces<T>>(ceil_div(cols, kPiece<T>), [&](auto l, auto r) {
         using At = RowAt<T, decltype(l)::value, decltype(r)::value>;
-        p.blocks = std::max<int64_t>(1, std::min({ceil_div(n, (int64_t)At::kRows), (int64_t)1024, most}));
+        const int64_t steps = std::max<int64_t>(1, ceil_div(n, (int64_t)At::kRows));  // of kRows rows
+        p.blocks = ceil_div(steps, ceil_div(steps, std::min<int64_t>(768, most)));   // (equal shares)
     });
     if (!held) {
         p.wide = true;
@@ -381,7 +404,7 @@ int gs_rms_norm(const void *X, int64_t ldx, const void *R, int64_t ldr, int dtyp
                     scales, blocks, rstd);
             };
             const int64_t pieces = SAVE ? (int64_t)blocks * (kMxBlock / kPiece<T>) : ceil_div(cols, kPiece<T>);
-            const bool held = with_row(pieces, [&](auto l, auto r) {
+            const bool held = with_row<8, 512, 4>(pieces, [&](auto l, auto r) {
                 constexpr int L = decltype(l)::value, N = decltype(r)::value;
                 using At = RowAt<T, L, N>;
                 nt ? run(k_norm<T, L, N, SAVE, true>, ceil_div(rows, (int64_t)At::kRows), At::kThreads)
@@ -440,7 +463,7 @@ int gs_rms_norm_grad(const void *H, int64_t ldh, const float *rstd, const void *
                     (const T *)H, ldh, rstd, (const T *)dY, ldy, w, w_dtype == GS_F32, (const T *)dH, ldd, rows, (int)cols, (T *)dX,
                     ldx, dots, dw ? part : nullptr);
             } else {
-                with_row(ceil_div(cols, kPiece<T>), [&](auto l, auto r) {
+                with_row<8, 512, kGradPieces<T>>(ceil_div(cols, kPiece<T>), [&](auto l, auto r) {
                     constexpr int L = decltype(l)::value, N = decltype(r)::value;
                     auto run = [&](auto kernel) {
                         kernel<<<(unsigned)p.blocks, RowAt<T, L, N>::kThreads, 0, s>>>(

@@ -21,9 +21,20 @@ namespace {
 
 constexpr float kLog2e = 1.4426950408889634f;
 constexpr float kInf = __builtin_inff();
+template <class T> constexpr uint32_t kNegInf = sizeof(T) == 4 ? 0xff800000u : 0xff80ff80u;
 
 // exp(x), x <= 0 or NaN; 0 below 2^-126.
 __device__ __forceinline__ float exp_neg(float x) { return __builtin_amdgcn_exp2f(x * kLog2e); }
+
+// The weights of a row's logits are 2^((x - m) k), with k = c log2(e).  (As 2^(x k - m k), with
+// one operation less, they would not be right where m k leaves the type's range: rows of its
+// lowest number.)
+struct Scale {
+    float k, m;
+    __device__ __forceinline__ Scale(float k_, float m_) : k(k_), m(m_ == -kInf ? 0.0f : m_) {}
+    __device__ __forceinline__ float power(float x) const { return (x - m) * k; }
+};
+constexpr float kLn2 = 0.6931471805599453f;
 
 // Whole numbers in the order of the values: -0 as +0, every NaN above +inf, 0 below everything.
 __device__ __forceinline__ uint32_t order_key(float x)
@@ -53,6 +64,12 @@ struct ScoreOut {
 // What a row's results are made of.
 struct RowStats {
     float m, S, X;  // maximum, sum of exp(x), sum of exp(x) x
+    // From the sums of the weights, and of weight times power.
+    __device__ __forceinline__ void set(float sum, float powers)
+    {
+        S = m == -kInf ? __builtin_nanf("") : sum;
+        X = powers * kLn2;
+    }
 };
 
 __device__ __forceinline__ void write_scores(const RowStats &t, float logS, int64_t row, const ScoreOut &out, const ClassIds &ids,
@@ -69,37 +86,52 @@ struct Teacher {
     const void *t;
     bool t32;
     int k;
-    float c;     // 1 / temperature
+    float c;      // 1 / temperature
+    float k2;     // log2(e) / temperature
     float scale;  // temperature^2
 };
+// Alternative i of a row: its class (negative: none) and what teacher and student give it.
+template <class T> struct Alternative {
+    int64_t id;
+    float t, s;
+    __device__ __forceinline__ void load(const Teacher &te, int64_t row, int i, bool in)
+    {
+        const int64_t at = row * te.k + i;
+        id = in && i < te.k ? te.ids.at(at) : -1;
+        t = id >= 0 ? load_either(te.t, te.t32, at) : 0.0f;
+    }
+    __device__ __forceinline__ void look_up(const T *p, int v)
+    {
+        if (t == -kInf) id = -1;
+        s = id < 0 ? 0.0f : id < v ? to_f32(p[id]) : __builtin_nanf("");
+    }
+};
+// first: the lane's first alternative, looked up.
 template <class T, int L>
-__device__ __forceinline__ void write_loss(const RowStats &st, float logS, const T *s, int64_t row, bool in, int v, const Teacher &te,
-                                           int lane, float *tmp, float *loss)
+__device__ __forceinline__ void write_loss(const RowStats &st, float logS, const T *p, int64_t row, bool in, int v, const Teacher &te,
+                                           int lane, const Alternative<T> &first, float *tmp, float *loss)
 {
     auto each = [&](auto &&f) {
-        for (int i = lane; i < te.k; i += L) {
-            const int64_t at = row * te.k + i;
-            const int64_t id = in ? te.ids.at(at) : -1;
-            const float t = in ? load_either(te.t, te.t32, at) : 0.0f;
-            if (id >= 0 && !(t == -kInf)) f(id, t);
+        if (first.id >= 0) f(first);
+        for (int i = lane + L; i < te.k; i += L) {
+            Alternative<T> a;
+            a.load(te, row, i, in);
+            a.look_up(p, v);
+            if (a.id >= 0) f(a);
         }
     };
     float tm = -kInf;
-    each([&](int64_t, float t) { tm = fmaxf(tm, t); });
+    each([&](const Alternative<T> &a) { tm = fmaxf(tm, a.t); });
     tm = row_fold<L>(tm, tmp, [](float a, float b) { return fmaxf(a, b); });
-    float W = 0.0f, D = 0.0f, any = 0.0f;
-    each([&](int64_t id, float t) {
-        const float d = (t - tm) * te.c, w = exp_neg(d);
-        const float x = id < v ? (to_f32(s[id]) - st.m) * te.c : __builtin_nanf("");
-        W += w;
-        if (!(w == 0.0f)) D = __builtin_fmaf(w, d - x, D);
-        if (id >= v) D = x;
-        any = 1.0f;
+    float sums[3] = {0.0f, 0.0f, 0.0f};  // of the weights, of weight (log q' - log p'), of the alternatives
+    each([&](const Alternative<T> &a) {
+        const float d = (a.t - tm) * te.c, w = exp_neg(d), x = (a.s - st.m) * te.c;
+        sums[0] += w;
+        if (!(w == 0.0f) || x != x) sums[1] = __builtin_fmaf(w, d - x, sums[1]);
+        sums[2] += 1.0f;
     });
-    W = row_sum<L>(W, tmp);
-    D = row_sum<L>(D, tmp);
-    any = row_sum<L>(any, tmp);
-    if (in && lane == 0) loss[row] = any > 0.0f ? te.scale * (D / W + (logS - logf(W))) : 0.0f;
+    row_sums<L, 3>(sums, tmp);
+    if (in && lane == 0) loss[row] = sums[2] > 0.0f ? te.scale * (sums[1] / sums[0] + (logS - logf(sums[0]))) : 0.0f;
 }
 
 // ------------------------------------------------------------ rows in registers
@@ -115,14 +147,18 @@ __global__ __launch_bounds__(kRowThreads) void k_scores_held(const T *__restrict
         const bool in = row < n;
         const T *p = s + row * ld;
         float x[R][E];
+        Alternative<T> first;
         {
-            V q[R];
+            RowPiece<T> q[R];
 #pragma unroll
-            for (int i = 0; i < R; i++) q[i] = load_elems<T, E, NT>(p + At::col(i), in ? v - At::col(i) : 0);
+            for (int i = 0; i < R; i++) q[i].template load<NT>(p, At::col(i), v, in);
+            if constexpr (TEACHER) first.load(te, row, At::lane(), in);
 #pragma unroll
-            for (int i = 0; i < R; i++)
+            for (int i = 0; i < R; i++) {
+                const V t = q[i].get(At::col(i), v, kNegInf<T>);
 #pragma unroll
-                for (int e = 0; e < E; e++) x[i][e] = At::col(i) + e < v ? to_f32(q[i][e]) : -kInf;
+                for (int e = 0; e < E; e++) x[i][e] = to_f32(t[e]);
+            }
         }
         int64_t id = -1;
         float given = 0.0f;
@@ -132,26 +168,30 @@ __global__ __launch_bounds__(kRowThreads) void k_scores_held(const T *__restrict
                 if (id >= 0 && id < v) given = to_f32(p[id]);
             }
         }
+        if constexpr (TEACHER) first.look_up(p, v);
         RowStats t{-kInf, 0.0f, 0.0f};
 #pragma unroll
         for (int i = 0; i < R; i++)
 #pragma unroll
             for (int e = 0; e < E; e++) t.m = fmaxf(t.m, x[i][e]);
         t.m = group_fold<L>(t.m, [](float a, float b) { return fmaxf(a, b); });
-        const float c = TEACHER ? te.c : 1.0f;
+        const Scale by(TEACHER ? te.k2 : kLog2e, t.m);
+        float sums[2] = {0.0f, 0.0f};
 #pragma unroll
         for (int i = 0; i < R; i++)
 #pragma unroll
             for (int e = 0; e < E; e++) {
-                const float d = (x[i][e] - t.m) * c, w = exp_neg(d);
-                t.S += w;
-                if constexpr (!TEACHER) t.X += w == 0.0f ? 0.0f : w * d;
+                const float d = by.power(x[i][e]), w = __builtin_amdgcn_exp2f(d);
+                sums[0] += w;
+                // (0 where d is -inf: its maximum with -2^126 is finite, the weight 0)
+                if constexpr (!TEACHER) sums[1] = __builtin_fmaf(w, fmaxf(d, -0x1p126f), sums[1]);
             }
-        t.S = group_sum<L>(t.S);
-        if constexpr (!TEACHER) t.X = group_sum<L>(t.X);
+        sums[0] = group_sum<L>(sums[0]);
+        if constexpr (!TEACHER) sums[1] = group_sum<L>(sums[1]);
+        t.set(sums[0], sums[1]);
         const float logS = logf(t.S);
         if constexpr (TEACHER) {
-            write_loss<T, L>(t, logS, p, row, in, v, te, At::lane(), (float *)nullptr, out.lp);
+            write_loss<T, L>(t, logS, p, row, in, v, te, At::lane(), first, (float *)nullptr, out.lp);
             if (in && At::lane() == 0) out.stats[row] = make_float2(t.m, t.S);
         } else {
             if (in && At::lane() == 0) write_scores(t, logS, row, out, ids, given, id, v);
@@ -198,7 +238,7 @@ __global__ __launch_bounds__(kRowThreads) void k_scores_held(const T *__restrict
 // is not below that bound is collected in LDS, a few times k of it; its order decides.  Where
 // that is more than LDS holds (long runs of equal logits, rows that ascend) or the row has a
 // NaN, the k-th best is found digit by digit in passes of its own.
-constexpr int kWideUnits = 4;      // pieces of a thread in flight
+template <class T> constexpr int kWideUnits = sizeof(T) == 4 ? 4 : 2;  // pieces of a thread at a time, 16 elements
 constexpr int kTopGroups = 256;
 constexpr int kTopKeep = 3072;     // collected at most
 constexpr int kTopMax = 128;
@@ -296,60 +336,67 @@ template <class T, int NTH, bool TEACHER, bool TOP>
 __global__ __launch_bounds__(NTH) void k_scores_wide(const T *__restrict__ s, int64_t ld, int64_t n, int v, ClassIds ids, Teacher te,
                                                     ScoreOut out)
 {
-    constexpr int E = kPiece<T>, U = kWideUnits;
+    constexpr int E = kPiece<T>, U = kWideUnits<T>;
     using V = typename Elems<T, E>::type;
     __shared__ std::conditional_t<TOP, WideLds<NTH>, uint8_t> lds;
-    __shared__ float fold[NTH / kWave];
-    const float c = TEACHER ? te.c : 1.0f;
+    __shared__ float fold[3 * NTH / kWave];
+    const float k = TEACHER ? te.k2 : kLog2e;
     for (int64_t row = blockIdx.x; row < n; row += gridDim.x) {
         const T *p = s + row * ld;
         if constexpr (TOP) {
             if (threadIdx.x == 0) lds.kept = 0;  // (bound_of_groups' barriers come before its first use)
         }
-        RowStats t{-kInf, 0.0f, 0.0f};
+        Alternative<T> first;
+        if constexpr (TEACHER) first.load(te, row, threadIdx.x, true);
+        float top = -kInf, sums[2] = {0.0f, 0.0f};
+        Scale by(k, top);
         float least = kInf;  // collected from here on
+        int parts = 0;
+        RowPiece<T> q[U];
+#pragma unroll
+        for (int i = 0; i < U; i++) q[i].load(p, (i * NTH + (int)threadIdx.x) * E, v);
         for (int c0 = 0; c0 < v; c0 += NTH * U * E) {
-            V q[U];
+            float x[U][E], high[U], here = -kInf;
 #pragma unroll
             for (int i = 0; i < U; i++) {
-                const int col = c0 + (i * NTH + threadIdx.x) * E;
-                q[i] = load_elems<T, E>(p + col, v - col);
-            }
-            float m = t.m;
-            float x[U][E];
-#pragma unroll
-            for (int i = 0; i < U; i++)
+                const V w = q[i].get(c0 + (i * NTH + (int)threadIdx.x) * E, v, kNegInf<T>);
+                high[i] = -kInf;
 #pragma unroll
                 for (int e = 0; e < E; e++) {
-                    x[i][e] = c0 + (i * NTH + (int)threadIdx.x) * E + e < v ? to_f32(q[i][e]) : -kInf;
-                    m = fmaxf(m, x[i][e]);
+                    x[i][e] = to_f32(w[e]);
+                    high[i] = fmaxf(high[i], x[i][e]);
                 }
-            const float base = m == -kInf ? 0.0f : m;
-            const float d0 = t.m == -kInf ? 0.0f : (t.m - base) * c, f = exp_neg(d0);
-            if constexpr (!TEACHER) t.X = f * __builtin_fmaf(t.S, d0, t.X);
-            t.S *= f;
-            t.m = m;
+                here = fmaxf(here, high[i]);
+            }
+            if (c0 + NTH * U * E < v)  // (the next ones while these are worked on)
+#pragma unroll
+                for (int i = 0; i < U; i++) q[i].load(p, c0 + ((U + i) * NTH + (int)threadIdx.x) * E, v);
+            if (here > top) {
+                const Scale next(k, here);
+                const float up = top == -kInf ? 0.0f : (by.m - next.m) * k, f = __builtin_amdgcn_exp2f(up);
+                if constexpr (!TEACHER) sums[1] = f * __builtin_fmaf(sums[0], up, sums[1]);
+                sums[0] *= f;
+                top = here;
+                by = next;
+            }
 #pragma unroll
             for (int i = 0; i < U; i++)
 #pragma unroll
                 for (int e = 0; e < E; e++) {
-                    const float d = (x[i][e] - base) * c, w = exp_neg(d);
-                    t.S += w;
-                    if constexpr (!TEACHER) t.X += w == 0.0f ? 0.0f : w * d;
+                    const float d = by.power(x[i][e]), w = __builtin_amdgcn_exp2f(d);
+                    sums[0] += w;
+                    if constexpr (!TEACHER) sums[1] = __builtin_fmaf(w, fmaxf(d, -0x1p126f), sums[1]);
                 }
             if constexpr (TOP) {
-                if (c0 == 0) {
+                // (after 1, 2, 4 .. parts, of all that has been seen)
+                if ((parts & (parts + 1)) == 0) {
                     const bool some = (int)threadIdx.x * E < v;
-                    least = key_value(std::max(bound_of_groups<NTH>(some ? order_key(m) : 0, out.top, lds), 0x007fffffu));
+                    least = key_value(std::max(bound_of_groups<NTH>(some ? order_key(top) : 0, out.top, lds), 0x007fffffu));
                 }
-                float here = -kInf;
+                parts++;
 #pragma unroll
                 for (int i = 0; i < U; i++)
-#pragma unroll
-                    for (int e = 0; e < E; e++) here = fmaxf(here, x[i][e]);
-                if (here >= least) {
-#pragma unroll
-                    for (int i = 0; i < U; i++)
+                    if (high[i] >= least) {
 #pragma unroll
                         for (int e = 0; e < E; e++) {
                             const int col = c0 + (i * NTH + (int)threadIdx.x) * E + e;
@@ -358,22 +405,23 @@ __global__ __launch_bounds__(NTH) void k_scores_wide(const T *__restrict__ s, in
                                 if (at < kTopKeep) lds.keep[at] = order64(order_key(x[i][e]), col);
                             }
                         }
-                }
+                    }
             }
         }
+        if constexpr (TEACHER) first.look_up(p, v);
         // the threads' sums joined
+        RowStats t;
         {
-            const float m = row_fold<NTH>(t.m, fold, [](float a, float b) { return fmaxf(a, b); });
-            const float base = m == -kInf ? 0.0f : m;
-            const float d0 = t.m == -kInf ? 0.0f : (t.m - base) * c, f = exp_neg(d0);
-            if constexpr (!TEACHER) t.X = row_sum<NTH>(f * __builtin_fmaf(t.S, d0, t.X), fold);
-            t.S = row_sum<NTH>(t.S * f, fold);
-            t.m = m;
-            if (m == -kInf) t.S = __builtin_nanf("");
+            t.m = row_fold<NTH>(top, fold, [](float a, float b) { return fmaxf(a, b); });
+            const Scale all(k, t.m);
+            const float up = top == -kInf ? 0.0f : (by.m - all.m) * k, f = __builtin_amdgcn_exp2f(up);
+            float both[2] = {sums[0] * f, f * __builtin_fmaf(sums[0], up, sums[1])};
+            row_sums<NTH, 2>(both, fold);
+            t.set(both[0], both[1]);
         }
         const float logS = logf(t.S);
         if constexpr (TEACHER) {
-            write_loss<T, NTH>(t, logS, p, row, true, v, te, threadIdx.x, fold, out.lp);
+            write_loss<T, NTH>(t, logS, p, row, true, v, te, threadIdx.x, first, fold, out.lp);
             if (threadIdx.x == 0) out.stats[row] = make_float2(t.m, t.S);
         } else if (threadIdx.x == 0) {
             const int64_t id = out.lp ? ids.at(row) : -1;
@@ -406,38 +454,50 @@ struct GradIn {
     const float *g, *e, *entropy;  // NULL: none
 };
 
-template <class T, int L, bool NT>
+template <class T, int L, int R, bool NT>
 __global__ __launch_bounds__(kRowThreads) void k_scores_grad(const T *s, int64_t ld, int64_t n, int v, int span, ClassIds ids, GradIn a,
                                                             T *out, int64_t ldo)
 {
-    constexpr int E = kPiece<T>, U = 4;
+    constexpr int E = kPiece<T>;
     using V = typename Elems<T, E>::type;
     constexpr int kRows = kRowThreads / L;
     const int lane = threadIdx.x % L, c1 = blockIdx.y * span, c2 = c1 + span < v ? c1 + span : v;
-    for (int64_t row = (int64_t)blockIdx.x * kRows + threadIdx.x / L; row < n; row += (int64_t)gridDim.x * kRows) {
-        const float2 st = a.stats[row];
-        const int64_t id = a.g ? ids.at(row) : -1;
-        float g = a.g && id >= 0 ? a.g[row] : 0.0f;
+    constexpr int STEP = L * R * E;
+    for (int64_t row = (int64_t)blockIdx.x * kRows + threadIdx.x / L, at = (int64_t)blockIdx.x * kRows; at < n;
+         row += (int64_t)gridDim.x * kRows, at += (int64_t)gridDim.x * kRows) {
+        const bool in = row < n;
+        RowPiece<T> q[R];
+        auto load = [&](int c0) {
+#pragma unroll
+            for (int i = 0; i < R; i++) q[i].template load<NT>(s + row * ld, c0 + (i * L + lane) * E, v, in);
+        };
+        load(c1);
+        const float2 st = in ? a.stats[row] : make_float2(0.0f, 1.0f);
+        const int64_t id = in && a.g ? ids.at(row) : -1;
+        float g = id >= 0 ? a.g[row] : 0.0f;
         if (id >= v) g = __builtin_nanf("");
-        const float e0 = a.e ? a.e[row] : 0.0f, H = a.e ? a.entropy[row] : 0.0f;
-        const float inv = 1.0f / st.y, shift = H - logf(st.y);
-        for (int c0 = c1 + lane * E; c0 < c2; c0 += L * E * U) {
-            V q[U];
+        const float e0 = in && a.e ? a.e[row] : 0.0f, H = in && a.e ? a.entropy[row] : 0.0f;
+        // -g p - e p (log p + H) = weight (fa power + fb)
+        const Scale by(kLog2e, st.x);
+        const float f = 1.0f / st.y, fa = -e0 * kLn2 * f, fb = (-g - e0 * (H - logf(st.y))) * f;
+        const int mine = id >= 0 && id < v ? (int)id : -1;
+        for (int c0 = c1; c0 < c2; c0 += STEP) {
+            V x[R];
 #pragma unroll
-            for (int i = 0; i < U; i++) q[i] = load_elems<T, E, NT>(s + row * ld + c0 + i * L * E, c2 - c0 - i * L * E);
+            for (int i = 0; i < R; i++) x[i] = q[i].get(c0 + (i * L + lane) * E, v);
+            if (c0 + STEP < c2) load(c0 + STEP);
 #pragma unroll
-            for (int i = 0; i < U; i++) {
-                const int col = c0 + i * L * E;
+            for (int i = 0; i < R; i++) {
+                const int col = c0 + (i * L + lane) * E;
                 V o;
 #pragma unroll
                 for (int e = 0; e < E; e++) {
-                    const float x = to_f32(q[i][e]) - st.x, p = exp_neg(x) * inv;
-                    float d = -g * p;
-                    if (a.e) d = __builtin_fmaf(-e0, p == 0.0f ? 0.0f : p * (x + shift), d);
-                    if (col + e == id) d += g;
-                    o[e] = from_f32<T>(d);
+                    const float d = by.power(to_f32(x[i][e])), weight = __builtin_amdgcn_exp2f(d);
+                    float y = weight * (a.e ? __builtin_fmaf(fa, fmaxf(d, -0x1p100f), fb) : fb);
+                    if (col + e == mine) y += g;
+                    o[e] = from_f32<T>(y);
                 }
-                store_elems<T, E, NT>(out + row * ldo + col, o, c2 - col);
+                store_elems<T, E, NT>(out + row * ldo + col, o, in ? c2 - col : 0);
             }
         }
     }
@@ -454,77 +514,83 @@ __device__ __forceinline__ void stores_meet()
 // The distillation loss's gradient.  The elements at the teacher's classes, which may be the
 // same class twice, are made by a lane for each of them and stored over what the row's pass
 // left there.  LDS: per row `kp` ids, weights and values.
-template <class T, int L, bool NT>
+template <class T, int L, int R, bool NT>
 __global__ __launch_bounds__(kRowThreads) void k_distill_grad(const T *s, int64_t ld, int64_t n, int v, int span, Teacher te, GradIn a,
                                                              int kp, T *out, int64_t ldo)
 {
-    constexpr int E = kPiece<T>, U = 4;
+    constexpr int E = kPiece<T>, STEP = L * R * E;
     using V = typename Elems<T, E>::type;
     constexpr int kRows = kRowThreads / L;
     extern __shared__ __align__(16) uint8_t lds[];
-    __shared__ float fold[kRowThreads / kWave];
+    __shared__ float fold[2 * kRowThreads / kWave];
     const int lane = threadIdx.x % L, c1 = blockIdx.y * span, c2 = c1 + span < v ? c1 + span : v;
     int *id = (int *)lds + 3 * kp * (threadIdx.x / L);
     float *w = (float *)id + kp, *val = w + kp;
     for (int64_t r0 = (int64_t)blockIdx.x * kRows; r0 < n; r0 += (int64_t)gridDim.x * kRows) {
         const int64_t row = r0 + threadIdx.x / L;
         const bool in = row < n;
+        const T *p = s + row * ld;
+        RowPiece<T> q[R];
+        auto load = [&](int c0) {
+#pragma unroll
+            for (int i = 0; i < R; i++) q[i].template load<NT>(p, c0 + (i * L + lane) * E, v, in);
+        };
+        load(c1);
         const float2 st = in ? a.stats[row] : make_float2(0.0f, 1.0f);
+        const Scale by(te.k2, st.x);
         const float inv = 1.0f / st.y;
-        float tm = -kInf, bad = 0.0f;
+        float tm = -kInf, sums[2] = {0.0f, 0.0f};  // the weights' sum; 1 for a class, infinity for one that is not there
         for (int i = lane; i < kp; i += L) {
-            const int64_t at = row * te.k + i;
-            int64_t j = in && i < te.k ? te.ids.at(at) : -1;
-            const float t = j >= 0 ? load_either(te.t, te.t32, at) : 0.0f;
-            if (t == -kInf) j = -1;
-            if (j >= v) bad = 1.0f;
-            id[i] = j < v ? (int)j : -1;
-            w[i] = t;
-            if (j >= 0) tm = fmaxf(tm, t);
+            Alternative<T> one;
+            one.load(te, row, i, in);
+            if (one.t == -kInf) one.id = -1;
+            const bool there = one.id >= 0 && one.id < v;
+            if (one.id >= 0) {
+                sums[1] += there ? 1.0f : kInf;
+                tm = fmaxf(tm, one.t);
+            }
+            id[i] = there ? (int)one.id : -1;
+            w[i] = one.t;
+            // (the student's probability there, for now)
+            if (there && one.id >= c1 && one.id < c2) val[i] = __builtin_amdgcn_exp2f(by.power(to_f32(p[one.id]))) * inv;
         }
         tm = row_fold<L>(tm, fold, [](float x, float y) { return fmaxf(x, y); });
-        float W = 0.0f;
         for (int i = lane; i < kp; i += L) {
             w[i] = id[i] >= 0 ? exp_neg((w[i] - tm) * te.c) : 0.0f;
-            W += w[i];
+            sums[0] += w[i];
         }
-        W = row_sum<L>(W, fold);
-        bad = row_sum<L>(bad, fold);
-        float any = 0.0f;
-        for (int i = lane; i < te.k; i += L) any += id[i] >= 0 ? 1.0f : 0.0f;
-        any = row_sum<L>(any, fold);
+        row_sums<L, 2>(sums, fold);
         // (NaN where the teacher's weights are, 0 where the row has none of them)
-        const float gT = bad > 0.0f ? __builtin_nanf("") : any > 0.0f && in ? a.g[row] / te.c * (W / W) : 0.0f;
-        __syncthreads();
+        const float gT = sums[1] == kInf ? __builtin_nanf("") : sums[1] > 0.0f ? a.g[row] / te.c * (sums[0] / sums[0]) : 0.0f;
+        const float inv_w = 1.0f / sums[0];
+        __syncthreads();  // (ids and weights are there; out may be s: its elements have been read)
         for (int i = lane; i < te.k; i += L) {
             const int j = id[i];
             if (j < c1 || j >= c2) continue;
-            float q = 0.0f;
+            float sum = 0.0f;
             for (int o = 0; o < kp; o += 4) {
                 const int4 jj = *reinterpret_cast<const int4 *>(id + o);
                 const float4 ww = *reinterpret_cast<const float4 *>(w + o);
-                q += jj.x == j ? ww.x : 0.0f;
-                q += jj.y == j ? ww.y : 0.0f;
-                q += jj.z == j ? ww.z : 0.0f;
-                q += jj.w == j ? ww.w : 0.0f;
+                sum += jj.x == j ? ww.x : 0.0f;
+                sum += jj.y == j ? ww.y : 0.0f;
+                sum += jj.z == j ? ww.z : 0.0f;
+                sum += jj.w == j ? ww.w : 0.0f;
             }
-            const float x = (to_f32(s[row * ld + j]) - st.x) * te.c;
-            val[i] = gT * (exp_neg(x) * inv - q / W);
+            val[i] = gT == 0.0f ? 0.0f : gT * (val[i] - sum * inv_w);
         }
-        __syncthreads();  // (out may be s: its elements have been read)
-        const bool none = gT == 0.0f;
-        for (int c0 = c1 + lane * E; c0 < c2 && in; c0 += L * E * U) {
-            V q[U];
+        const float f = gT * inv;
+        for (int c0 = c1; c0 < c2; c0 += STEP) {
+            V x[R];
 #pragma unroll
-            for (int i = 0; i < U; i++) q[i] = load_elems<T, E, NT>(s + row * ld + c0 + i * L * E, c2 - c0 - i * L * E);
+            for (int i = 0; i < R; i++) x[i] = q[i].get(c0 + (i * L + lane) * E, v);
+            if (c0 + STEP < c2) load(c0 + STEP);
 #pragma unroll
-            for (int i = 0; i < U; i++) {
-                const int col = c0 + i * L * E;
+            for (int i = 0; i < R; i++) {
+                const int col = c0 + (i * L + lane) * E;
                 V o;
 #pragma unroll
-                for (int e = 0; e < E; e++)
-                    o[e] = none ? T(0) : from_f32<T>(gT * (exp_neg((to_f32(q[i][e]) - st.x) * te.c) * inv));
-                store_elems<T, E, NT>(out + row * ldo + col, o, c2 - col);
+                for (int e = 0; e < E; e++) o[e] = gT == 0.0f ? T(0) : from_f32<T>(f * __builtin_amdgcn_exp2f(by.power(to_f32(x[i][e]))));
+                store_elems<T, E, NT>(out + row * ldo + col, o, in ? c2 - col : 0);
             }
         }
         stores_meet();
@@ -559,30 +625,28 @@ Teacher check_teacher(const void *ids, int id_bytes, const void *t, int t_dtype,
     if (n > 0 && !t) fail(GS_ERR_INVALID_ARG, "the teacher's logits are null");
     if ((uintptr_t)t % size) fail(GS_ERR_INVALID_ARG, "the teacher's logits are not aligned");
     return {check_ids("the teacher's classes", ids, id_bytes, n), t, t_dtype == GS_F32, (int)k, (float)(1.0 / temperature),
-            (float)(temperature * temperature)};
+            (float)(1.4426950408889634 / temperature), (float)(temperature * temperature)};
 }
 
-// Rows up to 64 pieces of 16 bytes are held by eight lanes, up to 512 by a wave.
+// Rows that a wave holds stay in registers; wider ones take a workgroup, the larger the fewer
+// they are (the chip holds 2,048 of 256 threads).
+constexpr int64_t kHeldPieces = 256;
 template <class T, bool TEACHER>
 void launch_scores(const T *s, int64_t ld, int64_t n, int64_t v, const ClassIds &ids, const Teacher &te, const ScoreOut &out,
                    hipStream_t st)
 {
     const int64_t pieces = ceil_div(v, kPiece<T>);
     const bool nt = streams((double)n * v * sizeof(T), v, sizeof(T), {{s, ld}});
-    bool done = false;
-    if (pieces <= 512)
-        done = with_row(pieces, [&](auto l, auto r) {
-            constexpr int L = decltype(l)::value, R = decltype(r)::value;
-            if constexpr (L <= kWave) {
-                const unsigned grid = (unsigned)std::min<int64_t>(ceil_div(n, (int64_t)(kRowThreads / L)), 1 << 20);
-                nt ? k_scores_held<T, L, R, TEACHER, true><<<grid, kRowThreads, 0, st>>>(s, ld, n, (int)v, ids, te, out)
-                   : k_scores_held<T, L, R, TEACHER, false><<<grid, kRowThreads, 0, st>>>(s, ld, n, (int)v, ids, te, out);
-            }
-        });
-    if (done) return;
+    const bool held = pieces <= kHeldPieces && with_row<4, kWave, 4>(pieces, [&](auto l, auto r) {
+        constexpr int L = decltype(l)::value, R = decltype(r)::value;
+        const unsigned grid = (unsigned)std::min<int64_t>(ceil_div(n, (int64_t)(kRowThreads / L)), 1 << 20);
+        nt ? k_scores_held<T, L, R, TEACHER, true><<<grid, kRowThreads, 0, st>>>(s, ld, n, (int)v, ids, te, out)
+           : k_scores_held<T, L, R, TEACHER, false><<<grid, kRowThreads, 0, st>>>(s, ld, n, (int)v, ids, te, out);
+    });
+    if (held) return;
     const unsigned grid = (unsigned)std::min<int64_t>(n, 1 << 20);
     auto go = [&](auto kernel, int threads) { kernel<<<grid, threads, 0, st>>>(s, ld, n, (int)v, ids, te, out); };
-    const bool large = pieces > 4096;
+    const bool large = pieces > 2048 && n < 2048;
     if constexpr (TEACHER)
         large ? go(k_scores_wide<T, 1024, true, false>, 1024) : go(k_scores_wide<T, 256, true, false>, 256);
     else if (out.top)
@@ -591,21 +655,20 @@ void launch_scores(const T *s, int64_t ld, int64_t n, int64_t v, const ClassIds 
         large ? go(k_scores_wide<T, 1024, false, false>, 1024) : go(k_scores_wide<T, 256, false, false>, 256);
 }
 
-// go(L, span, grid): eight lanes a row up to 64 pieces, a wave up to 1024, else a workgroup
-// for 16 pieces a thread.
+// go(L, R, span, grid): rows that a wave holds, else workgroups for spans of a row.
 template <class T, class Go> void grad_shape(int64_t n, int64_t v, Go &&go)
 {
     const int64_t pieces = ceil_div(v, kPiece<T>);
-    auto grid = [&](int64_t rows) { return (unsigned)std::min<int64_t>(ceil_div(n, rows), 1 << 20); };
-    if (pieces <= 64)
-        go(std::integral_constant<int, 8>{}, (int)v, dim3(grid(kRowThreads / 8)));
-    else if (pieces <= 1024)
-        go(std::integral_constant<int, 64>{}, (int)v, dim3(grid(kRowThreads / 64)));
-    else {
-        const int span = kRowThreads * 16 * kPiece<T>;
-        const unsigned parts = (unsigned)ceil_div(v, span);
-        go(std::integral_constant<int, kRowThreads>{}, span, dim3((unsigned)std::min<int64_t>(n, (1 << 22) / parts), parts));
-    }
+    if (with_row<4, kWave, 4>(pieces, [&](auto l, auto r) {
+            go(l, r, (int)v, dim3((unsigned)std::min<int64_t>(ceil_div(n, (int64_t)kRowThreads / decltype(l)::value), 1 << 20)));
+        }))
+        return;
+    // (spans of whole steps, as many as make 2,048 workgroups with the rows)
+    constexpr int R = 4, STEP = kRowThreads * R * kPiece<T>;
+    const int64_t steps = ceil_div(v, STEP), want = std::min(steps, ceil_div(2048, std::max<int64_t>(1, n)));
+    const int64_t span = ceil_div(steps, want) * STEP;
+    go(std::integral_constant<int, kRowThreads>{}, std::integral_constant<int, R>{}, (int)span,
+       dim3((unsigned)std::min<int64_t>(n, 1 << 20), (unsigned)ceil_div(v, span)));
 }
 
 }  // namespace
@@ -649,12 +712,12 @@ int gs_log_probs_grad(const void *s, int64_t ld, int dtype, int64_t n, int64_t v
         auto go = [&](auto type) {
             using T = decltype(type);
             const bool nt = streams(2.0 * n * v * sizeof(T), v, sizeof(T), {{s, ld}, {out, ldo}});
-            grad_shape<T>(n, v, [&](auto l, int span, dim3 grid) {
-                constexpr int L = decltype(l)::value;
+            grad_shape<T>(n, v, [&](auto l, auto r, int span, dim3 grid) {
+                constexpr int L = decltype(l)::value, R = decltype(r)::value;
                 auto run = [&](auto kernel) {
                     kernel<<<grid, kRowThreads, 0, (hipStream_t)stream>>>((const T *)s, ld, n, (int)v, span, id, a, (T *)out, ldo);
                 };
-                nt ? run(k_scores_grad<T, L, true>) : run(k_scores_grad<T, L, false>);
+                nt ? run(k_scores_grad<T, L, R, true>) : run(k_scores_grad<T, L, R, false>);
             });
         };
         dtype == GS_F32 ? go(0.0f) : go(u16(0));
@@ -696,9 +759,9 @@ int gs_distill_grad(const void *s, int64_t ld, int dtype, int64_t n, int64_t v, 
         const int kp = (int)ceil_div(k, 4) * 4;
         auto go = [&](auto type) {
             using T = decltype(type);
-            grad_shape<T>(n, v, [&](auto l, int span, dim3 grid) {
-                constexpr int L = decltype(l)::value;
-                k_distill_grad<T, L, false><<<grid, kRowThreads, (kRowThreads / L) * 3 * kp * 4, (hipStream_t)stream>>>(
+            grad_shape<T>(n, v, [&](auto l, auto r, int span, dim3 grid) {
+                constexpr int L = decltype(l)::value, R = decltype(r)::value;
+                k_distill_grad<T, L, R, false><<<grid, kRowThreads, (kRowThreads / L) * 3 * kp * 4, (hipStream_t)stream>>>(
                     (const T *)s, ld, n, (int)v, span, te, a, kp, (T *)out, ldo);
             });
         };
