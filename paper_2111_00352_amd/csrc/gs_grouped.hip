@@ -58,14 +58,22 @@ __device__ __forceinline__ int64_t lane_value(int64_t v, int lane)
     const uint32_t lo = __builtin_amdgcn_readlane((int)(uint32_t)v, lane), hi = __builtin_amdgcn_readlane((int)(v >> 32), lane);
     return (int64_t)((uint64_t)hi << 32 | lo);
 }
+// The same for every lane, and told to be (divisions are made in vector registers).
+__device__ __forceinline__ int64_t uniform(int64_t v)
+{
+    const uint32_t lo = __builtin_amdgcn_readfirstlane((int)(uint32_t)v), hi = __builtin_amdgcn_readfirstlane((int)(v >> 32));
+    return (int64_t)((uint64_t)hi << 32 | lo);
+}
 // ends: whether the segments without a group count.  EMPTY: a group without rows has `per` items too.
-template <bool EMPTY>
+// The item of workgroup `id`, SPREAD: so that each accelerator die has an equal contiguous
+// run of the items there are (a launch has more workgroups than that).
+template <bool EMPTY, bool SPREAD>
 __device__ __forceinline__ Segment find_segment(const Offsets &o, int64_t step, int64_t per, bool ends, int64_t id)
 {
-    int64_t base = 0;
-    for (int j0 = 0; j0 < o.groups + 2; j0 += kWave) {
+    // segments j0 + lane: rows, items
+    auto look = [&](int j0, int64_t &r0, int64_t &r1) {
         const int j = j0 + lane_id();
-        int64_t r0 = 0, r1 = 0;
+        r0 = r1 = 0;
         if (j <= o.groups + 1) {
             r0 = j == 0 ? 0 : o.at(j - 1);
             r1 = j == o.groups + 1 ? o.rows : o.at(j);
@@ -74,8 +82,21 @@ __device__ __forceinline__ Segment find_segment(const Offsets &o, int64_t step, 
         const bool group = j >= 1 && j <= o.groups;
         int64_t items = (r1 - r0 + step - 1) / step;
         if (EMPTY && items == 0) items = 1;
-        if (!(group || (ends && j <= o.groups + 1))) items = 0;
-        int64_t inc = items * per;
+        return group || (ends && j <= o.groups + 1) ? items * per : 0;
+    };
+    int64_t r0, r1, items = look(0, r0, r1);
+    if constexpr (SPREAD) {
+        int64_t all = (int64_t)wave_sum_u64((unsigned long long)items);
+        for (int j0 = kWave; j0 < o.groups + 2; j0 += kWave) {
+            int64_t q0, q1;
+            all += (int64_t)wave_sum_u64((unsigned long long)look(j0, q0, q1));
+        }
+        if (id >= all) return {-1, 0, 0, 0, 0};
+        id = xcd_tile(id, all);
+    }
+    int64_t base = 0;
+    for (int j0 = 0;;) {
+        int64_t inc = items;
 #pragma unroll
         for (int d = 1; d < kWave; d <<= 1) {
             const int64_t up = __shfl_up(inc, d, kWave);
@@ -85,12 +106,13 @@ __device__ __forceinline__ Segment find_segment(const Offsets &o, int64_t step, 
         const unsigned long long past = __ballot(inc > id);
         if (past) {
             const int l = __ffsll(past) - 1;
-            const int64_t first = lane_value(inc - items * per, l);
+            const int64_t first = lane_value(inc - items, l);
             return {j0 + l, lane_value(r0, l), lane_value(r1, l), id - first, first};
         }
         base = lane_value(inc, kWave - 1);
+        if ((j0 += kWave) >= o.groups + 2) return {-1, 0, 0, 0, 0};
+        items = look(j0, r0, r1);
     }
-    return {-1, 0, 0, 0, 0};
 }
 
 // ------------------------------------------------------------------ operands
@@ -354,19 +376,37 @@ __device__ __forceinline__ void tile_store(const f32x16 (&acc)[WT][WT], uint8_t 
 
 template <int WT> constexpr int kTileLds = 2 * 2 * 64 * WT * kLine;
 
-// C's tiles.  Tiles of a group go in blocks of eight along its rows, all of the columns for
-// each, so that operands are met again in a cache.
+// Where a segment's tile starts.  Tiles of a group go in blocks of eight along its rows, all of
+// the columns for each, so that operands are met again in a cache.
+__device__ __forceinline__ void place_tile(const Segment &s, int side, int tiles_n, int64_t &r0, int64_t &c0)
+{
+    const int64_t tiles = (s.r1 - s.r0 + side - 1) / side, block = s.local / (8 * tiles_n), rest = s.local - block * 8 * tiles_n;
+    const int64_t high = std::min<int64_t>(8, tiles - block * 8);
+    r0 = uniform(s.r0 + (block * 8 + rest % high) * side);
+    c0 = uniform(rest / high * side);
+}
+
+// Zeros in a tile of rows without a group.
+template <int SIDE, class T> __device__ void zero_tile(T *C, int64_t ldc, int64_t r0, int64_t r1, int64_t c0, int64_t c1)
+{
+    constexpr int E = kPiece<T>, LANES = SIDE / E;
+    for (int64_t r = r0 + threadIdx.x / LANES; r < std::min(r0 + SIDE, r1); r += 256 / LANES) {
+        const int64_t c = c0 + threadIdx.x % LANES * E;
+        if (c < c1) store_elems<T, E>(C + r * ldc + c, typename Elems<T, E>::type{}, c1 - c);
+    }
+}
+
+// C's tiles.
 template <class LA, class LB, class TO, int WT>
 __global__ __launch_bounds__(256, WT == 1 ? 4 : 2) void k_grouped(LA A, LB W, int64_t w_step, Offsets off, int64_t k, int64_t n, bool fill,
                                                                   int tiles_n, TO *__restrict__ C, int64_t ldc)
 {
     __shared__ __align__(1024) uint8_t lds[kTileLds<WT>];
     constexpr int SIDE = 64 * WT;
-    const Segment s = find_segment<false>(off, SIDE, tiles_n, fill, xcd_tile(blockIdx.x, gridDim.x));
+    const Segment s = find_segment<false, true>(off, SIDE, tiles_n, fill, blockIdx.x);
     if (s.index < 0) return;
-    const int64_t tiles = (s.r1 - s.r0 + SIDE - 1) / SIDE, block = s.local / (8 * tiles_n), rest = s.local - block * 8 * tiles_n;
-    const int64_t high = std::min<int64_t>(8, tiles - block * 8);
-    const int64_t r0 = s.r0 + (block * 8 + rest % high) * SIDE, c0 = rest / high * SIDE;
+    int64_t r0, c0;
+    place_tile(s, SIDE, tiles_n, r0, c0);
     f32x16 acc[WT][WT];
 #pragma unroll
     for (int i = 0; i < WT; i++)
@@ -380,6 +420,217 @@ __global__ __launch_bounds__(256, WT == 1 ? 4 : 2) void k_grouped(LA A, LB W, in
     tile_store<TO, WT>(acc, lds, C, ldc, r0, s.r1, c0, n);
 }
 
+// -------------------------------------------------------------- large tiles
+//
+// bf16 tiles of 256 x 256, a wave 128 x 128 of it: of what LDS serves in a cycle the
+// fragments take half then (all of it at 128 x 128).  Rows of whole aligned 16-byte pieces,
+// k in whole chunks.  A goes from memory to LDS without passing registers, two chunks ahead; W
+// comes through registers, where it is turned if its k is not contiguous, and is loaded a
+// chunk before it is stored.  The last quarter of a chunk is multiplied after the workgroup has
+// met, while the next one's first fragments are read.
+
+__device__ __forceinline__ __amdgpu_buffer_rsrc_t buffer_of(const void *p)
+{
+    return __builtin_amdgcn_make_buffer_rsrc(const_cast<void *>(p), 0, -1, 0x00020000);
+}
+
+// A: eight rows of a chunk a load, eight loads of a wave: rows 64 wave + 8 q .. + 7.  Offsets of
+// this lane's row and piece (in the order in which LDS wants them) from the tile's first row;
+// rows past the last one repeat it.
+struct TileLoad {
+    uint32_t at[8];
+    __device__ __forceinline__ void set(int64_t rows, int64_t ld)
+    {
+        const int wave = threadIdx.x / kWave, lane = threadIdx.x % kWave;
+#pragma unroll
+        for (int q = 0; q < 8; q++) {
+            const int row = 64 * wave + 8 * q + lane / 8, piece = lane % 8 ^ (row >> 1 & 7);
+            at[q] = (uint32_t)(std::min<int64_t>(row, rows - 1) * ld * 2) + piece * 16;
+        }
+    }
+    __device__ __forceinline__ void go(const __amdgpu_buffer_rsrc_t &from, uint32_t k_bytes, uint8_t *__restrict__ to) const
+    {
+        const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
+#pragma unroll
+        for (int q = 0; q < 8; q++)
+            __builtin_amdgcn_raw_ptr_buffer_load_lds(from, (__attribute__((address_space(3))) void *)(to + (64 * wave + 8 * q) * kLine), 16,
+                                                     at[q], k_bytes, 0, 0);
+    }
+};
+// W: eight neighbouring k of eight neighbouring columns in a thread (TURN: W is k x n), or of
+// eight columns 32 apart (n x k).
+template <bool TURN> struct TileWeights {
+    uint32_t at[TURN ? 1 : 8], step;
+    u32x4 v[8];
+    __device__ __forceinline__ void set(int64_t cols, int64_t ld)
+    {
+        const int64_t piece = threadIdx.x % 8, c = threadIdx.x / 8;
+        if constexpr (TURN) {
+            step = (uint32_t)ld * 2;
+            at[0] = (uint32_t)(piece * 8 * ld * 2 + std::min<int64_t>(c * 8, cols - 8) * 2);
+        } else {
+#pragma unroll
+            for (int i = 0; i < 8; i++) at[i] = (uint32_t)(std::min<int64_t>(c + 32 * i, cols - 1) * ld * 2 + piece * 16);
+        }
+    }
+    __device__ __forceinline__ void load(const __amdgpu_buffer_rsrc_t &from, uint32_t k_bytes)
+    {
+#pragma unroll
+        for (int e = 0; e < 8; e++)
+            v[e] = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(from, TURN ? at[0] + e * step : at[TURN ? 0 : e], k_bytes, 0));
+    }
+    __device__ __forceinline__ void store(uint8_t *__restrict__ to) const
+    {
+#pragma unroll
+        for (int i = 0; i < 8; i++) {
+            u32x4 o = v[i];
+            if constexpr (TURN)
+#pragma unroll
+                for (int e = 0; e < 4; e++)
+                    o[e] = __builtin_amdgcn_perm(v[2 * e + 1][i / 2], v[2 * e][i / 2], i % 2 ? 0x07060302 : 0x05040100);
+            *reinterpret_cast<u32x4 *>(piece_at(to, TURN ? threadIdx.x / 8 * 8 + i : threadIdx.x / 8 + 32 * i, threadIdx.x % 8)) = o;
+        }
+    }
+};
+
+struct TileFrags {
+    u32x4 a[4], b[4];
+    __device__ __forceinline__ void read(const uint8_t *a_from, const uint8_t *b_from, int q, int ra, int rb, int half, int swz)
+    {
+        const int p = ((2 * q + half) ^ swz) * 16;
+        // (in the order in which tile_multiply takes them)
+        a[0] = *reinterpret_cast<const u32x4 *>(a_from + p + ra * kLine);
+#pragma unroll
+        for (int i = 0; i < 4; i++) b[i] = *reinterpret_cast<const u32x4 *>(b_from + p + (rb + 32 * i) * kLine);
+#pragma unroll
+        for (int i = 1; i < 4; i++) a[i] = *reinterpret_cast<const u32x4 *>(a_from + p + (ra + 32 * i) * kLine);
+    }
+};
+__device__ __forceinline__ void tile_multiply(f32x16 (&acc)[4][4], const TileFrags &f)
+{
+#pragma unroll
+    for (int i = 0; i < 4; i++)
+#pragma unroll
+        for (int j = 0; j < 4; j++) acc[i][j] = multiply<u16>(f.b[j], f.a[i], acc[i][j]);
+}
+// Of the instructions up to the next sched_barrier: sixteen multiplications, an LDS read after
+// every other one (all four waves' reads would wait for each other behind every one), between
+// them V loads from memory and W LDS writes.
+template <int V, int W> __device__ __forceinline__ void interleave()
+{
+#pragma unroll
+    for (int i = 0; i < 8; i++) {
+        __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+        __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
+        __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+        if constexpr (V) __builtin_amdgcn_sched_group_barrier(0x010, V, 0);
+        if constexpr (W) __builtin_amdgcn_sched_group_barrier(0x200, W, 0);
+    }
+}
+
+struct TilePlace {
+    int ra, rb, half, swz;
+};
+// One chunk, which lies in a_from and b_from.  A's chunk after the next goes to a_to, W's next
+// one from registers to b_to, and the one after it, at kb, is loaded there.  held: the last
+// quarter of the chunk before (FIRST: there is none), on return this one's.
+template <bool TURN, bool FIRST>
+__device__ __forceinline__ void tile_chunk(uint8_t *__restrict__ a_to, uint8_t *__restrict__ b_to, const uint8_t *__restrict__ a_from,
+                                           const uint8_t *__restrict__ b_from, const __amdgpu_buffer_rsrc_t &ga,
+                                           const __amdgpu_buffer_rsrc_t &gb, const TileLoad &la, TileWeights<TURN> &lb, uint32_t ka,
+                                           uint32_t kb, const TilePlace &at, f32x16 (&acc)[4][4], TileFrags &held)
+{
+    TileFrags f;
+    f.read(a_from, b_from, 0, at.ra, at.rb, at.half, at.swz);
+    la.go(ga, ka, a_to);
+    if constexpr (!FIRST) {
+        tile_multiply(acc, held);
+        interleave<1, 0>();
+    }
+    __builtin_amdgcn_sched_barrier(0);
+    held.read(a_from, b_from, 1, at.ra, at.rb, at.half, at.swz);
+    tile_multiply(acc, f);
+    interleave<0, 0>();
+    __builtin_amdgcn_sched_barrier(0);
+    f.read(a_from, b_from, 2, at.ra, at.rb, at.half, at.swz);
+    lb.store(b_to);
+    tile_multiply(acc, held);
+    interleave<0, 1>();
+    __builtin_amdgcn_sched_barrier(0);
+    held.read(a_from, b_from, 3, at.ra, at.rb, at.half, at.swz);
+    lb.load(gb, kb);
+    tile_multiply(acc, f);
+    interleave<1, 0>();
+    __builtin_amdgcn_sched_barrier(0);
+}
+// A's chunk that is multiplied next has arrived (at most 16 loads are younger), this wave's LDS
+// operations are done, and so are all others'.  Not __syncthreads: it would wait for the loads to
+// LDS that are to be under way.
+__device__ __forceinline__ void tile_meet()
+{
+    __builtin_amdgcn_sched_barrier(0);
+    asm volatile("" ::: "memory");
+    __builtin_amdgcn_s_waitcnt(0x4070);  // vmcnt(16) lgkmcnt(0)
+    __builtin_amdgcn_s_barrier();
+    asm volatile("" ::: "memory");
+    __builtin_amdgcn_sched_barrier(0);
+}
+
+// kc: chunks of k.
+template <bool TURN, class TO>
+__global__ __launch_bounds__(256, 1) void k_grouped_large(const u16 *__restrict__ A, int64_t lda, const u16 *__restrict__ W, int64_t ldw,
+                                                        int64_t w_step, Offsets off, int kc, int64_t n, bool fill, int tiles_n,
+                                                        TO *__restrict__ C, int64_t ldc)
+{
+    constexpr int STAGE = 256 * kLine;
+    __shared__ __align__(1024) uint8_t lds[5 * STAGE];  // three of A, two of W
+    const Segment s = find_segment<false, true>(off, 256, tiles_n, fill, blockIdx.x);
+    if (s.index < 0) return;
+    int64_t r0, c0;
+    place_tile(s, 256, tiles_n, r0, c0);
+    if (s.index < 1 || s.index > off.groups) {
+        zero_tile<256>(C, ldc, r0, s.r1, c0, n);
+        return;
+    }
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave), lane = threadIdx.x % kWave;
+    const TilePlace at{wave / 2 * 128 + lane % 32, wave % 2 * 128 + lane % 32, lane / 32, lane >> 1 & 7};
+    const u16 *B = W + (s.index - 1) * w_step;
+    const __amdgpu_buffer_rsrc_t ga = buffer_of(A + r0 * lda), gb = buffer_of(TURN ? B + c0 : B + c0 * ldw);
+    const uint32_t sb = TURN ? (uint32_t)ldw * 2 * 64 : kLine;
+    auto chunk = [&](int c) { return (uint32_t)std::min(c, kc - 1); };  // (what is loaded past the last one is not used)
+    TileLoad la;
+    TileWeights<TURN> lb;
+    TileFrags held;
+    f32x16 acc[4][4];
+#pragma unroll
+    for (int i = 0; i < 4; i++)
+#pragma unroll
+        for (int j = 0; j < 4; j++) acc[i][j] = f32x16{};
+    la.set(s.r1 - r0, lda);
+    lb.set(n - c0, ldw);
+    uint8_t *a0 = lds, *a1 = lds + STAGE, *a2 = lds + 2 * STAGE, *b0 = lds + 3 * STAGE, *b1 = lds + 4 * STAGE;
+    la.go(ga, 0, a0);
+    lb.load(gb, 0);
+    lb.store(b0);
+    la.go(ga, chunk(1) * kLine, a1);
+    lb.load(gb, chunk(1) * sb);
+    tile_meet();
+    tile_chunk<TURN, true>(a2, b1, a0, b0, ga, gb, la, lb, chunk(2) * kLine, chunk(2) * sb, at, acc, held);
+#pragma unroll 1
+    for (int c = 1; c < kc; c++) {
+        uint8_t *t = a0;
+        a0 = a1, a1 = a2, a2 = t;
+        t = b0;
+        b0 = b1, b1 = t;
+        tile_meet();
+        tile_chunk<TURN, false>(a2, b1, a0, b0, ga, gb, la, lb, chunk(c + 2) * kLine, chunk(c + 2) * sb, at, acc, held);
+    }
+    tile_multiply(acc, held);
+    __builtin_amdgcn_s_waitcnt(0x0070);  // vmcnt(0) lgkmcnt(0): nothing is on its way to LDS any more
+    __syncthreads();
+    tile_store<TO, 4>(acc, lds, C, ldc, r0, s.r1, c0, n);
+}
+
 // dW: chunks of `per` rows of a group, a tile of it each; out is the chunk's a x b, or the
 // group's if a chunk is all of a group (per past the rows).
 template <class LA, class LG, int WT>
@@ -388,7 +639,7 @@ __global__ __launch_bounds__(256, WT == 1 ? 3 : 2) void k_grouped_grad(LA A, LG 
 {
     __shared__ __align__(1024) uint8_t lds[kTileLds<WT>];
     constexpr int SIDE = 64 * WT;
-    const Segment s = find_segment<true>(off, per, 1, false, blockIdx.x);
+    const Segment s = find_segment<true, false>(off, per, 1, false, blockIdx.x);
     if (s.index < 0) return;
     const int64_t k0 = s.r0 + s.local * per, k1 = std::min(k0 + per, s.r1);
     const int64_t a0 = (int64_t)(blockIdx.y / tiles_b) * SIDE, b0 = (int64_t)(blockIdx.y % tiles_b) * SIDE;
@@ -505,6 +756,24 @@ static int grouped_matmul(const Operand &A, int a_dtype, int64_t rows, const voi
         check_operand("C", C, rows, outw, ldc, csize);
         if (rows == 0) return;
         const hipStream_t s = (hipStream_t)stream;
+        // Large tiles where there are enough to fill the chip: rows of whole aligned pieces, k
+        // of whole chunks, offsets in a matrix of 32 bits.
+        const bool pieces = !A.saved && w_dtype == GS_BF16 && in % 64 == 0 && in >= 128 && A.ld % 8 == 0 && (uintptr_t)A.p % 16 == 0 &&
+                            ldw % 8 == 0 && w_step % 8 == 0 && (uintptr_t)W % 16 == 0 && (transpose || (n % 8 == 0 && n >= 8)) &&
+                            256 * A.ld < (1 << 30) && (transpose ? 256 : k) * ldw < (1 << 30);
+        const int64_t large_n = ceil_div(outw, 256), large = (ceil_div(rows, 256) + groups + 2) * large_n;
+        if (pieces && rows >= 128 * groups && ceil_div(rows, 256) * large_n >= 128 && large <= INT32_MAX / 256) {
+            auto run = [&](auto kernel, auto type) {
+                kernel<<<(unsigned)large, 256, 0, s>>>((const u16 *)A.p, A.ld, (const u16 *)W, ldw, w_step, off, (int)(in / 64), outw,
+                                                       fill != 0, (int)large_n, (decltype(type) *)C, ldc);
+            };
+            if (transpose)
+                c_dtype == GS_F32 ? run(k_grouped_large<false, float>, 0.0f) : run(k_grouped_large<false, u16>, u16(0));
+            else
+                c_dtype == GS_F32 ? run(k_grouped_large<true, float>, 0.0f) : run(k_grouped_large<true, u16>, u16(0));
+            GS_HIP(hipGetLastError());
+            return;
+        }
         const int wt = rows <= 64 * groups || outw <= 64 ? 1 : 2;
         const int64_t tiles_n = ceil_div(outw, 64 * wt), grid = (ceil_div(rows, 64 * wt) + groups + 2) * tiles_n;
         if (grid > INT32_MAX / 256) fail(GS_ERR_UNSUPPORTED, "the product has too many tiles");

@@ -218,6 +218,26 @@ def test_grouped_matmul(rows, k, n, offsets, dtype, back, a8):
     assert _around_is_nan(out, wide_out)
 
 
+@pytest.mark.parametrize("k", [128, 192, 320])
+@pytest.mark.parametrize("back", [False, True])
+@pytest.mark.parametrize("out", ["f32", "bf16"])
+def test_grouped_matmul_in_large_tiles(k, back, out):
+    """bf16 tiles of 256 x 256, rows and columns that end inside one, rows without a group."""
+    offsets, n, rows = [100, 100, 613, 614, 1638, 2090], 4104, 2100
+    rng = np.random.default_rng(k)
+    A = torch.from_numpy(rng.standard_normal((rows, k)).astype(np.float32)).bfloat16().to(DEV)
+    W = torch.from_numpy(rng.standard_normal((5, n, k) if back else (5, k, n)).astype(np.float32)).bfloat16().to(DEV)
+    off = torch.tensor(offsets, device=DEV)
+    want, M = oracle.grouped(_np(A), _np(W), offsets, back)
+    got = gs.grouped_matmul(A, W, off, transpose=back, dtype=TYPES[out])
+    _close(got, want, (2 * k + 4) * U * M + HALF[out] * np.abs(want))
+    keep = torch.full((rows, n), 7.0, dtype=TYPES[out], device=DEV)
+    gs.grouped_matmul(A, W, off, transpose=back, out=keep)
+    assert torch.equal(keep[100:2090], got[100:2090]) and (keep[:100] == 7).all() and (keep[2090:] == 7).all()
+    small = gs.grouped_matmul(A[:300], W, off.clamp(max=300), transpose=back, dtype=TYPES[out])
+    _close(small, want[:300], (2 * k + 4) * U * M[:300] + HALF[out] * np.abs(want[:300]))
+
+
 @pytest.mark.parametrize("rows,k,n,offsets", GROUPED + [(9000, 40, 24, [0, 3000, 3000, 8999, 9000]), (20000, 33, 65, [0, 20000])])
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
 @pytest.mark.parametrize("a8", [False, True])
