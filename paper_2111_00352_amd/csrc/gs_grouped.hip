@@ -67,6 +67,21 @@ __device__ __forceinline__ int64_t uniform(int64_t v)
 // ends: whether the segments without a group count.  EMPTY: a group without rows has `per` items too.
 // The item of workgroup `id`, SPREAD: so that each accelerator die has an equal contiguous
 // run of the items there are (a launch has more workgroups than that).
+template <bool EMPTY>
+__device__ __forceinline__ int64_t count_items(const Offsets &o, int64_t step, int64_t per, bool ends)
+{
+    int64_t all = 0;
+    for (int j = lane_id(); j < o.groups + 2; j += kWave) {
+        if (j == 0 || j > o.groups) {
+            const int64_t n = j == 0 ? o.at(0) : o.rows - o.at(o.groups);
+            if (ends) all += (n + step - 1) / step * per;
+        } else {
+            const int64_t n = o.at(j) - o.at(j - 1), items = n > 0 ? (n + step - 1) / step : 0;
+            all += (EMPTY && items == 0 ? 1 : items) * per;
+        }
+    }
+    return (int64_t)wave_sum_u64((unsigned long long)all);
+}
 template <bool EMPTY, bool SPREAD>
 __device__ __forceinline__ Segment find_segment(const Offsets &o, int64_t step, int64_t per, bool ends, int64_t id)
 {
@@ -86,11 +101,7 @@ __device__ __forceinline__ Segment find_segment(const Offsets &o, int64_t step, 
     };
     int64_t r0, r1, items = look(0, r0, r1);
     if constexpr (SPREAD) {
-        int64_t all = (int64_t)wave_sum_u64((unsigned long long)items);
-        for (int j0 = kWave; j0 < o.groups + 2; j0 += kWave) {
-            int64_t q0, q1;
-            all += (int64_t)wave_sum_u64((unsigned long long)look(j0, q0, q1));
-        }
+        const int64_t all = count_items<EMPTY>(o, step, per, ends);
         if (id >= all) return {-1, 0, 0, 0, 0};
         id = xcd_tile(id, all);
     }
@@ -631,6 +642,246 @@ __global__ __launch_bounds__(256, 1) void k_grouped_large(const u16 *__restrict_
     tile_store<TO, 4>(acc, lds, C, ldc, r0, s.r1, c0, n);
 }
 
+// ------------------------------------------------------------------ layers
+//
+// Many rows, up to 256 of k, bf16 on the matrix cores: bound by A and C.  A workgroup of eight
+// waves keeps 32 NT columns of a group's matrix in LDS, as the fragments that the instructions
+// take, and goes through a contiguous run of the rows; each wave takes 32 RB of them at a time
+// straight from memory into fragments (a lane 16 neighbouring k of its row), the next ones
+// loaded meanwhile.  A new matrix is put into LDS only where the run meets a new group.
+//
+// fp32 matrices (beside activations in 8 bits, whose values bf16 holds exactly) are cut into three
+// bf16 parts, whose sum they are from 2^-110 on: three exact products for one in fp32 at 16 times
+// its rate.
+
+constexpr int kPanelWaves = 8;
+constexpr int kPanelStage = 32 * (kLine + 16);  // bytes of a wave's way out through LDS
+
+// k of element i of step ks (16 of k) in half h of a wave.
+__device__ __forceinline__ int panel_k(int ks, int half) { return 32 * (ks / 2) + 16 * half + 8 * (ks % 2); }
+
+// Rows of A on their way: 32 of k (step j) of a row, 16 of them in this lane.
+struct SavedRows {
+    const uint8_t *codes, *scales;
+    int64_t code_pitch, scale_pitch;
+    float zero;  // the code of 0: signed codes are taken 128 higher
+    int k;
+    struct Row {
+        const uint8_t *codes, *scales;
+    };
+    struct Held {
+        u32x4 c;
+        int s;
+    };
+    __device__ __forceinline__ Row row(int64_t r, int half) const
+    {
+        return {codes + r * code_pitch + 16 * half, scales + r * scale_pitch};
+    }
+    __device__ __forceinline__ void load(Held &h, const Row &r, int j, int) const
+    {
+        h.c = u32x4{};
+        h.s = 0;
+        if (32 * j < k) {  // (the same for all lanes; codes behind the last column are 0)
+            h.c = *reinterpret_cast<const u32x4 *>(r.codes + 32 * j);
+            h.s = r.scales[j];
+        }
+    }
+    __device__ __forceinline__ void fragments(const Held &h, int, int, u32x4 (&f)[2]) const
+    {
+        const float s = mx_scale(h.s), z = -zero * s;
+        const uint32_t flip = zero != 0.0f ? 0x80808080u : 0u;
+#pragma unroll
+        for (int w = 0; w < 4; w++) {
+            const uint32_t c = h.c[w] ^ flip;
+            uint32_t v[4];
+#pragma unroll
+            for (int e = 0; e < 4; e++) v[e] = __float_as_uint(__builtin_fmaf((float)(c >> (8 * e) & 255), s, z));  // (exact)
+#pragma unroll
+            for (int e = 0; e < 2; e++) f[w / 2][w % 2 * 2 + e] = __builtin_amdgcn_perm(v[2 * e + 1], v[2 * e], 0x07060302);
+        }
+    }
+};
+struct Bf16Rows {
+    const u16 *p;
+    int64_t ld;
+    int k;  // at least 8
+    typedef const u16 *Row;
+    struct Held {
+        u32x4 v[2];
+    };
+    __device__ __forceinline__ Row row(int64_t r, int) const { return p + r * ld; }
+    // (the row's last 16 bytes for those that go past it)
+    __device__ __forceinline__ int at(int j, int half, int i) const { return std::min(32 * j + 16 * half + 8 * i, k - 8); }
+    __device__ __forceinline__ void load(Held &h, const Row &r, int j, int half) const
+    {
+#pragma unroll
+        for (int i = 0; i < 2; i++) h.v[i] = __builtin_bit_cast(u32x4, load_elems<u16, 8>(r + at(j, half, i), 8));
+    }
+    __device__ __forceinline__ void fragments(const Held &h, int j, int half, u32x4 (&f)[2]) const
+    {
+#pragma unroll
+        for (int i = 0; i < 2; i++) {
+            f[i] = h.v[i];
+            if (32 * j + 32 > k) {
+                RowPiece<u16> q;
+                q.v = __builtin_bit_cast(typename RowPiece<u16>::V, h.v[i]);
+                q.shift = 32 * j + 16 * half + 8 * i - at(j, half, i);
+                f[i] = __builtin_bit_cast(u32x4, q.get(0, k));
+            }
+        }
+    }
+};
+
+// Columns c0 .. of a matrix of T (transpose: of its rows) as fragments: 1 KB for each of P
+// parts of each 32 columns of each step of 16 k.
+template <class T, int J, int NT, int P>
+__device__ __forceinline__ void fill_panel(uint8_t *lds, const T *W, int64_t ld, bool transpose, int k, int64_t c0, int64_t n)
+{
+    for (int e = threadIdx.x; e < 2 * J * NT * kWave; e += kPanelWaves * kWave) {
+        const int lane = e % kWave, t = e / kWave % NT, ks = e / kWave / NT;
+        const int64_t c = c0 + 32 * t + lane % 32;
+        const int k0 = panel_k(ks, lane / 32);
+        uint32_t part[P][8];
+#pragma unroll
+        for (int i = 0; i < 8; i++) {
+            T v = T(0);
+            if (c < n && k0 + i < k) v = transpose ? W[c * ld + k0 + i] : W[(k0 + i) * ld + c];
+            float rest = to_f32(v);
+            const bool whole = fabsf(rest) == __builtin_inff();  // (infinity is all in the first part)
+#pragma unroll
+            for (int q = 0; q < P; q++) {
+                part[q][i] = __float_as_uint(rest);
+                rest -= __uint_as_float(part[q][i] & 0xffff0000u);
+                if (whole) rest = 0.0f;
+            }
+        }
+#pragma unroll
+        for (int q = 0; q < P; q++) {
+            u32x4 f;
+#pragma unroll
+            for (int i = 0; i < 4; i++) f[i] = __builtin_amdgcn_perm(part[q][2 * i + 1], part[q][2 * i], 0x07060302);
+            *reinterpret_cast<u32x4 *>(lds + ((ks * NT + t) * P + q) * 1024 + lane * 16) = f;
+        }
+    }
+}
+
+template <class Rows, class TW, class TO, int J, int NT, int RB, int P>
+__global__ __launch_bounds__(kPanelWaves * kWave, 2) void k_grouped_panel(Rows A, const TW *__restrict__ W, int64_t ldw, int64_t w_step,
+                                                                        bool transpose, Offsets off, int k, int64_t n, bool fill,
+                                                                        TO *__restrict__ C, int64_t ldc)
+{
+    constexpr int ROWS = kPanelWaves * 32 * RB, E = kPiece<TO>;
+    __shared__ __align__(1024) uint8_t lds[2 * J * NT * P * 1024 + kPanelWaves * kPanelStage];
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave), lane = threadIdx.x % kWave, half = lane / 32;
+    uint8_t *mine = lds + 2 * J * NT * P * 1024 + wave * kPanelStage;
+    const int64_t c0 = (int64_t)blockIdx.y * 32 * NT;
+    const int64_t all = uniform(count_items<false>(off, ROWS, 1, fill));
+    int64_t item = uniform(all * blockIdx.x / gridDim.x);
+    const int64_t last = uniform(all * (blockIdx.x + 1) / gridDim.x);
+    if (item >= last) return;
+    // this wave's rows of an item
+    struct Strip {
+        int64_t r0, r1;
+        int segment;
+    };
+    Segment seg = find_segment<false, false>(off, ROWS, 1, fill, item);
+    int64_t base = seg.r0 + seg.local * ROWS;
+    auto strip = [&] { return Strip{base + wave * 32 * RB, seg.r1, seg.index}; };
+    typename Rows::Held held[RB][J];
+    typename Rows::Row row[RB];
+    auto set_rows = [&](const Strip &s) {  // (rows past the last one repeat it; a strip without rows takes any)
+#pragma unroll
+        for (int i = 0; i < RB; i++)
+            row[i] = A.row(std::max<int64_t>(0, std::min(s.r0 + 32 * i + lane % 32, s.r1 - 1)), half);
+    };
+    auto load = [&](int j) {
+#pragma unroll
+        for (int i = 0; i < RB; i++) A.load(held[i][j], row[i], j, half);
+    };
+    Strip now = strip();
+    set_rows(now);
+#pragma unroll
+    for (int j = 0; j < J; j++) load(j);
+    int panel = -1;
+    for (; item < last; item++) {
+        const bool group = now.segment >= 1 && now.segment <= off.groups;
+        if (group && now.segment != panel) {
+            panel = now.segment;
+            __syncthreads();
+            fill_panel<TW, J, NT, P>(lds, W + (panel - 1) * w_step, ldw, transpose, k, c0, n);
+            __syncthreads();
+        }
+        Strip next = now;
+        if (item + 1 < last) {
+            base += ROWS;
+            if (base >= seg.r1) {
+                seg = find_segment<false, false>(off, ROWS, 1, fill, item + 1);
+                base = seg.r0 + seg.local * ROWS;
+            }
+            next = strip();
+        }
+        set_rows(next);
+        f32x16 acc[RB][NT];
+#pragma unroll
+        for (int i = 0; i < RB; i++)
+#pragma unroll
+            for (int t = 0; t < NT; t++) acc[i][t] = f32x16{};
+        if (group && now.r0 < now.r1) {
+#pragma unroll
+            for (int j = 0; j < J; j++) {
+                u32x4 a[RB][2];
+#pragma unroll
+                for (int i = 0; i < RB; i++) A.fragments(held[i][j], j, half, a[i]);
+                load(j);
+#pragma unroll
+                for (int h = 0; h < 2; h++)
+#pragma unroll
+                    for (int t = 0; t < NT; t++)
+#pragma unroll
+                        for (int q = P - 1; q >= 0; q--) {
+                            const u32x4 b = *reinterpret_cast<const u32x4 *>(lds + (((2 * j + h) * NT + t) * P + q) * 1024 + lane * 16);
+#pragma unroll
+                            for (int i = 0; i < RB; i++) acc[i][t] = multiply<u16>(b, a[i][h], acc[i][t]);
+                        }
+            }
+        } else {
+#pragma unroll
+            for (int j = 0; j < J; j++) load(j);
+        }
+        if (now.r0 < now.r1) {
+            // out through LDS, 128 bytes of a row at a time
+            constexpr int TILES = sizeof(TO) == 4 ? 1 : 2, PITCH = kLine + 16;
+#pragma unroll
+            for (int i = 0; i < RB; i++)
+#pragma unroll
+                for (int t = 0; t < NT; t += TILES) {
+#pragma unroll
+                    for (int u = 0; u < TILES; u++)
+#pragma unroll
+                        for (int g = 0; g < 4; g++) {
+                            typedef TO quad __attribute__((ext_vector_type(4)));
+                            const f32x16 &v = acc[i][t + u];
+                            *reinterpret_cast<quad *>(mine + lane % 32 * PITCH + (32 * u + 8 * g + 4 * half) * sizeof(TO)) =
+                                quad{from_f32<TO>(v[4 * g]), from_f32<TO>(v[4 * g + 1]), from_f32<TO>(v[4 * g + 2]), from_f32<TO>(v[4 * g + 3])};
+                        }
+                    __builtin_amdgcn_wave_barrier();  // (a wave's LDS operations keep their order)
+                    typename Elems<TO, E>::type out[4];
+#pragma unroll
+                    for (int q = 0; q < 4; q++)
+                        out[q] = *reinterpret_cast<const typename Elems<TO, E>::type *>(mine + (8 * q + lane / 8) * PITCH + lane % 8 * 16);
+                    __builtin_amdgcn_wave_barrier();
+                    const int64_t c = c0 + 32 * t + lane % 8 * E;
+#pragma unroll
+                    for (int q = 0; q < 4; q++) {
+                        const int64_t r = now.r0 + 32 * i + 8 * q + lane / 8;
+                        if (r < now.r1 && c < n) store_elems<TO, E, true, false>(C + r * ldc + c, out[q], n - c);
+                    }
+                }
+        }
+        now = next;
+    }
+}
+
 // dW: chunks of `per` rows of a group, a tile of it each; out is the chunk's a x b, or the
 // group's if a chunk is all of a group (per past the rows).
 template <class LA, class LG, int WT>
@@ -771,6 +1022,51 @@ static int grouped_matmul(const Operand &A, int a_dtype, int64_t rows, const voi
                 c_dtype == GS_F32 ? run(k_grouped_large<false, float>, 0.0f) : run(k_grouped_large<false, u16>, u16(0));
             else
                 c_dtype == GS_F32 ? run(k_grouped_large<true, float>, 0.0f) : run(k_grouped_large<true, u16>, u16(0));
+            GS_HIP(hipGetLastError());
+            return;
+        }
+        // Layers: bf16 operands or 8-bit rows, k up to 256, many rows of a group.
+        if (in >= 16 && in <= 256 && rows >= 1024 * groups && rows >= 16384 && (A.saved || w_dtype == GS_BF16)) {
+            const int j = (int)ceil_div(in, 32);
+            auto run = [&](auto rows_of, auto w, auto out, auto jc, auto nt, auto rb, auto parts) {
+                using TW = decltype(w);
+                using TO = decltype(out);
+                constexpr int J = decltype(jc)::value, NT = decltype(nt)::value, RB = decltype(rb)::value, P = decltype(parts)::value;
+                const int64_t panels = ceil_div(outw, 32 * NT);
+                const int64_t x = std::min<int64_t>(ceil_div(rows, kPanelWaves * 32 * RB) + groups + 2, std::max<int64_t>(32, 256 / panels));
+                k_grouped_panel<decltype(rows_of), TW, TO, J, NT, RB, P><<<dim3((unsigned)x, (unsigned)panels), kPanelWaves * kWave, 0, s>>>(
+                    rows_of, (const TW *)W, ldw, w_step, transpose != 0, off, (int)in, outw, fill != 0, (TO *)C, ldc);
+            };
+            auto with_j = [&](auto rows_of, auto w, auto out, auto parts) {
+                using std::integral_constant;
+                const integral_constant<int, 1> c1;
+                const integral_constant<int, 2> c2;
+                const integral_constant<int, 4> c4;
+                const integral_constant<int, 8> c8;
+                auto with_n = [&](auto jc, auto rb) {
+                    // (what LDS and registers hold)
+                    constexpr bool DENSE = std::is_same_v<decltype(rows_of), Bf16Rows>;
+                    if constexpr (decltype(jc)::value * decltype(parts)::value > 12 || (DENSE && decltype(jc)::value > 4))
+                        run(rows_of, w, out, jc, c2, rb, parts);
+                    else
+                        outw <= 64 ? run(rows_of, w, out, jc, c2, rb, parts) : run(rows_of, w, out, jc, c4, rb, parts);
+                };
+                constexpr bool DENSE = std::is_same_v<decltype(rows_of), Bf16Rows>;
+                const integral_constant<int, DENSE ? 1 : 2> rb4;
+                j <= 1 ? with_n(c1, c2) : j <= 2 ? with_n(c2, c2) : j <= 4 ? with_n(c4, rb4) : with_n(c8, c1);
+            };
+            auto with_out = [&](auto rows_of, auto w, auto parts) {
+                c_dtype == GS_F32 ? with_j(rows_of, w, 0.0f, parts) : with_j(rows_of, w, u16(0), parts);
+            };
+            const std::integral_constant<int, 1> one;
+            const std::integral_constant<int, 3> three;
+            if (A.saved) {
+                const SavedRows r{A.saved->codes, A.saved->scales, saved_code_pitch(in), saved_scale_pitch(in),
+                                  A.saved->act == GS_ACT_RELU ? 0.0f : 128.0f, (int)in};
+                w_dtype == GS_F32 ? with_out(r, 0.0f, three) : with_out(r, u16(0), one);
+            } else {
+                with_out(Bf16Rows{(const u16 *)A.p, A.ld, (int)in}, u16(0), one);
+            }
             GS_HIP(hipGetLastError());
             return;
         }

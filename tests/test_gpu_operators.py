@@ -218,6 +218,47 @@ def test_grouped_matmul(rows, k, n, offsets, dtype, back, a8):
     assert _around_is_nan(out, wide_out)
 
 
+LAYERS = [("bf16", False), ("bf16", True), ("f32", True)]  # W's type, A in 8 bits
+
+
+@pytest.mark.parametrize("k,n", [(16, 40), (31, 64), (47, 130), (64, 128), (100, 33), (128, 128), (255, 70), (256, 200)])
+@pytest.mark.parametrize("dtype,a8", LAYERS)
+@pytest.mark.parametrize("back", [False, True])
+def test_grouped_matmul_of_layers(k, n, dtype, a8, back):
+    """Many rows: matrices kept in LDS, groups that end inside a wave's rows, none, short and rows without one."""
+    offsets = [70, 70, 6000, 6001, 12345, 12345, 17990, 18000]
+    rows = 18100
+    A = _hidden(rows, k, k + n, "f32" if a8 else dtype).clamp(-1e6, 1e6)
+    rng = np.random.default_rng(k)
+    W = torch.from_numpy(rng.standard_normal((7, n, k) if back else (7, k, n)).astype(np.float32)).to(TYPES[dtype]).to(DEV)
+    off = torch.tensor(offsets, device=DEV)
+    Ad = gs.save_activation(A.to(DEV), "relu" if n % 2 else "none")[1] if a8 else _inside(A.to(DEV))[0]
+    want, M = oracle.grouped(_np(Ad.dequantize()) if a8 else _np(A), _np(W), offsets, back)
+    for out in ("f32", "bf16"):
+        got = gs.grouped_matmul(Ad, W, off, transpose=back, dtype=TYPES[out])
+        _close(got, want, (2 * 3 * k + 4) * U * M + HALF[out] * np.abs(want), out)  # (three products for an fp32 one)
+    keep, wide = _inside(torch.full((rows, n), 7.0, device=DEV))
+    gs.grouped_matmul(Ad, W, off, transpose=back, out=keep, dtype=torch.float32)
+    full = gs.grouped_matmul(Ad, W, off, transpose=back, dtype=torch.float32)
+    assert torch.equal(keep[70:18000], full[70:18000]) and (keep[:70] == 7).all() and (keep[18000:] == 7).all()
+    assert _around_is_nan(keep, wide)
+
+
+def test_grouped_layers_infinite_weights_and_unfinite_rows():
+    rows = 20000
+    A = torch.ones(rows, 64)
+    A[5, 3] = float("nan")
+    W = torch.ones(1, 64, 32)
+    W[0, 0, 1] = float("inf")
+    W[0, 7, 2] = float("nan")
+    W[0, :, 3] = 2.0 ** -100 * 1.2345678
+    off = torch.tensor([0, rows], device=DEV)
+    got = gs.grouped_matmul(gs.save_activation(A.to(DEV), "none")[1], W.to(DEV), off)
+    assert torch.isnan(got[5]).all() and torch.isinf(got[:5, 1]).all() and torch.isnan(got[:, 2]).all()
+    _close(got[:5, 3], np.full(5, 64 * float(W[0, 0, 3])), 400 * U * 64 * float(W[0, 0, 3]))
+    assert (got[:5, 0] == 64).all()
+
+
 @pytest.mark.parametrize("k", [128, 192, 320])
 @pytest.mark.parametrize("back", [False, True])
 @pytest.mark.parametrize("out", ["f32", "bf16"])
