@@ -248,47 +248,6 @@ template <class T> struct AcrossRows {
     }
 };
 
-// The same from 8-bit activations.
-template <class T> struct SavedAcrossRows {
-    typedef T type;
-    const uint8_t *codes, *scales;
-    int64_t code_pitch, scale_pitch;
-    CodeValue value;
-    template <int N> struct Bytes {
-        typedef std::conditional_t<N == 2, u16, uint32_t> type;
-    };
-    template <int ROWS> struct Held {
-        typename Bytes<ROWS / 32>::type c[kPiece<T>];
-        uint8_t s[kPiece<T>];
-    };
-    template <int ROWS> __device__ __forceinline__ void load(Held<ROWS> &h, int64_t r0, int64_t r1, int64_t k0, int64_t k1) const
-    {
-        constexpr int E = kPiece<T>, N = ROWS / 32;
-        static_assert(N == 2 || N == 4);
-        const int64_t k = k0 + threadIdx.x % 8 * E, r = r0 + threadIdx.x / 8 * N;
-#pragma unroll
-        for (int e = 0; e < E; e++) {
-            h.c[e] = 0;
-            h.s[e] = 0;
-            if (k + e < k1 && r < r1) {
-                h.c[e] = *reinterpret_cast<const typename Bytes<N>::type *>(codes + (k + e) * code_pitch + r);
-                h.s[e] = scales[(k + e) * scale_pitch + r / kMxBlock];
-            }
-        }
-    }
-    template <int ROWS> __device__ __forceinline__ void store(const Held<ROWS> &h, uint8_t *lds) const
-    {
-        constexpr int E = kPiece<T>, N = ROWS / 32;
-#pragma unroll
-        for (int i = 0; i < N; i++) {
-            typename Elems<T, E>::type v;
-#pragma unroll
-            for (int e = 0; e < E; e++) v[e] = from_f32<T>(value(h.c[e], i) * mx_scale(h.s[e]));
-            *reinterpret_cast<u32x4 *>(piece_at(lds, threadIdx.x / 8 * N + i, threadIdx.x % 8)) = __builtin_bit_cast(u32x4, v);
-        }
-    }
-};
-
 // --------------------------------------------------------------------- tile
 
 // c + b a^T over 32 bytes of k of 32 rows of either: a lane holds 16 bytes of row lane % 32.
@@ -882,25 +841,174 @@ __global__ __launch_bounds__(kPanelWaves * kWave, 2) void k_grouped_panel(Rows A
     }
 }
 
-// dW: chunks of `per` rows of a group, a tile of it each; out is the chunk's a x b, or the
-// group's if a chunk is all of a group (per past the rows).
-template <class LA, class LG, int WT>
-__global__ __launch_bounds__(256, WT == 1 ? 3 : 2) void k_grouped_grad(LA A, LG G, Offsets off, int64_t a, int64_t b, int64_t per,
-                                                                       int tiles_b, float *__restrict__ out)
+// ---------------------------------------------------------- weight gradients
+//
+// The summed index is the rows, along which neither operand is contiguous.  A workgroup of eight
+// waves makes a tile of 128 WA x 64 WB (all of a layer's gradient, so that each operand is read
+// once) from a run of a group's rows; a wave loads whole rows of a chunk, eight (fp32: four) of
+// them, N columns a lane, which are 16 bytes along k for each column when they are put into LDS.
+// Bound by the loads: two chunks are under way in registers while a third is multiplied.
+// Runs end in partial products, which a second launch adds in order.
+
+constexpr int kGradThreads = 512;
+
+// Place of piece p of row r: writes of lanes whose rows are 1, 2 or 4 apart and reads of
+// neighbouring rows both spread over LDS's banks.
+__device__ __forceinline__ uint8_t *grad_piece(uint8_t *lds, int row, int piece)
 {
-    __shared__ __align__(1024) uint8_t lds[kTileLds<WT>];
-    constexpr int SIDE = 64 * WT;
+    return lds + row * kLine + ((piece ^ ((row >> 1 ^ row >> 4) & 7)) << 4);
+}
+
+// Columns c0 .. c0 + 64 N - 1 of rows: a lane's are `at` .. at + N - 1.
+template <class T, int N> struct GradDense {
+    typedef T type;
+    const T *p;
+    int64_t ld;
+    int64_t width;
+    struct Held {
+        typename Elems<T, N>::type v[kPiece<T>];
+    };
+    // (the last columns for lanes that would go past them: several lanes then hold the same)
+    __device__ __forceinline__ int64_t column(int64_t c0) const
+    {
+        return std::max<int64_t>(0, std::min(c0 + threadIdx.x % kWave * N, width - N));
+    }
+    __device__ __forceinline__ void load(Held &h, int e, int64_t row, int64_t at) const
+    {
+        h.v[e] = load_elems<T, N>(p + row * ld + at, width - at);
+    }
+    __device__ __forceinline__ void none(Held &h, int e) const { h.v[e] = typename Elems<T, N>::type{}; }
+    __device__ __forceinline__ u32x4 column_of(const Held &h, int i) const { return turned<T, N>(h.v, i); }
+};
+template <class T, int N> struct GradSaved {
+    typedef T type;
+    const uint8_t *codes, *scales;
+    int64_t code_pitch, scale_pitch;
+    CodeValue value;
+    typedef std::conditional_t<N == 1, uint8_t, std::conditional_t<N == 2, u16, uint32_t>> Word;
+    struct Held {
+        Word c[kPiece<T>];
+        uint8_t s[kPiece<T>];
+    };
+    __device__ __forceinline__ int64_t column(int64_t c0) const
+    {
+        return std::min<int64_t>(c0 + threadIdx.x % kWave * N, code_pitch - N);
+    }
+    __device__ __forceinline__ void load(Held &h, int e, int64_t row, int64_t at) const
+    {
+        h.c[e] = *reinterpret_cast<const Word *>(codes + row * code_pitch + at);
+        h.s[e] = scales[row * scale_pitch + at / kMxBlock];
+    }
+    __device__ __forceinline__ void none(Held &h, int e) const
+    {
+        h.c[e] = 0;
+        h.s[e] = 0;
+    }
+    __device__ __forceinline__ u32x4 column_of(const Held &h, int i) const
+    {
+        typename Elems<T, kPiece<T>>::type v;
+#pragma unroll
+        for (int e = 0; e < kPiece<T>; e++) v[e] = from_f32<T>(value(h.c[e], i) * mx_scale(h.s[e]));
+        return __builtin_bit_cast(u32x4, v);
+    }
+};
+
+// Chunks of `per` rows of a group, a tile of it each; out is the chunk's a x b (one chunk a
+// group: the group's).  A's lanes hold 2 WA columns, G's WB.
+template <class LA, class LG, int WA, int WB>
+__global__ __launch_bounds__(kGradThreads, 2) void k_grouped_grad(LA A, LG G, Offsets off, int64_t a, int64_t b, int64_t per, int tiles_b,
+                                                                 float *__restrict__ out)
+{
+    using T = typename LA::type;
+    constexpr int SA = 128 * WA, SB = 64 * WB, STAGE = (SA + SB) * kLine, E = kPiece<T>;
+    __shared__ __align__(1024) uint8_t lds[2 * STAGE];
     const Segment s = find_segment<true, false>(off, per, 1, false, blockIdx.x);
     if (s.index < 0) return;
-    const int64_t k0 = s.r0 + s.local * per, k1 = std::min(k0 + per, s.r1);
-    const int64_t a0 = (int64_t)(blockIdx.y / tiles_b) * SIDE, b0 = (int64_t)(blockIdx.y % tiles_b) * SIDE;
-    f32x16 acc[WT][WT];
+    const int64_t k0 = uniform(s.r0 + s.local * per), k1 = uniform(std::min(s.r0 + (s.local + 1) * per, s.r1));
+    const int64_t a0 = (int64_t)(blockIdx.y / tiles_b) * SA, b0 = (int64_t)(blockIdx.y % tiles_b) * SB;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave), lane = threadIdx.x % kWave, half = lane / 32;
+    const int64_t ca = A.column(a0), cb = G.column(b0);
+    struct Held {
+        typename LA::Held a;
+        typename LG::Held b;
+    } h0, h1;
+    auto load = [&](Held &h, int64_t k) {
+        k += wave * E;
+        if (k + E <= k1) {
 #pragma unroll
-    for (int i = 0; i < WT; i++)
+            for (int e = 0; e < E; e++) {
+                A.load(h.a, e, k + e, ca);
+                G.load(h.b, e, k + e, cb);
+            }
+        } else {
 #pragma unroll
-        for (int j = 0; j < WT; j++) acc[i][j] = f32x16{};
-    tile_sums<LA, LG, WT>(A, G, a0, a, b0, b, k0, k1, lds, acc);
-    tile_store<float, WT>(acc, lds, out + (int64_t)blockIdx.x * a * b, b, a0, a, b0, b);
+            for (int e = 0; e < E; e++) {
+                A.none(h.a, e);
+                G.none(h.b, e);
+                if (k + e < k1) {
+                    A.load(h.a, e, k + e, ca);
+                    G.load(h.b, e, k + e, cb);
+                }
+            }
+        }
+    };
+    // (a lane moved back from the end of the rows may hold columns before the tile's first)
+    const int la = (int)(ca - a0), lb = (int)(cb - b0);
+    auto store = [&](const Held &h, uint8_t *to) {
+#pragma unroll
+        for (int i = 0; i < 2 * WA; i++)
+            if (la + i >= 0) *reinterpret_cast<u32x4 *>(grad_piece(to, la + i, wave)) = A.column_of(h.a, i);
+#pragma unroll
+        for (int i = 0; i < WB; i++)
+            if (lb + i >= 0) *reinterpret_cast<u32x4 *>(grad_piece(to + SA * kLine, lb + i, wave)) = G.column_of(h.b, i);
+    };
+    f32x16 acc[WA][WB];
+#pragma unroll
+    for (int i = 0; i < WA; i++)
+#pragma unroll
+        for (int j = 0; j < WB; j++) acc[i][j] = f32x16{};
+    const int ra = wave / 2 * 32 * WA + lane % 32, rb = wave % 2 * 32 * WB + lane % 32;
+    auto work = [&](uint8_t *from) {
+#pragma unroll
+        for (int q = 0; q < 4; q++) {
+            u32x4 fa[WA], fb[WB];
+#pragma unroll
+            for (int i = 0; i < WA; i++) fa[i] = *reinterpret_cast<const u32x4 *>(grad_piece(from, ra + 32 * i, 2 * q + half));
+#pragma unroll
+            for (int j = 0; j < WB; j++) fb[j] = *reinterpret_cast<const u32x4 *>(grad_piece(from + SA * kLine, rb + 32 * j, 2 * q + half));
+#pragma unroll
+            for (int i = 0; i < WA; i++)
+#pragma unroll
+                for (int j = 0; j < WB; j++) acc[i][j] = multiply<T>(fb[j], fa[i], acc[i][j]);
+        }
+    };
+    constexpr int64_t STEP = kChunk<T>;
+    load(h0, k0);
+    load(h1, k0 + STEP);
+    store(h0, lds);
+    __syncthreads();
+    for (int64_t k = k0; k < k1; k += 2 * STEP) {
+        load(h0, k + 2 * STEP);
+        work(lds);
+        store(h1, lds + STAGE);
+        __syncthreads();
+        load(h1, k + 3 * STEP);
+        if (k + STEP < k1) work(lds + STAGE);
+        store(h0, lds);
+        __syncthreads();
+    }
+    float *to = out + (int64_t)blockIdx.x * a * b;
+#pragma unroll
+    for (int i = 0; i < WA; i++)
+#pragma unroll
+        for (int j = 0; j < WB; j++)
+#pragma unroll
+            for (int g = 0; g < 4; g++) {
+                const int64_t r = a0 + ra + 32 * i, c = b0 + wave % 2 * 32 * WB + 32 * j + 8 * g + 4 * half;
+                const f32x16 &v = acc[i][j];
+                if (r < a && c < b)
+                    store_elems<float, 4>(to + r * b + c, typename Elems<float, 4>::type{v[4 * g], v[4 * g + 1], v[4 * g + 2], v[4 * g + 3]}, b - c);
+            }
 }
 // The chunks of a group added in order: 256 threads, four elements each; blockIdx.y the group.
 __global__ __launch_bounds__(256) void k_grouped_join(const float *__restrict__ part, Offsets off, int64_t ab, int64_t per,
@@ -923,9 +1031,14 @@ __global__ __launch_bounds__(256) void k_grouped_join(const float *__restrict__ 
     if (e >= ab) return;
     float4 s = make_float4(0, 0, 0, 0);
     const int64_t end = std::min(first + mine, all);  // (offsets that descend: no more than there are)
-    for (int64_t c = first; c < end; c++) {
-        const auto v = load_elems<float, 4>(part + c * ab + e, ab - e);
-        s.x += v[0], s.y += v[1], s.z += v[2], s.w += v[3];
+    constexpr int U = 8;  // partials in flight
+    for (int64_t c = first; c < end; c += U) {
+        typename Elems<float, 4>::type v[U];
+#pragma unroll
+        for (int u = 0; u < U; u++) v[u] = load_elems<float, 4>(part + std::min(c + u, end - 1) * ab + e, ab - e);
+#pragma unroll
+        for (int u = 0; u < U; u++)
+            if (c + u < end) s.x += v[u][0], s.y += v[u][1], s.z += v[u][2], s.w += v[u][3];
     }
     store_elems<float, 4>(out + blockIdx.y * ab + e, typename Elems<float, 4>::type{s.x, s.y, s.z, s.w}, ab - e);
 }
@@ -949,20 +1062,21 @@ struct Operand {  // dense, or saved
     const gs_saved *saved;
 };
 
-// Rows of a chunk, and how many chunks there can be: enough workgroups to fill the chip
-// twice, chains of at most 8,192 rows.
+// Rows of a run, and how many runs there can be: a workgroup for each compute unit, chains of
+// at most 8,192 rows.
 struct GroupedGradPlan {
     int64_t per, chunks, tiles_a, tiles_b;
     bool direct;
-    int wt;
+    int wa, wb;
 };
 GroupedGradPlan grouped_grad_plan(int64_t rows, int64_t groups, int64_t a, int64_t b)
 {
     GroupedGradPlan p;
-    p.wt = a <= 64 && b <= 64 ? 1 : 2;
-    p.tiles_a = ceil_div(a, 64 * p.wt);
-    p.tiles_b = ceil_div(b, 64 * p.wt);
-    const int64_t tiles = p.tiles_a * p.tiles_b, want = std::max<int64_t>(1, 1024 / tiles);
+    p.wa = a <= 128 ? 1 : 2;
+    p.wb = b <= 64 ? 1 : 2;
+    p.tiles_a = ceil_div(a, 128 * p.wa);
+    p.tiles_b = ceil_div(b, 64 * p.wb);
+    const int64_t tiles = p.tiles_a * p.tiles_b, want = std::max<int64_t>(1, 256 / tiles);
     p.per = std::min<int64_t>(8192, std::max<int64_t>(256, ceil_div(ceil_div(rows, want), 64) * 64));
     // (what partial sums would take: at most 1 GB of them)
     const int64_t most = std::max<int64_t>(1, ((int64_t)1 << 28) / (a * b));
@@ -1125,24 +1239,27 @@ static int grouped_weight_grad(const Operand &A, int a_dtype, int64_t rows, int6
         if (p.tiles_a * p.tiles_b > 65535) fail(GS_ERR_UNSUPPORTED, "the product has too many tiles");
         const hipStream_t s = (hipStream_t)stream;
         float *part = p.direct ? out : (float *)work;
-        auto go = [&](auto la, auto lg) {
-            using LA = decltype(la);
-            using LG = decltype(lg);
-            auto run = [&](auto kernel) {
-                kernel<<<dim3((unsigned)p.chunks, (unsigned)(p.tiles_a * p.tiles_b)), 256, 0, s>>>(la, lg, off, a, b, p.per,
-                                                                                                 (int)p.tiles_b, part);
-            };
-            p.wt == 1 ? run(k_grouped_grad<LA, LG, 1>) : run(k_grouped_grad<LA, LG, 2>);
+        auto go = [&](auto la, auto lg, auto wa, auto wb) {
+            k_grouped_grad<decltype(la), decltype(lg), decltype(wa)::value, decltype(wb)::value>
+                <<<dim3((unsigned)p.chunks, (unsigned)(p.tiles_a * p.tiles_b)), kGradThreads, 0, s>>>(la, lg, off, a, b, p.per,
+                                                                                                    (int)p.tiles_b, part);
+        };
+        auto with_tile = [&](auto type, auto wa, auto wb) {
+            using T = decltype(type);
+            constexpr int WA = decltype(wa)::value, WB = decltype(wb)::value;
+            if (p.wa != WA || p.wb != WB) return;
+            const GradDense<T, WB> g{(const T *)G, ldg, b};
+            if (A.saved)
+                go(GradSaved<T, 2 * WA>{A.saved->codes, A.saved->scales, saved_code_pitch(a), saved_scale_pitch(a),
+                                        {A.saved->act == GS_ACT_RELU}},
+                   g, wa, wb);
+            else
+                go(GradDense<T, 2 * WA>{(const T *)A.p, A.ld, a}, g, wa, wb);
         };
         auto with_type = [&](auto type) {
-            using T = decltype(type);
-            const AcrossRows<T> g{(const T *)G, ldg};
-            if (A.saved)
-                go(SavedAcrossRows<T>{A.saved->codes, A.saved->scales, saved_code_pitch(a), saved_scale_pitch(a),
-                                      {A.saved->act == GS_ACT_RELU}},
-                   g);
-            else
-                go(AcrossRows<T>{(const T *)A.p, A.ld}, g);
+            const std::integral_constant<int, 1> one;
+            const std::integral_constant<int, 2> two;
+            with_tile(type, one, one), with_tile(type, one, two), with_tile(type, two, one), with_tile(type, two, two);
         };
         dtype == GS_F32 ? with_type(0.0f) : with_type(u16(0));
         GS_HIP(hipGetLastError());
