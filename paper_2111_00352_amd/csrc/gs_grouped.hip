@@ -217,10 +217,21 @@ template <class T> struct SavedAlongRows {
 // 16 bytes of column c of E rows of `N` columns.
 template <class T, int N> __device__ __forceinline__ u32x4 turned(const typename Elems<T, N>::type (&v)[kPiece<T>], int c)
 {
-    typename Elems<T, kPiece<T>>::type o;
+    u32x4 o;
+    if constexpr (sizeof(T) == 4) {
 #pragma unroll
-    for (int e = 0; e < kPiece<T>; e++) o[e] = v[e][c];
-    return __builtin_bit_cast(u32x4, o);
+        for (int e = 0; e < 4; e++) o[e] = __float_as_uint(v[e][c]);
+    } else if constexpr (N == 1) {
+#pragma unroll
+        for (int e = 0; e < 4; e++) o[e] = v[2 * e][0] | (uint32_t)v[2 * e + 1][0] << 16;
+    } else {  // halves of two words each
+        typedef uint32_t words __attribute__((ext_vector_type(N / 2)));
+#pragma unroll
+        for (int e = 0; e < 4; e++)
+            o[e] = __builtin_amdgcn_perm(__builtin_bit_cast(words, v[2 * e + 1])[c / 2], __builtin_bit_cast(words, v[2 * e])[c / 2],
+                                         c % 2 ? 0x07060302 : 0x05040100);
+    }
+    return o;
 }
 
 // k is the matrix's row: element (r, k) at p[k * ld + r].  A thread takes E neighbouring k of
@@ -388,6 +399,148 @@ __global__ __launch_bounds__(256, WT == 1 ? 4 : 2) void k_grouped(LA A, LB W, in
         tile_sums<LA, LB, WT>(A, B, r0, s.r1, c0, n, 0, k, lds, acc);
     }
     tile_store<TO, WT>(acc, lds, C, ldc, r0, s.r1, c0, n);
+}
+
+// ------------------------------------------------------------------ few rows
+//
+// Up to 32 rows of a group a workgroup: bound by reading the groups' matrices.  Four waves share
+// 32 N columns and split k, a step of two pieces (16 in bf16, 8 in fp32) each at a time; a lane
+// loads the fragments of its N columns straight from memory, turned in registers where k is the
+// matrix's row, two steps ahead.  The waves' sums meet in LDS.
+
+constexpr int kFewWaves = 4;
+
+// 16 bytes along k of a row of A, from k on.
+template <class T> __device__ __forceinline__ u32x4 row_piece(const AlongRows<T> &A, int64_t r, int64_t k, int64_t k1)
+{
+    return __builtin_bit_cast(u32x4, load_elems<T, kPiece<T>>(A.p + r * A.ld + k, k1 - k));
+}
+template <class T> __device__ __forceinline__ u32x4 row_piece(const SavedAlongRows<T> &A, int64_t r, int64_t k, int64_t k1)
+{
+    constexpr int E = kPiece<T>;
+    typename Elems<T, E>::type v{};
+    if (k < k1) {  // (codes behind the last column are 0)
+        const auto c = *reinterpret_cast<const typename Codes<E>::type *>(A.codes + r * A.code_pitch + k);
+        const float s = mx_scale(A.scales[r * A.scale_pitch + k / kMxBlock]);
+#pragma unroll
+        for (int e = 0; e < E; e++) v[e] = from_f32<T>(A.value(code_word<E>(c, e / 4), e % 4) * s);
+    }
+    return __builtin_bit_cast(u32x4, v);
+}
+
+template <class LA, class T, bool TURN, int N, class TO>
+__global__ __launch_bounds__(kFewWaves * kWave, 3) void k_grouped_few(LA A, const T *__restrict__ W, int64_t ldw, int64_t w_step, Offsets off,
+                                                                    int64_t k, int64_t n, bool fill, int tiles_n, TO *__restrict__ C,
+                                                                    int64_t ldc)
+{
+    constexpr int E = kPiece<T>, STEP = 2 * E, SIDE = 32 * N;
+    __shared__ float red[kFewWaves][16][kWave];
+    const Segment s = find_segment<false, true>(off, 32, tiles_n, fill, blockIdx.x);
+    if (s.index < 0) return;
+    const int64_t r0 = uniform(s.r0 + s.local / tiles_n * 32), c0 = uniform(s.local % tiles_n * SIDE);
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave), lane = threadIdx.x % kWave, half = lane / 32;
+    const int64_t rows = std::min<int64_t>(32, s.r1 - r0);
+    if (s.index < 1 || s.index > off.groups) {
+        for (int i = threadIdx.x; i < 32 * SIDE; i += kFewWaves * kWave)
+            if (i / SIDE < rows && c0 + i % SIDE < n) C[(r0 + i / SIDE) * ldc + c0 + i % SIDE] = TO(0);
+        return;
+    }
+    const T *B = W + (s.index - 1) * w_step;
+    const int64_t row = r0 + std::min<int64_t>(lane % 32, rows - 1);
+    // A lane's columns (n >= N).  TURN: N neighbouring ones, moved back from the end (several
+    // lanes then have the same); else N of them 32 apart, the last one for those past it.
+    auto column = [&](int l, int i) -> int64_t {
+        if constexpr (TURN)
+            return std::min(c0 + l * N, n - N) + i;
+        else
+            return std::min(c0 + l + 32 * i, n - 1);
+    };
+    struct Step {
+        u32x4 a;
+        typename Elems<T, N>::type v[TURN ? E : 1];
+        u32x4 w[TURN ? 1 : N];
+    };
+    const T *base[TURN ? 1 : N];
+#pragma unroll
+    for (int i = 0; i < (TURN ? 1 : N); i++) base[i] = B + (TURN ? column(lane % 32, 0) + half * E * ldw : column(lane % 32, i) * ldw + half * E);
+    auto load = [&](Step &t, int64_t at) {  // whole steps
+        t.a = row_piece(A, row, at + half * E, at + STEP);
+        if constexpr (TURN) {
+            const T *p = base[0] + at * ldw;
+#pragma unroll
+            for (int e = 0; e < E; e++) t.v[e] = load_elems<T, N, true>(p + e * ldw, N);
+        } else {
+#pragma unroll
+            for (int i = 0; i < N; i++) t.w[i] = __builtin_bit_cast(u32x4, load_elems<T, E, true>(base[i] + at, E));
+        }
+    };
+    auto load_end = [&](Step &t, int64_t at) {  // zeros from k on
+        const int64_t ka = at + half * E;
+        t.a = row_piece(A, row, ka, k);
+        if constexpr (TURN) {
+#pragma unroll
+            for (int e = 0; e < E; e++) t.v[e] = load_elems<T, N>(base[0] + (at + e) * ldw, ka + e < k ? N : 0);
+        } else {
+#pragma unroll
+            for (int i = 0; i < N; i++) t.w[i] = __builtin_bit_cast(u32x4, load_elems<T, E>(base[i] + at, k - ka));
+        }
+    };
+    f32x16 acc[N];
+#pragma unroll
+    for (int i = 0; i < N; i++) acc[i] = f32x16{};
+    auto work = [&](const Step &t) {
+#pragma unroll
+        for (int i = 0; i < N; i++) {
+            if constexpr (TURN)
+                acc[i] = multiply<T>(turned<T, N>(t.v, i), t.a, acc[i]);
+            else
+                acc[i] = multiply<T>(t.w[i], t.a, acc[i]);
+        }
+    };
+    constexpr int64_t NEXT = kFewWaves * STEP;
+    const int64_t whole = k - STEP;  // the last place a whole step can start at
+    Step t0, t1, t2;
+    int64_t at = wave * STEP;
+    if (at <= whole) load(t0, at);
+    if (at + NEXT <= whole) load(t1, at + NEXT);
+    for (; at + 2 * NEXT <= whole; at += 3 * NEXT) {
+        load(t2, at + 2 * NEXT);
+        work(t0);
+        if (at + 3 * NEXT <= whole) load(t0, at + 3 * NEXT);
+        work(t1);
+        if (at + 4 * NEXT <= whole) load(t1, at + 4 * NEXT);
+        work(t2);
+    }
+    if (at <= whole) {
+        work(t0);
+        at += NEXT;
+        if (at <= whole) {
+            work(t1);
+            at += NEXT;
+        }
+    }
+    if (at < k) {
+        load_end(t0, at);
+        work(t0);
+    }
+    // Sums of the matrix's columns 8 (e / 4) + 4 half + e % 4 (of 32) by A's row lane % 32.
+#pragma unroll
+    for (int i = 0; i < N; i++) {
+        if (i) __syncthreads();
+#pragma unroll
+        for (int e = 0; e < 16; e++) red[wave][e][lane] = acc[i][e];
+        __syncthreads();
+#pragma unroll
+        for (int q = 0; q < 16 / kFewWaves; q++) {
+            const int e = wave * (16 / kFewWaves) + q;
+            float v = 0.0f;
+#pragma unroll
+            for (int w = 0; w < kFewWaves; w++) v += red[w][e][lane];
+            const int l = 8 * (e / 4) + 4 * half + e % 4;
+            const int64_t c = column(l, i);
+            if (lane % 32 < rows && c < n) C[(r0 + lane % 32) * ldc + c] = from_f32<TO>(v);
+        }
+    }
 }
 
 // -------------------------------------------------------------- large tiles
@@ -1181,6 +1334,41 @@ static int grouped_matmul(const Operand &A, int a_dtype, int64_t rows, const voi
             } else {
                 with_out(Bf16Rows{(const u16 *)A.p, A.ld, (int)in}, u16(0), one);
             }
+            GS_HIP(hipGetLastError());
+            return;
+        }
+        // Few rows: the matrices are what is read.  Narrow tiles while there would be fewer than two
+        // workgroups a compute unit.
+        if (rows <= 32 * groups && in >= 64 && outw >= 4) {
+            auto run = [&](auto la, auto type, auto out, auto turn, auto cols) {
+                using T = decltype(type);
+                using TO = decltype(out);
+                constexpr int N = decltype(cols)::value;
+                const int64_t tiles_n = ceil_div(outw, 32 * N), grid = (ceil_div(rows, 32) + groups + 2) * tiles_n;
+                if (grid > INT32_MAX / 512) fail(GS_ERR_UNSUPPORTED, "the product has too many tiles");
+                k_grouped_few<decltype(la), T, decltype(turn)::value, N, TO><<<(unsigned)grid, kFewWaves * kWave, 0, s>>>(
+                    la, (const T *)W, ldw, w_step, off, in, outw, fill != 0, (int)tiles_n, (TO *)C, ldc);
+            };
+            const bool wide = std::min(rows, groups) * ceil_div(outw, 128) >= 512;
+            auto with_n = [&](auto la, auto type, auto out, auto turn) {
+                wide ? run(la, type, out, turn, std::integral_constant<int, 4>{}) : run(la, type, out, turn, std::integral_constant<int, 2>{});
+            };
+            auto with_out = [&](auto la, auto type) {
+                if (c_dtype == GS_F32)
+                    transpose ? with_n(la, type, 0.0f, std::false_type{}) : with_n(la, type, 0.0f, std::true_type{});
+                else
+                    transpose ? with_n(la, type, u16(0), std::false_type{}) : with_n(la, type, u16(0), std::true_type{});
+            };
+            auto with_type = [&](auto type) {
+                using T = decltype(type);
+                if (A.saved)
+                    with_out(SavedAlongRows<T>{A.saved->codes, A.saved->scales, saved_code_pitch(in), saved_scale_pitch(in),
+                                               {A.saved->act == GS_ACT_RELU}},
+                             type);
+                else
+                    with_out(AlongRows<T>{(const T *)A.p, A.ld}, type);
+            };
+            w_dtype == GS_F32 ? with_type(0.0f) : with_type(u16(0));
             GS_HIP(hipGetLastError());
             return;
         }

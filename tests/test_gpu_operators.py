@@ -218,6 +218,30 @@ def test_grouped_matmul(rows, k, n, offsets, dtype, back, a8):
     assert _around_is_nan(out, wide_out)
 
 
+@pytest.mark.parametrize("k,n", [(64, 4), (71, 131), (256, 129), (1000, 520), (4096, 64), (67, 2100)])
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("back", [False, True])
+@pytest.mark.parametrize("a8", [False, True])
+def test_grouped_matmul_of_few_rows(k, n, dtype, back, a8):
+    """One to 70 rows of a group: the reads of its matrix are shared, k and columns end inside a step."""
+    if back:
+        k, n = n, k
+    offsets = [0, 1, 1, 3, 36, 106, 107, 107, 108, 110]
+    A = _hidden(111, n if back else k, k + n, dtype).clamp(-1e6, 1e6)
+    rng = np.random.default_rng(k)
+    W = torch.from_numpy(rng.standard_normal((9, k, n)).astype(np.float32)).to(TYPES[dtype]).to(DEV)
+    off = torch.tensor(offsets, device=DEV)
+    Ad = gs.save_activation(A.to(DEV), "none" if n % 2 else "relu")[1] if a8 else _inside(A.to(DEV))[0]
+    want, M = oracle.grouped(_np(Ad.dequantize()) if a8 else _np(A), _np(W), offsets, back)
+    for out in ("f32", "bf16"):
+        got = gs.grouped_matmul(Ad, W, off, transpose=back, dtype=TYPES[out])
+        _close(got, want, (2 * (n if back else k) + 20) * U * M + HALF[out] * np.abs(want), out)
+    keep, wide = _inside(torch.full(want.shape, 7.0, device=DEV))
+    gs.grouped_matmul(Ad, W, off, transpose=back, out=keep, dtype=torch.float32)
+    assert torch.equal(keep[:110], gs.grouped_matmul(Ad, W, off, transpose=back, dtype=torch.float32)[:110])
+    assert (keep[110:] == 7).all() and _around_is_nan(keep, wide)
+
+
 LAYERS = [("bf16", False), ("bf16", True), ("f32", True)]  # W's type, A in 8 bits
 
 
