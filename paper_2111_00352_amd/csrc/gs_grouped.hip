@@ -429,7 +429,7 @@ template <class T> __device__ __forceinline__ u32x4 row_piece(const SavedAlongRo
 }
 
 template <class LA, class T, bool TURN, int N, class TO>
-__global__ __launch_bounds__(kFewWaves * kWave, 3) void k_grouped_few(LA A, const T *__restrict__ W, int64_t ldw, int64_t w_step, Offsets off,
+__global__ __launch_bounds__(kFewWaves * kWave, N == 4 ? 2 : 3) void k_grouped_few(LA A, const T *__restrict__ W, int64_t ldw, int64_t w_step, Offsets off,
                                                                     int64_t k, int64_t n, bool fill, int tiles_n, TO *__restrict__ C,
                                                                     int64_t ldc)
 {

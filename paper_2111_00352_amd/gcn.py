@@ -22,8 +22,12 @@ layer's weight gradient and the ReLU's mask from those; "mxfp4" also forms the d
 products H W and G W^T in MXFP4 (weight gradients stay in fp32).  These layers have first
 derivatives only.
 
+A ``Teacher`` in the place of the target T trains the network by distillation: each row's
+loss is the divergence from a trained network's best classes (``teach``) instead of the
+squared distance from a row of T.
+
 Command line (end-to-end timing of one workload):
-    python -m paper_2111_00352_amd.gcn --config 2 --epochs 10 [--lowbit saved8|mxfp4]
+    python -m paper_2111_00352_amd.gcn --config 2 --epochs 10 [--lowbit saved8|mxfp4] [--distill K]
 """
 from __future__ import annotations
 
@@ -32,12 +36,13 @@ import json
 import os
 import sys
 import time
+from typing import NamedTuple
 
 import torch
 from torch.utils._device import DeviceContext
 
 import paper_2111_00352_amd as gs
-from paper_2111_00352_amd import SelectContext
+from paper_2111_00352_amd import SelectContext, layers
 
 
 class Adjacency:
@@ -215,6 +220,14 @@ class _ReluLinear(torch.autograd.Function):
 LOWBIT = (None, "saved8", "mxfp4")
 
 
+class Teacher(NamedTuple):
+    """What a network is distilled from: each row's best classes and their log probabilities."""
+
+    ids: torch.Tensor
+    logp: torch.Tensor
+    temperature: float = 1.0
+
+
 class GCN2:
     """Weights of the two layers (fp32, on the device); forward and SGD step.
     lowbit: None, "saved8" or "mxfp4" (see the module's text); P1 is then not kept
@@ -237,6 +250,8 @@ class GCN2:
         return aggregate(_Linear.apply(H1, self.W2), adj), P1
 
     def loss(self, Out, T):
+        if isinstance(T, Teacher):
+            return layers.distill_loss(Out, T.ids, T.logp, T.temperature).mean()
         return ((Out - T) ** 2).sum() / (2.0 * Out.shape[0])
 
     def step(self, X, T, adj: Adjacency, lr: float):
@@ -251,6 +266,15 @@ class GCN2:
             self.W1 -= lr * self.W1.grad
             self.W2 -= lr * self.W2.grad
         return loss.detach(), Out.detach(), None if P1 is None else P1.detach()
+
+
+def teach(model: GCN2, X, adj: Adjacency, top: int, temperature: float = 1.0) -> Teacher:
+    """The `top` best classes that the network gives each row of X."""
+    with torch.no_grad():
+        Out, _ = model.forward(X, adj)
+        none = torch.full((Out.shape[0],), -1, dtype=torch.int32, device=Out.device)
+        found = gs.log_probs(Out, none, top=top)
+    return Teacher(found.top_ids, found.top_logp, temperature)
 
 
 def train(adj: Adjacency, X, T, W1, W2, epochs: int, lr: float, graph: bool = False,
@@ -345,6 +369,8 @@ def main():
     ap.add_argument("--lr", type=float, default=0.02)
     ap.add_argument("--graph", action="store_true", help="replay a captured training step after two epochs")
     ap.add_argument("--lowbit", choices=[m for m in LOWBIT if m], help="8-bit saved activations, MXFP4 products")
+    ap.add_argument("--distill", type=int, metavar="K", help="train on the K best classes of an fp32 network trained first")
+    ap.add_argument("--temperature", type=float, default=2.0, help="of the distillation")
     a = ap.parse_args()
     sys.path.insert(0, os.path.dirname(os.path.dirname(os.path.abspath(__file__))))
     import graphgen
@@ -357,10 +383,14 @@ def main():
     W1 = torch.from_numpy(graphgen.features_x(g.F, a.hidden, 4100 + a.config, "normal")).to(dev) / g.F ** 0.5
     W2 = torch.from_numpy(graphgen.features_x(a.hidden, a.out, 4200 + a.config, "normal")).to(dev) / a.hidden ** 0.5
     T = torch.from_numpy(graphgen.features_x(g.R, a.out, 4300 + a.config, "normal")).to(dev)
+    if a.distill:
+        teacher = Adjacency(row, col, val, (g.R, g.C), SelectContext("model"), key=1, symmetric=bool(g.meta.get("symmetric", False)))
+        T = teach(train(teacher, X, T, W1, W2, a.epochs, a.lr)[0], X, teacher, a.distill, a.temperature)
+        teacher.ctx.close()
     res = end_to_end(row, col, val, (g.R, g.C), X, T, W1, W2, a.epochs, a.lr,
                      symmetric=bool(g.meta.get("symmetric", False)), graph=a.graph, lowbit=a.lowbit)
     print(json.dumps({"workload": g.name, "epochs": a.epochs, "hidden": a.hidden, "out": a.out,
-                      "graph": a.graph, "lowbit": a.lowbit, **res}))
+                      "graph": a.graph, "lowbit": a.lowbit, **({"distill": a.distill} if a.distill else {}), **res}))
 
 
 if __name__ == "__main__":
