@@ -498,7 +498,7 @@ int gs_log_probs_grad(const void *s, int64_t ld, int dtype, int64_t n, int64_t v
  * top_logits / T over a row's alternatives and p that of s / T over all classes,
  *   loss = T^2 sum q (log q - log p)
  * and 0 for a row without an alternative; NaN where an id is v or more.  stats (n
- * x 2): the largest logit and the sum of exp((s_j - m) / T). */
+ * x 4, 16-byte aligned): what the gradient takes. */
 int gs_distill_loss(const void *s, int64_t ld, int dtype, int64_t n, int64_t v, const void *top_ids, int id_bytes,
                     const void *top_logits, int t_dtype, int64_t k, double temperature, float *loss, float *stats, gs_stream stream);
 

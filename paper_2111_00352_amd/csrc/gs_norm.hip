@@ -43,9 +43,7 @@ __global__ __launch_bounds__((RowAt<T, L, R>::kThreads)) void k_norm(const T *__
     __shared__ double tmp[L > kWave ? L / kWave : 1];
     float wt[R][E];
 #pragma unroll
-    for (int i = 0; i < R; i++)
-#pragma unroll
-        for (int e = 0; e < E; e++) wt[i][e] = !w ? 1.0f : At::col(i) + e < cols ? load_either(w, w32, At::col(i) + e) : 0.0f;
+    for (int i = 0; i < R; i++) load_weights<E>(w, w32, At::col(i), cols, wt[i]);
     const double inv = 1.0 / cols;
     // (rows of a wave that are past the last one go along: every lane takes part in the sums)
     for (int64_t row = At::first_row(), at = (int64_t)blockIdx.x * At::kRows; at < n; row += At::row_step(), at += At::row_step()) {
@@ -118,12 +116,11 @@ __global__ __launch_bounds__((RowAt<T, L, R>::kThreads)) void k_norm_grad(const 
     __shared__ float sums[L <= kWave ? kSums : 1][L <= kWave ? L * R * E : 1];
     float wt[R][E], dw[R][E];
 #pragma unroll
-    for (int i = 0; i < R; i++)
+    for (int i = 0; i < R; i++) {
+        load_weights<E>(w, w32, At::col(i), cols, wt[i]);
 #pragma unroll
-        for (int e = 0; e < E; e++) {
-            wt[i][e] = !w ? 1.0f : At::col(i) + e < cols ? load_either(w, w32, At::col(i) + e) : 0.0f;
-            dw[i][e] = 0.0f;
-        }
+        for (int e = 0; e < E; e++) dw[i][e] = 0.0f;
+    }
     const float inv = 1.0f / (float)cols;
     // the next row is loaded while this one is worked on
     RowPiece<T> hp[R], gp[R], dp[R];
@@ -248,10 +245,10 @@ __global__ __launch_bounds__(kWideThreads) void k_norm_wide(const T *__restrict_
         for (int c0 = 0; c0 < end; c0 += kWideThreads * E) {  // (all lanes of a wave: blocks are found across lanes)
             const int c = c0 + threadIdx.x * E;
             const V v = load_elems<T, E>(from + c, cols - c);
-            float y[E];
+            float y[E], wt[E];
+            load_weights<E>(w, w32, c, cols, wt);
 #pragma unroll
-            for (int e = 0; e < E; e++)
-                y[e] = c + e < cols ? to_f32(v[e]) * r * (w ? load_either(w, w32, c + e) : 1.0f) : 0.0f;
+            for (int e = 0; e < E; e++) y[e] = c + e < cols ? to_f32(v[e]) * r * wt[e] : 0.0f;
             if constexpr (!SAVE) {
                 V o;
 #pragma unroll
@@ -284,10 +281,11 @@ __global__ __launch_bounds__(kWideThreads) void k_norm_dot(const T *__restrict__
         for (int c = threadIdx.x * E; c < cols; c += kWideThreads * E) {
             const auto h = load_elems<T, E>(H + row * ldh + c, cols - c);
             const auto g = load_elems<T, E>(dY + row * ldy + c, cols - c);
+            float wt[E];
+            load_weights<E>(w, w32, c, cols, wt);
 #pragma unroll
             for (int e = 0; e < E; e++)
-                if (c + e < cols)
-                    run = __builtin_fmaf(to_f32(g[e]) * (w ? load_either(w, w32, c + e) : 1.0f), to_f32(h[e]) * r, run);
+                if (c + e < cols) run = __builtin_fmaf(to_f32(g[e]) * wt[e], to_f32(h[e]) * r, run);
             if (++k % 16 == 0) {
                 dot += run;
                 run = 0.0f;
@@ -398,8 +396,12 @@ int gs_rms_norm(const void *X, int64_t ldx, const void *R, int64_t ldr, int dtyp
             using T = decltype(type);
             constexpr bool SAVE = decltype(save)::value;
             uint8_t *codes = saved ? saved->codes : nullptr, *scales = saved ? saved->scales : nullptr;
-            auto run = [&](auto kernel, int64_t grid, int threads) {
-                kernel<<<(unsigned)std::min<int64_t>(grid, 1 << 20), threads, 0, s>>>(
+            // Workgroups that go on to further rows load the weights once for them: 87,335 x 2048 bf16 into
+            // 8 bits 117 us by 8,192 workgroups, 125 by one for each set of rows, 1,000,000 x 17 fp32 30 and
+            // 39; fp32 rows of three pieces a lane and more keep the chip busier without (2,000,000 x 128 with
+            // a residual 536 and 513).
+            auto run = [&](auto kernel, int64_t grid, int threads, bool once) {
+                kernel<<<(unsigned)std::min<int64_t>(grid, once ? 1 << 20 : 8192), threads, 0, s>>>(
                     (const T *)X, ldx, (const T *)R, ldr, w, w_dtype == GS_F32, eps, rows, (int)cols, (T *)H, ldh, (T *)Y, ldy, codes,
                     scales, blocks, rstd);
             };
@@ -407,10 +409,11 @@ int gs_rms_norm(const void *X, int64_t ldx, const void *R, int64_t ldr, int dtyp
             const bool held = with_row<8, 512, 4>(pieces, [&](auto l, auto r) {
                 constexpr int L = decltype(l)::value, N = decltype(r)::value;
                 using At = RowAt<T, L, N>;
-                nt ? run(k_norm<T, L, N, SAVE, true>, ceil_div(rows, (int64_t)At::kRows), At::kThreads)
-                   : run(k_norm<T, L, N, SAVE, false>, ceil_div(rows, (int64_t)At::kRows), At::kThreads);
+                constexpr bool ONCE = sizeof(T) == 4 && N >= 3;
+                nt ? run(k_norm<T, L, N, SAVE, true>, ceil_div(rows, (int64_t)At::kRows), At::kThreads, ONCE)
+                   : run(k_norm<T, L, N, SAVE, false>, ceil_div(rows, (int64_t)At::kRows), At::kThreads, ONCE);
             });
-            if (!held) run(k_norm_wide<T, SAVE>, rows, kWideThreads);
+            if (!held) run(k_norm_wide<T, SAVE>, rows, kWideThreads, false);
         };
         if (dtype == GS_F32)
             saved ? go(0.0f, std::true_type{}) : go(0.0f, std::false_type{});

@@ -254,5 +254,29 @@ __device__ __forceinline__ float load_either(const void *p, bool wide, int64_t i
 {
     return wide ? ((const float *)p)[i] : to_f32(((const u16 *)p)[i]);
 }
+// E of them (a weight for each column) from column c on, ones without an array, zeros past the last.
+template <int E> __device__ __forceinline__ void load_weights(const void *p, bool wide, int c, int cols, float (&w)[E])
+{
+    if (!p) {
+#pragma unroll
+        for (int e = 0; e < E; e++) w[e] = 1.0f;
+    } else if (c + E <= cols) {
+        if (wide) {
+#pragma unroll
+            for (int q = 0; q < E / 4; q++) {
+                const auto v = load_elems<float, 4>((const float *)p + c + 4 * q, 4);
+#pragma unroll
+                for (int e = 0; e < 4; e++) w[4 * q + e] = v[e];
+            }
+        } else {
+            const auto v = load_elems<u16, E>((const u16 *)p + c, E);
+#pragma unroll
+            for (int e = 0; e < E; e++) w[e] = to_f32(v[e]);
+        }
+    } else {
+#pragma unroll
+        for (int e = 0; e < E; e++) w[e] = c + e < cols ? load_either(p, wide, c + e) : 0.0f;
+    }
+}
 
 }  // namespace gs

@@ -106,10 +106,12 @@ template <class T> struct Alternative {
         s = id < 0 ? 0.0f : id < v ? to_f32(p[id]) : __builtin_nanf("");
     }
 };
-// first: the lane's first alternative, looked up.
+// The loss, and the statistics that its gradient takes: m, S, the teacher's largest logit and
+// 1 / the sum of its weights; 0 instead of that for a row without alternatives, NaN where a
+// class is not there.  first: the lane's first alternative, looked up.
 template <class T, int L>
 __device__ __forceinline__ void write_loss(const RowStats &st, float logS, const T *p, int64_t row, bool in, int v, const Teacher &te,
-                                           int lane, const Alternative<T> &first, float *tmp, float *loss)
+                                           int lane, const Alternative<T> &first, float *tmp, float *loss, float4 *stats)
 {
     auto each = [&](auto &&f) {
         if (first.id >= 0) f(first);
@@ -123,19 +125,24 @@ __device__ __forceinline__ void write_loss(const RowStats &st, float logS, const
     float tm = -kInf;
     each([&](const Alternative<T> &a) { tm = fmaxf(tm, a.t); });
     tm = row_fold<L>(tm, tmp, [](float a, float b) { return fmaxf(a, b); });
-    float sums[3] = {0.0f, 0.0f, 0.0f};  // of the weights, of weight (log q' - log p'), of the alternatives
+    // of the weights, of weight (log q' - log p'), of the alternatives (infinity for one that is not there)
+    float sums[3] = {0.0f, 0.0f, 0.0f};
     each([&](const Alternative<T> &a) {
         const float d = (a.t - tm) * te.c, w = exp_neg(d), x = (a.s - st.m) * te.c;
         sums[0] += w;
         if (!(w == 0.0f) || x != x) sums[1] = __builtin_fmaf(w, d - x, sums[1]);
-        sums[2] += 1.0f;
+        sums[2] += a.id < v ? 1.0f : kInf;
     });
     row_sums<L, 3>(sums, tmp);
-    if (in && lane == 0) loss[row] = sums[2] > 0.0f ? te.scale * (sums[1] / sums[0] + (logS - logf(sums[0]))) : 0.0f;
+    if (in && lane == 0) {
+        loss[row] = sums[2] > 0.0f ? te.scale * (sums[1] / sums[0] + (logS - logf(sums[0]))) : 0.0f;
+        stats[row] = make_float4(st.m, st.S, tm, sums[2] == kInf ? __builtin_nanf("") : sums[2] > 0.0f ? 1.0f / sums[0] : 0.0f);
+    }
 }
 
 // ------------------------------------------------------------ rows in registers
 
+// (the next rows are loaded while these are worked on; L > 64: a workgroup's row, no alternatives)
 template <class T, int L, int R, bool TEACHER, bool NT>
 __global__ __launch_bounds__(kRowThreads) void k_scores_held(const T *__restrict__ s, int64_t ld, int64_t n, int v, ClassIds ids,
                                                             Teacher te, ScoreOut out)
@@ -143,38 +150,44 @@ __global__ __launch_bounds__(kRowThreads) void k_scores_held(const T *__restrict
     using At = RowAt<T, L, R>;
     constexpr int E = At::E;
     using V = typename Elems<T, E>::type;
+    __shared__ float tmp[3 * kRowThreads / kWave];
+    RowPiece<T> q[R];
+    Alternative<T> ahead;
+    int64_t id_ahead = -1;
+    auto load = [&](int64_t row) {
+        const bool in = row < n;
+#pragma unroll
+        for (int i = 0; i < R; i++) q[i].template load<NT>(s + row * ld, At::col(i), v, in);
+        if constexpr (TEACHER)
+            ahead.load(te, row, At::lane(), in);
+        else
+            id_ahead = in && out.lp && At::lane() == 0 ? ids.at(row) : -1;
+    };
+    load(At::first_row());
     for (int64_t row = At::first_row(), at = (int64_t)blockIdx.x * At::kRows; at < n; row += At::row_step(), at += At::row_step()) {
         const bool in = row < n;
         const T *p = s + row * ld;
         float x[R][E];
-        Alternative<T> first;
-        {
-            RowPiece<T> q[R];
 #pragma unroll
-            for (int i = 0; i < R; i++) q[i].template load<NT>(p, At::col(i), v, in);
-            if constexpr (TEACHER) first.load(te, row, At::lane(), in);
+        for (int i = 0; i < R; i++) {
+            const V t = q[i].get(At::col(i), v, kNegInf<T>);
 #pragma unroll
-            for (int i = 0; i < R; i++) {
-                const V t = q[i].get(At::col(i), v, kNegInf<T>);
-#pragma unroll
-                for (int e = 0; e < E; e++) x[i][e] = to_f32(t[e]);
-            }
+            for (int e = 0; e < E; e++) x[i][e] = to_f32(t[e]);
         }
-        int64_t id = -1;
+        Alternative<T> first = ahead;
+        const int64_t id = id_ahead;
         float given = 0.0f;
-        if constexpr (!TEACHER) {
-            if (in && out.lp && At::lane() == 0) {
-                id = ids.at(row);
-                if (id >= 0 && id < v) given = to_f32(p[id]);
-            }
-        }
-        if constexpr (TEACHER) first.look_up(p, v);
+        if constexpr (TEACHER)
+            first.look_up(p, v);
+        else if (id >= 0 && id < v)
+            given = to_f32(p[id]);
+        load(row + At::row_step());
         RowStats t{-kInf, 0.0f, 0.0f};
 #pragma unroll
         for (int i = 0; i < R; i++)
 #pragma unroll
             for (int e = 0; e < E; e++) t.m = fmaxf(t.m, x[i][e]);
-        t.m = group_fold<L>(t.m, [](float a, float b) { return fmaxf(a, b); });
+        t.m = row_fold<L>(t.m, tmp, [](float a, float b) { return fmaxf(a, b); });
         const Scale by(TEACHER ? te.k2 : kLog2e, t.m);
         float sums[2] = {0.0f, 0.0f};
 #pragma unroll
@@ -186,17 +199,19 @@ __global__ __launch_bounds__(kRowThreads) void k_scores_held(const T *__restrict
                 // (0 where d is -inf: its maximum with -2^126 is finite, the weight 0)
                 if constexpr (!TEACHER) sums[1] = __builtin_fmaf(w, fmaxf(d, -0x1p126f), sums[1]);
             }
-        sums[0] = group_sum<L>(sums[0]);
-        if constexpr (!TEACHER) sums[1] = group_sum<L>(sums[1]);
+        if constexpr (TEACHER)
+            sums[0] = row_sum<L>(sums[0], tmp);
+        else
+            row_sums<L, 2>(sums, tmp);
         t.set(sums[0], sums[1]);
         const float logS = logf(t.S);
         if constexpr (TEACHER) {
-            write_loss<T, L>(t, logS, p, row, in, v, te, At::lane(), first, (float *)nullptr, out.lp);
-            if (in && At::lane() == 0) out.stats[row] = make_float2(t.m, t.S);
+            write_loss<T, L>(t, logS, p, row, in, v, te, At::lane(), first, tmp, out.lp, (float4 *)out.stats);
         } else {
             if (in && At::lane() == 0) write_scores(t, logS, row, out, ids, given, id, v);
             // the best, one after another: the largest left, of the lowest index
-            if (out.top) {
+            if (L <= kWave && out.top) {
+                constexpr int G = L <= kWave ? L : kWave;
                 uint32_t key[R][E];
 #pragma unroll
                 for (int i = 0; i < R; i++)
@@ -213,9 +228,9 @@ __global__ __launch_bounds__(kRowThreads) void k_scores_held(const T *__restrict
                                 best = key[i][e];
                                 col = At::col(i) + e;
                             }
-                    const uint32_t top = group_fold_u<L>(best, [](uint32_t a, uint32_t b) { return a > b ? a : b; });
+                    const uint32_t top = group_fold_u<G>(best, [](uint32_t a, uint32_t b) { return a > b ? a : b; });
                     col = best == top ? col : 0x7fffffff;
-                    col = (int)group_fold_u<L>((uint32_t)col, [](uint32_t a, uint32_t b) { return a < b ? a : b; });
+                    col = (int)group_fold_u<G>((uint32_t)col, [](uint32_t a, uint32_t b) { return a < b ? a : b; });
                     if (in && At::lane() == 0) {
                         out.top_ids[row * out.top + j] = col;
                         out.top_lp[row * out.top + j] = key_value(top) - t.m - logS;
@@ -421,8 +436,7 @@ __global__ __launch_bounds__(NTH) void k_scores_wide(const T *__restrict__ s, in
         }
         const float logS = logf(t.S);
         if constexpr (TEACHER) {
-            write_loss<T, NTH>(t, logS, p, row, true, v, te, threadIdx.x, first, fold, out.lp);
-            if (threadIdx.x == 0) out.stats[row] = make_float2(t.m, t.S);
+            write_loss<T, NTH>(t, logS, p, row, true, v, te, threadIdx.x, first, fold, out.lp, (float4 *)out.stats);
         } else if (threadIdx.x == 0) {
             const int64_t id = out.lp ? ids.at(row) : -1;
             write_scores(t, logS, row, out, ids, id >= 0 && id < v ? to_f32(p[id]) : 0.0f, id, v);
@@ -447,10 +461,51 @@ __global__ __launch_bounds__(NTH) void k_scores_wide(const T *__restrict__ s, in
 
 // ---------------------------------------------------------------- gradients
 
-// Rows (L lanes each), or pieces of rows of a workgroup (L = kRowThreads: blockIdx.y the
-// piece, of `span` columns).
+// Rows of L lanes, or spans of rows of a workgroup (blockIdx.y: the span), R pieces of a lane at
+// a time; the next ones, of this row or of the next, are loaded while these are worked on.
+
+// What a lane goes through: steps of its row's span, then of the row after it.
+template <class T, int L, int R, bool NT> struct GradWalk {
+    static constexpr int E = kPiece<T>, STEP = L * R * E, kRows = kRowThreads / L;
+    using V = typename Elems<T, E>::type;
+    const T *s;
+    int64_t ld, n, row, at;  // at: the workgroup's first row
+    int v, c1, c2, c0;
+    RowPiece<T> q[R];
+    __device__ __forceinline__ static int lane() { return threadIdx.x % L; }
+    __device__ __forceinline__ int col(int i) const { return c0 + (i * L + lane()) * E; }
+    __device__ __forceinline__ GradWalk(const T *s_, int64_t ld_, int64_t n_, int v_, int span)
+        : s(s_), ld(ld_), n(n_), row((int64_t)blockIdx.x * kRows + threadIdx.x / L), at((int64_t)blockIdx.x * kRows), v(v_),
+          c1(blockIdx.y * span), c2(c1 + span < v_ ? c1 + span : v_), c0(c1)
+    {
+        load();
+    }
+    __device__ __forceinline__ void load()
+    {
+#pragma unroll
+        for (int i = 0; i < R; i++) q[i].template load<NT>(s + row * ld, col(i), v, row < n);
+    }
+    __device__ __forceinline__ void take(V (&x)[R]) const
+    {
+#pragma unroll
+        for (int i = 0; i < R; i++) x[i] = q[i].get(col(i), v);
+    }
+    // On to the next step; true: of the same row.
+    __device__ __forceinline__ bool next()
+    {
+        c0 += STEP;
+        const bool same = c0 < c2;
+        if (!same) {
+            c0 = c1;
+            row += (int64_t)gridDim.x * kRows;
+            at += (int64_t)gridDim.x * kRows;
+        }
+        load();
+        return same;
+    }
+};
 struct GradIn {
-    const float2 *stats;
+    const float *stats;
     const float *g, *e, *entropy;  // NULL: none
 };
 
@@ -458,37 +513,42 @@ template <class T, int L, int R, bool NT>
 __global__ __launch_bounds__(kRowThreads) void k_scores_grad(const T *s, int64_t ld, int64_t n, int v, int span, ClassIds ids, GradIn a,
                                                             T *out, int64_t ldo)
 {
-    constexpr int E = kPiece<T>;
-    using V = typename Elems<T, E>::type;
-    constexpr int kRows = kRowThreads / L;
-    const int lane = threadIdx.x % L, c1 = blockIdx.y * span, c2 = c1 + span < v ? c1 + span : v;
-    constexpr int STEP = L * R * E;
-    for (int64_t row = (int64_t)blockIdx.x * kRows + threadIdx.x / L, at = (int64_t)blockIdx.x * kRows; at < n;
-         row += (int64_t)gridDim.x * kRows, at += (int64_t)gridDim.x * kRows) {
+    using Walk = GradWalk<T, L, R, NT>;
+    using V = typename Walk::V;
+    constexpr int E = Walk::E;
+    Walk walk(s, ld, n, v, span);
+    struct Given {
+        float2 st;
+        int64_t id;
+        float g, e, H;
+    } ahead;
+    auto look = [&](int64_t row) {
         const bool in = row < n;
-        RowPiece<T> q[R];
-        auto load = [&](int c0) {
-#pragma unroll
-            for (int i = 0; i < R; i++) q[i].template load<NT>(s + row * ld, c0 + (i * L + lane) * E, v, in);
-        };
-        load(c1);
-        const float2 st = in ? a.stats[row] : make_float2(0.0f, 1.0f);
-        const int64_t id = in && a.g ? ids.at(row) : -1;
-        float g = id >= 0 ? a.g[row] : 0.0f;
-        if (id >= v) g = __builtin_nanf("");
-        const float e0 = in && a.e ? a.e[row] : 0.0f, H = in && a.e ? a.entropy[row] : 0.0f;
+        ahead.st = in ? ((const float2 *)a.stats)[row] : make_float2(0.0f, 1.0f);
+        ahead.id = in && a.g ? ids.at(row) : -1;
+        ahead.g = in && a.g ? a.g[row] : 0.0f;
+        ahead.e = in && a.e ? a.e[row] : 0.0f;
+        ahead.H = in && a.e ? a.entropy[row] : 0.0f;
+    };
+    look(walk.row);
+    while (walk.at < n) {
+        const int64_t row = walk.row;
+        const Given gv = ahead;
+        const float g = gv.id < 0 ? 0.0f : gv.id < v ? gv.g : __builtin_nanf("");
+        const int mine = gv.id >= 0 && gv.id < v ? (int)gv.id : -1;
         // -g p - e p (log p + H) = weight (fa power + fb)
-        const Scale by(kLog2e, st.x);
-        const float f = 1.0f / st.y, fa = -e0 * kLn2 * f, fb = (-g - e0 * (H - logf(st.y))) * f;
-        const int mine = id >= 0 && id < v ? (int)id : -1;
-        for (int c0 = c1; c0 < c2; c0 += STEP) {
+        const Scale by(kLog2e, gv.st.x);
+        const float f = 1.0f / gv.st.y, fa = -gv.e * kLn2 * f, fb = (-g - gv.e * (gv.H - logf(gv.st.y))) * f;
+        bool more = true;
+        while (more) {
             V x[R];
-#pragma unroll
-            for (int i = 0; i < R; i++) x[i] = q[i].get(c0 + (i * L + lane) * E, v);
-            if (c0 + STEP < c2) load(c0 + STEP);
+            walk.take(x);
+            const int c0 = walk.c0;
+            more = walk.next();
+            if (!more) look(walk.row);
 #pragma unroll
             for (int i = 0; i < R; i++) {
-                const int col = c0 + (i * L + lane) * E;
+                const int col = c0 + (i * L + walk.lane()) * E;
                 V o;
 #pragma unroll
                 for (int e = 0; e < E; e++) {
@@ -497,18 +557,22 @@ __global__ __launch_bounds__(kRowThreads) void k_scores_grad(const T *s, int64_t
                     if (col + e == mine) y += g;
                     o[e] = from_f32<T>(y);
                 }
-                store_elems<T, E, NT>(out + row * ldo + col, o, in ? c2 - col : 0);
+                store_elems<T, E, NT>(out + row * ldo + col, o, row < n ? walk.c2 - col : 0);
             }
         }
     }
 }
 
-// Waits for this thread's stores, then for the other threads of the workgroup.
-__device__ __forceinline__ void stores_meet()
+// What the L lanes of a row have written to LDS and stored is seen by all of them.
+template <int L> __device__ __forceinline__ void lanes_meet()
 {
-    __builtin_amdgcn_fence(__ATOMIC_RELEASE, "workgroup");
-    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-    __syncthreads();
+    if constexpr (L <= kWave) {  // (a wave's LDS operations and its stores keep their order)
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+        __builtin_amdgcn_wave_barrier();
+        asm volatile("" ::: "memory");
+    } else {
+        __syncthreads();  // (stores of a workgroup's waves reach memory in the order of its barriers)
+    }
 }
 
 // The distillation loss's gradient.  The elements at the teacher's classes, which may be the
@@ -518,52 +582,43 @@ template <class T, int L, int R, bool NT>
 __global__ __launch_bounds__(kRowThreads) void k_distill_grad(const T *s, int64_t ld, int64_t n, int v, int span, Teacher te, GradIn a,
                                                              int kp, T *out, int64_t ldo)
 {
-    constexpr int E = kPiece<T>, STEP = L * R * E;
-    using V = typename Elems<T, E>::type;
-    constexpr int kRows = kRowThreads / L;
+    using Walk = GradWalk<T, L, R, NT>;
+    using V = typename Walk::V;
+    constexpr int E = Walk::E;
     extern __shared__ __align__(16) uint8_t lds[];
-    __shared__ float fold[2 * kRowThreads / kWave];
-    const int lane = threadIdx.x % L, c1 = blockIdx.y * span, c2 = c1 + span < v ? c1 + span : v;
     int *id = (int *)lds + 3 * kp * (threadIdx.x / L);
     float *w = (float *)id + kp, *val = w + kp;
-    for (int64_t r0 = (int64_t)blockIdx.x * kRows; r0 < n; r0 += (int64_t)gridDim.x * kRows) {
-        const int64_t row = r0 + threadIdx.x / L;
+    Walk walk(s, ld, n, v, span);
+    const int c1 = walk.c1, c2 = walk.c2, lane = walk.lane();
+    float4 st_ahead;
+    float g_ahead;
+    Alternative<T> one_ahead;
+    auto look = [&](int64_t row) {
+        const bool in = row < n;
+        st_ahead = in ? ((const float4 *)a.stats)[row] : make_float4(0.0f, 1.0f, 0.0f, 0.0f);
+        g_ahead = in ? a.g[row] : 0.0f;
+        one_ahead.load(te, row, lane, in);
+    };
+    look(walk.row);
+    while (walk.at < n) {
+        const int64_t row = walk.row;
         const bool in = row < n;
         const T *p = s + row * ld;
-        RowPiece<T> q[R];
-        auto load = [&](int c0) {
-#pragma unroll
-            for (int i = 0; i < R; i++) q[i].template load<NT>(p, c0 + (i * L + lane) * E, v, in);
-        };
-        load(c1);
-        const float2 st = in ? a.stats[row] : make_float2(0.0f, 1.0f);
+        const float4 st = st_ahead;
         const Scale by(te.k2, st.x);
         const float inv = 1.0f / st.y;
-        float tm = -kInf, sums[2] = {0.0f, 0.0f};  // the weights' sum; 1 for a class, infinity for one that is not there
+        // (NaN where the teacher's weights are or a class is not there, 0 for a row without alternatives)
+        const float gT = st.w == 0.0f ? 0.0f : g_ahead / te.c + (st.w - st.w);
+        // the student's probability and the teacher's at each alternative in the span
         for (int i = lane; i < kp; i += L) {
-            Alternative<T> one;
-            one.load(te, row, i, in);
-            if (one.t == -kInf) one.id = -1;
-            const bool there = one.id >= 0 && one.id < v;
-            if (one.id >= 0) {
-                sums[1] += there ? 1.0f : kInf;
-                tm = fmaxf(tm, one.t);
-            }
+            Alternative<T> one = one_ahead;
+            if (i >= L) one.load(te, row, i, in);
+            const bool there = one.id >= 0 && one.id < v && one.t != -kInf;
             id[i] = there ? (int)one.id : -1;
-            w[i] = one.t;
-            // (the student's probability there, for now)
+            w[i] = there ? exp_neg((one.t - st.z) * te.c) * st.w : 0.0f;
             if (there && one.id >= c1 && one.id < c2) val[i] = __builtin_amdgcn_exp2f(by.power(to_f32(p[one.id]))) * inv;
         }
-        tm = row_fold<L>(tm, fold, [](float x, float y) { return fmaxf(x, y); });
-        for (int i = lane; i < kp; i += L) {
-            w[i] = id[i] >= 0 ? exp_neg((w[i] - tm) * te.c) : 0.0f;
-            sums[0] += w[i];
-        }
-        row_sums<L, 2>(sums, fold);
-        // (NaN where the teacher's weights are, 0 where the row has none of them)
-        const float gT = sums[1] == kInf ? __builtin_nanf("") : sums[1] > 0.0f ? a.g[row] / te.c * (sums[0] / sums[0]) : 0.0f;
-        const float inv_w = 1.0f / sums[0];
-        __syncthreads();  // (ids and weights are there; out may be s: its elements have been read)
+        lanes_meet<L>();  // (out may be s: its elements have been read)
         for (int i = lane; i < te.k; i += L) {
             const int j = id[i];
             if (j < c1 || j >= c2) continue;
@@ -576,14 +631,16 @@ __global__ __launch_bounds__(kRowThreads) void k_distill_grad(const T *s, int64_
                 sum += jj.z == j ? ww.z : 0.0f;
                 sum += jj.w == j ? ww.w : 0.0f;
             }
-            val[i] = gT == 0.0f ? 0.0f : gT * (val[i] - sum * inv_w);
+            val[i] = gT == 0.0f ? 0.0f : gT * (val[i] - sum);
         }
         const float f = gT * inv;
-        for (int c0 = c1; c0 < c2; c0 += STEP) {
+        bool more = true;
+        while (more) {
             V x[R];
-#pragma unroll
-            for (int i = 0; i < R; i++) x[i] = q[i].get(c0 + (i * L + lane) * E, v);
-            if (c0 + STEP < c2) load(c0 + STEP);
+            walk.take(x);
+            const int c0 = walk.c0;
+            more = walk.next();
+            if (!more) look(walk.row);
 #pragma unroll
             for (int i = 0; i < R; i++) {
                 const int col = c0 + (i * L + lane) * E;
@@ -593,10 +650,10 @@ __global__ __launch_bounds__(kRowThreads) void k_distill_grad(const T *s, int64_
                 store_elems<T, E, NT>(out + row * ldo + col, o, in ? c2 - col : 0);
             }
         }
-        stores_meet();
+        lanes_meet<L>();
         for (int i = lane; i < te.k; i += L)
             if (id[i] >= c1 && id[i] < c2) out[row * ldo + id[i]] = from_f32<T>(val[i]);
-        __syncthreads();  // (before the next rows')
+        lanes_meet<L>();  // (before the next rows')
     }
 }
 
@@ -628,18 +685,21 @@ Teacher check_teacher(const void *ids, int id_bytes, const void *t, int t_dtype,
             (float)(1.4426950408889634 / temperature), (float)(temperature * temperature)};
 }
 
-// Rows that a wave holds stay in registers; wider ones take a workgroup, the larger the fewer
-// they are (the chip holds 2,048 of 256 threads).
-constexpr int64_t kHeldPieces = 256;
+// Rows that a workgroup (with alternatives to find: a wave) holds stay in registers; wider
+// ones take a workgroup a row, the larger the fewer they are (the chip holds 2,048 of 256 threads).
+// A workgroup takes one set of rows: 2,048 that go on to further ones are slower (2,000,000 x 47:
+// scores 113 and 88 us, gradient 256 and 223).
+constexpr int64_t kRowBlocks = 1 << 20;
 template <class T, bool TEACHER>
 void launch_scores(const T *s, int64_t ld, int64_t n, int64_t v, const ClassIds &ids, const Teacher &te, const ScoreOut &out,
                    hipStream_t st)
 {
     const int64_t pieces = ceil_div(v, kPiece<T>);
-    const bool nt = streams((double)n * v * sizeof(T), v, sizeof(T), {{s, ld}});
-    const bool held = pieces <= kHeldPieces && with_row<4, kWave, 4>(pieces, [&](auto l, auto r) {
+    // (past the caches only where a load takes whole lines: 2,000,000 x 48 86 us, past them 158)
+    const bool nt = pieces > 32 && streams((double)n * v * sizeof(T), v, sizeof(T), {{s, ld}});
+    const bool held = pieces <= (out.top ? 4 * kWave : 4 * kRowThreads) && with_row<4, kRowThreads, 4>(pieces, [&](auto l, auto r) {
         constexpr int L = decltype(l)::value, R = decltype(r)::value;
-        const unsigned grid = (unsigned)std::min<int64_t>(ceil_div(n, (int64_t)(kRowThreads / L)), 1 << 20);
+        const unsigned grid = (unsigned)std::min<int64_t>(ceil_div(n, (int64_t)(kRowThreads / L)), kRowBlocks);
         nt ? k_scores_held<T, L, R, TEACHER, true><<<grid, kRowThreads, 0, st>>>(s, ld, n, (int)v, ids, te, out)
            : k_scores_held<T, L, R, TEACHER, false><<<grid, kRowThreads, 0, st>>>(s, ld, n, (int)v, ids, te, out);
     });
@@ -655,20 +715,19 @@ void launch_scores(const T *s, int64_t ld, int64_t n, int64_t v, const ClassIds 
         large ? go(k_scores_wide<T, 1024, false, false>, 1024) : go(k_scores_wide<T, 256, false, false>, 256);
 }
 
-// go(L, R, span, grid): rows that a wave holds, else workgroups for spans of a row.
+// go(L, R, span, grid): rows that a workgroup holds, else spans of four steps of wider ones
+// (4096 x 50,257 bf16: 192 us; whole rows 222).
 template <class T, class Go> void grad_shape(int64_t n, int64_t v, Go &&go)
 {
     const int64_t pieces = ceil_div(v, kPiece<T>);
-    if (with_row<4, kWave, 4>(pieces, [&](auto l, auto r) {
-            go(l, r, (int)v, dim3((unsigned)std::min<int64_t>(ceil_div(n, (int64_t)kRowThreads / decltype(l)::value), 1 << 20)));
+    if (with_row<4, kRowThreads, 4>(pieces, [&](auto l, auto r) {
+            go(l, r, (int)v, dim3((unsigned)std::min<int64_t>(ceil_div(n, (int64_t)kRowThreads / decltype(l)::value), kRowBlocks)));
         }))
         return;
-    // (spans of whole steps, as many as make 2,048 workgroups with the rows)
     constexpr int R = 4, STEP = kRowThreads * R * kPiece<T>;
-    const int64_t steps = ceil_div(v, STEP), want = std::min(steps, ceil_div(2048, std::max<int64_t>(1, n)));
-    const int64_t span = ceil_div(steps, want) * STEP;
-    go(std::integral_constant<int, kRowThreads>{}, std::integral_constant<int, R>{}, (int)span,
-       dim3((unsigned)std::min<int64_t>(n, 1 << 20), (unsigned)ceil_div(v, span)));
+    constexpr int span = 4 * STEP;
+    go(std::integral_constant<int, kRowThreads>{}, std::integral_constant<int, R>{}, span,
+       dim3((unsigned)std::min<int64_t>(n, kRowBlocks), (unsigned)ceil_div(v, span)));
 }
 
 }  // namespace
@@ -708,7 +767,7 @@ int gs_log_probs_grad(const void *s, int64_t ld, int dtype, int64_t n, int64_t v
         if (n > 0 && (!stats || (dentropy && !entropy))) fail(GS_ERR_INVALID_ARG, "null statistics");
         if ((uintptr_t)stats % 8) fail(GS_ERR_INVALID_ARG, "stats are not 8-byte aligned");
         if (n == 0) return;
-        const GradIn a{(const float2 *)stats, dlogp, dentropy, entropy};
+        const GradIn a{stats, dlogp, dentropy, entropy};
         auto go = [&](auto type) {
             using T = decltype(type);
             const bool nt = streams(2.0 * n * v * sizeof(T), v, sizeof(T), {{s, ld}, {out, ldo}});
@@ -732,7 +791,7 @@ int gs_distill_loss(const void *s, int64_t ld, int dtype, int64_t n, int64_t v, 
         check_logits(s, ld, dtype, n, v);
         const Teacher te = check_teacher(top_ids, id_bytes, top_logits, t_dtype, n, k, temperature);
         if (n > 0 && (!loss || !stats)) fail(GS_ERR_INVALID_ARG, "null output");
-        if ((uintptr_t)stats % 8) fail(GS_ERR_INVALID_ARG, "stats are not 8-byte aligned");
+        if ((uintptr_t)stats % 16) fail(GS_ERR_INVALID_ARG, "stats are not 16-byte aligned");
         if (n == 0) return;
         const ScoreOut out{loss, nullptr, (float2 *)stats, 0, nullptr, nullptr};
         const ClassIds none{nullptr, false};
@@ -753,9 +812,9 @@ int gs_distill_grad(const void *s, int64_t ld, int dtype, int64_t n, int64_t v, 
         check_operand("out", out, n, v, ldo, dtype_size(dtype));
         const Teacher te = check_teacher(top_ids, id_bytes, top_logits, t_dtype, n, k, temperature);
         if (n > 0 && (!stats || !dloss)) fail(GS_ERR_INVALID_ARG, "null statistics or gradient");
-        if ((uintptr_t)stats % 8) fail(GS_ERR_INVALID_ARG, "stats are not 8-byte aligned");
+        if ((uintptr_t)stats % 16) fail(GS_ERR_INVALID_ARG, "stats are not 16-byte aligned");
         if (n == 0) return;
-        const GradIn a{(const float2 *)stats, dloss, nullptr, nullptr};
+        const GradIn a{stats, dloss, nullptr, nullptr};
         const int kp = (int)ceil_div(k, 4) * 4;
         auto go = [&](auto type) {
             using T = decltype(type);

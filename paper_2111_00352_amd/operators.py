@@ -290,8 +290,8 @@ def distill_loss(logits: torch.Tensor, top_ids: torch.Tensor, top_logits: torch.
     of = logits
     logits, ld, code, (n, v), s = _dense(logits, "logits")
     k, id_bytes, t_code = _teacher(top_ids, top_logits, n, logits.get_device())
-    both = torch.empty(3 * n, dtype=torch.float32, device=logits.device)
-    stats, loss = both[:2 * n].view(n, 2), both[2 * n:]
+    both = torch.empty(5 * n, dtype=torch.float32, device=logits.device)
+    stats, loss = both[:4 * n].view(n, 4), both[4 * n:]
     _raise(lib().gs_distill_loss(logits.data_ptr(), ld, code, n, v, top_ids.data_ptr(), id_bytes, top_logits.data_ptr(), t_code, k,
                                  float(temperature), loss.data_ptr(), stats.data_ptr(), s))
     return _results((loss, stats), of, top_logits)
@@ -307,7 +307,7 @@ def distill_grad(logits: torch.Tensor, top_ids: torch.Tensor, top_logits: torch.
     logits, ld, code, (n, v), s = _dense(logits, "logits")
     at = logits.get_device()
     k, id_bytes, t_code = _teacher(top_ids, top_logits, n, at)
-    _array(stats, "stats", (n, 2), _F32, at)
+    _array(stats, "stats", (n, 4), _F32, at)
     _array(dloss, "dloss", (n,), _F32, at)
     D, ldo = _out(out, (n, v), logits.dtype, logits.device, of)
     _raise(lib().gs_distill_grad(logits.data_ptr(), ld, code, n, v, top_ids.data_ptr(), id_bytes, top_logits.data_ptr(), t_code, k,

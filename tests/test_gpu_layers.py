@@ -258,6 +258,7 @@ def test_two_threads_at_once():
 def test_refusals():
     X, R, w, W, off, s, ids, tid, t, g = _operands(20, 64, 30, 11)
     found = gs.log_probs(s, ids)
+    stats = gs.distill_loss(s, tid, t)[1]
     r = torch.ones(20, device=DEV)
     S = gs.save_activation(X, "none")[1]
     for call in (
@@ -275,8 +276,8 @@ def test_refusals():
         lambda: gs.log_probs_grad(s, ids, found, g[:3]), lambda: gs.log_probs_grad(s[:3], ids, found, g), lambda: gs.log_probs_grad(s, ids, found, g.double()),
         lambda: gs.distill_loss(s, tid[:, :0], t[:, :0]), lambda: gs.distill_loss(s, tid, t[:, :3]), lambda: gs.distill_loss(s, tid.t(), t),
         lambda: gs.distill_loss(s, torch.zeros(20, 129, dtype=torch.int32, device=DEV), torch.zeros(20, 129, device=DEV)),
-        lambda: gs.distill_grad(s, tid, t, g, g), lambda: gs.distill_grad(s, tid, t, found.stats, g[:2]),
-        lambda: gs.distill_grad(s, tid, t, found.stats, g, out=s[:, :5]),
+        lambda: gs.distill_grad(s, tid, t, g, g), lambda: gs.distill_grad(s, tid, t, found.stats, g), lambda: gs.distill_grad(s, tid, t, stats, g[:2]),
+        lambda: gs.distill_grad(s, tid, t, stats, g, out=s[:, :5]),
     ):
         with pytest.raises(ValueError):
             call()
@@ -289,13 +290,14 @@ def test_refusals():
 def test_no_gradient_is_dropped_unseen():
     X, R, w, W, off, s, ids, tid, t, g = _operands(20, 64, 30, 12)
     found = gs.log_probs(s, ids)
+    stats = gs.distill_loss(s, tid, t)[1]
     r = torch.ones(20, device=DEV)
     need = lambda x: x.detach().requires_grad_()  # noqa: E731
     for call in (lambda: gs.rms_norm(need(X))[0], lambda: gs.rms_norm(X, need(w))[2], lambda: gs.rms_norm(X, w, need(R))[1],
                  lambda: gs.rms_norm_grad(X, r, need(R))[0], lambda: gs.grouped_matmul(need(X), W, off), lambda: gs.grouped_matmul(X, need(W), off),
                  lambda: gs.grouped_weight_grad(X, need(R), off), lambda: gs.log_probs(need(s), ids).entropy, lambda: gs.log_probs(need(s), ids).logp,
                  lambda: gs.log_probs_grad(need(s), ids, found, g), lambda: gs.distill_loss(need(s), tid, t)[0], lambda: gs.distill_loss(s, tid, need(t))[0],
-                 lambda: gs.distill_grad(s, tid, t, found.stats, need(g))):
+                 lambda: gs.distill_grad(s, tid, t, stats, need(g))):
         with pytest.raises(RuntimeError, match="no gradient"):
             call().sum().backward()
         with torch.no_grad():
