@@ -100,7 +100,7 @@ template <class T> struct Alternative {
         id = in && i < te.k ? te.ids.at(at) : -1;
         t = id >= 0 ? load_either(te.t, te.t32, at) : 0.0f;
     }
-    __device__ __forceinline__ void look_up(const T *p, int v)
+    __device__ __forceinline__ void look_up(const T *p, int v)  // (in memory or in LDS)
     {
         if (t == -kInf) id = -1;
         s = id < 0 ? 0.0f : id < v ? to_f32(p[id]) : __builtin_nanf("");
@@ -243,6 +243,84 @@ __global__ __launch_bounds__(kRowThreads) void k_scores_held(const T *__restrict
                 }
             }
         }
+    }
+}
+
+// ------------------------------------------------- short rows, one behind the other
+//
+// Up to 128 logits a row, rows that follow each other without a gap: a workgroup copies its rows'
+// bytes to LDS as whole aligned lines and takes rows from there, L lanes a row, every L-th
+// element a lane's; gradients go back the same way.  (In pieces of 16 bytes of each row: gradient of
+// 2,000,000 x 47 fp32 223 us for 149, of 1,500,000 x 64 190 for 147, distillation 145 and 283 for 127 and
+// 221, 125 and 231 for 113 and 201.  Scores alone are not quicker so: 88 and 91, 80 and 90.)
+constexpr int kFlatMost = 128;
+
+// Rows in LDS: behind each other, with a piece between them where whole pieces make a row and
+// an even number of them would put many rows on the same banks.
+struct FlatRows {
+    int v, pitch;
+    uint32_t m;  // ceil(2^24 / v): i / v = i m / 2^24 for i below 2^16 (v <= 128)
+    template <class T> static FlatRows of(int v)
+    {
+        constexpr int E = kPiece<T>;
+        return {v, v % E == 0 && v / E % 2 == 0 ? v + E : v, (uint32_t)(((1u << 24) + v - 1) / v)};
+    }
+    __device__ __forceinline__ int place(int i) const  // of element i of the rows
+    {
+        return pitch == v ? i : i + (int)((uint64_t)(uint32_t)i * m >> 24) * (pitch - v);
+    }
+    template <class T, int L> __host__ __device__ int elems() const  // of LDS, for whole pieces
+    {
+        constexpr int E = kPiece<T>;
+        return (kRowThreads / L * pitch + E - 1) / E * E;
+    }
+};
+// Copies `count` elements between memory and LDS (16-byte aligned both).
+template <class T> __device__ __forceinline__ void flat_load(const T *from, T *to, int count, const FlatRows &f)
+{
+    constexpr int E = kPiece<T>;
+    for (int i = threadIdx.x * E; i < count; i += kRowThreads * E)
+        *reinterpret_cast<typename Elems<T, E>::type *>(to + f.place(i)) = load_elems<T, E, true>(from + i, count - i);
+}
+template <class T> __device__ __forceinline__ void flat_store(T *to, const T *from, int count, const FlatRows &f)
+{
+    constexpr int E = kPiece<T>;
+    for (int i = threadIdx.x * E; i < count; i += kRowThreads * E)
+        store_elems<T, E, true>(to + i, *reinterpret_cast<const typename Elems<T, E>::type *>(from + f.place(i)), count - i);
+}
+
+// The loss against a teacher.
+template <class T, int L, int C>
+__global__ __launch_bounds__(kRowThreads) void k_flat_loss(const T *__restrict__ s, int64_t n, FlatRows f, Teacher te, ScoreOut out)
+{
+    constexpr int ROWS = kRowThreads / L;
+    extern __shared__ __align__(16) uint8_t lds[];
+    T *all = (T *)lds;
+    const int v = f.v, lane = threadIdx.x % L, mine = threadIdx.x / L;
+    for (int64_t r0 = (int64_t)blockIdx.x * ROWS; r0 < n; r0 += (int64_t)gridDim.x * ROWS) {
+        const int64_t row = r0 + mine;
+        const bool in = row < n;
+        const T *p = all + mine * f.pitch;
+        Alternative<T> first;
+        first.load(te, row, lane, in);
+        flat_load(s + r0 * v, all, (int)std::min<int64_t>(ROWS, n - r0) * v, f);
+        __syncthreads();
+        float x[C], sum = 0.0f;
+        RowStats t{-kInf, 0.0f, 0.0f};
+#pragma unroll
+        for (int i = 0; i < C; i++) {
+            const int c = lane + L * i;
+            x[i] = in && c < v ? to_f32(p[c]) : -kInf;
+            t.m = fmaxf(t.m, x[i]);
+        }
+        t.m = group_fold<L>(t.m, [](float a, float b) { return fmaxf(a, b); });
+        const Scale by(te.k2, t.m);
+#pragma unroll
+        for (int i = 0; i < C; i++) sum += __builtin_amdgcn_exp2f(by.power(x[i]));
+        t.set(group_sum<L>(sum), 0.0f);
+        first.look_up(p, v);
+        write_loss<T, L>(t, logf(t.S), p, row, in, v, te, lane, first, (float *)nullptr, out.lp, (float4 *)out.stats);
+        __syncthreads();  // (before the next rows')
     }
 }
 
@@ -563,6 +641,82 @@ __global__ __launch_bounds__(kRowThreads) void k_scores_grad(const T *s, int64_t
     }
 }
 
+// Short rows: see k_flat_loss.  TEACHER: the distillation loss's gradient, else the scores'.
+constexpr int kFlatAlternatives = 32;
+template <class T, int L, int C, bool TEACHER>
+__global__ __launch_bounds__(kRowThreads) void k_flat_grad(const T *s, int64_t n, FlatRows f, ClassIds ids, Teacher te, GradIn a, int kp, T *out)
+{
+    const int v = f.v;
+    constexpr int ROWS = kRowThreads / L;
+    extern __shared__ __align__(16) uint8_t lds[];
+    T *all = (T *)lds;
+    const int lane = threadIdx.x % L, mine = threadIdx.x / L;
+    T *p = all + mine * f.pitch;
+    int *alt = (int *)(all + f.template elems<T, L>()) + 2 * kp * mine;  // classes and weights of the row's alternatives
+    float *w = (float *)alt + kp;
+    for (int64_t r0 = (int64_t)blockIdx.x * ROWS; r0 < n; r0 += (int64_t)gridDim.x * ROWS) {
+        const int64_t row = r0 + mine;
+        const bool in = row < n;
+        const int count = (int)std::min<int64_t>(ROWS, n - r0) * v;
+        flat_load(s + r0 * v, all, count, f);
+        float m, fa = 0.0f, fb, g = 0.0f;
+        int given = -1;
+        if constexpr (TEACHER) {
+            const float4 st = in ? ((const float4 *)a.stats)[row] : make_float4(0.0f, 1.0f, 0.0f, 0.0f);
+            m = st.x;
+            g = in && st.w != 0.0f ? a.g[row] / te.c + (st.w - st.w) : 0.0f;
+            fb = g / st.y;
+            for (int i = lane; i < kp; i += L) {
+                Alternative<T> one;
+                one.load(te, row, i, in);
+                const bool there = one.id >= 0 && one.id < v && one.t != -kInf;
+                alt[i] = there ? (int)one.id : -1;
+                w[i] = there ? exp_neg((one.t - st.z) * te.c) * st.w : 0.0f;
+            }
+        } else {
+            const float2 st = in ? ((const float2 *)a.stats)[row] : make_float2(0.0f, 1.0f);
+            const int64_t id = in && a.g ? ids.at(row) : -1;
+            const float e = in && a.e ? a.e[row] : 0.0f, H = in && a.e ? a.entropy[row] : 0.0f;
+            g = id < 0 ? 0.0f : id < v ? a.g[row] : __builtin_nanf("");
+            given = id >= 0 && id < v ? (int)id : -1;
+            m = st.x;
+            const float inv = 1.0f / st.y;
+            fa = -e * kLn2 * inv;
+            fb = (-g - e * (H - logf(st.y))) * inv;
+        }
+        __syncthreads();
+        const Scale by(TEACHER ? te.k2 : kLog2e, m);
+        float y[C];
+#pragma unroll
+        for (int i = 0; i < C; i++) {
+            const int c = lane + L * i;
+            const float d = by.power(in && c < v ? to_f32(p[c]) : 0.0f), weight = __builtin_amdgcn_exp2f(d);
+            if constexpr (TEACHER) {
+                y[i] = g == 0.0f ? 0.0f : weight * fb;
+            } else {
+                y[i] = weight * (a.e ? __builtin_fmaf(fa, fmaxf(d, -0x1p100f), fb) : fb);
+                if (c == given) y[i] += g;
+            }
+        }
+        // (a lane's own elements: what an alternative adds to one is found before it is rounded)
+        if constexpr (TEACHER) {
+            for (int o = 0; o < kp; o++) {
+                const int at = alt[o] - lane;
+                const float add = g * w[o];
+#pragma unroll
+                for (int i = 0; i < C; i++)
+                    if (at == L * i && g != 0.0f) y[i] -= add;
+            }
+        }
+#pragma unroll
+        for (int i = 0; i < C; i++)
+            if (in && lane + L * i < v) p[lane + L * i] = from_f32<T>(y[i]);
+        __syncthreads();
+        flat_store(out + r0 * v, all, count, f);
+        __syncthreads();  // (before the next rows')
+    }
+}
+
 // What the L lanes of a row have written to LDS and stored is seen by all of them.
 template <int L> __device__ __forceinline__ void lanes_meet()
 {
@@ -685,6 +839,33 @@ Teacher check_teacher(const void *ids, int id_bytes, const void *t, int t_dtype,
             (float)(1.4426950408889634 / temperature), (float)(temperature * temperature)};
 }
 
+// Whether rows are short and without gaps; go(L, C): lanes and elements.
+template <class T> bool flat_rows(int64_t v, std::initializer_list<std::pair<const void *, int64_t>> operands)
+{
+    if (v > kFlatMost || v < 8) return false;
+    for (const auto &[p, ld] : operands)
+        if ((uintptr_t)p % 16 || ld != v) return false;
+    return true;
+}
+template <class Go> void with_flat(int64_t v, Go &&go)
+{
+    using std::integral_constant;
+    const integral_constant<int, 4> l4;
+    const integral_constant<int, 8> l8;
+    if (v <= 16)
+        go(l4, integral_constant<int, 4>{});
+    else if (v <= 32)
+        go(l4, integral_constant<int, 8>{});
+    else if (v <= 48)
+        go(l4, integral_constant<int, 12>{});
+    else if (v <= 64)
+        go(l4, integral_constant<int, 16>{});
+    else if (v <= 96)
+        go(l8, integral_constant<int, 12>{});
+    else
+        go(l8, integral_constant<int, 16>{});
+}
+
 // Rows that a workgroup (with alternatives to find: a wave) holds stay in registers; wider
 // ones take a workgroup a row, the larger the fewer they are (the chip holds 2,048 of 256 threads).
 // A workgroup takes one set of rows: 2,048 that go on to further ones are slower (2,000,000 x 47:
@@ -697,6 +878,17 @@ void launch_scores(const T *s, int64_t ld, int64_t n, int64_t v, const ClassIds 
     const int64_t pieces = ceil_div(v, kPiece<T>);
     // (past the caches only where a load takes whole lines: 2,000,000 x 48 86 us, past them 158)
     const bool nt = pieces > 32 && streams((double)n * v * sizeof(T), v, sizeof(T), {{s, ld}});
+    if constexpr (TEACHER) {
+        if (flat_rows<T>(v, {{s, ld}})) {
+            with_flat(v, [&](auto l, auto c) {
+                constexpr int L = decltype(l)::value, C = decltype(c)::value;
+                const unsigned grid = (unsigned)std::min<int64_t>(ceil_div(n, (int64_t)(kRowThreads / L)), kRowBlocks);
+                const FlatRows f = FlatRows::of<T>((int)v);
+                k_flat_loss<T, L, C><<<grid, kRowThreads, f.template elems<T, L>() * sizeof(T), st>>>(s, n, f, te, out);
+            });
+            return;
+        }
+    }
     const bool held = pieces <= (out.top ? 4 * kWave : 4 * kRowThreads) && with_row<4, kRowThreads, 4>(pieces, [&](auto l, auto r) {
         constexpr int L = decltype(l)::value, R = decltype(r)::value;
         const unsigned grid = (unsigned)std::min<int64_t>(ceil_div(n, (int64_t)(kRowThreads / L)), kRowBlocks);
@@ -770,6 +962,16 @@ int gs_log_probs_grad(const void *s, int64_t ld, int dtype, int64_t n, int64_t v
         const GradIn a{stats, dlogp, dentropy, entropy};
         auto go = [&](auto type) {
             using T = decltype(type);
+            if (flat_rows<T>(v, {{s, ld}, {out, ldo}})) {
+                with_flat(v, [&](auto l, auto c) {
+                    constexpr int L = decltype(l)::value, C = decltype(c)::value;
+                    const unsigned grid = (unsigned)std::min<int64_t>(ceil_div(n, (int64_t)(kRowThreads / L)), kRowBlocks);
+                    const FlatRows f = FlatRows::of<T>((int)v);
+                    k_flat_grad<T, L, C, false><<<grid, kRowThreads, f.template elems<T, L>() * sizeof(T), (hipStream_t)stream>>>(
+                        (const T *)s, n, f, id, Teacher{}, a, 0, (T *)out);
+                });
+                return;
+            }
             const bool nt = streams(2.0 * n * v * sizeof(T), v, sizeof(T), {{s, ld}, {out, ldo}});
             grad_shape<T>(n, v, [&](auto l, auto r, int span, dim3 grid) {
                 constexpr int L = decltype(l)::value, R = decltype(r)::value;
@@ -818,6 +1020,17 @@ int gs_distill_grad(const void *s, int64_t ld, int dtype, int64_t n, int64_t v, 
         const int kp = (int)ceil_div(k, 4) * 4;
         auto go = [&](auto type) {
             using T = decltype(type);
+            if (k <= kFlatAlternatives && flat_rows<T>(v, {{s, ld}, {out, ldo}})) {
+                with_flat(v, [&](auto l, auto c) {
+                    constexpr int L = decltype(l)::value, C = decltype(c)::value, ROWS = kRowThreads / L;
+                    const unsigned grid = (unsigned)std::min<int64_t>(ceil_div(n, (int64_t)ROWS), kRowBlocks);
+                    const FlatRows f = FlatRows::of<T>((int)v);
+                    const size_t lds = f.template elems<T, L>() * sizeof(T) + (size_t)ROWS * 2 * kp * 4;
+                    k_flat_grad<T, L, C, true><<<grid, kRowThreads, lds, (hipStream_t)stream>>>(
+                        (const T *)s, n, f, ClassIds{nullptr, false}, te, a, kp, (T *)out);
+                });
+                return;
+            }
             grad_shape<T>(n, v, [&](auto l, auto r, int span, dim3 grid) {
                 constexpr int L = decltype(l)::value, R = decltype(r)::value;
                 k_distill_grad<T, L, R, false><<<grid, kRowThreads, (kRowThreads / L) * 3 * kp * 4, (hipStream_t)stream>>>(

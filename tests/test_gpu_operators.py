@@ -359,7 +359,7 @@ def test_grouped_one_matrix_for_all_groups_and_no_rows():
 
 # ---------------------------------------------------------------------- scores
 
-SCORE_SHAPES = [(1, 1), (3, 2), (70, 47), (33, 256), (9, 257), (11, 349), (5, 1024), (4, 2500), (3, 5000), (2, 20011), (2, 70000)]
+SCORE_SHAPES = [(1, 1), (3, 2), (200, 13), (65, 31), (70, 47), (131, 65), (41, 127), (90, 16), (33, 64), (50, 72), (70, 128), (33, 256), (9, 257), (11, 349), (5, 1024), (4, 2500), (3, 5000), (2, 20011), (2, 70000)]
 
 
 def _logits(n, v, seed, dtype, masked=True):
@@ -390,8 +390,11 @@ def _sum_terms(v):
 
 @pytest.mark.parametrize("n,v", SCORE_SHAPES)
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
-def test_log_probs(n, v, dtype):
-    s, wide = _inside(_logits(n, v, n + v, dtype).to(DEV))
+@pytest.mark.parametrize("apart", [True, False])
+def test_log_probs(n, v, dtype, apart):
+    s = _logits(n, v, n + v, dtype).to(DEV)
+    if apart:
+        s, wide = _inside(s)
     rng = np.random.default_rng(v)
     ids = rng.integers(0, v, n)
     ids[0] = 0
@@ -426,13 +429,13 @@ def test_log_probs(n, v, dtype):
         if ee is not None:
             tol += np.abs(_np(ee))[:, None] * ((p * rp + FLUSH) * inner + p * (tolH[:, None] + 4 * U * (np.abs(x) + logS[:, None] + inner)))
         _close(d, w, tol + HALF[dtype] * np.abs(w), "gradient")
-    assert _around_is_nan(s, wide)
-    flat = s.contiguous()
+    assert not apart or _around_is_nan(s, wide)
+    flat = s.clone().contiguous()
     first = gs.log_probs_grad(flat, it, got, g, e)
     assert gs.log_probs_grad(flat, it, got, g, e, out=flat) is flat and torch.equal(flat, first)  # in place
 
 
-@pytest.mark.parametrize("v", [5, 300, 3000, 40000])
+@pytest.mark.parametrize("v", [5, 47, 300, 3000, 40000])
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
 def test_log_probs_of_rows_without_a_distribution(v, dtype):
     s = torch.zeros(9, v)
@@ -470,10 +473,13 @@ def test_log_probs_of_rows_without_a_distribution(v, dtype):
 @pytest.mark.parametrize("n,v", SCORE_SHAPES)
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
 @pytest.mark.parametrize("T", [1.0, 2.5])
-def test_distill(n, v, dtype, T):
+@pytest.mark.parametrize("apart", [True, False])
+def test_distill(n, v, dtype, T, apart):
     rng = np.random.default_rng(n * v)
-    s, wide = _inside(_logits(n, v, n + v, dtype, masked=False).to(DEV))
-    k = min(v, 1 + (n * 7 + v) % 128)
+    s = _logits(n, v, n + v, dtype, masked=False).to(DEV)
+    if apart:
+        s, wide = _inside(s)
+    k = min(v, 1 + (n * 7 + v) % (128 if apart else 32))
     ids = np.stack([rng.permutation(v)[:k] for _ in range(n)])
     t = 3 * rng.standard_normal((n, k)).astype(np.float32)
     if k > 3:
@@ -508,9 +514,11 @@ def test_distill(n, v, dtype, T):
     np.add.at(tol, (rows, ids.ravel()[on.ravel()]), (q * U * (4 * dd + 2 * k + 20)).ravel()[on.ravel()])
     w = d * g[:, None]
     _close(got, w, np.abs(g)[:, None] * T * tol + (HALF[dtype] + 4 * U) * np.abs(w), "gradient")
-    assert _around_is_nan(s, wide)
-    flat = s.contiguous()
-    assert gs.distill_grad(flat, it, tt, stats, gt, T, out=flat) is flat and torch.equal(flat, got)
+    assert not apart or _around_is_nan(s, wide)
+    flat = s.clone().contiguous()
+    first = gs.distill_grad(flat, it, tt, stats, gt, T)
+    _close(first, w, np.abs(g)[:, None] * T * tol + (HALF[dtype] + 4 * U) * np.abs(w), "gradient")
+    assert gs.distill_grad(flat, it, tt, stats, gt, T, out=flat) is flat and torch.equal(flat, first)
 
 
 def test_distill_masked_and_bad():
