@@ -410,16 +410,16 @@ __global__ __launch_bounds__(256, WT == 1 ? 4 : 2) void k_grouped(LA A, LB W, in
 
 constexpr int kFewWaves = 4;
 
-// 16 bytes along k of a row of A, from k on.
-template <class T> __device__ __forceinline__ u32x4 row_piece(const AlongRows<T> &A, int64_t r, int64_t k, int64_t k1)
+// 16 bytes along k of a row of A, from k on, `valid` elements of them.
+template <class T> __device__ __forceinline__ u32x4 row_piece(const AlongRows<T> &A, int64_t r, int64_t k, int64_t valid)
 {
-    return __builtin_bit_cast(u32x4, load_elems<T, kPiece<T>>(A.p + r * A.ld + k, k1 - k));
+    return __builtin_bit_cast(u32x4, load_elems<T, kPiece<T>>(A.p + r * A.ld + k, valid));
 }
-template <class T> __device__ __forceinline__ u32x4 row_piece(const SavedAlongRows<T> &A, int64_t r, int64_t k, int64_t k1)
+template <class T> __device__ __forceinline__ u32x4 row_piece(const SavedAlongRows<T> &A, int64_t r, int64_t k, int64_t valid)
 {
     constexpr int E = kPiece<T>;
     typename Elems<T, E>::type v{};
-    if (k < k1) {  // (codes behind the last column are 0)
+    if (valid > 0) {  // (codes behind the last column are 0)
         const auto c = *reinterpret_cast<const typename Codes<E>::type *>(A.codes + r * A.code_pitch + k);
         const float s = mx_scale(A.scales[r * A.scale_pitch + k / kMxBlock]);
 #pragma unroll
@@ -464,7 +464,7 @@ __global__ __launch_bounds__(kFewWaves * kWave, N == 4 ? 2 : 3) void k_grouped_f
 #pragma unroll
     for (int i = 0; i < (TURN ? 1 : N); i++) base[i] = B + (TURN ? column(lane % 32, 0) + half * E * ldw : column(lane % 32, i) * ldw + half * E);
     auto load = [&](Step &t, int64_t at) {  // whole steps
-        t.a = row_piece(A, row, at + half * E, at + STEP);
+        t.a = row_piece(A, row, at + half * E, E);
         if constexpr (TURN) {
             const T *p = base[0] + at * ldw;
 #pragma unroll
@@ -476,7 +476,7 @@ __global__ __launch_bounds__(kFewWaves * kWave, N == 4 ? 2 : 3) void k_grouped_f
     };
     auto load_end = [&](Step &t, int64_t at) {  // zeros from k on
         const int64_t ka = at + half * E;
-        t.a = row_piece(A, row, ka, k);
+        t.a = row_piece(A, row, ka, k - ka);
         if constexpr (TURN) {
 #pragma unroll
             for (int e = 0; e < E; e++) t.v[e] = load_elems<T, N>(base[0] + (at + e) * ldw, ka + e < k ? N : 0);
@@ -1012,8 +1012,8 @@ __device__ __forceinline__ uint8_t *grad_piece(uint8_t *lds, int row, int piece)
     return lds + row * kLine + ((piece ^ ((row >> 1 ^ row >> 4) & 7)) << 4);
 }
 
-// Columns c0 .. c0 + 64 N - 1 of rows: a lane's are `at` .. at + N - 1.
-template <class T, int N> struct GradDense {
+// Columns c0 .. c0 + 64 N - 1 of rows: a lane's are `at` .. at + N - 1.  NARROW: there are fewer than N.
+template <class T, int N, bool NARROW = false> struct GradDense {
     typedef T type;
     const T *p;
     int64_t ld;
@@ -1028,7 +1028,7 @@ template <class T, int N> struct GradDense {
     }
     __device__ __forceinline__ void load(Held &h, int e, int64_t row, int64_t at) const
     {
-        h.v[e] = load_elems<T, N>(p + row * ld + at, width - at);
+        h.v[e] = load_elems<T, N>(p + row * ld + at, NARROW ? width - at : N);
     }
     __device__ __forceinline__ void none(Held &h, int e) const { h.v[e] = typename Elems<T, N>::type{}; }
     __device__ __forceinline__ u32x4 column_of(const Held &h, int i) const { return turned<T, N>(h.v, i); }
@@ -1085,25 +1085,27 @@ __global__ __launch_bounds__(kGradThreads, 2) void k_grouped_grad(LA A, LG G, Of
         typename LA::Held a;
         typename LG::Held b;
     } h0, h1;
+    // (loads that are always made, from the last row where there are no more, so that the wait for one
+    // chunk's need not be one for the next's: with loads behind branches this took 51 us)
     auto load = [&](Held &h, int64_t k) {
         k += wave * E;
-        if (k + E <= k1) {
 #pragma unroll
-            for (int e = 0; e < E; e++) {
-                A.load(h.a, e, k + e, ca);
-                G.load(h.b, e, k + e, cb);
-            }
-        } else {
-#pragma unroll
-            for (int e = 0; e < E; e++) {
-                A.none(h.a, e);
-                G.none(h.b, e);
-                if (k + e < k1) {
-                    A.load(h.a, e, k + e, ca);
-                    G.load(h.b, e, k + e, cb);
-                }
-            }
+        for (int e = 0; e < E; e++) {
+            const int64_t row = std::min(k + e, off.rows - 1);
+            A.load(h.a, e, row, ca);
+            G.load(h.b, e, row, cb);
         }
+    };
+    // Rows from k1 on, of other groups or none, as zeros.
+    auto end = [&](Held &h, int64_t k) {
+        k += wave * E;
+        if (k + E > k1)
+#pragma unroll
+            for (int e = 0; e < E; e++)
+                if (k + e >= k1) {
+                    A.none(h.a, e);
+                    G.none(h.b, e);
+                }
     };
     // (a lane moved back from the end of the rows may hold columns before the tile's first)
     const int la = (int)(ca - a0), lb = (int)(cb - b0);
@@ -1136,19 +1138,24 @@ __global__ __launch_bounds__(kGradThreads, 2) void k_grouped_grad(LA A, LG G, Of
         }
     };
     constexpr int64_t STEP = kChunk<T>;
-    load(h0, k0);
-    load(h1, k0 + STEP);
-    store(h0, lds);
-    __syncthreads();
-    for (int64_t k = k0; k < k1; k += 2 * STEP) {
-        load(h0, k + 2 * STEP);
-        work(lds);
-        store(h1, lds + STAGE);
-        __syncthreads();
-        load(h1, k + 3 * STEP);
-        if (k + STEP < k1) work(lds + STAGE);
+    if (k0 < k1) {
+        load(h0, k0);
+        load(h1, k0 + STEP);
+        end(h0, k0);
         store(h0, lds);
         __syncthreads();
+        for (int64_t k = k0; k < k1; k += 2 * STEP) {
+            load(h0, k + 2 * STEP);
+            work(lds);
+            end(h1, k + STEP);
+            store(h1, lds + STAGE);
+            __syncthreads();
+            load(h1, k + 3 * STEP);
+            if (k + STEP < k1) work(lds + STAGE);
+            end(h0, k + 2 * STEP);
+            store(h0, lds);
+            __syncthreads();
+        }
     }
     float *to = out + (int64_t)blockIdx.x * a * b;
 #pragma unroll
@@ -1441,6 +1448,8 @@ static int grouped_weight_grad(const Operand &A, int a_dtype, int64_t rows, int6
                 go(GradSaved<T, 2 * WA>{A.saved->codes, A.saved->scales, saved_code_pitch(a), saved_scale_pitch(a),
                                         {A.saved->act == GS_ACT_RELU}},
                    g, wa, wb);
+            else if (WA == 1 && a < 2)
+                go(GradDense<T, 2, true>{(const T *)A.p, A.ld, a}, g, std::integral_constant<int, 1>{}, wb);
             else
                 go(GradDense<T, 2 * WA>{(const T *)A.p, A.ld, a}, g, wa, wb);
         };
