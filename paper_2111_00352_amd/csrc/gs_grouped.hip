@@ -1012,7 +1012,8 @@ __device__ __forceinline__ uint8_t *grad_piece(uint8_t *lds, int row, int piece)
     return lds + row * kLine + ((piece ^ ((row >> 1 ^ row >> 4) & 7)) << 4);
 }
 
-// Columns c0 .. c0 + 64 N - 1 of rows: a lane's are `at` .. at + N - 1.  NARROW: there are fewer than N.
+// Columns c0 .. c0 + 64 N - 1 of rows, N of a lane: those from column() on.  A row's address is the
+// same for all lanes, but for a lane's own 32 bits.  NARROW: there are fewer than N columns.
 template <class T, int N, bool NARROW = false> struct GradDense {
     typedef T type;
     const T *p;
@@ -1021,48 +1022,77 @@ template <class T, int N, bool NARROW = false> struct GradDense {
     struct Held {
         typename Elems<T, N>::type v[kPiece<T>];
     };
+    struct Row {
+        const T *p;
+    };
     // (the last columns for lanes that would go past them: several lanes then hold the same)
     __device__ __forceinline__ int64_t column(int64_t c0) const
     {
         return std::max<int64_t>(0, std::min(c0 + threadIdx.x % kWave * N, width - N));
     }
-    __device__ __forceinline__ void load(Held &h, int e, int64_t row, int64_t at) const
+    __device__ __forceinline__ Row row(int64_t r, int64_t c) const { return {p + r * ld + c}; }
+    __device__ __forceinline__ void move(Row &r, bool on) const { r.p += on ? ld : 0; }
+    __device__ __forceinline__ void load(Held &h, int e, const Row &r, uint32_t at, int64_t) const
     {
-        h.v[e] = load_elems<T, N>(p + row * ld + at, NARROW ? width - at : N);
+        h.v[e] = load_elems<T, N>(r.p + at, NARROW ? width - at : N);
     }
     __device__ __forceinline__ void none(Held &h, int e) const { h.v[e] = typename Elems<T, N>::type{}; }
-    __device__ __forceinline__ u32x4 column_of(const Held &h, int i) const { return turned<T, N>(h.v, i); }
+    template <class F> __device__ __forceinline__ void columns(const Held &h, F put) const
+    {
+#pragma unroll
+        for (int i = 0; i < N; i++) put(i, turned<T, N>(h.v, i));
+    }
 };
 template <class T, int N> struct GradSaved {
     typedef T type;
     const uint8_t *codes, *scales;
     int64_t code_pitch, scale_pitch;
-    CodeValue value;
+    uint32_t sign;  // 128 where codes have a sign, else 0
     typedef std::conditional_t<N == 1, uint8_t, std::conditional_t<N == 2, u16, uint32_t>> Word;
     struct Held {
         Word c[kPiece<T>];
         uint8_t s[kPiece<T>];
     };
+    struct Row {
+        const uint8_t *codes, *scales;
+    };
     __device__ __forceinline__ int64_t column(int64_t c0) const
     {
         return std::min<int64_t>(c0 + threadIdx.x % kWave * N, code_pitch - N);
     }
-    __device__ __forceinline__ void load(Held &h, int e, int64_t row, int64_t at) const
+    __device__ __forceinline__ Row row(int64_t r, int64_t c) const { return {codes + r * code_pitch + c, scales + r * scale_pitch}; }
+    __device__ __forceinline__ void move(Row &r, bool on) const
     {
-        h.c[e] = *reinterpret_cast<const Word *>(codes + row * code_pitch + at);
-        h.s[e] = scales[row * scale_pitch + at / kMxBlock];
+        r.codes += on ? code_pitch : 0;
+        r.scales += on ? scale_pitch : 0;
+    }
+    __device__ __forceinline__ void load(Held &h, int e, const Row &r, uint32_t at, int64_t column) const
+    {
+        h.c[e] = *reinterpret_cast<const Word *>(r.codes + at);
+        h.s[e] = r.scales[(uint32_t)(column / kMxBlock)];
     }
     __device__ __forceinline__ void none(Held &h, int e) const
     {
         h.c[e] = 0;
         h.s[e] = 0;
     }
-    __device__ __forceinline__ u32x4 column_of(const Held &h, int i) const
+    // (128 is added to a signed code by turning its highest bit, and taken from the number again)
+    template <class F> __device__ __forceinline__ void columns(const Held &h, F put) const
     {
-        typename Elems<T, kPiece<T>>::type v;
+        float scale[kPiece<T>];
+        const float less = (float)sign;
 #pragma unroll
-        for (int e = 0; e < kPiece<T>; e++) v[e] = from_f32<T>(value(h.c[e], i) * mx_scale(h.s[e]));
-        return __builtin_bit_cast(u32x4, v);
+        for (int e = 0; e < kPiece<T>; e++) scale[e] = mx_scale(h.s[e]);
+#pragma unroll
+        for (int i = 0; i < N; i++) {
+            typename Elems<T, kPiece<T>>::type v;
+#pragma unroll
+            for (int e = 0; e < kPiece<T>; e++) {
+                const uint32_t word = h.c[e] ^ sign * 0x01010101u;
+                v[e] = from_f32<T>(((float)(word >> (8 * i) & 255) - less) * scale[e]);
+            }
+            put(i, __builtin_bit_cast(u32x4, v));
+        }
     }
 };
 
@@ -1081,19 +1111,27 @@ __global__ __launch_bounds__(kGradThreads, 2) void k_grouped_grad(LA A, LG G, Of
     const int64_t a0 = (int64_t)(blockIdx.y / tiles_b) * SA, b0 = (int64_t)(blockIdx.y % tiles_b) * SB;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave), lane = threadIdx.x % kWave, half = lane / 32;
     const int64_t ca = A.column(a0), cb = G.column(b0);
+    // (a lane moved back from the end of the rows may hold columns before the tile's first)
+    const int la = (int)(ca - a0), lb = (int)(cb - b0);
+    const int64_t fa = std::max<int64_t>(0, a0 - 4), fb = std::max<int64_t>(0, b0 - 4), last = off.rows - 1;
+    const uint32_t at_a = (uint32_t)(ca - fa), at_b = (uint32_t)(cb - fb);
     struct Held {
         typename LA::Held a;
         typename LG::Held b;
     } h0, h1;
     // (loads that are always made, from the last row where there are no more, so that the wait for one
-    // chunk's need not be one for the next's: with loads behind branches this took 51 us)
+    // chunk's need not be one for the next's)
     auto load = [&](Held &h, int64_t k) {
-        k += wave * E;
+        k = std::min(k + wave * E, last);
+        const int more = (int)std::min<int64_t>(last - k, E);
+        auto ra = A.row(k, fa);
+        auto rb = G.row(k, fb);
 #pragma unroll
         for (int e = 0; e < E; e++) {
-            const int64_t row = std::min(k + e, off.rows - 1);
-            A.load(h.a, e, row, ca);
-            G.load(h.b, e, row, cb);
+            A.load(h.a, e, ra, at_a, ca);
+            G.load(h.b, e, rb, at_b, cb);
+            A.move(ra, e < more);
+            G.move(rb, e < more);
         }
     };
     // Rows from k1 on, of other groups or none, as zeros.
@@ -1107,15 +1145,13 @@ __global__ __launch_bounds__(kGradThreads, 2) void k_grouped_grad(LA A, LG G, Of
                     G.none(h.b, e);
                 }
     };
-    // (a lane moved back from the end of the rows may hold columns before the tile's first)
-    const int la = (int)(ca - a0), lb = (int)(cb - b0);
     auto store = [&](const Held &h, uint8_t *to) {
-#pragma unroll
-        for (int i = 0; i < 2 * WA; i++)
-            if (la + i >= 0) *reinterpret_cast<u32x4 *>(grad_piece(to, la + i, wave)) = A.column_of(h.a, i);
-#pragma unroll
-        for (int i = 0; i < WB; i++)
-            if (lb + i >= 0) *reinterpret_cast<u32x4 *>(grad_piece(to + SA * kLine, lb + i, wave)) = G.column_of(h.b, i);
+        A.columns(h.a, [&](int i, u32x4 v) {
+            if (la + i >= 0) *reinterpret_cast<u32x4 *>(grad_piece(to, la + i, wave)) = v;
+        });
+        G.columns(h.b, [&](int i, u32x4 v) {
+            if (lb + i >= 0) *reinterpret_cast<u32x4 *>(grad_piece(to + SA * kLine, lb + i, wave)) = v;
+        });
     };
     f32x16 acc[WA][WB];
 #pragma unroll
@@ -1446,7 +1482,7 @@ static int grouped_weight_grad(const Operand &A, int a_dtype, int64_t rows, int6
             const GradDense<T, WB> g{(const T *)G, ldg, b};
             if (A.saved)
                 go(GradSaved<T, 2 * WA>{A.saved->codes, A.saved->scales, saved_code_pitch(a), saved_scale_pitch(a),
-                                        {A.saved->act == GS_ACT_RELU}},
+                                        A.saved->act == GS_ACT_RELU ? 0u : 128u},
                    g, wa, wb);
             else if (WA == 1 && a < 2)
                 go(GradDense<T, 2, true>{(const T *)A.p, A.ld, a}, g, std::integral_constant<int, 1>{}, wb);
