@@ -1159,19 +1159,22 @@ __global__ __launch_bounds__(kGradThreads, 2) void k_grouped_grad(LA A, LG G, Of
 #pragma unroll
         for (int j = 0; j < WB; j++) acc[i][j] = f32x16{};
     const int ra = wave / 2 * 32 * WA + lane % 32, rb = wave % 2 * 32 * WB + lane % 32;
+    // (waves past the gradient's last row or column multiply nothing)
+    const bool mine = a0 + wave / 2 * 32 * WA < a && b0 + wave % 2 * 32 * WB < b;
     auto work = [&](uint8_t *from) {
+        if (mine)
 #pragma unroll
-        for (int q = 0; q < 4; q++) {
-            u32x4 fa[WA], fb[WB];
+            for (int q = 0; q < 4; q++) {
+                u32x4 fa[WA], fb[WB];
 #pragma unroll
-            for (int i = 0; i < WA; i++) fa[i] = *reinterpret_cast<const u32x4 *>(grad_piece(from, ra + 32 * i, 2 * q + half));
+                for (int i = 0; i < WA; i++) fa[i] = *reinterpret_cast<const u32x4 *>(grad_piece(from, ra + 32 * i, 2 * q + half));
 #pragma unroll
-            for (int j = 0; j < WB; j++) fb[j] = *reinterpret_cast<const u32x4 *>(grad_piece(from + SA * kLine, rb + 32 * j, 2 * q + half));
+                for (int j = 0; j < WB; j++) fb[j] = *reinterpret_cast<const u32x4 *>(grad_piece(from + SA * kLine, rb + 32 * j, 2 * q + half));
 #pragma unroll
-            for (int i = 0; i < WA; i++)
+                for (int i = 0; i < WA; i++)
 #pragma unroll
-                for (int j = 0; j < WB; j++) acc[i][j] = multiply<T>(fb[j], fa[i], acc[i][j]);
-        }
+                    for (int j = 0; j < WB; j++) acc[i][j] = multiply<T>(fb[j], fa[i], acc[i][j]);
+            }
     };
     constexpr int64_t STEP = kChunk<T>;
     if (k0 < k1) {
