@@ -800,14 +800,14 @@ struct SavedRows {
     }
     __device__ __forceinline__ void fragments(const Held &h, int, int, u32x4 (&f)[2]) const
     {
-        const float s = mx_scale(h.s), z = -zero * s;
+        const float s = mx_scale(h.s);
         const uint32_t flip = zero != 0.0f ? 0x80808080u : 0u;
 #pragma unroll
         for (int w = 0; w < 4; w++) {
             const uint32_t c = h.c[w] ^ flip;
             uint32_t v[4];
 #pragma unroll
-            for (int e = 0; e < 4; e++) v[e] = __float_as_uint(__builtin_fmaf((float)(c >> (8 * e) & 255), s, z));  // (exact)
+            for (int e = 0; e < 4; e++) v[e] = __float_as_uint(((float)(c >> (8 * e) & 255) - zero) * s);  // (exact)
 #pragma unroll
             for (int e = 0; e < 2; e++) f[w / 2][w % 2 * 2 + e] = __builtin_amdgcn_perm(v[2 * e + 1], v[2 * e], 0x07060302);
         }

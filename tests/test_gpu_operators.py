@@ -283,6 +283,24 @@ def test_grouped_layers_infinite_weights_and_unfinite_rows():
     assert (got[:5, 0] == 64).all()
 
 
+@pytest.mark.parametrize("rows", [40, 2000, 20000])
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_grouped_codes_of_the_largest_numbers(rows, dtype):
+    """Steps of 2^121: a signed code's number is finite where 128 steps are not."""
+    rng = np.random.default_rng(rows)
+    A = torch.from_numpy(((rng.random((rows, 64)) - 0.5) * 6.7e38).astype(np.float32))
+    W = torch.from_numpy((rng.standard_normal((2, 64, 32)) * 2.0 ** -30).astype(np.float32)).to(TYPES[dtype]).to(DEV)
+    offsets = [0, rows // 3, rows]
+    Ad = gs.save_activation(A.to(DEV), "none")[1]
+    assert int(Ad.scales.max()) == 127 + 121 and Ad.dequantize().isfinite().all()
+    want, M = oracle.grouped(_np(Ad.dequantize()), _np(W), offsets, False)
+    got = gs.grouped_matmul(Ad, W, torch.tensor(offsets, device=DEV), dtype=torch.float32)
+    _close(got, want, (2 * 3 * 64 + 20) * U * M + U * np.abs(want))
+    G = (torch.ones(rows, 24) * 2.0 ** -30).to(TYPES[dtype]).to(DEV)
+    want, M = oracle.grouped_grad(_np(Ad.dequantize()), _np(G), offsets)
+    _close(gs.grouped_weight_grad(Ad, G, torch.tensor(offsets, device=DEV)), want, (2 * rows + 4) * U * M)
+
+
 @pytest.mark.parametrize("k", [128, 192, 320])
 @pytest.mark.parametrize("back", [False, True])
 @pytest.mark.parametrize("out", ["f32", "bf16"])
