@@ -1319,14 +1319,30 @@ static int grouped_matmul(const Operand &A, int a_dtype, int64_t rows, const voi
             fail(GS_ERR_INVALID_ARG, "W: span is not addressable");
         check_operand("C", C, rows, outw, ldc, csize);
         if (rows == 0) return;
+        const Extent c{C, rows, outw * csize, ldc * csize};
+        if (!A.saved) check_apart("C", c, "A", {A.p, rows, in * dtype_size(a_dtype), A.ld * dtype_size(a_dtype)});
+        const int64_t matrix = ((k - 1) * ldw + n) * wsize;
+        check_apart("C", c, "W", {W, groups, matrix, std::max(w_step * wsize, matrix)});
         const hipStream_t s = (hipStream_t)stream;
-        // Large tiles where there are enough to fill the chip: rows of whole aligned pieces, k
-        // of whole chunks, offsets in a matrix of 32 bits.
+        // Which kernel: all figures are us, groups of equal sizes, one set of operands after the other.
+        //
+        // Large tiles: rows of whole aligned pieces, k of whole chunks, offsets in a matrix of 32 bits; enough
+        // of them to keep half of the chip (rows x 1024 x 1024: 64 tiles 37 and 32 in tiles of 128, 128 tiles
+        // 38 and 41, 256 tiles 43 and 76) that are half full of rows (8192 x 2048 x 4096: 128 rows a group 323
+        // and 315, 256 171 and 288) and of columns (262,144 x 128 x 128: 57 and 37).
         const bool pieces = !A.saved && w_dtype == GS_BF16 && in % 64 == 0 && in >= 128 && A.ld % 8 == 0 && (uintptr_t)A.p % 16 == 0 &&
                             ldw % 8 == 0 && w_step % 8 == 0 && (uintptr_t)W % 16 == 0 && (transpose || (n % 8 == 0 && n >= 8)) &&
                             256 * A.ld < (1 << 30) && (transpose ? 256 : k) * ldw < (1 << 30);
         const int64_t large_n = ceil_div(outw, 256), large = (ceil_div(rows, 256) + groups + 2) * large_n;
-        if (pieces && rows >= 128 * groups && ceil_div(rows, 256) * large_n >= 128 && large <= INT32_MAX / 256) {
+        // Layers: bf16 operands or 8-bit rows, k from 16 to 256 (262,144 x 8 x 64: 29 and 29 in tiles, x 16 x 64:
+        // 12 and 29), many rows, 256 and more of a group.  Against fp32 matrices from 32,768 rows on (x 128 x
+        // 128: 21 and 20, 16,384 rows 21 and 14, 65,536 rows 22 and 30), bf16 from 196,608 (131,072 rows 25 and
+        // 21, 262,144 rows 33 and 37, 2,097,152 rows 218 and 319); 262,144 x 128 x 128 of fp32 with 256 rows
+        // a group 107 and 183, with 128 302 and 292.  Large tiles are better where both k and n are
+        // (131,072 x 256 x 256: 52 and 41).
+        const bool layers = in >= 16 && in <= 256 && rows >= 256 * groups && (A.saved || w_dtype == GS_BF16) &&
+                            rows >= (w_dtype == GS_F32 ? 32768 : 196608) && !(pieces && in > 128 && outw > 128);
+        if (pieces && !layers && outw > 128 && rows >= 128 * groups && ceil_div(rows, 256) * large_n >= 128 && large <= INT32_MAX / 256) {
             auto run = [&](auto kernel, auto type) {
                 kernel<<<(unsigned)large, 256, 0, s>>>((const u16 *)A.p, A.ld, (const u16 *)W, ldw, w_step, off, (int)(in / 64), outw,
                                                        fill != 0, (int)large_n, (decltype(type) *)C, ldc);
@@ -1338,8 +1354,7 @@ static int grouped_matmul(const Operand &A, int a_dtype, int64_t rows, const voi
             GS_HIP(hipGetLastError());
             return;
         }
-        // Layers: bf16 operands or 8-bit rows, k up to 256, many rows of a group.
-        if (in >= 16 && in <= 256 && rows >= 1024 * groups && rows >= 16384 && (A.saved || w_dtype == GS_BF16)) {
+        if (layers) {
             const int j = (int)ceil_div(in, 32);
             auto run = [&](auto rows_of, auto w, auto out, auto jc, auto nt, auto rb, auto parts) {
                 using TW = decltype(w);
@@ -1383,8 +1398,8 @@ static int grouped_matmul(const Operand &A, int a_dtype, int64_t rows, const voi
             GS_HIP(hipGetLastError());
             return;
         }
-        // Few rows: the matrices are what is read.  Narrow tiles while there would be fewer than two
-        // workgroups a compute unit.
+        // Few rows: the matrices are what is read (64 groups, 1024 x 1024 bf16: 32 rows a group 35 and 47 in
+        // tiles, 48 56 and 50; 512 x 512 fp32: 32 rows 22 and 32, 64 36 and 32).
         if (rows <= 32 * groups && in >= 64 && outw >= 4) {
             auto run = [&](auto la, auto type, auto out, auto turn, auto cols) {
                 using T = decltype(type);
@@ -1395,7 +1410,9 @@ static int grouped_matmul(const Operand &A, int a_dtype, int64_t rows, const voi
                 k_grouped_few<decltype(la), T, decltype(turn)::value, N, TO><<<(unsigned)grid, kFewWaves * kWave, 0, s>>>(
                     la, (const T *)W, ldw, w_step, off, in, outw, fill != 0, (int)tiles_n, (TO *)C, ldc);
             };
-            const bool wide = std::min(rows, groups) * ceil_div(outw, 128) >= 512;
+            // 128 columns a workgroup where there is one a compute unit, else 64 (2048 x 1024 bf16, 8 groups:
+            // 20 and 17, 32 groups 25 and 29; 512 x 512 fp32, 64 groups 18 and 19)
+            const bool wide = std::min(rows, groups) * ceil_div(outw, 128) >= 256;
             auto with_n = [&](auto la, auto type, auto out, auto turn) {
                 wide ? run(la, type, out, turn, std::integral_constant<int, 4>{}) : run(la, type, out, turn, std::integral_constant<int, 2>{});
             };
@@ -1418,7 +1435,9 @@ static int grouped_matmul(const Operand &A, int a_dtype, int64_t rows, const voi
             GS_HIP(hipGetLastError());
             return;
         }
-        const int wt = rows <= 64 * groups || outw <= 64 ? 1 : 2;
+        // Tiles of 64 x 64 where ones of 128 x 128 would be half empty or too few (1024 x 1024 bf16, 256 rows a
+        // group: 128 of them 25 and 31, 256 of them 42 and 32; 64 groups of 64 rows 49 and 51, of 96 85 and 52).
+        const int wt = rows <= 64 * groups || outw <= 64 || ceil_div(rows, 128) * ceil_div(outw, 128) < 192 ? 1 : 2;
         const int64_t tiles_n = ceil_div(outw, 64 * wt), grid = (ceil_div(rows, 64 * wt) + groups + 2) * tiles_n;
         if (grid > INT32_MAX / 256) fail(GS_ERR_UNSUPPORTED, "the product has too many tiles");
         auto go = [&](auto la, auto lb, auto out) {

@@ -388,6 +388,10 @@ int gs_rms_norm(const void *X, int64_t ldx, const void *R, int64_t ldr, int dtyp
         if (rows > 0 && !rstd) fail(GS_ERR_INVALID_ARG, "rstd is null");
         if (w && (uintptr_t)w % dtype_size(w_dtype)) fail(GS_ERR_INVALID_ARG, "w is not aligned to its elements");
         if (rows == 0) return;
+        const auto extent = [&](const void *p, int64_t ld) { return Extent{p, rows, cols * size, ld * size}; };
+        const Extent x = extent(X, ldx), r = extent(R, ldr), h = extent(R ? H : nullptr, ldh), y = extent(Y, ldy);
+        check_apart("H", h, "X", x, true), check_apart("H", h, "R", r, true);
+        check_apart("Y", y, "X", x), check_apart("Y", y, "R", r), check_apart("Y", y, "H", h);
         const hipStream_t s = (hipStream_t)stream;
         const int blocks = (int)saved_scale_pitch(cols);
         const double bytes = (double)rows * cols * (size * (R ? 3 : 1) + (saved ? 1 : size));
@@ -450,6 +454,10 @@ int gs_rms_norm_grad(const void *H, int64_t ldh, const float *rstd, const void *
         if (work_bytes < need || !work)
             fail(GS_ERR_INVALID_ARG, "workspace of %llu bytes is below the %llu needed",
                  (unsigned long long)(work ? work_bytes : 0), (unsigned long long)need);
+        const auto extent = [&](const void *p, int64_t ld) { return Extent{p, rows, cols * size, ld * size}; };
+        const Extent dx = extent(dX, ldx);
+        check_apart("dX", dx, "H", extent(H, ldh)), check_apart("dX", dx, "dY", extent(dY, ldy));
+        check_apart("dX", dx, "dH", extent(dH, ldd), true);
         const hipStream_t s = (hipStream_t)stream;
         float *part = (float *)work;
         const double bytes = (double)rows * cols * size * (dH ? 4 : 3);

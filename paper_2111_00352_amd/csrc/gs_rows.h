@@ -12,6 +12,26 @@
 
 namespace gs {
 
+// A matrix that a call reads or writes, its sizes in bytes; NULL: not there.
+struct Extent {
+    const void *p;
+    int64_t rows, width, pitch;
+};
+// Refuses an output that shares bytes with an operand.  Of matrices of one pitch, parts of the
+// same rows may lie beside each other, and with `same` the operand may be the output itself.
+inline void check_apart(const char *output, const Extent &out, const char *name, const Extent &in, bool same = false)
+{
+    if (!out.p || !in.p || out.rows == 0 || in.rows == 0) return;
+    const int64_t a = (int64_t)(uintptr_t)out.p, b = (int64_t)(uintptr_t)in.p;
+    if (a + (out.rows - 1) * out.pitch + out.width <= b || b + (in.rows - 1) * in.pitch + in.width <= a) return;
+    if (out.pitch == in.pitch) {
+        if (same && a == b) return;
+        const int64_t d = ((b - a) % out.pitch + out.pitch) % out.pitch;
+        if (d >= out.width && d + in.width <= out.pitch) return;
+    }
+    fail(GS_ERR_INVALID_ARG, "%s overlaps %s", output, name);
+}
+
 // Elements of 16 bytes.
 template <class T> constexpr int kPiece = sizeof(T) == 4 ? 4 : 8;
 

@@ -958,6 +958,8 @@ int gs_log_probs_grad(const void *s, int64_t ld, int dtype, int64_t n, int64_t v
         const ClassIds id = dlogp ? check_ids("ids", ids, id_bytes, n) : ClassIds{nullptr, false};
         if (n > 0 && (!stats || (dentropy && !entropy))) fail(GS_ERR_INVALID_ARG, "null statistics");
         if ((uintptr_t)stats % 8) fail(GS_ERR_INVALID_ARG, "stats are not 8-byte aligned");
+        check_apart("out", {out, n, v * dtype_size(dtype), ldo * dtype_size(dtype)}, "logits",
+                    {s, n, v * dtype_size(dtype), ld * dtype_size(dtype)}, true);
         if (n == 0) return;
         const GradIn a{stats, dlogp, dentropy, entropy};
         auto go = [&](auto type) {
@@ -1015,6 +1017,8 @@ int gs_distill_grad(const void *s, int64_t ld, int dtype, int64_t n, int64_t v, 
         const Teacher te = check_teacher(top_ids, id_bytes, top_logits, t_dtype, n, k, temperature);
         if (n > 0 && (!stats || !dloss)) fail(GS_ERR_INVALID_ARG, "null statistics or gradient");
         if ((uintptr_t)stats % 16) fail(GS_ERR_INVALID_ARG, "stats are not 16-byte aligned");
+        check_apart("out", {out, n, v * dtype_size(dtype), ldo * dtype_size(dtype)}, "logits",
+                    {s, n, v * dtype_size(dtype), ld * dtype_size(dtype)}, true);
         if (n == 0) return;
         const GradIn a{stats, dloss, nullptr, nullptr};
         const int kp = (int)ceil_div(k, 4) * 4;

@@ -242,6 +242,21 @@ def test_grouped_matmul_of_few_rows(k, n, dtype, back, a8):
     assert (keep[110:] == 7).all() and _around_is_nan(keep, wide)
 
 
+@pytest.mark.parametrize("k,n", [(64, 1100), (71, 901), (200, 2051)])
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("back", [False, True])
+def test_grouped_matmul_of_few_rows_of_many_groups(k, n, dtype, back):
+    """Enough columns for the wider of the two kernels."""
+    rng = np.random.default_rng(n)
+    offsets = np.concatenate([[0], np.cumsum(rng.integers(0, 4, 40))])
+    rows = int(offsets[-1]) + 2
+    A = _inside(_hidden(rows, k, k, dtype).clamp(-1e6, 1e6).to(DEV))[0]
+    W = torch.from_numpy(rng.standard_normal((40, n, k) if back else (40, k, n)).astype(np.float32)).to(TYPES[dtype]).to(DEV)
+    want, M = oracle.grouped(_np(A), _np(W), offsets.tolist(), back)
+    got = gs.grouped_matmul(A, W, torch.from_numpy(offsets).to(DEV), transpose=back)
+    _close(got, want, (2 * k + 20) * U * M + HALF[dtype] * np.abs(want))
+
+
 LAYERS = [("bf16", False), ("bf16", True), ("f32", True)]  # W's type, A in 8 bits
 
 
@@ -250,26 +265,32 @@ LAYERS = [("bf16", False), ("bf16", True), ("f32", True)]  # W's type, A in 8 bi
 @pytest.mark.parametrize("back", [False, True])
 def test_grouped_matmul_of_layers(k, n, dtype, a8, back):
     """Many rows: matrices kept in LDS, groups that end inside a wave's rows, none, short and rows without one."""
-    offsets = [70, 70, 6000, 6001, 12345, 12345, 17990, 18000]
-    rows = 18100
+    at = 18 if dtype == "f32" else 110  # (thousands of rows)
+    offsets = [70, 70, 6000, 6001, 12345, 12345, 2 * at * 1000 - 10, 2 * at * 1000]
+    rows = offsets[-1] + 100
     A = _hidden(rows, k, k + n, "f32" if a8 else dtype).clamp(-1e6, 1e6)
     rng = np.random.default_rng(k)
     W = torch.from_numpy(rng.standard_normal((7, n, k) if back else (7, k, n)).astype(np.float32)).to(TYPES[dtype]).to(DEV)
     off = torch.tensor(offsets, device=DEV)
     Ad = gs.save_activation(A.to(DEV), "relu" if n % 2 else "none")[1] if a8 else _inside(A.to(DEV))[0]
-    want, M = oracle.grouped(_np(Ad.dequantize()) if a8 else _np(A), _np(W), offsets, back)
+    Av, Wv = (Ad.dequantize() if a8 else Ad).double(), W.double().transpose(1, 2).contiguous() if back else W.double()
+    want, M = torch.zeros(rows, n, dtype=torch.float64, device=DEV), torch.zeros(rows, n, dtype=torch.float64, device=DEV)
+    for g, (a, b) in enumerate(zip(offsets, offsets[1:])):
+        want[a:b], M[a:b] = Av[a:b] @ Wv[g], Av[a:b].abs() @ Wv[g].abs()
+    want, M = _np(want), _np(M)
     for out in ("f32", "bf16"):
         got = gs.grouped_matmul(Ad, W, off, transpose=back, dtype=TYPES[out])
         _close(got, want, (2 * 3 * k + 4) * U * M + HALF[out] * np.abs(want), out)  # (three products for an fp32 one)
     keep, wide = _inside(torch.full((rows, n), 7.0, device=DEV))
     gs.grouped_matmul(Ad, W, off, transpose=back, out=keep, dtype=torch.float32)
     full = gs.grouped_matmul(Ad, W, off, transpose=back, dtype=torch.float32)
-    assert torch.equal(keep[70:18000], full[70:18000]) and (keep[:70] == 7).all() and (keep[18000:] == 7).all()
+    end = offsets[-1]
+    assert torch.equal(keep[70:end], full[70:end]) and (keep[:70] == 7).all() and (keep[end:] == 7).all()
     assert _around_is_nan(keep, wide)
 
 
 def test_grouped_layers_infinite_weights_and_unfinite_rows():
-    rows = 20000
+    rows = 40000
     A = torch.ones(rows, 64)
     A[5, 3] = float("nan")
     W = torch.ones(1, 64, 32)
@@ -283,7 +304,7 @@ def test_grouped_layers_infinite_weights_and_unfinite_rows():
     assert (got[:5, 0] == 64).all()
 
 
-@pytest.mark.parametrize("rows", [40, 2000, 20000])
+@pytest.mark.parametrize("rows", [40, 2000, 40000, 200000])
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
 def test_grouped_codes_of_the_largest_numbers(rows, dtype):
     """Steps of 2^121: a signed code's number is finite where 128 steps are not."""

@@ -64,6 +64,7 @@ def _saved(rows=4, cols=8, act=0, codes=256, scales=256):
 
 
 P, BAD, NOT = 512, gs.ERR_INVALID_ARG, gs.ERR_UNSUPPORTED
+P2, P3, P4 = (P + (i << 20) for i in range(1, 4))  # (apart from each other, whatever the sizes here)
 
 
 def _with(args, **changes):
@@ -72,14 +73,15 @@ def _with(args, **changes):
 
 
 NORM = ("X ldx R ldr dtype rows cols w w_dtype eps H ldh Y ldy saved rstd stream".split(),
-        [P, 8, P, 8, 0, 4, 8, P, 0, 1e-6, P, 8, P, 8, None, P, None])
+        [P, 8, P2, 8, 0, 4, 8, P, 0, 1e-6, P3, 8, P4, 8, None, P, None])
 
 
 @pytest.mark.parametrize("changes", [
-    dict(X=None), dict(ldx=7), dict(X=P + 2), dict(dtype=2), dict(dtype=-1), dict(rows=-1), dict(rows=1 << 31), dict(cols=0), dict(R=P, ldr=7),
+    dict(X=None), dict(ldx=7), dict(X=P + 2), dict(dtype=2), dict(dtype=-1), dict(rows=-1), dict(rows=1 << 31), dict(cols=0), dict(ldr=7),
     dict(H=None), dict(ldh=7), dict(Y=None), dict(ldy=7), dict(saved=_saved()), dict(Y=None, saved=_saved(act=1)),
     dict(Y=None, saved=_saved(cols=9)), dict(Y=None, saved=_saved(codes=264)), dict(rstd=None), dict(w=P + 2), dict(w_dtype=3), dict(eps=-1.0),
-    dict(eps=float("nan")), dict(eps=float("inf")), dict(ldx=1 << 61)])
+    dict(eps=float("nan")), dict(eps=float("inf")), dict(ldx=1 << 61),
+    dict(H=P + 4), dict(H=P2 + 32), dict(H=P, ldh=9), dict(Y=P), dict(Y=P2), dict(Y=P3), dict(Y=P3 + 124), dict(Y=P3 - 124)])
 def test_norm_refuses(changes):
     assert gs.lib().gs_rms_norm(*_with(NORM, **changes)) == BAD
 
@@ -91,12 +93,13 @@ def test_norm_refuses_too_wide_and_takes_no_rows():
 
 
 NORM_GRAD = ("H ldh rstd dY ldy dtype rows cols w w_dtype dH ldd dX ldx dw work bytes stream".split(),
-             [P, 8, P, P, 8, 0, 4, 8, P, 0, P, 8, P, 8, P, P, 1 << 20, None])
+             [P, 8, P, P2, 8, 0, 4, 8, P, 0, P3, 8, P4, 8, P, P, 1 << 20, None])
 
 
 @pytest.mark.parametrize("changes", [
     dict(H=None), dict(ldh=7), dict(rstd=None), dict(dY=None), dict(ldy=7), dict(dtype=5), dict(rows=-1), dict(cols=0), dict(w=P + 1), dict(w_dtype=2),
-    dict(ldd=7), dict(dX=None), dict(ldx=7), dict(work=None), dict(bytes=3)])
+    dict(ldd=7), dict(dX=None), dict(ldx=7), dict(work=None), dict(bytes=3),
+    dict(dX=P), dict(dX=P2), dict(dX=P3 + 4), dict(dX=P3, ldx=9)])
 def test_norm_grad_refuses(changes):
     assert gs.lib().gs_rms_norm_grad(*_with(NORM_GRAD, **changes)) == BAD
 
@@ -119,13 +122,14 @@ def test_workspaces():
 
 
 GROUPED = ("A lda dtype rows W ldw step groups k n transpose offsets bytes fill C ldc c_dtype stream".split(),
-           [P, 8, 0, 4, P, 16, 128, 3, 8, 16, 0, P, 4, 1, P, 16, 0, None])
+           [P, 8, 0, 4, P2, 16, 128, 3, 8, 16, 0, P, 4, 1, P3, 16, 0, None])
 
 
 @pytest.mark.parametrize("changes", [
     dict(A=None), dict(lda=7), dict(dtype=2), dict(rows=-1), dict(W=None), dict(ldw=15), dict(step=-1), dict(step=1 << 61), dict(groups=0), dict(k=0),
     dict(n=0), dict(transpose=1), dict(offsets=None), dict(offsets=P + 2), dict(bytes=2), dict(bytes=8, offsets=P + 4), dict(C=None), dict(ldc=15),
-    dict(c_dtype=7), dict(C=P + 2)])
+    dict(c_dtype=7), dict(C=P + 2), dict(C=P), dict(C=P + 32), dict(lda=24, ldc=24, C=P + 28), dict(C=P2),
+    dict(C=P2 + 1532), dict(C=P2 + 508, step=0), dict(C=P2 - 252)])
 def test_grouped_matmul_refuses(changes):
     assert gs.lib().gs_grouped_matmul(*_with(GROUPED, **changes)) == BAD
 
@@ -172,13 +176,13 @@ def test_log_probs_limits():
     assert L.gs_log_probs(*_with(SCORES, n=0, s=None, ids=None, logp=None, top_ids=None, top_logp=None)) == 0
 
 
-SCORES_GRAD = ("s ld dtype n v ids bytes stats g e entropy out ldo stream".split(), [P, 8, 0, 4, 8, P, 4, P, P, P, P, P, 8, None])
+SCORES_GRAD = ("s ld dtype n v ids bytes stats g e entropy out ldo stream".split(), [P, 8, 0, 4, 8, P, 4, P, P, P, P, P2, 8, None])
 DISTILL = ("s ld dtype n v ids bytes t t_dtype k T loss stats stream".split(), [P, 8, 0, 4, 8, P, 4, P, 0, 2, 1.0, P, P, None])
-DISTILL_GRAD = ("s ld dtype n v ids bytes t t_dtype k T stats g out ldo stream".split(), [P, 8, 0, 4, 8, P, 4, P, 0, 2, 1.0, P, P, P, 8, None])
+DISTILL_GRAD = ("s ld dtype n v ids bytes t t_dtype k T stats g out ldo stream".split(), [P, 8, 0, 4, 8, P, 4, P, 0, 2, 1.0, P, P, P2, 8, None])
 
 
 @pytest.mark.parametrize("changes", [dict(s=None), dict(ld=7), dict(ids=None), dict(stats=None), dict(stats=P + 4), dict(entropy=None), dict(out=None),
-                                     dict(ldo=7), dict(bytes=3), dict(dtype=9)])
+                                     dict(ldo=7), dict(bytes=3), dict(dtype=9), dict(out=P, ldo=9), dict(out=P + 4)])
 def test_log_probs_grad_refuses(changes):
     assert gs.lib().gs_log_probs_grad(*_with(SCORES_GRAD, **changes)) == BAD
 
@@ -195,6 +199,8 @@ def test_distill_limits():
     assert gs.lib().gs_distill_loss(*_with(DISTILL, loss=None)) == BAD
     assert gs.lib().gs_distill_grad(*_with(DISTILL_GRAD, g=None)) == BAD
     assert gs.lib().gs_distill_grad(*_with(DISTILL_GRAD, out=None)) == BAD
+    assert gs.lib().gs_distill_grad(*_with(DISTILL_GRAD, out=P, ldo=9)) == BAD
+    assert gs.lib().gs_distill_grad(*_with(DISTILL_GRAD, out=P - 4)) == BAD
     assert gs.lib().gs_distill_grad(*_with(DISTILL_GRAD, n=0, s=None, out=None, ids=None, t=None, stats=None, g=None)) == 0
 
 
