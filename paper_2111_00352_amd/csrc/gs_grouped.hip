@@ -9,12 +9,14 @@
 // each finds its group and rows itself, from a prefix sum over the groups' tiles that a wave
 // makes with its lanes.
 //
-// All three are one tile kernel.  A tile's operands lie in LDS by rows of 128 bytes along the
-// summed index, 64 elements in bf16, 32 in fp32, so that a lane's fragment of a matrix
+// Products go by tiles of 64 x 64 or 128 x 128, and where they fit by kernels for few rows (bound by the
+// matrices), for large products in bf16 (by the matrix cores) and for layers of many rows (by A and C);
+// weight gradients have one of their own.  A tile's operands lie in LDS by rows of 128 bytes
+// along the summed index, 64 elements in bf16, 32 in fp32, so that a lane's fragment of a matrix
 // instruction is 16 bytes there.  Operands whose summed index is not the one that is
 // contiguous in memory are turned on their way through registers.  Activations in the 8 bits
 // of a norm or a saved activation are exact in bf16 and become the product's type there too.
-// fp32 operands are multiplied in fp32 (V_MFMA_F32_32X32X2_F32).
+// fp32 operands are multiplied in fp32 (V_MFMA_F32_32X32X2_F32), but for layers.
 #include <algorithm>
 #include <type_traits>
 
@@ -377,7 +379,8 @@ template <int SIDE, class T> __device__ void zero_tile(T *C, int64_t ldc, int64_
     }
 }
 
-// C's tiles.
+// C's tiles, of any form.  Bound by latency where it is taken: a tile has few chunks, each a trip
+// through registers (one ahead) and LDS.  30,011 rows x 255 to 47 columns, 40 groups, bf16: 10.5 us.
 template <class LA, class LB, class TO, int WT>
 __global__ __launch_bounds__(256, WT == 1 ? 4 : 2) void k_grouped(LA A, LB W, int64_t w_step, Offsets off, int64_t k, int64_t n, bool fill,
                                                                   int tiles_n, TO *__restrict__ C, int64_t ldc)
@@ -406,7 +409,8 @@ __global__ __launch_bounds__(256, WT == 1 ? 4 : 2) void k_grouped(LA A, LB W, in
 // Up to 32 rows of a group a workgroup: bound by reading the groups' matrices.  Four waves share
 // 32 N columns and split k, a step of two pieces (16 in bf16, 8 in fp32) each at a time; a lane
 // loads the fragments of its N columns straight from memory, turned in registers where k is the
-// matrix's row, two steps ahead.  The waves' sums meet in LDS.
+// matrix's row, two steps ahead.  The waves' sums meet in LDS.  16 rows of as many groups, 4096 x 4096
+// bf16, take 81 us: 537 MB at 6.7 TB/s.
 
 constexpr int kFewWaves = 4;
 
@@ -550,7 +554,9 @@ __global__ __launch_bounds__(kFewWaves * kWave, N == 4 ? 2 : 3) void k_grouped_f
 // k in whole chunks.  A goes from memory to LDS without passing registers, two chunks ahead; W
 // comes through registers, where it is turned if its k is not contiguous, and is loaded a
 // chunk before it is stored.  The last quarter of a chunk is multiplied after the workgroup has
-// met, while the next one's first fragments are read.
+// met, while the next one's first fragments are read.  16,384 x 4096 x 4096 in 16 equal groups takes
+// 543 us, 1.01 PFLOP/s: with one workgroup a compute unit nothing covers a chunk's end, nor a
+// tile's first loads and its stores.
 
 __device__ __forceinline__ __amdgpu_buffer_rsrc_t buffer_of(const void *p)
 {
@@ -756,7 +762,8 @@ __global__ __launch_bounds__(256, 1) void k_grouped_large(const u16 *__restrict_
 
 // ------------------------------------------------------------------ layers
 //
-// Many rows, up to 256 of k, bf16 on the matrix cores: bound by A and C.  A workgroup of eight
+// Many rows, up to 256 of k, bf16 on the matrix cores: bound by reading A and writing C (2,097,152 x 128
+// x 128 bf16 218 us, 4.9 TB/s; 2,000,000 rows of 8 bits against fp32 matrices 295, 4.4).  A workgroup of eight
 // waves keeps 32 NT columns of a group's matrix in LDS, as the fragments that the instructions
 // take, and goes through a contiguous run of the rows; each wave takes 32 RB of them at a time
 // straight from memory into fragments (a lane 16 neighbouring k of its row), the next ones
@@ -1000,8 +1007,9 @@ __global__ __launch_bounds__(kPanelWaves * kWave, 2) void k_grouped_panel(Rows A
 // waves makes a tile of 128 WA x 64 WB (all of a layer's gradient, so that each operand is read
 // once) from a run of a group's rows; a wave loads whole rows of a chunk, eight (fp32: four) of
 // them, N columns a lane, which are 16 bytes along k for each column when they are put into LDS.
-// Bound by the loads: two chunks are under way in registers while a third is multiplied.
-// Runs end in partial products, which a second launch adds in order.
+// Bound by the loads' way: two chunks are under way in registers (a third spills) while one is multiplied.
+// Runs end in partial products, which a second launch adds in order.  204,800 rows of 256 codes and
+// 128 bf16, 9 groups: 41 us and 10 for the 34 MB of partials; bytes alone would take 16.
 
 constexpr int kGradThreads = 512;
 

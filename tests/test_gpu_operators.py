@@ -474,6 +474,24 @@ def test_log_probs(n, v, dtype, apart):
     assert gs.log_probs_grad(flat, it, got, g, e, out=flat) is flat and torch.equal(flat, first)  # in place
 
 
+@pytest.mark.parametrize("v", [3001, 20_000, 128_000])
+@pytest.mark.parametrize("n", [3, 600])
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_log_probs_many_best_of_wide_rows(n, v, dtype):
+    """Far more than the 128 best are collected and sorted out again; bf16 rows are full of equal logits."""
+    rng = np.random.default_rng(v)
+    s = torch.from_numpy(rng.standard_normal((n, v)).astype(np.float32)).to(TYPES[dtype])
+    s[1, :v // 2] = -np.inf
+    s[2] = torch.arange(v) % 700
+    got = gs.log_probs(s.to(DEV), torch.zeros(n, dtype=torch.int64, device=DEV), top=128)
+    rows = [0, 1, 2, n - 1]
+    want = oracle.best(_np(s[rows]), 128)
+    assert np.array_equal(_np(got.top_ids[rows]), want)
+    every = np.take_along_axis(_np(torch.log_softmax(s[rows].double(), 1)), want, 1)
+    # (the sum of v weights, each off by (2|x| + 4) U, by lanes: v / 256 and some after another)
+    _close(got.top_logp[rows], every, U * (2 * 700 + 4 + v / 128 + 40 + 8 * np.abs(every)))
+
+
 @pytest.mark.parametrize("v", [5, 47, 300, 3000, 40000])
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
 def test_log_probs_of_rows_without_a_distribution(v, dtype):
