@@ -286,6 +286,10 @@ def test_grouped_matmul_of_layers(k, n, dtype, a8, back):
     full = gs.grouped_matmul(Ad, W, off, transpose=back, dtype=torch.float32)
     end = offsets[-1]
     assert torch.equal(keep[70:end], full[70:end]) and (keep[:70] == 7).all() and (keep[end:] == 7).all()
+    # matrices further apart than their sizes, at odd elements
+    apart = torch.full((7, W.shape[1] + 2, W.shape[2] + 3), float("nan"), dtype=W.dtype, device=DEV)[:, 1:-1, 2:-1]
+    apart.copy_(W)
+    assert torch.equal(gs.grouped_matmul(Ad, apart, off, transpose=back, dtype=torch.float32), full)
     assert _around_is_nan(keep, wide)
 
 
@@ -338,6 +342,9 @@ def test_grouped_matmul_in_large_tiles(k, back, out):
     keep = torch.full((rows, n), 7.0, dtype=TYPES[out], device=DEV)
     gs.grouped_matmul(A, W, off, transpose=back, out=keep)
     assert torch.equal(keep[100:2090], got[100:2090]) and (keep[:100] == 7).all() and (keep[2090:] == 7).all()
+    apart = torch.full((5, W.shape[1] + 2, W.shape[2] + 8), float("nan"), dtype=W.dtype, device=DEV)[:, 1:-1, :-8]
+    apart.copy_(W)
+    assert torch.equal(gs.grouped_matmul(A, apart, off, transpose=back, dtype=TYPES[out]), got)
     small = gs.grouped_matmul(A[:300], W, off.clamp(max=300), transpose=back, dtype=TYPES[out])
     _close(small, want[:300], (2 * k + 4) * U * M[:300] + HALF[out] * np.abs(want[:300]))
 
