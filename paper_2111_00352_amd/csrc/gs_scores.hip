@@ -346,6 +346,7 @@ __device__ __forceinline__ u64 order64(uint32_t key, int64_t col) { return (u64)
 
 template <int NT> struct WideLds {
     uint32_t group[kTopGroups];
+    uint32_t bound;  // (not among the groups: waves still read it when the next bound's keys are written)
     u64 keep[kTopKeep];
     int kept;
     uint32_t hist[256];
@@ -372,10 +373,10 @@ template <int NT> __device__ __forceinline__ uint32_t bound_of_groups(uint32_t k
             for (int i = 0; i < kTopGroups / kWave; i++) c += __popcll(__ballot(g[i] >= (t | 1u << b)));
             if (c >= k) t |= 1u << b;
         }
-        if (threadIdx.x == 0) lds.group[0] = t;
+        if (threadIdx.x == 0) lds.bound = t;
     }
     __syncthreads();
-    return lds.group[0];
+    return lds.bound;
 }
 
 // The k best of a row, digit by digit: 4 of the key, 3 of the index.

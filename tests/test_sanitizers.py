@@ -5,9 +5,13 @@
   driven by tests/c/host_fuzz.cpp over the shipped and built-in models,
   every truncation of them and garbled variants, and edge-case aggregates;
 * the oracle (oracle/oracle.c), running its pin tests in a child process
-  with the sanitizer runtime preloaded.
+  with the sanitizer runtime preloaded;
+and under ThreadSanitizer:
+* what the threads of a workgroup share where the bound of a row's best classes
+  is found (csrc/gs_scores.hip, by tests/c/bound_race.cpp).
 """
 import os
+import re
 import shutil
 import subprocess
 import sys
@@ -52,3 +56,22 @@ def test_oracle_under_sanitizers():
                        capture_output=True, text=True, timeout=900, cwd=ROOT, env=env)
     assert r.returncode == 0, (r.stdout[-3000:], r.stderr[-3000:])
     assert " passed" in r.stdout
+
+
+def test_bound_of_the_best_under_thread_sanitizer(tmp_path):
+    """Bounds that a workgroup finds one behind the other: no thread's key of the next one is
+    written where another thread may still read the last one's bound."""
+    text = open(os.path.join(CSRC, "gs_scores.hip")).read()
+    parts = [re.search(begin + r".*?^}" + end, text, re.S | re.M).group(0)
+             for begin, end in ((r"template <int NT> struct WideLds \{", ";"), (r"template <int NT> __device__ [^\n]*bound_of_groups\(", ""))]
+    (tmp_path / "bound.inc").write_text("\n".join(parts))
+    exe = str(tmp_path / "bound_race")
+    built = subprocess.run(["g++", "-std=c++17", "-O1", "-g", "-fsanitize=thread", "-pthread", f'-DBOUND_SOURCE="{tmp_path}/bound.inc"', "-o", exe,
+                            os.path.join(ROOT, "tests", "c", "bound_race.cpp")], capture_output=True, text=True)
+    if "tsan" in built.stderr:
+        pytest.skip("no thread sanitizer")
+    assert built.returncode == 0, built.stderr
+    r = subprocess.run([exe], capture_output=True, text=True, timeout=300, env={**os.environ, "TSAN_OPTIONS": "halt_on_error=1"})
+    if "unexpected memory mapping" in r.stderr:
+        pytest.skip("the thread sanitizer does not run under this kernel")
+    assert r.returncode == 0 and "bound ok" in r.stdout, r.stderr[-4000:]
