@@ -37,6 +37,10 @@ struct Scale {
     float k, m;
     __device__ __forceinline__ Scale(float k_, float m_) : k(k_), m(m_ == -kInf ? 0.0f : m_) {}
     __device__ __forceinline__ float power(float x) const { return (x - m) * k; }
+    // Of what was summed with m, where the maximum is `next` from now on.  Not below -2^10, where the weight
+    // is 0 long since: its product with a sum of weights stays finite, also for a maximum that was the
+    // type's lowest number (classes masked with it, or with -1e38).
+    __device__ __forceinline__ float power_at(const Scale &next) const { return fmaxf((m - next.m) * k, -0x1p10f); }
 };
 constexpr float kLn2 = 0.6931471805599453f;
 
@@ -471,7 +475,7 @@ __global__ __launch_bounds__(NTH) void k_scores_wide(const T *__restrict__ s, in
                 for (int i = 0; i < U; i++) q[i].load(p, c0 + ((U + i) * NTH + (int)threadIdx.x) * E, v);
             if (here > top) {
                 const Scale next(k, here);
-                const float up = top == -kInf ? 0.0f : (by.m - next.m) * k, f = __builtin_amdgcn_exp2f(up);
+                const float up = top == -kInf ? 0.0f : by.power_at(next), f = __builtin_amdgcn_exp2f(up);
                 if constexpr (!TEACHER) sums[1] = f * __builtin_fmaf(sums[0], up, sums[1]);
                 sums[0] *= f;
                 top = here;
@@ -512,7 +516,7 @@ __global__ __launch_bounds__(NTH) void k_scores_wide(const T *__restrict__ s, in
         {
             t.m = row_fold<NTH>(top, fold, [](float a, float b) { return fmaxf(a, b); });
             const Scale all(k, t.m);
-            const float up = top == -kInf ? 0.0f : (by.m - all.m) * k, f = __builtin_amdgcn_exp2f(up);
+            const float up = top == -kInf ? 0.0f : by.power_at(all), f = __builtin_amdgcn_exp2f(up);
             float both[2] = {sums[0] * f, f * __builtin_fmaf(sums[0], up, sums[1])};
             row_sums<NTH, 2>(both, fold);
             t.set(both[0], both[1]);

@@ -601,3 +601,57 @@ def test_distill_masked_and_bad():
     want = oracle.distill(_np(s), ids.numpy(), _np(t), 1.0)
     _close(loss[5], want[0][5], 1e-5)
     _close(d[5], want[1][5], 1e-5)
+
+
+@pytest.mark.parametrize("v", [300, 5000, 9000, 20_011])
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("mask", ["lowest", -1e38, -1e30, -float("inf")])
+@pytest.mark.parametrize("top", [0, 20])
+def test_log_probs_of_partly_masked_rows(v, dtype, mask, top):
+    """Classes masked with a number, down to the type's lowest, beside others: they weigh nothing,
+    whatever a lane has seen before the row's largest logit, and neither do they in the gradient."""
+    low = torch.finfo(TYPES[dtype]).min if mask == "lowest" else mask
+    rng = np.random.default_rng(v)
+    s = torch.from_numpy(3 * rng.standard_normal((8, v))).float()
+    on = torch.ones(8, v, dtype=torch.bool)
+    on[1, :5 * v // 6] = False           # a masked beginning
+    on[2, v // 6:] = False               # and end
+    on[3] = False
+    on[3, v - 1] = True                  # one class left, the last or another
+    on[4] = False
+    on[4, v // 2] = True
+    on[5] = torch.arange(v) % 2 == 0
+    on[6] = torch.arange(v) // 1024 % 3 == 2
+    on[6, :3] = True
+    on[7] = torch.from_numpy(rng.random(v) < 0.02)
+    on[7, 0] = True
+    s[7] *= 20
+    s = torch.where(on, s.to(TYPES[dtype]), torch.tensor(low, dtype=TYPES[dtype]))
+    ids = on.float().argmax(1)           # a class that is left
+    g, e = (torch.from_numpy(rng.standard_normal(8).astype(np.float32)) for _ in range(2))
+    got = gs.log_probs(s.to(DEV), ids.to(DEV), top=top)
+    lp, H, every = oracle.scores(_np(s), ids.numpy())
+    there = on.numpy()
+    with np.errstate(invalid="ignore"):
+        x = _np(s) - _np(s).max(1, keepdims=True)
+    p, x = np.where(there, np.exp(np.where(there, every, 0)), 0), np.where(there, x, 0)
+    logS, ax, xx = np.log((np.exp(x) * there).sum(1)), (p * -x).sum(1), (p * x * x).sum(1)
+    tol = U * (4 * np.abs(x[np.arange(8), ids]) + 4 * logS + 2 * ax + _sum_terms(v))
+    tolH = U * (4 * logS + 2 * xx + (ax + 1) * (8 + _sum_terms(v)))
+    assert np.isfinite(H).all() and abs(H[3]) == abs(H[4]) == 0
+    _close(got.logp, lp, tol, "logp")
+    _close(got.entropy, H, tolH, "entropy")
+    want = oracle.best(_np(s), top)
+    assert np.array_equal(_np(got.top_ids), want)
+    rows = np.arange(8)[:, None]
+    left = there[rows, want]
+    _close(torch.where(torch.from_numpy(left).to(DEV), got.top_logp, torch.zeros_like(got.top_logp)), np.where(left, every[rows, want], 0),
+           U * (4 * np.abs(x[rows, want]) + (4 * logS + 2 * ax + _sum_terms(v))[:, None]), "top")
+    d = gs.log_probs_grad(s.to(DEV), ids.to(DEV), got, g.to(DEV), e.to(DEV))
+    assert (d[~on.to(DEV)] == 0).all()
+    w = np.where(there, oracle.scores_grad(np.where(there, every, -np.inf), H, ids.numpy(), _np(g), _np(e)), 0)
+    inner = np.where(there, np.abs(np.where(there, every, 0) + H[:, None]), 0)
+    rp = U * (2 * np.abs(x) + 12 + (2 * ax + _sum_terms(v))[:, None])
+    tol = np.abs(_np(g))[:, None] * (p * rp + FLUSH + 2 * U)
+    tol += np.abs(_np(e))[:, None] * ((p * rp + FLUSH) * inner + p * (tolH[:, None] + 4 * U * (np.abs(x) + logS[:, None] + inner)))
+    _close(d, w, tol + HALF[dtype] * np.abs(w), "gradient")
