@@ -30,6 +30,10 @@ template <class T> constexpr uint32_t kNegInf = sizeof(T) == 4 ? 0xff800000u : 0
 // exp(x), x <= 0 or NaN; 0 below 2^-126.
 __device__ __forceinline__ float exp_neg(float x) { return __builtin_amdgcn_exp2f(x * kLog2e); }
 
+// In the place of lower powers, down to -inf, whose weights are 0 long since: its product with what is
+// summed, or with a gradient, is finite.
+constexpr float kLeast = -0x1p10f;
+
 // The weights of a row's logits are 2^((x - m) k), with k = c log2(e).  (As 2^(x k - m k), with
 // one operation less, they would not be right where m k leaves the type's range: rows of its
 // lowest number.)
@@ -37,10 +41,9 @@ struct Scale {
     float k, m;
     __device__ __forceinline__ Scale(float k_, float m_) : k(k_), m(m_ == -kInf ? 0.0f : m_) {}
     __device__ __forceinline__ float power(float x) const { return (x - m) * k; }
-    // Of what was summed with m, where the maximum is `next` from now on.  Not below -2^10, where the weight
-    // is 0 long since: its product with a sum of weights stays finite, also for a maximum that was the
-    // type's lowest number (classes masked with it, or with -1e38).
-    __device__ __forceinline__ float power_at(const Scale &next) const { return fmaxf((m - next.m) * k, -0x1p10f); }
+    // Of what was summed with m, where the maximum is `next` from now on (m may have been the type's lowest
+    // number, of classes masked with it, or -1e38).
+    __device__ __forceinline__ float power_at(const Scale &next) const { return fmaxf((m - next.m) * k, kLeast); }
 };
 constexpr float kLn2 = 0.6931471805599453f;
 
@@ -204,8 +207,7 @@ __global__ __launch_bounds__(kRowThreads) void k_scores_held(const T *__restrict
             for (int e = 0; e < E; e++) {
                 const float d = by.power(x[i][e]), w = __builtin_amdgcn_exp2f(d);
                 sums[0] += w;
-                // (0 where d is -inf: its maximum with -2^126 is finite, the weight 0)
-                if constexpr (!TEACHER) sums[1] = __builtin_fmaf(w, fmaxf(d, -0x1p126f), sums[1]);
+                if constexpr (!TEACHER) sums[1] = __builtin_fmaf(w, fmaxf(d, kLeast), sums[1]);
             }
         if constexpr (TEACHER)
             sums[0] = row_sum<L>(sums[0], tmp);
@@ -487,7 +489,7 @@ __global__ __launch_bounds__(NTH) void k_scores_wide(const T *__restrict__ s, in
                 for (int e = 0; e < E; e++) {
                     const float d = by.power(x[i][e]), w = __builtin_amdgcn_exp2f(d);
                     sums[0] += w;
-                    if constexpr (!TEACHER) sums[1] = __builtin_fmaf(w, fmaxf(d, -0x1p126f), sums[1]);
+                    if constexpr (!TEACHER) sums[1] = __builtin_fmaf(w, fmaxf(d, kLeast), sums[1]);
                 }
             if constexpr (TOP) {
                 // (after 1, 2, 4 .. parts, of all that has been seen)
@@ -657,7 +659,7 @@ __global__ __launch_bounds__(kRowThreads) void k_scores_grad(const T *s, int64_t
 #pragma unroll
                 for (int e = 0; e < E; e++) {
                     const float d = by.power(to_f32(x[i][e])), weight = __builtin_amdgcn_exp2f(d);
-                    float y = weight * (a.e ? __builtin_fmaf(fa, fmaxf(d, -0x1p100f), fb) : fb);
+                    float y = weight * (a.e ? __builtin_fmaf(fa, fmaxf(d, kLeast), fb) : fb);
                     if (col + e == mine) y += g;
                     o[e] = from_f32<T>(y);
                 }
@@ -720,7 +722,7 @@ __global__ __launch_bounds__(kRowThreads) void k_flat_grad(const T *s, int64_t n
             if constexpr (TEACHER) {
                 y[i] = g == 0.0f ? 0.0f : weight * fb;
             } else {
-                y[i] = weight * (a.e ? __builtin_fmaf(fa, fmaxf(d, -0x1p100f), fb) : fb);
+                y[i] = weight * (a.e ? __builtin_fmaf(fa, fmaxf(d, kLeast), fb) : fb);
                 if (c == given) y[i] += g;
             }
         }

@@ -655,3 +655,25 @@ def test_log_probs_of_partly_masked_rows(v, dtype, mask, top):
     tol = np.abs(_np(g))[:, None] * (p * rp + FLUSH + 2 * U)
     tol += np.abs(_np(e))[:, None] * ((p * rp + FLUSH) * inner + p * (tolH[:, None] + 4 * U * (np.abs(x) + logS[:, None] + inner)))
     _close(d, w, tol + HALF[dtype] * np.abs(w), "gradient")
+
+
+@pytest.mark.parametrize("v", [5, 47, 300, 5000, 20_011])
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("scale", [1e9, 1e20])
+def test_large_entropy_gradients_beside_masked_classes(v, dtype, scale):
+    """A masked class has no gradient, however large the entropy's is."""
+    s = _logits(6, v, v, dtype)
+    s[3:, 1::3] = torch.finfo(TYPES[dtype]).min
+    on = s > -1e30
+    e = torch.full((6,), scale)
+    ids = torch.zeros(6, dtype=torch.int64)
+    got = gs.log_probs(s.to(DEV), ids.to(DEV))
+    d = gs.log_probs_grad(s.to(DEV), ids.to(DEV), got, None, e.to(DEV))
+    assert torch.isfinite(d).all() and (d[~on.to(DEV)] == 0).all()
+    small = gs.log_probs_grad(s.to(DEV), ids.to(DEV), got, None, torch.ones(6, device=DEV))
+    # weight (fa d + fb): fa and fb have two roundings for e each and two without, half a step for either result
+    w = _np(small) * float(np.float32(scale))
+    x = np.where(on.numpy(), _np(s) - _np(s).max(1, keepdims=True), 0)
+    S = (np.exp(x) * on.numpy()).sum(1, keepdims=True)
+    inner = np.exp(x) * on.numpy() / S * (np.abs(x) + np.abs(_np(got.entropy))[:, None] + np.log(S))
+    _close(d, w, scale * (8 * U * inner + FLUSH) + (2 * HALF[dtype] + 4 * U) * np.abs(w))
