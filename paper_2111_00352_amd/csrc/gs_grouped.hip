@@ -1331,7 +1331,10 @@ static int grouped_matmul(const Operand &A, int a_dtype, int64_t rows, const voi
         const Extent c{C, rows, outw * csize, ldc * csize};
         if (!A.saved) check_apart("C", c, "A", {A.p, rows, in * dtype_size(a_dtype), A.ld * dtype_size(a_dtype)});
         const int64_t matrix = ((k - 1) * ldw + n) * wsize;
-        check_apart("C", c, "W", {W, groups, matrix, std::max(w_step * wsize, matrix)});
+        // (matrices nearer to each other than their size, or one for all groups: what they take together)
+        const int64_t step = w_step * wsize;
+        check_apart("C", c, "W", step < matrix ? Extent{W, 1, (groups - 1) * step + matrix, (groups - 1) * step + matrix}
+                                               : Extent{W, groups, matrix, step});
         const hipStream_t s = (hipStream_t)stream;
         // Which kernel: all figures are us, groups of equal sizes, one set of operands after the other.
         //

@@ -677,3 +677,23 @@ def test_large_entropy_gradients_beside_masked_classes(v, dtype, scale):
     S = (np.exp(x) * on.numpy()).sum(1, keepdims=True)
     inner = np.exp(x) * on.numpy() / S * (np.abs(x) + np.abs(_np(got.entropy))[:, None] + np.log(S))
     _close(d, w, scale * (8 * U * inner + FLUSH) + (2 * HALF[dtype] + 4 * U) * np.abs(w))
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_grouped_result_right_behind_one_matrix_for_all(dtype):
+    """The result lies where the next group's matrix would be, if there were one for each."""
+    buffer = torch.zeros(64 * 64 + 320 * 64, dtype=TYPES[dtype], device=DEV)
+    W, out = buffer[:64 * 64].view(1, 64, 64), buffer[64 * 64:].view(320, 64)
+    W.normal_()
+    A = torch.randn(320, 64, device=DEV).to(TYPES[dtype])
+    off = torch.arange(0, 321, 20, device=DEV)
+    want, M = _np(A) @ _np(W[0]), np.abs(_np(A)) @ np.abs(_np(W[0]))
+    got = gs.grouped_matmul(A, W.expand(16, 64, 64), off, out=out)
+    assert got is out
+    _close(got, want, (2 * 64 + 4) * U * M + HALF[dtype] * np.abs(want))
+    # matrices side by side, in rows of three of them
+    side = torch.randn(64, 3, 64, device=DEV).to(TYPES[dtype])
+    got = gs.grouped_matmul(A, side.transpose(0, 1), torch.tensor([0, 100, 100, 320], device=DEV))
+    want = np.concatenate([_np(A[:100]) @ _np(side[:, 0]), _np(A[100:]) @ _np(side[:, 2])])
+    M = np.concatenate([np.abs(_np(A[:100])) @ np.abs(_np(side[:, 0])), np.abs(_np(A[100:])) @ np.abs(_np(side[:, 2]))])
+    _close(got, want, (2 * 64 + 4) * U * M + HALF[dtype] * np.abs(want))

@@ -211,3 +211,21 @@ def test_python_refuses_cpu_tensors():
                  lambda: gs.grouped_weight_grad(x, x, i), lambda: gs.log_probs(x, i), lambda: gs.distill_loss(x, i[:, None], x[:, :1])):
         with pytest.raises(ValueError):
             call()
+
+
+FAR = dict(rows=(1 << 31) - 1, A=1 << 44, W=1 << 40)  # (too many tiles: what is not refused before ends there, nothing is launched)
+
+
+@pytest.mark.parametrize("changes,size", [
+    (dict(step=0), 512), (dict(step=0, groups=1000), 512), (dict(step=0, groups=1), 512),  # one matrix for all
+    (dict(step=16, ldw=48), 7 * 192 + 2 * 64 + 64),                                        # matrices side by side
+    (dict(step=100), 2 * 400 + 512), (dict(step=128), 3 * 512), (dict(step=200), 2 * 800 + 512)])
+def test_results_right_behind_the_matrices_are_taken(changes, size):
+    """Only what the groups' matrices take is W's: a result may lie right behind or before them, not 4 bytes inside."""
+    L = gs.lib()
+    behind, before = FAR["W"] + size, FAR["W"] - 64 * FAR["rows"]
+    for C in (behind, behind + 4, behind + 1024, before):
+        assert L.gs_grouped_matmul(*_with(GROUPED, **FAR, **changes, C=C)) == NOT, L.gs_last_error()
+        assert b"too many tiles" in L.gs_last_error()
+    for C in (behind - 4, before + 4, FAR["W"]):
+        assert L.gs_grouped_matmul(*_with(GROUPED, **FAR, **changes, C=C)) == BAD and b"overlaps W" in L.gs_last_error()
