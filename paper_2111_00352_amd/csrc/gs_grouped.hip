@@ -1502,6 +1502,14 @@ static int grouped_weight_grad(const Operand &A, int a_dtype, int64_t rows, int6
             fail(GS_ERR_INVALID_ARG, "workspace of %llu bytes is below the %llu needed",
                  (unsigned long long)(work ? work_bytes : 0), (unsigned long long)need);
         if (p.tiles_a * p.tiles_b > 65535) fail(GS_ERR_UNSUPPORTED, "the product has too many tiles");
+        const auto whole = [](const void *p, int64_t bytes) { return Extent{p, 1, bytes, bytes}; };
+        const Extent made = whole(out, groups * a * b * 4), partial = whole(need ? work : nullptr, (int64_t)need);
+        const Extent g = {G, rows, b * dtype_size(dtype), ldg * dtype_size(dtype)};
+        check_apart("out", made, "G", g), check_apart("work", partial, "G", g), check_apart("work", partial, "out", made);
+        if (!A.saved) {
+            const Extent dense = {A.p, rows, a * dtype_size(dtype), A.ld * dtype_size(dtype)};
+            check_apart("out", made, "A", dense), check_apart("work", partial, "A", dense);
+        }
         const hipStream_t s = (hipStream_t)stream;
         float *part = p.direct ? out : (float *)work;
         auto go = [&](auto la, auto lg, auto wa, auto wb) {

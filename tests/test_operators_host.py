@@ -229,3 +229,28 @@ def test_results_right_behind_the_matrices_are_taken(changes, size):
         assert b"too many tiles" in L.gs_last_error()
     for C in (behind - 4, before + 4, FAR["W"]):
         assert L.gs_grouped_matmul(*_with(GROUPED, **FAR, **changes, C=C)) == BAD and b"overlaps W" in L.gs_last_error()
+
+
+GROUPED_GRAD_APART = (GROUPED_GRAD[0], [P, 8, P2, 16, 0, 4, 8, 16, 3, P, 4, P3, P4, 0, None])
+GRAD_BYTES, ROW_BYTES = 3 * 8 * 16 * 4, 16 * 4  # of the result, of a row of G
+
+
+@pytest.mark.parametrize("changes", [
+    dict(out=P), dict(out=P + 4 * 32 - 4), dict(out=P - GRAD_BYTES + 4), dict(out=P2), dict(out=P2 + 4 * ROW_BYTES - 4), dict(out=P2 - GRAD_BYTES + 4)])
+def test_weight_gradients_over_their_operands_are_refused(changes):
+    L = gs.lib()
+    assert L.gs_grouped_weight_grad(*_with(GROUPED_GRAD_APART, **changes)) == BAD and b"out overlaps" in L.gs_last_error()
+
+
+def test_workspaces_over_operands_are_refused():
+    L, need, rows = gs.lib(), ctypes.c_uint64(), 100_000
+    assert L.gs_grouped_weight_grad_workspace(rows, 3, 8, 16, ctypes.byref(need)) == 0 and need.value > 0
+    args = dict(rows=rows, A=1 << 40, G=2 << 40, out=3 << 40, work_bytes=need.value)
+    for work in (args["A"] + 32, args["A"] - need.value + 4, args["G"], args["G"] + rows * ROW_BYTES - 4, args["out"] + 4, args["out"] - 4):
+        assert L.gs_grouped_weight_grad(*_with(GROUPED_GRAD_APART, **args, work=work)) == BAD and b"work overlaps" in L.gs_last_error()
+    saved = ctypes.byref(gs._Saved(rows, 8, 0, 1 << 42, 1 << 43))
+    for work in (args["G"], args["out"] + 4):
+        assert L.gs_grouped_weight_grad_saved(saved, args["G"], 16, 0, 16, 3, P, 4, args["out"], work, need.value, None) == BAD
+        assert b"work overlaps" in L.gs_last_error()
+    assert L.gs_grouped_weight_grad_saved(saved, args["G"], 16, 0, 16, 3, P, 4, args["G"] + 4, 1 << 44, need.value, None) == BAD
+    assert b"out overlaps" in L.gs_last_error()
