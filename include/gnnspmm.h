@@ -417,8 +417,9 @@ int gs_mxfp4_matmul_workspace(int64_t m, int64_t n, int64_t k, int a_dtype, uint
  * head that answers and is trained.  Dense operands are fp32 or bf16 (a gs_dtype)
  * with any leading dimension >= their width; columns are at most 2^24, rows below
  * 2^31.  Sums, statistics and partial sums are fp32 or fp64, a result is rounded
- * once to its type.  Matrices that are written must not overlap the dense ones that are
- * read, except where a call says so: those overlaps are refused.
+ * once to its type.  Matrices that are written, codes and scales among them, and workspaces
+ * must not overlap the dense ones that are read, except where a call says so: those overlaps
+ * are refused.
  * All calls are deterministic, asynchronous on s and allocate nothing.
  */
 

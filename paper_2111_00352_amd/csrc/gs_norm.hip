@@ -394,6 +394,12 @@ int gs_rms_norm(const void *X, int64_t ldx, const void *R, int64_t ldr, int dtyp
         const Extent x = extent(X, ldx), r = extent(R, ldr), h = extent(R ? H : nullptr, ldh), y = extent(Y, ldy);
         check_apart("H", h, "X", x, true), check_apart("H", h, "R", r, true);
         check_apart("Y", y, "X", x), check_apart("Y", y, "R", r), check_apart("Y", y, "H", h);
+        if (saved) {
+            const Extent codes = {saved->codes, rows, saved_code_pitch(cols), saved_code_pitch(cols)};
+            const Extent scales = {saved->scales, rows, saved_scale_pitch(cols), saved_scale_pitch(cols)};
+            for (const Extent &part : {codes, scales})
+                check_apart("saved", part, "X", x), check_apart("saved", part, "R", r), check_apart("saved", part, "H", h);
+        }
         const hipStream_t s = (hipStream_t)stream;
         const int blocks = (int)saved_scale_pitch(cols);
         const double bytes = (double)rows * cols * (size * (R ? 3 : 1) + (saved ? 1 : size));
@@ -460,6 +466,9 @@ int gs_rms_norm_grad(const void *H, int64_t ldh, const float *rstd, const void *
         const Extent dx = extent(dX, ldx);
         check_apart("dX", dx, "H", extent(H, ldh)), check_apart("dX", dx, "dY", extent(dY, ldy));
         check_apart("dX", dx, "dH", extent(dH, ldd), true);
+        const Extent partial = {work, 1, (int64_t)need, (int64_t)need};
+        check_apart("work", partial, "H", extent(H, ldh)), check_apart("work", partial, "dY", extent(dY, ldy));
+        check_apart("work", partial, "dH", extent(dH, ldd)), check_apart("work", partial, "dX", dx);
         const hipStream_t s = (hipStream_t)stream;
         float *part = (float *)work;
         const double bytes = (double)rows * cols * size * (dH ? 4 : 3);

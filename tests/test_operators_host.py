@@ -254,3 +254,42 @@ def test_workspaces_over_operands_are_refused():
         assert b"work overlaps" in L.gs_last_error()
     assert L.gs_grouped_weight_grad_saved(saved, args["G"], 16, 0, 16, 3, P, 4, args["G"] + 4, 1 << 44, need.value, None) == BAD
     assert b"out overlaps" in L.gs_last_error()
+
+
+@pytest.mark.parametrize("codes,scales", [(P, 1 << 40), (P + 112, 1 << 40), (P - 112, 1 << 40), (P2, 1 << 40), (P3, 1 << 40), (1 << 40, P),
+                                          (1 << 40, P2 + 124), (1 << 40, P3 + 64)])
+def test_norms_saved_over_their_operands_are_refused(codes, scales):
+    """X, R and H are read and written while codes and scales of other rows are."""
+    L = gs.lib()
+    assert L.gs_rms_norm(*_with(NORM, Y=None, saved=_saved(codes=codes, scales=scales))) == BAD
+    assert b"saved overlaps" in L.gs_last_error()
+
+
+@pytest.mark.parametrize("work", [P, P + 124, P2, P3, P4, P4 - 28])
+def test_norm_gradients_workspaces_over_operands_are_refused(work):
+    L, need = gs.lib(), ctypes.c_uint64()
+    assert L.gs_rms_norm_grad_workspace(4, 8, 0, ctypes.byref(need)) == 0 and need.value == 32
+    assert L.gs_rms_norm_grad(*_with(NORM_GRAD, work=work, bytes=need.value)) == BAD and b"work overlaps" in L.gs_last_error()
+
+
+@pytest.mark.parametrize("changes", [
+    dict(A=None), dict(lda=7), dict(G=None), dict(ldg=15), dict(dtype=2), dict(rows=-1), dict(a=0), dict(b=0), dict(groups=0), dict(offsets=None),
+    dict(bytes=1), dict(out=None), dict(rows=100_000)])
+def test_grouped_weight_grad_refuses_for_the_reason(changes):
+    """The refusals, of operands that are apart from each other."""
+    L = gs.lib()
+    assert L.gs_grouped_weight_grad(*_with(GROUPED_GRAD_APART, **changes)) == BAD and b"overlap" not in L.gs_last_error()
+
+
+@pytest.mark.parametrize("changes", [
+    dict(H=None), dict(ldh=7), dict(rstd=None), dict(dY=None), dict(ldy=7), dict(dtype=5), dict(rows=-1), dict(cols=0), dict(w=P + 1), dict(w_dtype=2),
+    dict(ldd=7), dict(dX=None), dict(ldx=7), dict(work=None), dict(bytes=3)])
+def test_norm_grad_refuses_for_the_reason(changes):
+    L = gs.lib()
+    assert L.gs_rms_norm_grad(*_with(NORM_GRAD, **dict(dict(work=1 << 40), **changes))) == BAD and b"overlap" not in L.gs_last_error()
+
+
+@pytest.mark.parametrize("changes", [dict(dX=P), dict(dX=P2), dict(dX=P3 + 4), dict(dX=P3, ldx=9)])
+def test_norm_grad_refuses_results_over_operands(changes):
+    L = gs.lib()
+    assert L.gs_rms_norm_grad(*_with(NORM_GRAD, work=1 << 40, **changes)) == BAD and b"dX overlaps" in L.gs_last_error()
