@@ -966,6 +966,7 @@ int gs_log_probs(const void *s, int64_t ld, int dtype, int64_t n, int64_t v, con
         if (top > kTopMax) fail(GS_ERR_UNSUPPORTED, "top is at most %d", kTopMax);
         const ClassIds id = logp ? check_ids("ids", ids, id_bytes, n) : ClassIds{nullptr, false};
         if (n > 0 && top > 0 && (!top_ids || !top_logp)) fail(GS_ERR_INVALID_ARG, "null output");
+        if ((uintptr_t)stats % 8) fail(GS_ERR_INVALID_ARG, "stats are not 8-byte aligned");
         if (n == 0) return;
         const ScoreOut out{logp, entropy, (float2 *)stats, (int)top, top_ids, top_logp};
         const Teacher none{};

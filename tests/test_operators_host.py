@@ -293,3 +293,8 @@ def test_norm_grad_refuses_for_the_reason(changes):
 def test_norm_grad_refuses_results_over_operands(changes):
     L = gs.lib()
     assert L.gs_rms_norm_grad(*_with(NORM_GRAD, work=1 << 40, **changes)) == BAD and b"dX overlaps" in L.gs_last_error()
+
+
+def test_log_probs_refuses_statistics_that_are_not_aligned():
+    L = gs.lib()
+    assert L.gs_log_probs(*_with(SCORES, stats=P + 4)) == BAD and b"stats are not 8-byte aligned" in L.gs_last_error()
