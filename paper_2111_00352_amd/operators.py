@@ -237,9 +237,9 @@ def log_probs(logits: torch.Tensor, ids: torch.Tensor, top: int = 0, stream=None
     if not 0 <= top <= min(v, TOP_MAX):
         raise ValueError(f"top must be 0 to {min(v, TOP_MAX)}")
     dev = logits.device
-    # (one allocation: a small call is bound by such things)
-    both = torch.empty(n * (4 + top), dtype=torch.float32, device=dev)
-    stats, logp, entropy, best = both[:2 * n].view(n, 2), both[2 * n:3 * n], both[3 * n:4 * n], both[4 * n:].view(n, top)
+    # (each for itself: a caller may change one in place, or keep it alone)
+    logp, entropy = torch.empty(n, dtype=torch.float32, device=dev), torch.empty(n, dtype=torch.float32, device=dev)
+    stats, best = torch.empty((n, 2), dtype=torch.float32, device=dev), torch.empty((n, top), dtype=torch.float32, device=dev)
     top_ids = torch.empty((n, top), dtype=torch.int32, device=dev)
     _raise(lib().gs_log_probs(logits.data_ptr(), ld, code, n, v, ids.data_ptr(), id_bytes, logp.data_ptr(), entropy.data_ptr(),
                               stats.data_ptr(), top, top_ids.data_ptr(), best.data_ptr(), s))
@@ -290,8 +290,8 @@ def distill_loss(logits: torch.Tensor, top_ids: torch.Tensor, top_logits: torch.
     of = logits
     logits, ld, code, (n, v), s = _dense(logits, "logits")
     k, id_bytes, t_code = _teacher(top_ids, top_logits, n, logits.get_device())
-    both = torch.empty(5 * n, dtype=torch.float32, device=logits.device)
-    stats, loss = both[:4 * n].view(n, 4), both[4 * n:]
+    stats = torch.empty((n, 4), dtype=torch.float32, device=logits.device)
+    loss = torch.empty(n, dtype=torch.float32, device=logits.device)
     _raise(lib().gs_distill_loss(logits.data_ptr(), ld, code, n, v, top_ids.data_ptr(), id_bytes, top_logits.data_ptr(), t_code, k,
                                  float(temperature), loss.data_ptr(), stats.data_ptr(), s))
     return _results((loss, stats), of, top_logits)

@@ -355,3 +355,24 @@ def test_offsets_in_a_tensor_past_32_bits():
     X[-1] = 3.0
     Y, _, r = gs.rms_norm(X)
     assert (Y[-1] == 1).all() and (Y[-2] == 0).all()
+
+
+def test_results_are_changed_in_place_and_kept_alone():
+    """A loss is masked or turned in place, as any other; what is kept of a call's results holds no others' memory."""
+    X, R, w, W, off, s, ids, tid, t, g = _operands(300, 64, 90, 14)
+    mask = (torch.rand(300, device=DEV) < 0.5).float()
+    for make in (lambda x: layers.distill_loss(x, tid, t, 1.5), lambda x: layers.log_probs(x, ids)[0]):
+        grads = []
+        for change in (lambda y: y * mask, lambda y: y.mul_(mask), lambda y: y.neg_().neg_() * mask):
+            x = s.detach().requires_grad_()
+            change(make(x)).sum().backward()
+            grads.append(x.grad)
+        assert torch.equal(grads[0], grads[1]) and torch.equal(grads[0], grads[2]) and (grads[0] != 0).any()
+    x = s.detach().requires_grad_()
+    _, entropy = layers.log_probs(x, ids)
+    entropy.mul_(2.0)  # (the gradient reads it)
+    with pytest.raises(RuntimeError, match="modified by an inplace operation"):
+        entropy.sum().backward()
+    found = gs.log_probs(s, ids, top=3)
+    for result in (*found, *gs.distill_loss(s, tid, t)):
+        assert not result._is_view() and result.untyped_storage().nbytes() == result.numel() * 4
