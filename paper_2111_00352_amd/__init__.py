@@ -448,6 +448,14 @@ _STRIDED = torch.strided
 _tracing, _forward_ad = torch._C._get_tracing_state, torch.autograd.forward_ad
 
 
+def _seen(X: torch.Tensor):
+    """Refuses an operand that a trace or a forward-mode derivative follows: neither sees the library's calls."""
+    if _tracing() is not None:
+        raise RuntimeError("the library's operators cannot be traced: a trace would keep their results as constants")
+    if _forward_ad._current_level >= 0 and X.is_floating_point() and _forward_ad.unpack_dual(X).tangent is not None:
+        raise RuntimeError("the library's operators have no forward-mode derivative")
+
+
 def _dense(X: torch.Tensor, name: str, index: int | None = -1) -> tuple:
     """(tensor, leading dimension, dtype code, shape, current stream) of a 2-D fp32 or bf16
     operand on the current device, and on the GPU `index` of another operand (None: it is
@@ -455,10 +463,7 @@ def _dense(X: torch.Tensor, name: str, index: int | None = -1) -> tuple:
     code = _DTYPES.get(X.dtype) if isinstance(X, torch.Tensor) else None
     if code is None or X.layout != _STRIDED or len(shape := X.shape) != 2 or (at := X.get_device()) < 0:
         raise ValueError(f"{name} must be a 2-D CUDA float32 or bfloat16 tensor")
-    if _tracing() is not None:
-        raise RuntimeError("the library's operators cannot be traced: a trace would keep their results as constants")
-    if _forward_ad._current_level >= 0 and _forward_ad.unpack_dual(X).tangent is not None:
-        raise RuntimeError("the library's operators have no forward-mode derivative")
+    _seen(X)
     if at != torch._C._cuda_getDevice() or (index != -1 and at != index):
         raise ValueError(f"{name} is not on the current device, or not on the other operand's")
     if X.is_neg():

@@ -14,7 +14,7 @@ from typing import NamedTuple
 import torch
 
 from paper_2111_00352_amd import (
-    _DTYPES, SavedActivation, _check, _dense, _dtype_code, _NoGradient, _on, _out, _u64, _written, lib)
+    _DTYPES, SavedActivation, _check, _dense, _dtype_code, _NoGradient, _on, _out, _seen, _u64, _written, lib)
 
 TOP_MAX = 128  # alternatives of a row at most (log_probs, distill_loss)
 _INTS = {torch.int32: 4, torch.int64: 8}
@@ -27,6 +27,7 @@ def _array(t, name: str, shape: tuple, dtypes: dict, index: int) -> int:
     if code is None or t.get_device() != index or t.layout != torch.strided or tuple(t.shape) != shape or not t.is_contiguous():
         kinds = " or ".join(str(d)[6:] for d in dtypes)
         raise ValueError(f"{name} must be a contiguous CUDA {kinds} tensor of shape {shape} on the other operands' device")
+    _seen(t)
     if t.is_neg():
         raise ValueError(f"{name} must not be a negated view")
     return code
@@ -133,6 +134,7 @@ def grouped_matmul(A, W: torch.Tensor, offsets: torch.Tensor, transpose: bool = 
         return _on(stream, grouped_matmul, A, W, offsets, transpose, dtype, out)
     if not isinstance(W, torch.Tensor) or W.dtype not in _DTYPES or W.dim() != 3 or W.layout != torch.strided:
         raise ValueError("W must be a 3-D CUDA float32 or bfloat16 tensor")
+    _seen(W)
     saved = isinstance(A, SavedActivation)
     if saved:
         at, shape, of = A.device.index, A.shape, None

@@ -376,3 +376,24 @@ def test_results_are_changed_in_place_and_kept_alone():
     found = gs.log_probs(s, ids, top=3)
     for result in (*found, *gs.distill_loss(s, tid, t)):
         assert not result._is_view() and result.untyped_storage().nbytes() == result.numel() * 4
+
+
+def test_no_tangent_is_dropped_unseen():
+    """A dual number in the place of any operand that has values is refused, and a trace beside 8-bit rows."""
+    from torch.autograd import forward_ad
+    X, R, w, W, off, s, ids, tid, t, g = _operands(20, 64, 30, 15)
+    S = gs.save_activation(X, "none")[1]
+    found, (_, stats) = gs.log_probs(s, ids), gs.distill_loss(s, tid, t)
+    r = gs.rms_norm(X, w)[2]
+    with forward_ad.dual_level():
+        dual = lambda x: forward_ad.make_dual(x, torch.ones_like(x))  # noqa: E731
+        for call in (lambda: gs.rms_norm(X, dual(w)), lambda: gs.rms_norm(X, w, dual(R)), lambda: gs.rms_norm_grad(X, r, R, dual(w)),
+                     lambda: gs.rms_norm_grad(X, dual(r), R, w), lambda: gs.grouped_matmul(X, dual(W), off), lambda: gs.grouped_matmul(S, dual(W), off),
+                     lambda: gs.log_probs_grad(s, ids, found, dual(g)), lambda: gs.log_probs_grad(s, ids, found, g, dual(g)),
+                     lambda: gs.distill_loss(s, tid, dual(t)), lambda: gs.distill_grad(s, tid, dual(t), stats, g),
+                     lambda: gs.distill_grad(s, tid, t, stats, dual(g)), lambda: gs.grouped_weight_grad(S, dual(R), off)):
+            with pytest.raises(RuntimeError, match="forward-mode"):
+                call()
+        assert torch.equal(gs.grouped_matmul(S, W, off), gs.grouped_matmul(S, W, off))
+    with pytest.raises(RuntimeError, match="traced"):
+        torch.jit.trace(lambda x: gs.grouped_matmul(S, x, off), W)

@@ -298,3 +298,23 @@ def test_norm_grad_refuses_results_over_operands(changes):
 def test_log_probs_refuses_statistics_that_are_not_aligned():
     L = gs.lib()
     assert L.gs_log_probs(*_with(SCORES, stats=P + 4)) == BAD and b"stats are not 8-byte aligned" in L.gs_last_error()
+
+
+@pytest.mark.filterwarnings("ignore:.*torch.jit.trace.*:DeprecationWarning")
+def test_operands_that_are_followed_forwards_or_traced_are_refused():
+    """Every operand, not only the dense ones: a tangent would be lost, a trace replay what was in memory."""
+    import torch
+    from torch.autograd import forward_ad
+
+    from paper_2111_00352_amd import operators
+    x, W, off = torch.zeros(4, 3), torch.zeros(2, 3, 5), torch.tensor([0, 2, 4])
+    with forward_ad.dual_level():
+        for call in (lambda d: operators._array(d, "weight", (6,), operators._F32, -1), lambda d: gs.grouped_matmul(x, d.view(1, 2, 3), off)):
+            with pytest.raises(RuntimeError, match="forward-mode"):
+                call(forward_ad.make_dual(torch.zeros(6), torch.ones(6)))
+        assert operators._array(torch.zeros(6), "weight", (6,), operators._F32, -1) == 0
+        assert operators._array(off, "offsets", (3,), operators._INTS, -1) == 8
+    with pytest.raises(RuntimeError, match="traced"):
+        torch.jit.trace(lambda w: gs.grouped_matmul(x, w, off), W)
+    with pytest.raises(RuntimeError, match="traced"):
+        torch.jit.trace(lambda w: w * operators._array(w, "weight", (4,), operators._F32, -1), torch.zeros(4))
