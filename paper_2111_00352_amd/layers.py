@@ -2,7 +2,8 @@
 
 Each joins the library's forward and gradient calls for autograd; first derivatives only.
 They can be captured into a graph, forward and backward pass together, as long as no graph
-recorded outside the capture still holds the same parameters (an error otherwise).
+recorded outside the capture still holds the same parameters, directly or through other
+operations (an error where such a graph has one of these layers in it).
 
     Z, H = norm_grouped_linear(X, w, W, offsets, residual=H0)   # norm(X + H0) in 8 bits, by group
     Z = grouped_linear(X, W, offsets)
@@ -34,36 +35,46 @@ def _rows(t):
     return None if t is None else t.contiguous()
 
 
-# Of each leaf that a graph of these layers was recorded for eagerly: the graph's nodes that
-# still live.  Such a graph ties the leaf's gradient to the stream it was recorded on, and a
-# capture that goes backwards to the same leaf would have to wait for that stream, which
-# ends the process where the capture does: it is refused instead.
-_recorded: dict[int, tuple] = {}
+# The nodes of these layers that were recorded eagerly and still live.  Such a node's graph ties its
+# leaves' gradients to the stream it was recorded on, and a capture that goes backwards to the same
+# leaves, whatever lies between, would have to wait for that stream, which ends the process where the
+# capture does: it is refused instead.
+_recorded = weakref.WeakSet()
 
 
-def _watch(ctx, *inputs):
-    leaves = [t for t in inputs if t is not None and t.requires_grad and t.is_leaf]
-    if not leaves:
+def _record(ctx):
+    if any(ctx.needs_input_grad) and not torch.cuda.is_current_stream_capturing():
+        _recorded.add(ctx)
+
+
+def _leaves(tensors, nodes=()) -> dict:
+    """The leaves, by id, that tensors and nodes have their gradients from."""
+    leaves = {id(t): t for t in tensors if t.requires_grad and t.is_leaf}
+    left, seen = [t.grad_fn for t in tensors if t.grad_fn is not None] + list(nodes), set()
+    while left:
+        node = left.pop()
+        if node in seen:
+            continue
+        seen.add(node)
+        if (leaf := getattr(node, "variable", None)) is not None:
+            leaves[id(leaf)] = leaf
+        left += [n for n, _ in node.next_functions if n is not None]
+    return leaves
+
+
+def _may_record(*inputs):
+    """Refuses a capture of inputs whose leaves a graph recorded outside it holds."""
+    if not torch.is_grad_enabled() or not torch.cuda.is_current_stream_capturing() or not (held := list(_recorded)):
         return
-    if torch.cuda.is_current_stream_capturing():
-        for t in leaves:
-            leaf, nodes = _recorded.get(id(t), (None, ()))
-            if leaf is not None and leaf() is t and len(nodes):
-                raise RuntimeError("a graph recorded outside this capture holds the same parameter: delete what it computed first")
-        return
-    for t in leaves:
-        leaf, nodes = _recorded.get(id(t), (None, None))
-        if leaf is None or leaf() is not t:
-            at = id(t)
-            nodes = weakref.WeakSet()
-            _recorded[at] = (weakref.ref(t, lambda gone, at=at: _recorded.pop(at, None) if _recorded.get(at, (None,))[0] is gone else None), nodes)
-        nodes.add(ctx)
+    mine, others = _leaves([t for t in inputs if t is not None]), _leaves((), held)
+    if any(leaf is mine.get(at) for at, leaf in others.items()):
+        raise RuntimeError("a graph recorded outside this capture holds the same parameter: delete what it computed first")
 
 
 class _RmsNorm(torch.autograd.Function):
     @staticmethod
     def forward(ctx, X, weight, residual, eps):
-        _watch(ctx, X, weight, residual)
+        _record(ctx)
         ctx.set_materialize_grads(False)
         Y, H, r = gs.rms_norm(X, weight, residual, eps)
         ctx.save_for_backward(H, r, weight)
@@ -82,13 +93,14 @@ class _RmsNorm(torch.autograd.Function):
 
 def rms_norm(X, weight=None, residual=None, eps: float = 1e-6):
     """(Y, H): H = X + residual, Y its rows divided by their root mean square, times weight."""
+    _may_record(X, weight, residual)
     return _RmsNorm.apply(X, weight, residual, eps)
 
 
 class _GroupedLinear(torch.autograd.Function):
     @staticmethod
     def forward(ctx, X, W, offsets):
-        _watch(ctx, X, W)
+        _record(ctx)
         ctx.save_for_backward(X, W, offsets)
         return gs.grouped_matmul(X, W, offsets)
 
@@ -104,13 +116,14 @@ class _GroupedLinear(torch.autograd.Function):
 
 def grouped_linear(X, W, offsets):
     """Rows offsets[g] .. offsets[g+1] - 1 of X times W[g]; X and W of one type."""
+    _may_record(X, W)
     return _GroupedLinear.apply(X, W, offsets)
 
 
 class _NormGroupedLinear(torch.autograd.Function):
     @staticmethod
     def forward(ctx, X, weight, W, offsets, residual, eps):
-        _watch(ctx, X, weight, W, residual)
+        _record(ctx)
         ctx.set_materialize_grads(False)
         S, H, r = gs.rms_norm(X, weight, residual, eps, save=True)
         ctx.save_for_backward(H, r, weight, W, offsets, S.buffer)
@@ -137,13 +150,14 @@ def norm_grouped_linear(X, weight, W, offsets, residual=None, eps: float = 1e-6)
     """(Z, H): H = X + residual and the products by group of its norm, which is held in 8 bits
     between the forward and the backward pass and read so by the products; its rounding to
     8 bits counts as the identity backwards."""
+    _may_record(X, weight, W, residual)
     return _NormGroupedLinear.apply(X, weight, W, offsets, residual, eps)
 
 
 class _LogProbs(torch.autograd.Function):
     @staticmethod
     def forward(ctx, logits, ids):
-        _watch(ctx, logits)
+        _record(ctx)
         ctx.set_materialize_grads(False)
         found = gs.log_probs(logits, ids)
         ctx.save_for_backward(logits, ids, found.stats, found.entropy)
@@ -161,13 +175,14 @@ class _LogProbs(torch.autograd.Function):
 def log_probs(logits, ids):
     """(log probability of each row's class, entropy); rows with a negative class have 0 and no
     gradient by it."""
+    _may_record(logits)
     return _LogProbs.apply(logits, ids)
 
 
 class _DistillLoss(torch.autograd.Function):
     @staticmethod
     def forward(ctx, logits, top_ids, top_logits, temperature):
-        _watch(ctx, logits)
+        _record(ctx)
         loss, stats = gs.distill_loss(logits, top_ids, top_logits, temperature)
         ctx.save_for_backward(logits, top_ids, top_logits, stats)
         ctx.temperature = temperature
@@ -185,4 +200,5 @@ def distill_loss(logits, top_ids, top_logits, temperature: float = 1.0):
     gradient."""
     if top_logits.requires_grad:
         raise ValueError("the teacher's logits have no gradient: detach them")
+    _may_record(logits)
     return _DistillLoss.apply(logits, top_ids, top_logits, temperature)

@@ -397,3 +397,47 @@ def test_no_tangent_is_dropped_unseen():
         assert torch.equal(gs.grouped_matmul(S, W, off), gs.grouped_matmul(S, W, off))
     with pytest.raises(RuntimeError, match="traced"):
         torch.jit.trace(lambda x: gs.grouped_matmul(S, x, off), W)
+
+
+def test_captures_beside_an_eager_graph_of_weights_of_another_type():
+    """The parameters are reached through a conversion: a captured step is refused all the same, a captured forward
+    pass without gradients is taken."""
+    X, R, w, W, off = _inputs(400, 64, 32, 4, 16)
+    ids = torch.randint(0, 32, (400,), device=DEV)
+    W.requires_grad_()
+    X = X.bfloat16()
+
+    def step():
+        Z = layers.grouped_linear(X, W.bfloat16(), off)
+        return torch.autograd.grad(-layers.log_probs(Z, ids)[0].mean(), W)[0]
+
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        want = step()
+    torch.cuda.current_stream().wait_stream(side)
+    eager = layers.grouped_linear(X, W.bfloat16(), off)
+    torch.cuda.synchronize()
+    with pytest.raises(RuntimeError, match="holds the same parameter"):
+        with torch.cuda.graph(torch.cuda.CUDAGraph()):
+            step()
+    with pytest.raises(RuntimeError, match="holds the same parameter"):
+        with torch.cuda.graph(torch.cuda.CUDAGraph()):
+            layers.log_probs(eager * 2, ids)
+    answer = torch.cuda.CUDAGraph()
+    with torch.no_grad(), torch.cuda.graph(answer):
+        Z = layers.grouped_linear(X, W.bfloat16(), off)
+    for _ in range(3):
+        Z.zero_()
+        answer.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(Z, eager)
+    del eager
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        got = step()
+    for _ in range(3):
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(got, want)
+        layers.grouped_linear(X, W.bfloat16(), off).sum().backward()

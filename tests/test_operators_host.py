@@ -318,3 +318,51 @@ def test_operands_that_are_followed_forwards_or_traced_are_refused():
         torch.jit.trace(lambda w: gs.grouped_matmul(x, w, off), W)
     with pytest.raises(RuntimeError, match="traced"):
         torch.jit.trace(lambda w: w * operators._array(w, "weight", (4,), operators._F32, -1), torch.zeros(4))
+
+
+def test_captures_are_refused_where_an_eager_graph_holds_the_same_leaves(monkeypatch):
+    """What the layers know of graphs recorded outside a capture, without a GPU: a function of theirs in name only."""
+    import torch
+
+    from paper_2111_00352_amd import layers
+
+    class Layer(torch.autograd.Function):
+        @staticmethod
+        def forward(ctx, x, w):
+            layers._record(ctx)
+            return x * w
+
+        @staticmethod
+        def backward(ctx, d):
+            return d, d
+
+    def layer(x, w):
+        layers._may_record(x, w)
+        return Layer.apply(x, w)
+
+    capturing = False
+    monkeypatch.setattr(torch.cuda, "is_current_stream_capturing", lambda: capturing)
+    x, w, other = torch.ones(3), torch.ones(3, requires_grad=True), torch.ones(3, requires_grad=True)
+    for eager in (lambda: layer(x, w), lambda: layer(x, w.double()), lambda: layer(layer(x, w * 2) + 1, other), lambda: layer(x, w).sum().exp()):
+        kept = eager()
+        capturing = True
+        for call in (lambda: layer(x, w), lambda: layer(x, w.bfloat16()), lambda: layer(w.tanh(), other), lambda: layer(kept * 2, x)):
+            with pytest.raises(RuntimeError, match="holds the same parameter"):
+                call()
+        with torch.no_grad():  # (records nothing)
+            layer(x, w)
+            layer(x, w.double())
+        layer(x, x), layer(x, torch.ones(3, requires_grad=True))
+        capturing = False
+        layer(x, w).sum().backward()
+        del kept, call
+        capturing = True
+        inside = layer(x, w)  # (what is recorded inside is no hindrance to the rest of it)
+        (layer(inside, w.double()) + layer(x, w)).sum().backward()
+        capturing = False
+        del inside
+    with torch.no_grad():
+        y = layer(x, w)
+    capturing = True
+    layer(x, w)
+    assert not y.requires_grad
