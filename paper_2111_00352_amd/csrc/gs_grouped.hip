@@ -1013,6 +1013,7 @@ __global__ __launch_bounds__(kPanelWaves * kWave, 2) void k_grouped_panel(Rows A
 // 128 bf16, 9 groups: 41 us and 10 for the 34 MB of partials; bytes alone would take 16.
 
 constexpr int kGradThreads = 512;
+constexpr int64_t kGradChain = 8192;  // rows that are summed one after another
 
 // Place of piece p of row r: writes of lanes whose rows are 1, 2 or 4 apart and reads of
 // neighbouring rows both spread over LDS's banks.
@@ -1106,8 +1107,9 @@ template <class T, int N> struct GradSaved {
 };
 
 // Chunks of `per` rows of a group, a tile of it each; out is the chunk's a x b (one chunk a
-// group: the group's).  A's lanes hold 2 WA columns, G's WB.
-template <class LA, class LG, int WA, int WB>
+// group: the group's).  A's lanes hold 2 WA columns, G's WB.  LONG: `per` is more than a chain, chains are
+// added in memory (code of its own: in the others it would take 3 to 28 registers).
+template <class LA, class LG, int WA, int WB, bool LONG>
 __global__ __launch_bounds__(kGradThreads, 2) void k_grouped_grad(LA A, LG G, Offsets off, int64_t a, int64_t b, int64_t per, int tiles_b,
                                                                  float *__restrict__ out)
 {
@@ -1143,13 +1145,13 @@ __global__ __launch_bounds__(kGradThreads, 2) void k_grouped_grad(LA A, LG G, Of
             G.move(rb, e < more);
         }
     };
-    // Rows from k1 on, of other groups or none, as zeros.
-    auto end = [&](Held &h, int64_t k) {
+    // Rows `from` on, of the next chain, of other groups or none, as zeros.
+    auto end = [&](Held &h, int64_t k, int64_t from) {
         k += wave * E;
-        if (k + E > k1)
+        if (k + E > from)
 #pragma unroll
             for (int e = 0; e < E; e++)
-                if (k + e >= k1) {
+                if (k + e >= from) {
                     A.none(h.a, e);
                     G.none(h.b, e);
                 }
@@ -1186,39 +1188,50 @@ __global__ __launch_bounds__(kGradThreads, 2) void k_grouped_grad(LA A, LG G, Of
             }
     };
     constexpr int64_t STEP = kChunk<T>;
-    if (k0 < k1) {
-        load(h0, k0);
-        load(h1, k0 + STEP);
-        end(h0, k0);
-        store(h0, lds);
-        __syncthreads();
-        for (int64_t k = k0; k < k1; k += 2 * STEP) {
-            load(h0, k + 2 * STEP);
-            work(lds);
-            end(h1, k + STEP);
-            store(h1, lds + STAGE);
-            __syncthreads();
-            load(h1, k + 3 * STEP);
-            if (k + STEP < k1) work(lds + STAGE);
-            end(h0, k + 2 * STEP);
+    float *to = out + (int64_t)blockIdx.x * a * b;
+    for (int64_t c0 = k0;; c0 += kGradChain) {
+        const int64_t c1 = LONG ? std::min(c0 + kGradChain, k1) : k1;
+        if (c0 < c1) {
+            load(h0, c0);
+            load(h1, c0 + STEP);
+            end(h0, c0, c1);
             store(h0, lds);
             __syncthreads();
-        }
-    }
-    float *to = out + (int64_t)blockIdx.x * a * b;
-#pragma unroll
-    for (int i = 0; i < WA; i++)
-#pragma unroll
-        for (int j = 0; j < WB; j++)
-#pragma unroll
-            for (int g = 0; g < 4; g++) {
-                const int64_t r = a0 + ra + 32 * i, c = b0 + wave % 2 * 32 * WB + 32 * j + 8 * g + 4 * half;
-                const f32x16 &v = acc[i][j];
-                if (r < a && c < b)
-                    store_elems<float, 4>(to + r * b + c, typename Elems<float, 4>::type{v[4 * g], v[4 * g + 1], v[4 * g + 2], v[4 * g + 3]}, b - c);
+            for (int64_t k = c0; k < c1; k += 2 * STEP) {
+                load(h0, k + 2 * STEP);
+                work(lds);
+                end(h1, k + STEP, c1);
+                store(h1, lds + STAGE);
+                __syncthreads();
+                load(h1, k + 3 * STEP);
+                if (k + STEP < c1) work(lds + STAGE);
+                end(h0, k + 2 * STEP, c1);
+                store(h0, lds);
+                __syncthreads();
             }
+        }
+#pragma unroll
+        for (int i = 0; i < WA; i++)
+#pragma unroll
+            for (int j = 0; j < WB; j++)
+#pragma unroll
+                for (int g = 0; g < 4; g++) {
+                    const int64_t r = a0 + ra + 32 * i, c = b0 + wave % 2 * 32 * WB + 32 * j + 8 * g + 4 * half;
+                    if (r < a && c < b) {
+                        const f32x16 &v = acc[i][j];
+                        typename Elems<float, 4>::type sum = {v[4 * g], v[4 * g + 1], v[4 * g + 2], v[4 * g + 3]};
+                        if (LONG && c0 > k0) sum += load_elems<float, 4>(to + r * b + c, b - c);  // (this lane's own)
+                        store_elems<float, 4>(to + r * b + c, sum, b - c);
+                    }
+                }
+        if (!LONG || c1 >= k1) break;
+#pragma unroll
+        for (int i = 0; i < WA; i++)
+#pragma unroll
+            for (int j = 0; j < WB; j++) acc[i][j] = f32x16{};
+    }
 }
-// The chunks of a group added in order: 256 threads, four elements each; blockIdx.y the group.
+// The chunks of a group added in order, in 64 bits: 256 threads, four elements each; blockIdx.y the group.
 __global__ __launch_bounds__(256) void k_grouped_join(const float *__restrict__ part, Offsets off, int64_t ab, int64_t per,
                                                       int64_t all, float *__restrict__ out)
 {
@@ -1237,7 +1250,7 @@ __global__ __launch_bounds__(256) void k_grouped_join(const float *__restrict__ 
     first -= mine;
     const int64_t e = ((int64_t)blockIdx.x * 256 + threadIdx.x) * 4;
     if (e >= ab) return;
-    float4 s = make_float4(0, 0, 0, 0);
+    double s[4] = {};  // (a hundred thousand partials are possible)
     const int64_t end = std::min(first + mine, all);  // (offsets that descend: no more than there are)
     constexpr int U = 8;  // partials in flight
     for (int64_t c = first; c < end; c += U) {
@@ -1246,9 +1259,11 @@ __global__ __launch_bounds__(256) void k_grouped_join(const float *__restrict__ 
         for (int u = 0; u < U; u++) v[u] = load_elems<float, 4>(part + std::min(c + u, end - 1) * ab + e, ab - e);
 #pragma unroll
         for (int u = 0; u < U; u++)
-            if (c + u < end) s.x += v[u][0], s.y += v[u][1], s.z += v[u][2], s.w += v[u][3];
+            if (c + u < end)
+#pragma unroll
+                for (int i = 0; i < 4; i++) s[i] += v[u][i];
     }
-    store_elems<float, 4>(out + blockIdx.y * ab + e, typename Elems<float, 4>::type{s.x, s.y, s.z, s.w}, ab - e);
+    store_elems<float, 4>(out + blockIdx.y * ab + e, typename Elems<float, 4>::type{(float)s[0], (float)s[1], (float)s[2], (float)s[3]}, ab - e);
 }
 
 // ------------------------------------------------------------------- launch
@@ -1270,8 +1285,8 @@ struct Operand {  // dense, or saved
     const gs_saved *saved;
 };
 
-// Rows of a run, and how many runs there can be: a workgroup for each compute unit, chains of
-// at most 8,192 rows.
+// Rows of a run, and how many runs there can be: a workgroup for each compute unit, a run a chain
+// at most, unless so many partial products would take too much.
 struct GroupedGradPlan {
     int64_t per, chunks, tiles_a, tiles_b;
     bool direct;
@@ -1285,7 +1300,7 @@ GroupedGradPlan grouped_grad_plan(int64_t rows, int64_t groups, int64_t a, int64
     p.tiles_a = ceil_div(a, 128 * p.wa);
     p.tiles_b = ceil_div(b, 64 * p.wb);
     const int64_t tiles = p.tiles_a * p.tiles_b, want = std::max<int64_t>(1, 256 / tiles);
-    p.per = std::min<int64_t>(8192, std::max<int64_t>(256, ceil_div(ceil_div(rows, want), 64) * 64));
+    p.per = std::min<int64_t>(kGradChain, std::max<int64_t>(256, ceil_div(ceil_div(rows, want), 64) * 64));
     // (what partial sums would take: at most 1 GB of them)
     const int64_t most = std::max<int64_t>(1, ((int64_t)1 << 28) / (a * b));
     if (ceil_div(rows, p.per) + groups > most) p.per = ceil_div(ceil_div(rows, std::max<int64_t>(1, most - groups)), 64) * 64;
@@ -1513,9 +1528,13 @@ static int grouped_weight_grad(const Operand &A, int a_dtype, int64_t rows, int6
         const hipStream_t s = (hipStream_t)stream;
         float *part = p.direct ? out : (float *)work;
         auto go = [&](auto la, auto lg, auto wa, auto wb) {
-            k_grouped_grad<decltype(la), decltype(lg), decltype(wa)::value, decltype(wb)::value>
-                <<<dim3((unsigned)p.chunks, (unsigned)(p.tiles_a * p.tiles_b)), kGradThreads, 0, s>>>(la, lg, off, a, b, p.per,
-                                                                                                    (int)p.tiles_b, part);
+            constexpr int WA = decltype(wa)::value, WB = decltype(wb)::value;
+            auto run = [&](auto kernel) {
+                kernel<<<dim3((unsigned)p.chunks, (unsigned)(p.tiles_a * p.tiles_b)), kGradThreads, 0, s>>>(la, lg, off, a, b, p.per,
+                                                                                                          (int)p.tiles_b, part);
+            };
+            p.per > kGradChain ? run(k_grouped_grad<decltype(la), decltype(lg), WA, WB, true>)
+                               : run(k_grouped_grad<decltype(la), decltype(lg), WA, WB, false>);
         };
         auto with_tile = [&](auto type, auto wa, auto wb) {
             using T = decltype(type);

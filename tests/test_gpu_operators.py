@@ -697,3 +697,28 @@ def test_grouped_result_right_behind_one_matrix_for_all(dtype):
     want = np.concatenate([_np(A[:100]) @ _np(side[:, 0]), _np(A[100:]) @ _np(side[:, 2])])
     M = np.concatenate([np.abs(_np(A[:100])) @ np.abs(_np(side[:, 0])), np.abs(_np(A[100:])) @ np.abs(_np(side[:, 2]))])
     _close(got, want, (2 * 64 + 4) * U * M + HALF[dtype] * np.abs(want))
+
+
+@pytest.mark.parametrize("groups", [65_500, 65_535])
+@pytest.mark.parametrize("dtype,a8", [("f32", False), ("f32", True), ("bf16", False), ("bf16", True)])
+def test_grouped_weight_grad_where_there_is_room_for_few_partial_products(groups, dtype, a8):
+    """Half a million rows of one group among so many that runs are longer than 8,192 rows: no sum is.
+    fp32 sums of the first column's products one after another would lose half a last place each time."""
+    rows, a, b = 1 << 19, 64, 64
+    gen = torch.Generator(device=DEV).manual_seed(groups)
+    A = torch.rand(rows, a, device=DEV, generator=gen)
+    A[:, :2] = 1.0
+    A = A.to(TYPES[dtype])
+    Ad = gs.save_activation(A, "none")[1] if a8 else A
+    G = torch.rand(rows, b, device=DEV, generator=gen)
+    G[:, 0] = 1 + 2.0 ** -7
+    G = G.to(TYPES[dtype])
+    off = torch.zeros(groups + 1, dtype=torch.int32, device=DEV)
+    off[30_000:] = rows - 77
+    off[:29_999] = 11  # rows before the first and behind the last group
+    off[29_999] = 11
+    got = gs.grouped_weight_grad(Ad, G, off)
+    Av, Gv = (Ad.dequantize().float() if a8 else A.float())[11:rows - 77].double(), G[11:rows - 77].double()
+    want = _np(Av.t().contiguous() @ Gv)  # (all are positive: its own magnitude)
+    _close(got[29_999], want, (2 * 8192 + 2 * rows // 8192 + 8) * U * want)
+    assert int(got.count_nonzero()) == a * b
