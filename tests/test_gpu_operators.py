@@ -722,3 +722,79 @@ def test_grouped_weight_grad_where_there_is_room_for_few_partial_products(groups
     want = _np(Av.t().contiguous() @ Gv)  # (all are positive: its own magnitude)
     _close(got[29_999], want, (2 * 8192 + 2 * rows // 8192 + 8) * U * want)
     assert int(got.count_nonzero()) == a * b
+
+
+@pytest.mark.parametrize("n,a", [(100_003, 64), (60_000, 31), (50_001, 257), (20_000, 500), (9000, 1344), (5001, 4100), (2500, 8192), (1200, 20_011)])
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_rms_norm_grad_over_many_sets_of_rows(n, a, dtype):
+    """Workgroups that go on to further rows: dw over rows of +-1 and small whole gradients is exact, whatever the order."""
+    gen = torch.Generator().manual_seed(n)
+    H = (2 * torch.randint(0, 2, (n, a), generator=gen) - 1).to(TYPES[dtype]).to(DEV)
+    dY = torch.randint(-4, 5, (n, a), generator=gen).to(TYPES[dtype]).to(DEV)
+    dH = torch.randint(-4, 5, (n, a), generator=gen).to(TYPES[dtype]).to(DEV)
+    w = torch.ones(a, device=DEV)
+    Y, _, r = gs.rms_norm(H, w, eps=0.0)
+    assert (r == 1).all() and torch.equal(Y, H)
+    dX, dw = gs.rms_norm_grad(H, r, dY, w, dH)
+    Hd, dYd = H.double(), dY.double()
+    assert torch.equal(dw.double(), (dYd * Hd).sum(0))
+    want = _np(dH.double() + dYd - Hd * (dYd * Hd).mean(1, keepdim=True))
+    # (a row's sum of products is exact; its mean, the product with +-1, the sums: a rounding each, of numbers up to 12)
+    _close(dX, want, 4 * 12 * U + HALF[dtype] * np.abs(want), "dX")
+
+
+def _slices(n):
+    return [slice(0, 700), slice(n // 2 - 300, n // 2 + 400), slice(n - 701, n)]
+
+
+@pytest.mark.parametrize("n,a", [(700_001, 64), (400_001, 128), (30_001, 2048), (9001, 8192)])
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_norms_past_the_caches(n, a, dtype):
+    """Calls that move more than the caches hold have the bits of small ones on the same rows."""
+    X, R = (torch.randn(n, a, device=DEV).to(TYPES[dtype]) for _ in range(2))
+    w = 1 + 0.2 * torch.randn(a, device=DEV)
+    Y, H, r = gs.rms_norm(X, w, R)
+    S, H8, r8 = gs.rms_norm(X, w, R, save=True)
+    assert torch.equal(H, H8) and torch.equal(r, r8)
+    d, _ = gs.rms_norm_grad(H, r, X, w, R)
+    # (gradients of whole numbers, whose sums over the rows are exact)
+    one, whole = (X > 0).to(X.dtype) * 2 - 1, (4 * R).round().clamp(-4, 4)
+    dw = gs.rms_norm_grad(one, torch.ones_like(r), whole, w)[1]
+    assert torch.equal(dw.double(), (one.double() * whole.double()).sum(0))
+    for at in _slices(n):
+        y, h, t = gs.rms_norm(X[at], w, R[at])
+        s = gs.rms_norm(X[at], w, R[at], save=True)[0]
+        assert torch.equal(Y[at], y) and torch.equal(H[at], h) and torch.equal(r[at], t)
+        assert torch.equal(S.codes[at], s.codes) and torch.equal(S.scales[at], s.scales)
+        assert torch.equal(d[at], gs.rms_norm_grad(h, t, X[at], w, R[at])[0])
+
+
+@pytest.mark.parametrize("n,v", [(1_500_000, 48), (400_000, 256), (100_001, 1024), (30_000, 4096)])
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_scores_past_the_caches(n, v, dtype):
+    s = torch.randn(n, v, device=DEV).to(TYPES[dtype])
+    ids = torch.randint(-1, v, (n,), device=DEV)
+    tid, t = torch.randint(-1, v, (n, 5), device=DEV, dtype=torch.int32), torch.randn(n, 5, device=DEV)
+    g, e = torch.randn(n, device=DEV), torch.randn(n, device=DEV)
+    found, (loss, stats) = gs.log_probs(s, ids), gs.distill_loss(s, tid, t, 1.5)
+    d, dt = gs.log_probs_grad(s, ids, found, g, e), gs.distill_grad(s, tid, t, stats, g, 1.5)
+    for at in _slices(n):
+        small, (l, st) = gs.log_probs(s[at], ids[at]), gs.distill_loss(s[at], tid[at], t[at], 1.5)
+        for a, b in zip(found, small):
+            assert torch.equal(a[at], b)
+        assert torch.equal(loss[at], l) and torch.equal(stats[at], st)
+        assert torch.equal(d[at], gs.log_probs_grad(s[at], ids[at], small, g[at], e[at]))
+        assert torch.equal(dt[at], gs.distill_grad(s[at], tid[at], t[at], st, g[at], 1.5))
+
+
+@pytest.mark.parametrize("v", [20_000, 50_304])
+def test_wide_gradients_past_the_caches(v):
+    """Rows in spans of a workgroup: their gradient is the same as in a call of few rows."""
+    n = 4000
+    s = torch.randn(n, v, device=DEV)
+    ids, g = torch.randint(0, v, (n,), device=DEV), torch.randn(n, device=DEV)
+    found = gs.log_probs(s, ids)
+    d = gs.log_probs_grad(s, ids, found, g, g)
+    for at in (slice(0, 40), slice(n - 41, n)):
+        small = gs.LogProbs(*(x[at].contiguous() for x in found))
+        assert torch.equal(d[at], gs.log_probs_grad(s[at], ids[at], small, g[at], g[at]))
