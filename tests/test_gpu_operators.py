@@ -798,3 +798,102 @@ def test_wide_gradients_past_the_caches(v):
     for at in (slice(0, 40), slice(n - 41, n)):
         small = gs.LogProbs(*(x[at].contiguous() for x in found))
         assert torch.equal(d[at], gs.log_probs_grad(s[at], ids[at], small, g[at], g[at]))
+
+
+def _same(big, small, n):
+    for a, b in zip(big, small):
+        assert torch.equal(a[-n:], b)
+
+
+@pytest.mark.parametrize("n,v,dtype,top", [((1 << 26) + 1000, 9, "f32", 0), ((1 << 24) + 700, 70, "bf16", 3), ((1 << 20) + 700, 1100, "f32", 0),
+                                           ((1 << 20) + 700, 2100, "bf16", 5), ((1 << 20) + 700, 8200, "bf16", 0)])
+def test_more_rows_than_a_launch_has_workgroups_for(n, v, dtype, top):
+    """Workgroups of the scores that go on to further rows: the last rows have the bits of a small call."""
+    s = torch.empty(n, v, dtype=TYPES[dtype], device=DEV).normal_()
+    ids = torch.randint(0, v, (n,), device=DEV, dtype=torch.int32)
+    tid, t = torch.randint(0, v, (n, 3), device=DEV, dtype=torch.int32), torch.randn(n, 3, device=DEV)
+    g = torch.randn(n, device=DEV)
+    found, lost = gs.log_probs(s, ids, top=top), gs.distill_loss(s, tid, t)
+    k = 1000
+    small, l = gs.log_probs(s[-k:].clone(), ids[-k:], top=top), gs.distill_loss(s[-k:].clone(), tid[-k:], t[-k:])
+    _same(found, small, k)
+    _same(lost, l, k)
+    assert (found.logp < 0).all() and torch.isfinite(lost[0]).all()
+    tail = s[-k:].clone()
+    d = gs.log_probs_grad(s, ids, found, g, g)
+    assert torch.equal(d[-k:], gs.log_probs_grad(tail, ids[-k:], small, g[-k:], g[-k:]))
+    del d
+    d = gs.distill_grad(s, tid, t, lost[1], g, out=s)
+    assert torch.equal(d[-k:], gs.distill_grad(tail, tid[-k:], t[-k:], l[1], g[-k:]))
+
+
+def test_norm_of_more_rows_than_a_launch_has_workgroups_for():
+    n, a = (1 << 20) + 500, 6200
+    X = torch.empty(n, a, device=DEV).normal_()
+    Y, _, r = gs.rms_norm(X)
+    y, _, q = gs.rms_norm(X[-700:].clone())
+    assert torch.equal(Y[-700:], y) and torch.equal(r[-700:], q) and (r > 0.9).all()
+
+
+@pytest.mark.parametrize("k,n,a8,wtype", [(256, 256, False, "bf16"), (256, 48, False, "bf16"), (256, 40, True, "f32"), (300, 33, False, "bf16")])
+def test_products_of_rows_past_32_bits(k, n, a8, wtype):
+    """The last rows of operands whose elements are past 2^31 from their start, large tiles, layers and others."""
+    rows = (1 << 31) // k + 100_000
+    A = torch.empty(rows, k, dtype=torch.float32 if a8 else TYPES[wtype], device=DEV).normal_()
+    W = torch.randn(3, k, n, device=DEV).to(TYPES[wtype])
+    last = 600
+    off = torch.tensor([0, 1000, rows - last, rows], device=DEV)
+    Ad = gs.save_activation(A, "none")[1] if a8 else A
+    Av = gs.save_activation(A[-last:].clone(), "none")[1].dequantize() if a8 else A[-last:]
+    got = gs.grouped_matmul(Ad, W, off, dtype=torch.float32)
+    want, M = oracle.grouped(_np(Av), _np(W[2:]), [0, last], False)
+    _close(got[-last:], want, (2 * 3 * k + 4) * U * M + U * np.abs(want))
+    G = got.to(TYPES[wtype])
+    del got
+    dW = gs.grouped_weight_grad(Ad, G, off)
+    want, M = oracle.grouped_grad(_np(Av), _np(G[-last:]), [0, last])
+    _close(dW[2:], want, (2 * last + 4) * U * M)
+    assert torch.isfinite(dW).all()
+
+
+@pytest.mark.parametrize("rows", [40, 40 * 70])
+def test_matrices_past_32_bits(rows):
+    groups, k, n = 40, 8192, 8192
+    W = torch.empty(groups, k, n, dtype=torch.bfloat16, device=DEV).normal_()
+    A = torch.randn(rows, k, device=DEV).bfloat16()
+    off = torch.arange(0, rows + 1, rows // groups, device=DEV)
+    for back in (False, True):
+        C = gs.grouped_matmul(A, W, off, transpose=back, dtype=torch.float32)
+        at = slice(rows - rows // groups, rows)
+        Wl = W[-1].float().t().contiguous() if back else W[-1].float()
+        want, M = _np(A[at].double() @ Wl.double()), _np(A[at].double().abs() @ Wl.double().abs())
+        _close(C[at], want, (2 * k + 20) * U * M)
+    del W
+    G = C.bfloat16()
+    dW = gs.grouped_weight_grad(A, G, off)
+    want, M = oracle.grouped_grad(_np(A[at]), _np(G[at]), [0, rows // groups])
+    _close(dW[-1:], want, (2 * rows // groups + 4) * U * M)
+
+
+def test_no_rows_and_many_alternatives_of_few_classes():
+    E, i = torch.zeros(0, 12, device=DEV), torch.zeros(0, dtype=torch.int64, device=DEV)
+    found = gs.log_probs(E, i, top=3)
+    assert found.logp.shape == (0,) and found.top_ids.shape == (0, 3) and gs.log_probs_grad(E, i, found, found.logp, found.logp).shape == (0, 12)
+    loss, stats = gs.distill_loss(E, torch.zeros(0, 4, dtype=torch.int32, device=DEV), torch.zeros(0, 4, device=DEV))
+    assert loss.shape == (0,) and stats.shape == (0, 4)
+    assert gs.distill_grad(E, torch.zeros(0, 4, dtype=torch.int32, device=DEV), torch.zeros(0, 4, device=DEV), stats, loss).shape == (0, 12)
+    dX, dw = gs.rms_norm_grad(E, loss, E, torch.ones(12, device=DEV))
+    assert dX.shape == (0, 12) and (dw == 0).all()
+    S, _, _ = gs.rms_norm(E, save=True)
+    assert S.shape == (0, 12)
+    # 128 alternatives of a row, a few classes over and over
+    rng = np.random.default_rng(3)
+    for v, dtype in ((1, "f32"), (5, "f32"), (7, "bf16"), (60, "bf16"), (63, "f32")):
+        s = torch.from_numpy(rng.standard_normal((300, v)).astype(np.float32)).to(TYPES[dtype])
+        ids, t = rng.integers(-1, v, (300, 128)), rng.standard_normal((300, 128)).astype(np.float32)
+        loss, stats = gs.distill_loss(s.to(DEV), torch.from_numpy(ids).to(DEV), torch.from_numpy(t).to(DEV), 2.0)
+        d = gs.distill_grad(s.to(DEV), torch.from_numpy(ids).to(DEV), torch.from_numpy(t).to(DEV), stats, torch.ones(300, device=DEV), 2.0)
+        want, wd, _, _, _ = oracle.distill(_np(s), ids, t, 2.0)
+        # (128 weights one after another at most, each off by some U; logits and alternatives within 10 of their largest)
+        _close(loss, want, 4 * U * (128 + 4 * 10 + 30) * 10)
+        _close(d, wd, 2 * U * (2 * 128 + 8 * 10 + 40) + HALF[dtype] * np.abs(wd))
