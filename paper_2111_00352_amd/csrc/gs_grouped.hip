@@ -1231,7 +1231,7 @@ __global__ __launch_bounds__(kGradThreads, 2) void k_grouped_grad(LA A, LG G, Of
             for (int j = 0; j < WB; j++) acc[i][j] = f32x16{};
     }
 }
-// The chunks of a group added in order, in 64 bits: 256 threads, four elements each; blockIdx.y the group.
+// The chunks of a group added in order, every eight of them in 64 bits: 256 threads, four elements each; blockIdx.y the group.
 __global__ __launch_bounds__(256) void k_grouped_join(const float *__restrict__ part, Offsets off, int64_t ab, int64_t per,
                                                       int64_t all, float *__restrict__ out)
 {
@@ -1257,11 +1257,14 @@ __global__ __launch_bounds__(256) void k_grouped_join(const float *__restrict__ 
         typename Elems<float, 4>::type v[U];
 #pragma unroll
         for (int u = 0; u < U; u++) v[u] = load_elems<float, 4>(part + std::min(c + u, end - 1) * ab + e, ab - e);
+        float some[4] = {};
 #pragma unroll
         for (int u = 0; u < U; u++)
             if (c + u < end)
 #pragma unroll
-                for (int i = 0; i < 4; i++) s[i] += v[u][i];
+                for (int i = 0; i < 4; i++) some[i] += v[u][i];
+#pragma unroll
+        for (int i = 0; i < 4; i++) s[i] += some[i];
     }
     store_elems<float, 4>(out + blockIdx.y * ab + e, typename Elems<float, 4>::type{(float)s[0], (float)s[1], (float)s[2], (float)s[3]}, ab - e);
 }
