@@ -1010,7 +1010,8 @@ __global__ __launch_bounds__(kPanelWaves * kWave, 2) void k_grouped_panel(Rows A
 // them, N columns a lane, which are 16 bytes along k for each column when they are put into LDS.
 // Bound by the loads' way: two chunks are under way in registers (a third spills) while one is multiplied.
 // Runs end in partial products, which a second launch adds in order.  204,800 rows of 256 codes and
-// 128 bf16, 9 groups: 41 us and 10 for the 34 MB of partials; bytes alone would take 16.
+// 128 bf16, 9 groups: 41 us and 9 for the 34 MB of partials; bytes alone would take 16.  16,384 rows of
+// 4096 by 4096, 16 groups, bf16: 1,182 us, 465 TFLOP/s.
 
 constexpr int kGradThreads = 512;
 constexpr int64_t kGradChain = 8192;  // rows that are summed one after another

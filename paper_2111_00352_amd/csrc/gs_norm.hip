@@ -9,13 +9,16 @@
 //
 // H is rounded to its type before anything is made of it, so that the backward pass, which
 // reads it from memory, sees the numbers that were normalised.  Squares are exact in 64
-// bits and summed there: rows of any finite fp32 magnitude have their r, and a row's sum
-// costs a few instructions beside the loads that bound these kernels.
+// bits and summed there: no row is too large for its r, or too small while r is below 2^128 (past
+// that, with eps 0, it is infinite), and a row's sum costs a few instructions beside the loads
+// that bound these kernels.
 //
 // Both directions are one pass over memory, which bounds them: a row stays in registers between
 // its sum and its results.  2,000,000 x 128 fp32 with a residual into 8 bits takes 512 us (6.5
 // TB/s), the norm alone 335 (6.1), its gradient 611 (5.0); 20,000 x 8192 bf16 109 (6.0) and 238 (4.1).
 // Rows at odd offsets, whose 16-byte pieces straddle their loads' lines, cost up to a fifth more.
+// The gradient of bf16 rows that fill part of a workgroup's lanes is bound by its instructions and two
+// barriers a row: 186,011 x 1344 510 us (2.9 TB/s), where 200,000 x 1024 take 212 (5.8).
 #include <algorithm>
 #include <type_traits>
 

@@ -153,7 +153,9 @@ __device__ __forceinline__ void write_loss(const RowStats &st, float logS, const
 
 // ------------------------------------------------------------ rows in registers
 
-// (the next rows are loaded while these are worked on; L > 64: a workgroup's row, no alternatives)
+// (where there are more sets of rows than workgroups in a launch, 2^20, the next ones are loaded while these
+// are worked on; L > 64: a workgroup's row, no alternatives.  Each of the best classes is a scan of the row in
+// registers: 200,000 x 1000 fp32 153 us, 369 with 8 of them, 2,093 with 64.)
 template <class T, int L, int R, bool TEACHER, bool NT>
 __global__ __launch_bounds__(kRowThreads) void k_scores_held(const T *__restrict__ s, int64_t ld, int64_t n, int v, ClassIds ids,
                                                             Teacher te, ScoreOut out)
