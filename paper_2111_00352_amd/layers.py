@@ -42,8 +42,12 @@ def _rows(t):
 _recorded = weakref.WeakSet()
 
 
-def _record(ctx):
-    if any(ctx.needs_input_grad) and not torch.cuda.is_current_stream_capturing():
+def _capturing(t) -> bool:
+    return isinstance(t, torch.Tensor) and t.is_cuda and torch.cuda.is_current_stream_capturing()
+
+
+def _record(ctx, of):
+    if any(ctx.needs_input_grad) and not _capturing(of):
         _recorded.add(ctx)
 
 
@@ -64,7 +68,7 @@ def _leaves(tensors, nodes=()) -> dict:
 
 def _may_record(*inputs):
     """Refuses a capture of inputs whose leaves a graph recorded outside it holds."""
-    if not torch.is_grad_enabled() or not torch.cuda.is_current_stream_capturing() or not (held := list(_recorded)):
+    if not torch.is_grad_enabled() or not _capturing(inputs[0]) or not (held := list(_recorded)):
         return
     mine, others = _leaves([t for t in inputs if t is not None]), _leaves((), held)
     if any(leaf is mine.get(at) for at, leaf in others.items()):
@@ -74,7 +78,7 @@ def _may_record(*inputs):
 class _RmsNorm(torch.autograd.Function):
     @staticmethod
     def forward(ctx, X, weight, residual, eps):
-        _record(ctx)
+        _record(ctx, X)
         ctx.set_materialize_grads(False)
         Y, H, r = gs.rms_norm(X, weight, residual, eps)
         ctx.save_for_backward(H, r, weight)
@@ -100,7 +104,7 @@ def rms_norm(X, weight=None, residual=None, eps: float = 1e-6):
 class _GroupedLinear(torch.autograd.Function):
     @staticmethod
     def forward(ctx, X, W, offsets):
-        _record(ctx)
+        _record(ctx, X)
         ctx.save_for_backward(X, W, offsets)
         return gs.grouped_matmul(X, W, offsets)
 
@@ -123,7 +127,7 @@ def grouped_linear(X, W, offsets):
 class _NormGroupedLinear(torch.autograd.Function):
     @staticmethod
     def forward(ctx, X, weight, W, offsets, residual, eps):
-        _record(ctx)
+        _record(ctx, X)
         ctx.set_materialize_grads(False)
         S, H, r = gs.rms_norm(X, weight, residual, eps, save=True)
         ctx.save_for_backward(H, r, weight, W, offsets, S.buffer)
@@ -157,7 +161,7 @@ def norm_grouped_linear(X, weight, W, offsets, residual=None, eps: float = 1e-6)
 class _LogProbs(torch.autograd.Function):
     @staticmethod
     def forward(ctx, logits, ids):
-        _record(ctx)
+        _record(ctx, logits)
         ctx.set_materialize_grads(False)
         found = gs.log_probs(logits, ids)
         ctx.save_for_backward(logits, ids, found.stats, found.entropy)
@@ -182,7 +186,7 @@ def log_probs(logits, ids):
 class _DistillLoss(torch.autograd.Function):
     @staticmethod
     def forward(ctx, logits, top_ids, top_logits, temperature):
-        _record(ctx)
+        _record(ctx, logits)
         loss, stats = gs.distill_loss(logits, top_ids, top_logits, temperature)
         ctx.save_for_backward(logits, top_ids, top_logits, stats)
         ctx.temperature = temperature

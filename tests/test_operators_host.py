@@ -329,7 +329,7 @@ def test_captures_are_refused_where_an_eager_graph_holds_the_same_leaves(monkeyp
     class Layer(torch.autograd.Function):
         @staticmethod
         def forward(ctx, x, w):
-            layers._record(ctx)
+            layers._record(ctx, x)
             return x * w
 
         @staticmethod
@@ -341,7 +341,7 @@ def test_captures_are_refused_where_an_eager_graph_holds_the_same_leaves(monkeyp
         return Layer.apply(x, w)
 
     capturing = False
-    monkeypatch.setattr(torch.cuda, "is_current_stream_capturing", lambda: capturing)
+    monkeypatch.setattr(layers, "_capturing", lambda t: capturing)
     x, w, other = torch.ones(3), torch.ones(3, requires_grad=True), torch.ones(3, requires_grad=True)
     for eager in (lambda: layer(x, w), lambda: layer(x, w.double()), lambda: layer(layer(x, w * 2) + 1, other), lambda: layer(x, w).sum().exp()):
         kept = eager()
@@ -366,3 +366,15 @@ def test_captures_are_refused_where_an_eager_graph_holds_the_same_leaves(monkeyp
     capturing = True
     layer(x, w)
     assert not y.requires_grad
+
+
+def test_layers_refuse_cpu_tensors():
+    import torch
+
+    from paper_2111_00352_amd import layers
+    x, i = torch.zeros(2, 4), torch.zeros(2, dtype=torch.int64)
+    w, W = torch.ones(4, requires_grad=True), torch.zeros(1, 4, 4, requires_grad=True)
+    for call in (lambda: layers.rms_norm(x), lambda: layers.rms_norm(x, w), lambda: layers.rms_norm([1.0], w), lambda: layers.grouped_linear(x, W, i),
+                 lambda: layers.norm_grouped_linear(x, w, W, i), lambda: layers.log_probs(x * w, i), lambda: layers.distill_loss(x * w, i[:, None], x[:, :1])):
+        with pytest.raises(ValueError):
+            call()
