@@ -100,7 +100,11 @@ struct Teacher {
     float c;      // 1 / temperature
     float k2;     // log2(e) / temperature
     float scale;  // temperature^2
+    float tiny;   // c / kLossUnit
 };
+// What the sum of weight times (log q' - log p') is divided by: a hundred of them stay finite for classes that
+// the student masked with its type's lowest number, at any temperature.
+constexpr float kLossUnit = 0x1p24f;
 // Alternative i of a row: its class (negative: none) and what teacher and student give it.
 template <class T> struct Alternative {
     int64_t id;
@@ -136,17 +140,17 @@ __device__ __forceinline__ void write_loss(const RowStats &st, float logS, const
     float tm = -kInf;
     each([&](const Alternative<T> &a) { tm = fmaxf(tm, a.t); });
     tm = row_fold<L>(tm, tmp, [](float a, float b) { return fmaxf(a, b); });
-    // of the weights, of weight (log q' - log p'), of the alternatives (infinity for one that is not there)
+    // of the weights, of weight (log q' - log p') / kLossUnit, of the alternatives (infinity for one that is not there)
     float sums[3] = {0.0f, 0.0f, 0.0f};
     each([&](const Alternative<T> &a) {
-        const float d = (a.t - tm) * te.c, w = exp_neg(d), x = (a.s - st.m) * te.c;
+        const float d = a.t - tm, w = exp_neg(d * te.c), x = (a.s - st.m) * te.tiny;
         sums[0] += w;
-        if (!(w == 0.0f) || x != x) sums[1] = __builtin_fmaf(w, d - x, sums[1]);
+        if (!(w == 0.0f) || x != x) sums[1] = __builtin_fmaf(w, d * te.tiny - x, sums[1]);
         sums[2] += a.id < v ? 1.0f : kInf;
     });
     row_sums<L, 3>(sums, tmp);
     if (in && lane == 0) {
-        loss[row] = sums[2] > 0.0f ? te.scale * (sums[1] / sums[0] + (logS - logf(sums[0]))) : 0.0f;
+        loss[row] = sums[2] > 0.0f ? __builtin_fmaf(te.scale * kLossUnit, sums[1] / sums[0], te.scale * (logS - logf(sums[0]))) : 0.0f;
         stats[row] = make_float4(st.m, st.S, tm, sums[2] == kInf ? __builtin_nanf("") : sums[2] > 0.0f ? 1.0f / sums[0] : 0.0f);
     }
 }
@@ -866,7 +870,7 @@ Teacher check_teacher(const void *ids, int id_bytes, const void *t, int t_dtype,
     if (n > 0 && !t) fail(GS_ERR_INVALID_ARG, "the teacher's logits are null");
     if ((uintptr_t)t % size) fail(GS_ERR_INVALID_ARG, "the teacher's logits are not aligned");
     return {check_ids("the teacher's classes", ids, id_bytes, n), t, t_dtype == GS_F32, (int)k, (float)(1.0 / temperature),
-            (float)(1.4426950408889634 / temperature), (float)(temperature * temperature)};
+            (float)(1.4426950408889634 / temperature), (float)(temperature * temperature), (float)(1.0 / temperature) / kLossUnit};
 }
 
 // Whether rows are short and without gaps; go(L, C): lanes and elements.

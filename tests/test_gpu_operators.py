@@ -897,3 +897,35 @@ def test_no_rows_and_many_alternatives_of_few_classes():
         # (128 weights one after another at most, each off by some U; logits and alternatives within 10 of their largest)
         _close(loss, want, 4 * U * (128 + 4 * 10 + 30) * 10)
         _close(d, wd, 2 * U * (2 * 128 + 8 * 10 + 40) + HALF[dtype] * np.abs(wd))
+
+
+@pytest.mark.parametrize("v", [5, 47, 300, 2500, 20_011])
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("T", [0.01, 0.5, 1.0, 2.5])
+def test_distill_of_named_classes_masked_with_the_lowest_number(v, dtype, T):
+    """A student that masks classes its teacher names has a loss as large as the formula's, not infinity before it."""
+    rng = np.random.default_rng(v)
+    low = torch.finfo(TYPES[dtype]).min
+    s = torch.from_numpy(3 * rng.standard_normal((6, v))).float().to(TYPES[dtype])
+    ids = np.stack([rng.permutation(v)[:5] for _ in range(6)])
+    t = 0.02 * T * rng.standard_normal((6, 5)).astype(np.float32)
+    for r, masked in enumerate(([0], [0, 1], [0, 1, 2, 3], [4], [], [2, 3])):
+        for i in masked:
+            s[r, ids[r, i]] = low if r < 5 else -1e38
+    t[3, 4] -= 40 * T  # (of next to no weight)
+    it, tt = torch.from_numpy(ids), torch.from_numpy(t)
+    loss, stats = gs.distill_loss(s.to(DEV), it.to(DEV), tt.to(DEV), T)
+    want, d, q, at, lp = oracle.distill(_np(s), ids, t, T)
+    x, logS, ax, _ = _parts(_np(s), T)
+    dd, xa = np.abs(t - t.max(1, keepdims=True)) / T, np.abs(x[np.arange(6)[:, None], ids])
+    rS = 4 * ax + _sum_terms(v)
+    tol = T * T * U * ((q * (dd + xa) * (4 * dd + 2 * 5 + 20)).sum(1) + (q * 4 * xa).sum(1) + 6 * logS + 6 * np.log(6) + rS)
+    past = want > 3.4e38  # (at 2.5, where all but one are masked)
+    assert T > 1 or not past.any()
+    assert torch.isinf(loss.cpu()[torch.from_numpy(past)]).all()
+    _close(loss.cpu()[torch.from_numpy(~past)], want[~past], tol[~past], "loss")
+    g = torch.ones(6)
+    got = gs.distill_grad(s.to(DEV), it.to(DEV), tt.to(DEV), stats, g.to(DEV), T)
+    tol = np.exp(lp) * U * (4 * np.minimum(np.abs(x), 1e4) + 16 + rS[:, None]) + FLUSH
+    np.add.at(tol, (np.repeat(np.arange(6), 5), ids.ravel()), (q * U * (4 * dd + 2 * 5 + 20)).ravel())
+    _close(got, d, T * tol + (HALF[dtype] + 4 * U) * np.abs(d), "gradient")
